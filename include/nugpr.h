@@ -378,6 +378,70 @@ int nugpr_stats_read(nugpr_ctx* ctx, nugpr_stats* out /*HOST*/, int32_t reset);
  * against which hardware HBM byte counters are scaled.  Does not synchronise. */
 int nugpr_copy_probe(void* dst /*DEVICE*/, const void* src /*DEVICE*/, size_t bytes, void* stream);
 
+/* ---- Operators of sequence models ---------------------------------------------------------------------------------
+ * A point of the regression may be a sequence, its coordinates what a layer makes of that sequence.  Two operators of such
+ * a layer have the structure of the covariance above, dense blocks plus terms of low rank over rows stored one after the
+ * other with an array of offsets: linear attention with decay (a dense block inside a run of rows, a dim_k x dim_v state
+ * between runs) and a projection with low-rank adapters (one adapter a request, or a cluster).  They need no context.
+ *
+ *   - Their arrays are float32 or bfloat16 (dtype, the same for all that are not said to be float); sums, states and
+ *     decays are float32 in either case.
+ *   - Offsets are DEVICE int64 arrays (no call waits for them): sequence s owns rows offsets[s] .. offsets[s+1]-1; ascending,
+ *     empty sequences allowed, within 0 .. n_rows (offsets outside are taken as the nearest end: no access is out
+ *     of bounds).  Output rows that no sequence owns are set to zero unless said otherwise.
+ *   - The calls only enqueue, on the given stream and on the device that is current.  Those that need scratch memory take
+ *     a 256-byte aligned DEVICE workspace of the size that the call before them in this file gives; it must not
+ *     be used by other work until the call's kernels have ended.  Results do not depend on the order in which workgroups
+ *     run.  Inputs and outputs must not overlap unless said otherwise. */
+enum { NUGPR_FLOAT32 = 0, NUGPR_BFLOAT16 = 1 };
+
+/* Rows x heads x width array: value (row, head, j) at data[row * row_stride + head * head_stride + j] (strides in values, not
+ * negative).  Pointers and strides that are multiples of 16 bytes are read faster. */
+typedef struct {
+  void* data;          /* DEVICE */
+  int64_t row_stride, head_stride;
+} nugpr_heads;
+
+/* Linear attention with a decay for each head.  Query head h reads the state of key / value head j = h / (heads / kv_heads);
+ * within a sequence, with lam_j = exp(log_decay[j]) and S the dim_k x dim_v state of (sequence, j),
+ *   S_t = lam_j S_{t-1} + k_t v_t^T,      o_t = scale q_t S_t.
+ * log_decay <= 0 (-infinity: nothing is kept) is a constant of the layer: it gets no gradient. */
+typedef struct {
+  int32_t dtype;              /* of q, k, v, o and their gradients                                  */
+  int32_t heads, kv_heads;    /* kv_heads divides heads                                             */
+  int32_t dim_k, dim_v;       /* 1..128                                                             */
+  int64_t n_rows;             /* rows (tokens) in all; nugpr_decay_attention_step: requests         */
+  int32_t n_seqs;             /* sequences; nugpr_decay_attention_step: states that `state` holds   */
+  const int64_t* seq_offsets; /* DEVICE, n_seqs+1; not read by nugpr_decay_attention_step           */
+  const float* log_decay;     /* DEVICE, kv_heads                                                   */
+  double scale;               /* finite                                                             */
+  void* workspace;            /* DEVICE; not used by nugpr_decay_attention_step                     */
+  size_t workspace_bytes;
+} nugpr_decay_attention;
+
+/* Bytes of workspace that the two calls below need (backward != 0: the second one).  Only dtype, heads, kv_heads, dim_k, dim_v, n_rows
+ * and n_seqs are read; 0 on invalid input. */
+size_t nugpr_decay_attention_workspace_bytes(const nugpr_decay_attention* problem, int32_t backward);
+
+/* All rows of the packed sequences.  initial_state: DEVICE float n_seqs x kv_heads x dim_k x dim_v, or NULL = zero.
+ * final_state: the same, out, or NULL; it may be initial_state. */
+int nugpr_decay_attention_forward(const nugpr_decay_attention* problem, const nugpr_heads* q, const nugpr_heads* k,
+                                  const nugpr_heads* v, const float* initial_state, const nugpr_heads* o, float* final_state,
+                                  void* stream);
+
+/* Gradients, given d_o and (or NULL = zero) d_final_state; d_initial_state: out, or NULL; it may be d_final_state.  Those of
+ * key / value heads are sums over the query heads that read them.  Nothing of the forward pass is needed but its inputs. */
+int nugpr_decay_attention_backward(const nugpr_decay_attention* problem, const nugpr_heads* q, const nugpr_heads* k,
+                                   const nugpr_heads* v, const float* initial_state, const nugpr_heads* d_o,
+                                   const float* d_final_state, const nugpr_heads* dq, const nugpr_heads* dk,
+                                   const nugpr_heads* dv, float* d_initial_state, void* stream);
+
+/* One token for each of n_rows requests: row b advances state slots[b] (DEVICE int32; NULL: state b) of `state`, DEVICE float
+ * n_seqs x kv_heads x dim_k x dim_v, in place, and reads it.  A slot outside 0 .. n_seqs-1 stands for no
+ * request: its output is zero.  No two rows may name one state. */
+int nugpr_decay_attention_step(const nugpr_decay_attention* problem, const nugpr_heads* q, const nugpr_heads* k,
+                               const nugpr_heads* v, float* state, const int32_t* slots, const nugpr_heads* o, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

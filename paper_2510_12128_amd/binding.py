@@ -26,6 +26,8 @@ NUGPR_FD_FORWARD = 16
 NUGPR_COMPENSATE = 32
 NUGPR_PRECOND_COMPENSATED = 64
 
+NUGPR_FLOAT32, NUGPR_BFLOAT16 = 0, 1
+
 EXPORT_K, EXPORT_L, EXPORT_LINV, EXPORT_C, EXPORT_W, EXPORT_B, EXPORT_REPS = range(7)
 
 
@@ -57,6 +59,17 @@ class Stats(C.Structure):
     _fields_ = [(k, C.c_int64) for k in ("loss_evals", "pcg_solves", "pcg_iterations", "pcg_iterations_max",
                                           "products", "products_reused", "precond_applies",
                                           "matrices_assembled", "assembly_passes", "factorisations")]
+
+
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class DecayAttention(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim_k", C.c_int32),
+                ("dim_v", C.c_int32), ("n_rows", C.c_int64), ("n_seqs", C.c_int32), ("seq_offsets", C.c_void_p),
+                ("log_decay", C.c_void_p), ("scale", C.c_double), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
 
 
 _LIB = None
@@ -139,6 +152,15 @@ def load_library():
     lib.nugpr_stats_read.argtypes = [vp, C.POINTER(Stats), C.c_int32]
     lib.nugpr_copy_probe.restype = C.c_int
     lib.nugpr_copy_probe.argtypes = [vp, vp, C.c_size_t, vp]
+    da, hd = C.POINTER(DecayAttention), C.POINTER(Heads)
+    lib.nugpr_decay_attention_workspace_bytes.restype = C.c_size_t
+    lib.nugpr_decay_attention_workspace_bytes.argtypes = [da, C.c_int32]
+    lib.nugpr_decay_attention_forward.restype = C.c_int
+    lib.nugpr_decay_attention_forward.argtypes = [da, hd, hd, hd, vp, hd, vp, vp]
+    lib.nugpr_decay_attention_backward.restype = C.c_int
+    lib.nugpr_decay_attention_backward.argtypes = [da, hd, hd, hd, vp, hd, vp, hd, hd, hd, vp, vp]
+    lib.nugpr_decay_attention_step.restype = C.c_int
+    lib.nugpr_decay_attention_step.argtypes = [da, hd, hd, hd, vp, vp, hd, vp]
     _LIB = lib
     return lib
 

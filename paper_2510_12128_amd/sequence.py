@@ -1,0 +1,142 @@
+"""Operators of sequence models (include/nugpr.h has their definitions): same names as the C entry points, argument checks and
+marshalling only.  Arrays are CUDA tensors, float32 or bfloat16, of any strides with the last dimension contiguous; offsets,
+slots and the like stay on the device, and no call waits for the GPU.  Outputs and scratch memory are torch tensors on
+the current stream of the tensors' device."""
+from __future__ import annotations
+
+import ctypes as C
+
+from .binding import (DecayAttention, Heads, NUGPR_BFLOAT16, NUGPR_ERR_INVALID, NUGPR_FLOAT32, NugprError, _check,
+                      load_library)
+
+
+def _refuse(what):
+    raise NugprError(NUGPR_ERR_INVALID, what)
+
+
+def _types():
+    import torch
+    return torch, {torch.float32: NUGPR_FLOAT32, torch.bfloat16: NUGPR_BFLOAT16}
+
+
+def _tensor(t, name, like, shape, dtype):
+    """`t` as it is, or a refusal: on `like`'s device, of this shape (None: any) and type."""
+    if t.device != like.device or not t.is_cuda:
+        _refuse(f"{name} must be on the GPU that q or x is on")
+    if t.dtype != dtype:
+        _refuse(f"{name} must be {dtype}, not {t.dtype}")
+    if t.dim() != len(shape) or any(w is not None and w != s for w, s in zip(shape, t.shape)):
+        _refuse(f"{name} must have the shape {tuple('any' if w is None else w for w in shape)}, not {tuple(t.shape)}")
+    return t
+
+
+def _dense(t, name, like, shape, dtype):
+    if not _tensor(t, name, like, shape, dtype).is_contiguous():
+        _refuse(f"{name} must be contiguous")
+    return t
+
+
+def _inner(t, name):
+    if t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel():
+        _refuse(f"the last dimension of {name} must be contiguous")
+
+
+def _heads(t, name):
+    _inner(t, name)
+    return Heads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _stream(torch, device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _attention(q, k, v, log_decay, scale):
+    """The problem's structure with everything but sequences and workspace."""
+    torch, types = _types()
+    if q.dtype not in types:
+        _refuse(f"q must be float32 or bfloat16, not {q.dtype}")
+    if q.dim() != 3:
+        _refuse("q must be rows x heads x dim_k")
+    n = q.shape[0]
+    _tensor(q, "q", q, (n, None, None), q.dtype)
+    _tensor(k, "k", q, (n, None, q.shape[2]), q.dtype)
+    _tensor(v, "v", q, (n, k.shape[1], None), q.dtype)
+    _dense(log_decay, "log_decay", q, (k.shape[1],), torch.float32)
+    p = DecayAttention()
+    p.dtype, p.heads, p.kv_heads, p.dim_k, p.dim_v = types[q.dtype], q.shape[1], k.shape[1], q.shape[2], v.shape[2]
+    p.n_rows, p.log_decay = n, log_decay.data_ptr()
+    p.scale = float(scale)
+    return torch, p
+
+
+def _sequences(torch, p, q, seq_offsets, backward):
+    """Puts offsets and scratch memory into the problem; returns what has to stay alive during the call."""
+    _dense(seq_offsets, "seq_offsets", q, (None,), torch.int64)
+    if seq_offsets.shape[0] < 1:
+        _refuse("seq_offsets must have n_seqs + 1 entries")
+    p.n_seqs, p.seq_offsets = seq_offsets.shape[0] - 1, seq_offsets.data_ptr()
+    need = load_library().nugpr_decay_attention_workspace_bytes(C.byref(p), backward)
+    if need == 0:
+        raise NugprError(NUGPR_ERR_INVALID, load_library().nugpr_last_error_string().decode())
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device)       # (torch aligns allocations to 512 bytes)
+    p.workspace, p.workspace_bytes = ws.data_ptr(), need
+    return ws
+
+
+def _state(t, name, q, p, torch):
+    if t is None:
+        return None
+    return _dense(t, name, q, (p.n_seqs, p.kv_heads, p.dim_k, p.dim_v), torch.float32).data_ptr()
+
+
+def nugpr_decay_attention_forward(q, k, v, log_decay, seq_offsets, scale=1.0, initial_state=None):
+    """Linear attention with a decay for each head over packed sequences.
+
+    q (rows, heads, dim_k), k (rows, kv_heads, dim_k), v (rows, kv_heads, dim_v): float32 or bfloat16; log_decay (kv_heads,)
+    float32, <= 0; seq_offsets (n_seqs + 1,) int64; initial_state (n_seqs, kv_heads, dim_k, dim_v) float32 or None.
+    Returns o (rows, heads, dim_v) and the sequences' end states, float32."""
+    torch, p = _attention(q, k, v, log_decay, scale)
+    ws = _sequences(torch, p, q, seq_offsets, 0)  # noqa: F841
+    s0 = _state(initial_state, "initial_state", q, p, torch)
+    o = torch.empty((q.shape[0], p.heads, p.dim_v), dtype=q.dtype, device=q.device)
+    s1 = torch.empty((p.n_seqs, p.kv_heads, p.dim_k, p.dim_v), dtype=torch.float32, device=q.device)
+    with torch.cuda.device(q.device):
+        _check(load_library().nugpr_decay_attention_forward(
+            C.byref(p), C.byref(_heads(q, "q")), C.byref(_heads(k, "k")), C.byref(_heads(v, "v")), s0,
+            C.byref(_heads(o, "o")), s1.data_ptr(), _stream(torch, q.device)))
+    return o, s1
+
+
+def nugpr_decay_attention_backward(q, k, v, log_decay, seq_offsets, d_o, scale=1.0, initial_state=None,
+                                   d_final_state=None):
+    """Gradients of nugpr_decay_attention_forward's q, k, v (in their type) and initial state (float32), from d_o and, unless
+    None, d_final_state."""
+    torch, p = _attention(q, k, v, log_decay, scale)
+    ws = _sequences(torch, p, q, seq_offsets, 1)  # noqa: F841
+    s0 = _state(initial_state, "initial_state", q, p, torch)
+    s1 = _state(d_final_state, "d_final_state", q, p, torch)
+    _tensor(d_o, "d_o", q, (q.shape[0], p.heads, p.dim_v), q.dtype)
+    dq, dk, dv = (torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
+    ds = torch.empty((p.n_seqs, p.kv_heads, p.dim_k, p.dim_v), dtype=torch.float32, device=q.device)
+    with torch.cuda.device(q.device):
+        _check(load_library().nugpr_decay_attention_backward(
+            C.byref(p), C.byref(_heads(q, "q")), C.byref(_heads(k, "k")), C.byref(_heads(v, "v")), s0,
+            C.byref(_heads(d_o, "d_o")), s1, C.byref(_heads(dq, "dq")), C.byref(_heads(dk, "dk")),
+            C.byref(_heads(dv, "dv")), ds.data_ptr(), _stream(torch, q.device)))
+    return dq, dk, dv, ds
+
+
+def nugpr_decay_attention_step(q, k, v, log_decay, state, slots=None, scale=1.0):
+    """One token for each request: q (requests, heads, dim_k), k, v alike; state (n_states, kv_heads, dim_k, dim_v) float32 is
+    advanced in place, request b's at slots[b] (int32; None: b).  Returns o (requests, heads, dim_v)."""
+    torch, p = _attention(q, k, v, log_decay, scale)
+    p.n_seqs = state.shape[0] if state.dim() == 4 else 0
+    st = _state(state, "state", q, p, torch)
+    if slots is not None:
+        _dense(slots, "slots", q, (q.shape[0],), torch.int32)
+    o = torch.empty((q.shape[0], p.heads, p.dim_v), dtype=q.dtype, device=q.device)
+    with torch.cuda.device(q.device):
+        _check(load_library().nugpr_decay_attention_step(
+            C.byref(p), C.byref(_heads(q, "q")), C.byref(_heads(k, "k")), C.byref(_heads(v, "v")), st,
+            None if slots is None else slots.data_ptr(), C.byref(_heads(o, "o")), _stream(torch, q.device)))
+    return o
