@@ -442,6 +442,39 @@ int nugpr_decay_attention_backward(const nugpr_decay_attention* problem, const n
 int nugpr_decay_attention_step(const nugpr_decay_attention* problem, const nugpr_heads* q, const nugpr_heads* k,
                                const nugpr_heads* v, float* state, const int32_t* slots, const nugpr_heads* o, void* stream);
 
+/* A projection that all rows share, beside a low-rank adapter for each request (or cluster): row t of request s, a =
+ * adapter_of[s], gets
+ *   y_t = W x_t + scale B_a^T (A_a x_t),      A_a rank x dim_in, B_a rank x dim_out.
+ * Rows that no request owns, and those of a request whose adapter is outside 0 .. n_adapters-1, get W x_t alone. */
+typedef struct {
+  int32_t dtype;              /* of x, W, A, B, y and their gradients                               */
+  int32_t dim_in, dim_out;    /* 1..65536                                                           */
+  int32_t rank;               /* 1..128                                                             */
+  int32_t n_adapters;         /* >= 0                                                               */
+  int64_t n_rows;
+  int32_t n_seqs;             /* requests                                                           */
+  const int64_t* seq_offsets; /* DEVICE, n_seqs+1                                                   */
+  const int32_t* adapter_of;  /* DEVICE, n_seqs, or NULL: request s has adapter s                   */
+  const void* W;              /* DEVICE, dim_out x dim_in row-major                                 */
+  const void* A;              /* DEVICE, n_adapters x rank x dim_in                                 */
+  const void* B;              /* DEVICE, n_adapters x rank x dim_out                                */
+  double scale;               /* finite                                                             */
+  void* workspace;            /* DEVICE                                                             */
+  size_t workspace_bytes;
+} nugpr_adapter;
+
+/* Bytes of workspace that the two calls below need (backward != 0: the second one).  Only dtype, the dims, rank, n_adapters, n_rows
+ * and n_seqs are read; 0 on invalid input. */
+size_t nugpr_adapter_workspace_bytes(const nugpr_adapter* problem, int32_t backward);
+
+/* x: DEVICE n_rows x dim_in, row t at x + t * x_stride (values); y: DEVICE n_rows x dim_out, dense. */
+int nugpr_adapter_forward(const nugpr_adapter* problem, const void* x, int64_t x_stride, void* y, void* stream);
+
+/* Gradients of x (dense), A and B (every adapter's is written, zero where no row has it) from d_y, whose row t is at d_y + t *
+ * dy_stride.  W is fixed, as it is while adapters are trained: it gets none.  dx may be NULL. */
+int nugpr_adapter_backward(const nugpr_adapter* problem, const void* x, int64_t x_stride, const void* d_y, int64_t dy_stride,
+                           void* dx, void* dA, void* dB, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

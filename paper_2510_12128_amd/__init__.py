@@ -13,5 +13,6 @@ from .binding import (  # noqa: F401
     NUGPR_ERR_INVALID, NUGPR_ERR_WORKSPACE, NUGPR_ERR_HIP, NUGPR_ERR_STATE, NUGPR_ISOTROPIC,
 )
 from .sequence import (  # noqa: F401
-    nugpr_decay_attention_backward, nugpr_decay_attention_forward, nugpr_decay_attention_step,
+    nugpr_adapter_backward, nugpr_adapter_forward, nugpr_decay_attention_backward, nugpr_decay_attention_forward,
+    nugpr_decay_attention_step,
 )

@@ -72,6 +72,13 @@ class DecayAttention(C.Structure):
                 ("workspace_bytes", C.c_size_t)]
 
 
+class Adapter(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("dim_in", C.c_int32), ("dim_out", C.c_int32), ("rank", C.c_int32),
+                ("n_adapters", C.c_int32), ("n_rows", C.c_int64), ("n_seqs", C.c_int32), ("seq_offsets", C.c_void_p),
+                ("adapter_of", C.c_void_p), ("W", C.c_void_p), ("A", C.c_void_p), ("B", C.c_void_p),
+                ("scale", C.c_double), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 _LIB = None
 
 
@@ -161,6 +168,13 @@ def load_library():
     lib.nugpr_decay_attention_backward.argtypes = [da, hd, hd, hd, vp, hd, vp, hd, hd, hd, vp, vp]
     lib.nugpr_decay_attention_step.restype = C.c_int
     lib.nugpr_decay_attention_step.argtypes = [da, hd, hd, hd, vp, vp, hd, vp]
+    ad = C.POINTER(Adapter)
+    lib.nugpr_adapter_workspace_bytes.restype = C.c_size_t
+    lib.nugpr_adapter_workspace_bytes.argtypes = [ad, C.c_int32]
+    lib.nugpr_adapter_forward.restype = C.c_int
+    lib.nugpr_adapter_forward.argtypes = [ad, vp, C.c_int64, vp, vp]
+    lib.nugpr_adapter_backward.restype = C.c_int
+    lib.nugpr_adapter_backward.argtypes = [ad, vp, C.c_int64, vp, C.c_int64, vp, vp, vp, vp]
     _LIB = lib
     return lib
 

@@ -1,0 +1,676 @@
+// A projection that all rows share beside a low-rank adapter for each request, and its gradients:
+//
+//   y = x W^T + h B_a,      h = scale x A_a^T                 (a: the adapter of the row's request)
+//   dx = dy W + u A_a,      u = scale dy B_a^T
+//   dA_a = sum u^T x,       dB_a = sum h^T dy                 over the rows of all requests that have a
+//
+// h and u (rows x rank, float32, in the workspace) are one kernel's work (k_low); the large products take them as a few
+// more steps of their contraction (k_project, or k_project_few where there are few rows), the sums over rows are k_adapter_grad's.
+#include <cmath>
+
+#include "matrix_core.h"
+#include "nugpr_internal.h"
+#include "packed_rows.h"
+
+namespace nugpr {
+
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int LOW_LOG2 = 4;          // rows of a piece of k_low
+
+struct Requests {
+  const int64_t* off;
+  const int32_t* adapter_of;         // or null: request s has adapter s
+  int64_t n_rows;
+  int n_seqs, n_adapters;
+};
+
+// the adapter of a request, or -1
+__device__ inline int adapter(const Requests& q, int s) {
+  const int a = q.adapter_of ? q.adapter_of[s] : s;
+  return a >= 0 && a < q.n_adapters ? a : -1;
+}
+
+// 16 bytes of a row from column `col` on, zero past `width`
+template <class TR, bool AL>
+__device__ inline u32x4 run16(const typename TR::T* row, int64_t col, int64_t width) {
+  u32x4 v = {0, 0, 0, 0};
+  if constexpr (AL) {
+    if (col < width) v = *reinterpret_cast<const u32x4*>(row + col);
+  } else {
+#pragma unroll
+    for (int j = 0; j < TR::E; ++j)
+      if (col + j < width) {
+        if constexpr (TR::E == 8) v[j >> 1] |= (uint32_t)row[col + j] << (16 * (j & 1));
+        else v[j] = __builtin_bit_cast(uint32_t, row[col + j]);
+      }
+  }
+  return v;
+}
+
+// ---- h = scale x A_a^T --------------------------------------------------------------------------------------------------
+struct LowSide {
+  const void* x;          // rows x width
+  const void* A;          // adapters x rank x width
+  float* low;             // rows x padded rank
+  int64_t x_stride;
+  int width;
+};
+struct LowArgs {
+  LowSide side[2];
+  Requests q;
+  float scale;
+  int rank, padded;
+};
+
+// A workgroup takes 16 rows of one request and all of the rank; its waves split the width, operands go from memory straight
+// into registers (nothing is read twice but A, from L2), the waves' sums meet in LDS.
+template <class TR, bool AL, int TILES>
+__global__ __launch_bounds__(1024) void k_low(const LowArgs a) {
+  using T = typename TR::T;
+  extern __shared__ float red[];           // waves x 16 rows x 16 TILES
+  const LowSide& sd = a.side[blockIdx.y];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6, i = lane & 15, kg = lane >> 4;
+  const int item = blockIdx.x;
+  const int s = sequence_of(a.q.off, a.q.n_seqs, a.q.n_rows, LOW_LOG2, item);
+  if (s < 0) return;
+  const int64_t lo = clamped(a.q.off[s], 0, a.q.n_rows), hi = clamped(a.q.off[s + 1], lo, a.q.n_rows);
+  const int64_t row0 = lo + ((item - ((lo >> LOW_LOG2) + s)) << LOW_LOG2);
+  const int ad = adapter(a.q, s);
+  if (row0 >= hi || ad < 0) return;
+  const int rows = (int)min((int64_t)16, hi - row0);
+  const T* x = static_cast<const T*>(sd.x) + (row0 + i) * sd.x_stride;
+  const T* A = static_cast<const T*>(sd.A) + (int64_t)ad * a.rank * sd.width;
+  f32x4 acc[TILES];
+#pragma unroll
+  for (int n = 0; n < TILES; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int k = wave * TR::KS; k < sd.width; k += waves * TR::KS) {
+    const int col = k + kg * TR::E;
+    u32x4 xv = {0, 0, 0, 0};
+    if (i < rows) xv = run16<TR, AL>(x, col, sd.width);
+#pragma unroll
+    for (int n = 0; n < TILES; ++n) {
+      u32x4 av = {0, 0, 0, 0};
+      if (16 * n + i < a.rank) av = run16<TR, AL>(A + (int64_t)(16 * n + i) * sd.width, col, sd.width);
+      acc[n] = TR::mfma(__builtin_bit_cast(typename TR::Frag, xv), __builtin_bit_cast(typename TR::Frag, av), acc[n]);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < TILES; ++n)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) red[(wave * 16 + 4 * kg + r) * (16 * TILES) + 16 * n + i] = acc[n][r];
+  __syncthreads();
+  for (int e = tid; e < rows * a.padded; e += blockDim.x) {
+    const int r = e / a.padded, j = e - r * a.padded;
+    float sum = 0.f;
+    if (j < a.rank)
+      for (int w = 0; w < waves; ++w) sum += red[(w * 16 + r) * (16 * TILES) + j];
+    sd.low[(row0 + r) * a.padded + j] = a.scale * sum;
+  }
+}
+
+// ---- y = x W^T + h B_a, dx = dy W + u A_a ---------------------------------------------------------------------------------
+struct ProjectArgs {
+  const void *x, *W, *up;   // rows x width_k; W: n x k (NN: k x n); up: adapters x rank x n
+  const float* low;         // rows x padded rank
+  void* y;                  // rows x n, dense
+  int64_t x_stride;
+  Requests q;
+  int k, n, rank, padded;
+};
+
+// 128-byte steps of the contraction through LDS, the next step's loads in registers meanwhile; the accumulators' rows are the columns of
+// y (four in a row a lane).  The adapters are further steps at the end: for every request with rows in the tile, its rows of h
+// (in bfloat16 as two numbers, 16 bits in all) and 32 rows of B_a at a time.
+template <class TR, int BM, int BN, int WM, int WN, bool NN, bool AL>
+__global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
+  using T = typename TR::T;
+  using Frag = typename TR::Frag;
+  constexpr int KS = TR::KS, E = TR::E, BK = 128 / sizeof(T), PAD = 16 / sizeof(T);
+  constexpr int MT = BM / WM / 16, NTL = BN / WN / 16;        // a wave's tiles
+  constexpr int LDA = BK + PAD, LDN = BN + PAD;
+  constexpr int XA = BM * BK / E / THREADS, XB = (BN * BK / E + THREADS - 1) / THREADS;
+  static_assert(WM * WN == 4 && 2 * KS <= BK, "");
+  __shared__ __align__(16) T sA[BM * LDA];
+  __shared__ __align__(16) T sB[NN ? BK * LDN : (BN * LDA > KS * LDN ? BN * LDA : KS * LDN)];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, kg = lane >> 4;
+  const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+  const int64_t m0 = (int64_t)blockIdx.y * BM;
+  const int n0 = blockIdx.x * BN;
+  const int rows = (int)min((int64_t)BM, a.q.n_rows - m0);
+  const T* x = static_cast<const T*>(a.x) + m0 * a.x_stride;
+  const T* W = static_cast<const T*>(a.W);
+  f32x4 acc[NTL][MT];
+#pragma unroll
+  for (int n = 0; n < NTL; ++n)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  u32x4 ra[XA], rb[XB];
+  auto load = [&](int k0) {
+#pragma unroll
+    for (int p = 0; p < XA; ++p) {
+      const int c = tid + p * THREADS, row = c / (BK / E), col = c % (BK / E) * E;
+      ra[p] = row < rows ? run16<TR, AL>(x + (int64_t)row * a.x_stride, k0 + col, a.k) : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int p = 0; p < XB; ++p) {
+      const int c = tid + p * THREADS;
+      u32x4 v = {0, 0, 0, 0};
+      if constexpr (NN) {
+        const int row = c / (BN / E), col = c % (BN / E) * E;
+        if (row < BK && k0 + row < a.k) v = run16<TR, AL>(W + (int64_t)(k0 + row) * a.n, n0 + col, a.n);
+      } else {
+        const int row = c / (BK / E), col = c % (BK / E) * E;
+        if (row < BN && n0 + row < a.n) v = run16<TR, AL>(W + (int64_t)(n0 + row) * a.k, k0 + col, a.k);
+      }
+      rb[p] = v;
+    }
+  };
+  auto put = [&]() {
+#pragma unroll
+    for (int p = 0; p < XA; ++p) {
+      const int c = tid + p * THREADS;
+      *reinterpret_cast<u32x4*>(sA + c / (BK / E) * LDA + c % (BK / E) * E) = ra[p];
+    }
+#pragma unroll
+    for (int p = 0; p < XB; ++p) {
+      const int c = tid + p * THREADS;
+      if (c < BN * BK / E) {
+        if constexpr (NN) *reinterpret_cast<u32x4*>(sB + c / (BN / E) * LDN + c % (BN / E) * E) = rb[p];
+        else *reinterpret_cast<u32x4*>(sB + c / (BK / E) * LDA + c % (BK / E) * E) = rb[p];
+      }
+    }
+  };
+  load(0);
+  for (int k0 = 0; k0 < a.k; k0 += BK) {
+    __syncthreads();
+    put();
+    __syncthreads();
+    if (k0 + BK < a.k) load(k0 + BK);
+#pragma unroll
+    for (int k = 0; k < BK; k += KS) {
+      Frag xf[MT], wf[NTL];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) xf[m] = TR::row_frag(sA + (wm + 16 * m + i) * LDA, k, kg);
+#pragma unroll
+      for (int n = 0; n < NTL; ++n)
+        wf[n] = NN ? TR::col_frag(sB, LDN, k, wn + 16 * n, i, kg) : TR::row_frag(sB + (wn + 16 * n + i) * LDA, k, kg);
+#pragma unroll
+      for (int n = 0; n < NTL; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[n][m] = TR::mfma(wf[n], xf[m], acc[n][m]);
+    }
+  }
+  // the adapters
+  for (int at = 0; at < a.q.n_seqs; at += 64) {
+    // which of 64 requests have rows here
+    const int mine = at + lane;
+    int64_t lo = 0, hi = 0;
+    int ad = -1;
+    if (mine < a.q.n_seqs) {
+      lo = clamped(a.q.off[mine], m0, m0 + rows);
+      hi = clamped(a.q.off[mine + 1], lo, m0 + rows);
+      ad = adapter(a.q, mine);
+    }
+    uint64_t some = __ballot(hi > lo && ad >= 0);
+    while (some) {
+      const int from = __builtin_ctzll(some);
+      some &= some - 1;
+      const int rlo = __shfl((int)(lo - m0), from), rhi = __shfl((int)(hi - m0), from), one = __shfl(ad, from);
+      const T* up = static_cast<const T*>(a.up) + (int64_t)one * a.rank * a.n;
+      for (int j0 = 0; j0 < a.rank; j0 += KS) {
+        __syncthreads();
+        for (int c = tid; c < BM * KS / 4; c += THREADS) {
+          const int row = c / (KS / 4), col = c % (KS / 4) * 4;
+          f32x4 v = {0.f, 0.f, 0.f, 0.f};
+          if (row >= rlo && row < rhi) v = *reinterpret_cast<const f32x4*>(a.low + (m0 + row) * a.padded + j0 + col);
+          if constexpr (E == 8) {
+            *reinterpret_cast<u32x2*>(sA + row * LDA + col) = u32x2{two_upper(v[0], v[1]), two_upper(v[2], v[3])};
+            *reinterpret_cast<u32x2*>(sA + row * LDA + KS + col) =
+                u32x2{two_bf16(v[0] - upper(v[0]), v[1] - upper(v[1])), two_bf16(v[2] - upper(v[2]), v[3] - upper(v[3]))};
+          } else {
+            *reinterpret_cast<f32x4*>(sA + row * LDA + col) = v;
+          }
+        }
+        for (int c = tid; c < KS * BN / E; c += THREADS) {
+          const int row = c / (BN / E), col = c % (BN / E) * E;
+          *reinterpret_cast<u32x4*>(sB + row * LDN + col) =
+              j0 + row < a.rank ? run16<TR, AL>(up + (int64_t)(j0 + row) * a.n, n0 + col, a.n) : u32x4{0, 0, 0, 0};
+        }
+        __syncthreads();
+        Frag wf[NTL];
+#pragma unroll
+        for (int n = 0; n < NTL; ++n) wf[n] = TR::col_frag(sB, LDN, 0, wn + 16 * n, i, kg);
+#pragma unroll
+        for (int part = 0; part < TR::S_PARTS; ++part)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            const Frag xf = TR::row_frag(sA + (wm + 16 * m + i) * LDA, part * KS, kg);
+#pragma unroll
+            for (int n = 0; n < NTL; ++n) acc[n][m] = TR::mfma(wf[n], xf, acc[n][m]);
+          }
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int row = wm + 16 * m + i;
+    if (row >= rows) continue;
+    T* y = static_cast<T*>(a.y) + (m0 + row) * a.n;
+#pragma unroll
+    for (int n = 0; n < NTL; ++n) {
+      const int col = n0 + wn + 16 * n + 4 * kg;
+      const f32x4 v = acc[n][m];
+      if constexpr (AL) {
+        if (col < a.n) {
+          if constexpr (E == 8) *reinterpret_cast<u32x2*>(y + col) = u32x2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
+          else *reinterpret_cast<f32x4*>(y + col) = v;
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (col + r < a.n) y[col + r] = TR::put(v[r]);
+      }
+    }
+  }
+}
+
+// Few rows: W is read once, by 16 of its rows a workgroup whose eight waves split the contraction, and bounds the time.  Up to
+// 16 RT rows a workgroup (blockIdx.y: the next ones).
+constexpr int FEW_THREADS = 512;
+template <class TR, int RT, bool AL>
+__global__ __launch_bounds__(FEW_THREADS) void k_project_few(const ProjectArgs a) {
+  using T = typename TR::T;
+  using Frag = typename TR::Frag;
+  constexpr int WAVES = FEW_THREADS / 64, ROWS = 16 * RT;
+  __shared__ float red[WAVES][ROWS][17];
+  __shared__ int sAdapter[ROWS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, kg = lane >> 4;
+  const int n0 = blockIdx.x * 16;
+  const int64_t m0 = (int64_t)blockIdx.y * ROWS;
+  const int rows = (int)min((int64_t)ROWS, a.q.n_rows - m0);
+  const T* W = static_cast<const T*>(a.W) + (int64_t)(n0 + i) * a.k;
+  const T* x = static_cast<const T*>(a.x) + (m0 + i) * a.x_stride;
+  f32x4 acc[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const u32x4 none = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int k = wave * TR::KS; k < a.k; k += WAVES * TR::KS) {
+    const int col = k + kg * TR::E;
+    const u32x4 w = n0 + i < a.n ? run16<TR, AL>(W, col, a.k) : none;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const u32x4 v = 16 * r + i < rows ? run16<TR, AL>(x + 16 * r * a.x_stride, col, a.k) : none;
+      acc[r] = TR::mfma(__builtin_bit_cast(Frag, w), __builtin_bit_cast(Frag, v), acc[r]);
+    }
+  }
+  for (int r = wave; r < rows; r += WAVES) {
+    const int s = owner_of(a.q.off, a.q.n_seqs, m0 + r);
+    if (lane == 0) sAdapter[r] = s < 0 ? -1 : adapter(a.q, s);
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) red[wave][16 * r + i][4 * kg + j] = acc[r][j];
+  __syncthreads();
+  for (int e = tid; e < rows * 16; e += FEW_THREADS) {
+    const int row = e >> 4, col = e & 15;
+    if (n0 + col >= a.n) continue;
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) sum += red[w][row][col];
+    const int ad = sAdapter[row];
+    if (ad >= 0) {
+      const T* up = static_cast<const T*>(a.up) + (int64_t)ad * a.rank * a.n + n0 + col;
+      const float* low = a.low + (m0 + row) * a.padded;
+#pragma unroll 8
+      for (int j = 0; j < a.rank; ++j) sum = fmaf(low[j], TR::get(up[(int64_t)j * a.n]), sum);
+    }
+    static_cast<T*>(a.y)[(m0 + row) * a.n + n0 + col] = TR::put(sum);
+  }
+}
+
+// ---- dA_a = sum u^T x, dB_a = sum h^T dy ----------------------------------------------------------------------------------
+struct GradSide {
+  const void* x;           // rows x width
+  const float* low;        // rows x padded rank
+  void* out;               // adapters x rank x width
+  float* part;             // the same in float32 for each part of the rows, or null: there is one
+  int64_t x_stride;
+  int width, tiles;        // column tiles
+};
+struct GradArgs {
+  GradSide side[2];
+  Requests q;
+  int rank, padded;
+  int64_t per;             // rows of a part
+};
+
+constexpr int GRAD_COLS = 128, GRAD_ROWS = 64;
+
+// A workgroup takes 128 columns of one adapter's gradient and a part of the rows, and of these the requests that have the adapter.
+template <class TR, int JT, bool AL>
+__global__ __launch_bounds__(THREADS) void k_adapter_grad(const GradArgs a) {
+  using T = typename TR::T;
+  using Frag = typename TR::Frag;
+  constexpr int KS = TR::KS, E = TR::E, PAD = 16 / sizeof(T), LDX = GRAD_COLS + PAD, LDJ = 16 * JT + PAD;
+  constexpr int X = GRAD_ROWS * GRAD_COLS / E / THREADS;
+  __shared__ __align__(16) T sX[GRAD_ROWS * LDX];
+  __shared__ __align__(16) T sL[TR::S_PARTS][GRAD_ROWS * LDJ];
+  const int side = (int)blockIdx.x < a.side[0].tiles ? 0 : 1;
+  const GradSide& sd = a.side[side];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, kg = lane >> 4;
+  const int n0 = (blockIdx.x - (side ? a.side[0].tiles : 0)) * GRAD_COLS, ad = blockIdx.y;
+  const int64_t p0 = blockIdx.z * a.per, p1 = min(a.q.n_rows, p0 + a.per);
+  const T* x = static_cast<const T*>(sd.x);
+  f32x4 acc[2][JT];
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int j = 0; j < JT; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int at = 0; at < a.q.n_seqs; at += 64) {
+    const int mine = at + lane;
+    int64_t lo = 0, hi = 0;
+    if (mine < a.q.n_seqs && adapter(a.q, mine) == ad) {
+      lo = clamped(a.q.off[mine], p0, p1);
+      hi = clamped(a.q.off[mine + 1], lo, p1);
+    }
+    uint64_t some = __ballot(hi > lo);
+    while (some) {
+      const int from = __builtin_ctzll(some);
+      some &= some - 1;
+      const int64_t rlo = __shfl((long long)lo, from), rhi = __shfl((long long)hi, from);
+      for (int64_t r0 = rlo; r0 < rhi; r0 += GRAD_ROWS) {
+        const int rows = (int)min((int64_t)GRAD_ROWS, rhi - r0);
+        u32x4 v[X];
+#pragma unroll
+        for (int p = 0; p < X; ++p) {
+          const int c = tid + p * THREADS, row = c / (GRAD_COLS / E), col = c % (GRAD_COLS / E) * E;
+          v[p] = row < rows ? run16<TR, AL>(x + (r0 + row) * sd.x_stride, n0 + col, sd.width) : u32x4{0, 0, 0, 0};
+        }
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < X; ++p) {
+          const int c = tid + p * THREADS;
+          *reinterpret_cast<u32x4*>(sX + c / (GRAD_COLS / E) * LDX + c % (GRAD_COLS / E) * E) = v[p];
+        }
+        for (int c = tid; c < GRAD_ROWS * 4 * JT; c += THREADS) {
+          const int row = c / (4 * JT), col = c % (4 * JT) * 4;
+          f32x4 w = {0.f, 0.f, 0.f, 0.f};
+          if (row < rows && col < a.padded) w = *reinterpret_cast<const f32x4*>(sd.low + (r0 + row) * a.padded + col);
+          if constexpr (E == 8) {
+            *reinterpret_cast<u32x2*>(sL[0] + row * LDJ + col) = u32x2{two_upper(w[0], w[1]), two_upper(w[2], w[3])};
+            *reinterpret_cast<u32x2*>(sL[TR::S_PARTS - 1] + row * LDJ + col) =
+                u32x2{two_bf16(w[0] - upper(w[0]), w[1] - upper(w[1])), two_bf16(w[2] - upper(w[2]), w[3] - upper(w[3]))};
+          } else {
+            *reinterpret_cast<f32x4*>(sL[0] + row * LDJ + col) = w;
+          }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < GRAD_ROWS; k += KS) {
+          Frag xf[2];
+#pragma unroll
+          for (int m = 0; m < 2; ++m) xf[m] = TR::col_frag(sX, LDX, k, 32 * wave + 16 * m, i, kg);
+#pragma unroll
+          for (int part = 0; part < TR::S_PARTS; ++part)
+#pragma unroll
+            for (int j = 0; j < JT; ++j) {
+              const Frag lf = TR::col_frag(sL[part], LDJ, k, 16 * j, i, kg);
+#pragma unroll
+              for (int m = 0; m < 2; ++m) acc[m][j] = TR::mfma(xf[m], lf, acc[m][j]);
+            }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < JT; ++j) {
+    const int row = 16 * j + i;
+    if (row >= a.rank) continue;
+    const int64_t at = ((int64_t)ad * a.rank + row) * sd.width;
+    float* part = sd.part ? sd.part + (int64_t)blockIdx.z * a.q.n_adapters * a.rank * sd.width + at : nullptr;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int col = n0 + 32 * wave + 16 * m + 4 * kg + r;
+        if (col >= sd.width) continue;
+        if (part) part[col] = acc[m][j][r];
+        else static_cast<T*>(sd.out)[at + col] = TR::put(acc[m][j][r]);
+      }
+  }
+}
+
+struct SumArgs {
+  const float* part[2];
+  void* out[2];
+  int64_t count[2];
+  int parts;
+};
+template <class TR>
+__global__ __launch_bounds__(THREADS) void k_sum_grads(const SumArgs a) {
+  const int64_t e = (int64_t)blockIdx.x * THREADS + threadIdx.x, n = a.count[blockIdx.y];
+  if (e >= n) return;
+  const float* p = a.part[blockIdx.y] + e;
+  float sum = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < a.parts; ++k) sum += p[k * n];
+  static_cast<typename TR::T*>(a.out[blockIdx.y])[e] = TR::put(sum);
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------------
+int check(const nugpr_adapter* p) {
+  if (!p) { set_error("problem is null"); return NUGPR_ERR_INVALID; }
+  if (p->dtype != NUGPR_FLOAT32 && p->dtype != NUGPR_BFLOAT16) { set_error("dtype must be NUGPR_FLOAT32 or NUGPR_BFLOAT16"); return NUGPR_ERR_INVALID; }
+  if (p->dim_in < 1 || p->dim_in > 65536 || p->dim_out < 1 || p->dim_out > 65536) { set_error("dim_in and dim_out must be 1..65536"); return NUGPR_ERR_INVALID; }
+  if (p->rank < 1 || p->rank > 128) { set_error("rank must be 1..128"); return NUGPR_ERR_INVALID; }
+  if (p->n_adapters < 0 || p->n_adapters > 65535) { set_error("n_adapters must be 0..65535"); return NUGPR_ERR_INVALID; }
+  if (p->n_rows < 0 || p->n_rows > (int64_t)4 << 20) { set_error("n_rows must be 0..2^22"); return NUGPR_ERR_INVALID; }
+  if (p->n_seqs < 0 || p->n_seqs > 1 << 22) { set_error("n_seqs must be 0..2^22"); return NUGPR_ERR_INVALID; }
+  return NUGPR_OK;
+}
+
+size_t value_size(const nugpr_adapter* p) { return p->dtype == NUGPR_BFLOAT16 ? 2 : 4; }
+int padded_rank(const nugpr_adapter* p) { const int k = p->dtype == NUGPR_BFLOAT16 ? 32 : 16; return (p->rank + k - 1) / k * k; }
+size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+size_t low_bytes(const nugpr_adapter* p) { return rounded((size_t)p->n_rows * padded_rank(p) * sizeof(float)); }
+int grad_tiles(int width) { return (width + GRAD_COLS - 1) / GRAD_COLS; }
+// parts of the rows in the sums over them: about 512 workgroups, of 256 rows at least
+int grad_parts(const nugpr_adapter* p) {
+  const int64_t tiles = (int64_t)(grad_tiles(p->dim_in) + grad_tiles(p->dim_out)) * p->n_adapters;
+  if (tiles == 0) return 1;
+  int64_t parts = 512 / tiles;
+  if (parts > p->n_rows / 256) parts = p->n_rows / 256;
+  return parts < 1 ? 1 : (int)parts;
+}
+size_t part_bytes(const nugpr_adapter* p, int width) {
+  const int parts = grad_parts(p);
+  return parts == 1 ? 0 : rounded((size_t)parts * p->n_adapters * p->rank * width * sizeof(float));
+}
+
+bool wide(const void* x, int64_t stride, size_t value) {
+  return !(reinterpret_cast<uintptr_t>(x) & 15u) && stride % (16 / (int64_t)value) == 0;
+}
+
+int check_call(const nugpr_adapter* p, size_t need) {
+  if (!std::isfinite(p->scale)) { set_error("scale must be finite"); return NUGPR_ERR_INVALID; }
+  const size_t z = value_size(p);
+  if (p->n_seqs > 0 && !p->seq_offsets) { set_error("seq_offsets is null"); return NUGPR_ERR_INVALID; }
+  if (!p->W || (p->n_adapters > 0 && (!p->A || !p->B))) { set_error("W, A or B is null"); return NUGPR_ERR_INVALID; }
+  if ((reinterpret_cast<uintptr_t>(p->W) | reinterpret_cast<uintptr_t>(p->A) | reinterpret_cast<uintptr_t>(p->B)) % z) {
+    set_error("W, A or B misaligned");
+    return NUGPR_ERR_INVALID;
+  }
+  if (need && (!p->workspace || (reinterpret_cast<uintptr_t>(p->workspace) & 255u))) { set_error("workspace is null or not 256-byte aligned"); return NUGPR_ERR_WORKSPACE; }
+  if (p->workspace_bytes < need) { set_error("workspace smaller than nugpr_adapter_workspace_bytes()"); return NUGPR_ERR_WORKSPACE; }
+  return NUGPR_OK;
+}
+
+int check_rows(const void* x, int64_t stride, const char* name, size_t z) {
+  if (!x) { set_error(std::string(name) + " is null"); return NUGPR_ERR_INVALID; }
+  if (reinterpret_cast<uintptr_t>(x) % z) { set_error(std::string(name) + " misaligned"); return NUGPR_ERR_INVALID; }
+  if (stride < 0) { set_error(std::string(name) + ": negative stride"); return NUGPR_ERR_INVALID; }
+  return NUGPR_OK;
+}
+
+Requests requests(const nugpr_adapter* p) {
+  return Requests{p->seq_offsets, p->adapter_of, p->n_rows, p->n_adapters > 0 ? p->n_seqs : 0, p->n_adapters};
+}
+
+template <class TR, bool AL>
+void launch_low(const LowArgs& a, int sides, hipStream_t s) {
+  const unsigned items = (unsigned)((a.q.n_rows >> LOW_LOG2) + a.q.n_seqs);
+  const int tiles = (a.rank + 15) / 16;
+  // (few pieces: more waves each, to share the width)
+  int waves = items * sides < 512 ? 16 : 4;
+  if (tiles > 2) waves = min(waves, 8);
+  const dim3 grid(items, sides), threads(64 * waves);
+  const size_t lds = (size_t)waves * 16 * 16 * (tiles <= 1 ? 1 : tiles <= 2 ? 2 : tiles <= 4 ? 4 : 8) * sizeof(float);
+  if (tiles <= 1) hipLaunchKernelGGL((k_low<TR, AL, 1>), grid, threads, lds, s, a);
+  else if (tiles <= 2) hipLaunchKernelGGL((k_low<TR, AL, 2>), grid, threads, lds, s, a);
+  else if (tiles <= 4) hipLaunchKernelGGL((k_low<TR, AL, 4>), grid, threads, lds, s, a);
+  else hipLaunchKernelGGL((k_low<TR, AL, 8>), grid, threads, lds, s, a);
+}
+
+template <class TR, int BM, int BN, int WM, int WN, bool NN, bool AL>
+void launch_tiles(const ProjectArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((k_project<TR, BM, BN, WM, WN, NN, AL>), dim3((a.n + BN - 1) / BN, (unsigned)((a.q.n_rows + BM - 1) / BM)), dim3(THREADS), 0, s, a);
+}
+
+template <class TR, bool NN, bool AL>
+void launch_project(const ProjectArgs& a, hipStream_t s) {
+  if (!NN && a.q.n_rows <= 64) {
+    const dim3 grid((a.n + 15) / 16, 1);
+    if (a.q.n_rows <= 16) hipLaunchKernelGGL((k_project_few<TR, 1, AL>), grid, dim3(FEW_THREADS), 0, s, a);
+    else if (a.q.n_rows <= 32) hipLaunchKernelGGL((k_project_few<TR, 2, AL>), grid, dim3(FEW_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((k_project_few<TR, 4, AL>), grid, dim3(FEW_THREADS), 0, s, a);
+    return;
+  }
+  const int64_t large = ((a.q.n_rows + 127) / 128) * ((a.n + 127) / 128);
+  if (a.n <= 32) launch_tiles<TR, 128, 32, 4, 1, NN, AL>(a, s);
+  else if (large < 256) launch_tiles<TR, 64, 64, 2, 2, NN, AL>(a, s);
+  else launch_tiles<TR, 128, 128, 2, 2, NN, AL>(a, s);
+}
+
+template <class TR, bool AL>
+void launch_grad(const GradArgs& a, const SumArgs& sum, hipStream_t s) {
+  const int tiles = (a.rank + 15) / 16;
+  const dim3 grid(a.side[0].tiles + a.side[1].tiles, a.q.n_adapters, sum.parts);
+  if (tiles <= 1) hipLaunchKernelGGL((k_adapter_grad<TR, 1, AL>), grid, dim3(THREADS), 0, s, a);
+  else if (tiles <= 2) hipLaunchKernelGGL((k_adapter_grad<TR, 2, AL>), grid, dim3(THREADS), 0, s, a);
+  else if (tiles <= 4) hipLaunchKernelGGL((k_adapter_grad<TR, 4, AL>), grid, dim3(THREADS), 0, s, a);
+  else hipLaunchKernelGGL((k_adapter_grad<TR, 8, AL>), grid, dim3(THREADS), 0, s, a);
+  if (sum.parts > 1) {
+    const int64_t most = sum.count[0] > sum.count[1] ? sum.count[0] : sum.count[1];
+    hipLaunchKernelGGL((k_sum_grads<TR>), dim3((unsigned)((most + THREADS - 1) / THREADS), 2), dim3(THREADS), 0, s, sum);
+  }
+}
+
+template <class TR, bool AL>
+int run_forward(const nugpr_adapter* p, const void* x, int64_t x_stride, void* y, hipStream_t s) {
+  const Requests q = requests(p);
+  LowArgs l{};
+  l.q = q; l.scale = (float)p->scale; l.rank = p->rank; l.padded = padded_rank(p);
+  l.side[0] = LowSide{x, p->A, static_cast<float*>(p->workspace), x_stride, p->dim_in};
+  if (q.n_seqs > 0) launch_low<TR, AL>(l, 1, s);
+  const ProjectArgs a{x, p->W, p->B, l.side[0].low, y, x_stride, q, p->dim_in, p->dim_out, p->rank, l.padded};
+  launch_project<TR, false, AL>(a, s);
+  NUGPR_HIP(hipGetLastError());
+  return NUGPR_OK;
+}
+
+template <class TR, bool AL>
+int run_backward(const nugpr_adapter* p, const void* x, int64_t x_stride, const void* dy, int64_t dy_stride, void* dx, void* dA, void* dB,
+                 hipStream_t s) {
+  const Requests q = requests(p);
+  char* ws = static_cast<char*>(p->workspace);
+  const size_t each = low_bytes(p);
+  float *low = reinterpret_cast<float*>(ws), *up = reinterpret_cast<float*>(ws + each);
+  LowArgs l{};
+  l.q = q; l.scale = (float)p->scale; l.rank = p->rank; l.padded = padded_rank(p);
+  l.side[0] = LowSide{x, p->A, low, x_stride, p->dim_in};
+  l.side[1] = LowSide{dy, p->B, up, dy_stride, p->dim_out};
+  if (q.n_seqs > 0 && q.n_rows > 0) launch_low<TR, AL>(l, 2, s);
+  if (dx && q.n_rows > 0) {
+    const ProjectArgs a{dy, p->W, p->A, up, dx, dy_stride, q, p->dim_out, p->dim_in, p->rank, l.padded};
+    launch_project<TR, true, AL>(a, s);
+  }
+  if (p->n_adapters > 0) {
+    GradArgs g{};
+    SumArgs sum{};
+    const int parts = grad_parts(p);
+    float* pa = reinterpret_cast<float*>(ws + 2 * each);
+    float* pb = reinterpret_cast<float*>(ws + 2 * each + part_bytes(p, p->dim_in));
+    g.q = q; g.rank = p->rank; g.padded = l.padded;
+    g.per = (q.n_rows + parts - 1) / parts;
+    g.side[0] = GradSide{x, up, dA, parts > 1 ? pa : nullptr, x_stride, p->dim_in, grad_tiles(p->dim_in)};
+    g.side[1] = GradSide{dy, low, dB, parts > 1 ? pb : nullptr, dy_stride, p->dim_out, grad_tiles(p->dim_out)};
+    sum.parts = parts;
+    sum.part[0] = pa; sum.part[1] = pb; sum.out[0] = dA; sum.out[1] = dB;
+    sum.count[0] = (int64_t)p->n_adapters * p->rank * p->dim_in;
+    sum.count[1] = (int64_t)p->n_adapters * p->rank * p->dim_out;
+    launch_grad<TR, AL>(g, sum, s);
+  }
+  NUGPR_HIP(hipGetLastError());
+  return NUGPR_OK;
+}
+
+}  // namespace
+
+}  // namespace nugpr
+
+using namespace nugpr;
+
+#define NUGPR_TRY(call)                 \
+  do {                                  \
+    const int c__ = (call);             \
+    if (c__ != NUGPR_OK) return c__;    \
+  } while (0)
+
+extern "C" {
+
+size_t nugpr_adapter_workspace_bytes(const nugpr_adapter* p, int32_t backward) {
+  if (check(p) != NUGPR_OK) return 0;
+  return 256 + (backward ? 2 * low_bytes(p) + part_bytes(p, p->dim_in) + part_bytes(p, p->dim_out) : low_bytes(p));
+}
+
+int nugpr_adapter_forward(const nugpr_adapter* p, const void* x, int64_t x_stride, void* y, void* stream) {
+  NUGPR_TRY(check(p));
+  NUGPR_TRY(check_call(p, low_bytes(p)));
+  if (p->n_rows == 0) return NUGPR_OK;
+  const size_t z = value_size(p);
+  NUGPR_TRY(check_rows(x, x_stride, "x", z));
+  NUGPR_TRY(check_rows(y, p->dim_out, "y", z));
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const bool al = wide(x, x_stride, z) && wide(p->W, p->dim_in, z) && wide(p->A, p->dim_in, z) && wide(p->B, p->dim_out, z) && wide(y, p->dim_out, z);
+  if (p->dtype == NUGPR_BFLOAT16) return al ? run_forward<Bf16, true>(p, x, x_stride, y, s) : run_forward<Bf16, false>(p, x, x_stride, y, s);
+  return al ? run_forward<F32, true>(p, x, x_stride, y, s) : run_forward<F32, false>(p, x, x_stride, y, s);
+}
+
+int nugpr_adapter_backward(const nugpr_adapter* p, const void* x, int64_t x_stride, const void* d_y, int64_t dy_stride, void* dx, void* dA,
+                           void* dB, void* stream) {
+  NUGPR_TRY(check(p));
+  NUGPR_TRY(check_call(p, 2 * low_bytes(p) + part_bytes(p, p->dim_in) + part_bytes(p, p->dim_out)));
+  const size_t z = value_size(p);
+  if (p->n_rows > 0) {
+    NUGPR_TRY(check_rows(x, x_stride, "x", z));
+    NUGPR_TRY(check_rows(d_y, dy_stride, "d_y", z));
+  }
+  if (p->n_adapters > 0) {
+    NUGPR_TRY(check_rows(dA, p->dim_in, "dA", z));
+    NUGPR_TRY(check_rows(dB, p->dim_out, "dB", z));
+  }
+  if (dx) NUGPR_TRY(check_rows(dx, p->dim_in, "dx", z));
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const bool al = wide(x, x_stride, z) && wide(d_y, dy_stride, z) && wide(p->W, p->dim_in, z) && wide(p->A, p->dim_in, z) &&
+                  wide(p->B, p->dim_out, z) && wide(dx, p->dim_in, z);
+  if (p->dtype == NUGPR_BFLOAT16)
+    return al ? run_backward<Bf16, true>(p, x, x_stride, d_y, dy_stride, dx, dA, dB, s) : run_backward<Bf16, false>(p, x, x_stride, d_y, dy_stride, dx, dA, dB, s);
+  return al ? run_backward<F32, true>(p, x, x_stride, d_y, dy_stride, dx, dA, dB, s) : run_backward<F32, false>(p, x, x_stride, d_y, dy_stride, dx, dA, dB, s);
+}
+
+}  // extern "C"

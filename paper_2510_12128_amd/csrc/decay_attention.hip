@@ -15,6 +15,7 @@
 
 #include "matrix_core.h"
 #include "nugpr_internal.h"
+#include "packed_rows.h"
 
 namespace nugpr {
 
@@ -48,28 +49,6 @@ struct ScanArgs {
   int span_log2;          // rows of a span
   int items;              // spans that there may be
 };
-
-__device__ int64_t clamped(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
-
-// Sequence s has the span numbers from (offsets[s] >> span_log2) + s on: with ceil(rows / span) spans it ends before the next
-// one's, so no table of them is needed.  Finds the sequence of a span: the last one that begins at or before it.
-__device__ int sequence_of(const int64_t* off, int n_seqs, int64_t n_rows, int span_log2, int item) {
-  const int lane = threadIdx.x & 63;
-  int lo = 0, hi = n_seqs;                    // first number lies in [lo, hi)
-  while (hi - lo > 64) {                      // 64 probes a round
-    const int step = (hi - lo + 63) / 64;
-    const int at = lo + lane * step;
-    const bool before = at < hi && (clamped(off[at], 0, n_rows) >> span_log2) + at <= item;
-    const int n = __popcll(__ballot(before));
-    if (n == 0) return -1;
-    const int from = lo + (n - 1) * step;
-    hi = min(hi, from + step);
-    lo = from;
-  }
-  const int at = lo + lane;
-  const bool before = at < hi && (clamped(off[at], 0, n_rows) >> span_log2) + at <= item;
-  return lo + __popcll(__ballot(before)) - 1;
-}
 
 __device__ float log_of(const float* log_decay, int h) {
   const float g = log_decay[h];

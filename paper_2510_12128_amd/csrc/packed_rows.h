@@ -1,0 +1,51 @@
+// Sequences (or requests) packed one after the other: sequence s owns rows offsets[s] .. offsets[s + 1] - 1.  Offsets stay on
+// the device; kernels clamp them to the rows that there are, so that no offset leads out of bounds.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace nugpr {
+
+__device__ inline int64_t clamped(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// Sequence s has the piece numbers from (offsets[s] >> piece_log2) + s on: with ceil(rows / piece) pieces it ends before the next
+// one's, so no table of them is needed.  Finds the sequence of a piece: the last one that begins at or before it.
+__device__ inline int sequence_of(const int64_t* off, int n_seqs, int64_t n_rows, int piece_log2, int item) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n_seqs;                    // first number lies in [lo, hi)
+  while (hi - lo > 64) {                      // 64 probes a round
+    const int step = (hi - lo + 63) / 64;
+    const int at = lo + lane * step;
+    const bool before = at < hi && (clamped(off[at], 0, n_rows) >> piece_log2) + at <= item;
+    const int n = __popcll(__ballot(before));
+    if (n == 0) return -1;
+    const int from = lo + (n - 1) * step;
+    hi = min(hi, from + step);
+    lo = from;
+  }
+  const int at = lo + lane;
+  const bool before = at < hi && (clamped(off[at], 0, n_rows) >> piece_log2) + at <= item;
+  return lo + __popcll(__ballot(before)) - 1;
+}
+
+// The sequence that owns a row: the last one that begins at or before it, if it reaches that far; else -1.  (All lanes of a wave
+// with the same row.)
+__device__ inline int owner_of(const int64_t* off, int n_seqs, int64_t row) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n_seqs;
+  while (hi - lo > 64) {
+    const int step = (hi - lo + 63) / 64;
+    const int at = lo + lane * step;
+    const int n = __popcll(__ballot(at < hi && off[at] <= row));
+    if (n == 0) return -1;
+    const int from = lo + (n - 1) * step;
+    hi = min(hi, from + step);
+    lo = from;
+  }
+  const int at = lo + lane;
+  const int s = lo + __popcll(__ballot(at < hi && off[at] <= row)) - 1;
+  return s >= 0 && row < off[s + 1] ? s : -1;
+}
+
+}  // namespace nugpr

@@ -6,8 +6,8 @@ from __future__ import annotations
 
 import ctypes as C
 
-from .binding import (DecayAttention, Heads, NUGPR_BFLOAT16, NUGPR_ERR_INVALID, NUGPR_FLOAT32, NugprError, _check,
-                      load_library)
+from .binding import (Adapter, DecayAttention, Heads, NUGPR_BFLOAT16, NUGPR_ERR_INVALID, NUGPR_FLOAT32, NugprError,
+                      _check, load_library)
 
 
 def _refuse(what):
@@ -140,3 +140,58 @@ def nugpr_decay_attention_step(q, k, v, log_decay, state, slots=None, scale=1.0)
             C.byref(p), C.byref(_heads(q, "q")), C.byref(_heads(k, "k")), C.byref(_heads(v, "v")), st,
             None if slots is None else slots.data_ptr(), C.byref(_heads(o, "o")), _stream(torch, q.device)))
     return o
+
+
+def _adapter(x, W, A, B, offsets, adapter_of, scale, backward):
+    """The problem's structure and what has to stay alive during the call."""
+    torch, types = _types()
+    if x.dtype not in types:
+        _refuse(f"x must be float32 or bfloat16, not {x.dtype}")
+    if W.dim() != 2 or A.dim() != 3:
+        _refuse("W must be dim_out x dim_in and A adapters x rank x dim_in")
+    _tensor(x, "x", x, (None, W.shape[1]), x.dtype)
+    _inner(x, "x")
+    _dense(W, "W", x, (None, None), x.dtype)
+    _dense(A, "A", x, (None, None, W.shape[1]), x.dtype)
+    _dense(B, "B", x, (A.shape[0], A.shape[1], W.shape[0]), x.dtype)
+    _dense(offsets, "seq_offsets", x, (None,), torch.int64)
+    if offsets.shape[0] < 1:
+        _refuse("seq_offsets must have n_seqs + 1 entries")
+    p = Adapter()
+    p.dtype, p.dim_in, p.dim_out, p.rank, p.n_adapters = types[x.dtype], W.shape[1], W.shape[0], A.shape[1], A.shape[0]
+    p.n_rows, p.n_seqs, p.seq_offsets = x.shape[0], offsets.shape[0] - 1, offsets.data_ptr()
+    if adapter_of is not None:
+        p.adapter_of = _dense(adapter_of, "adapter_of", x, (p.n_seqs,), torch.int32).data_ptr()
+    p.W, p.A, p.B, p.scale = W.data_ptr(), A.data_ptr(), B.data_ptr(), float(scale)
+    need = load_library().nugpr_adapter_workspace_bytes(C.byref(p), backward)
+    if need == 0:
+        raise NugprError(NUGPR_ERR_INVALID, load_library().nugpr_last_error_string().decode())
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    p.workspace, p.workspace_bytes = ws.data_ptr(), need
+    return torch, p, ws
+
+
+def nugpr_adapter_forward(x, W, A, B, seq_offsets, adapter_of=None, scale=1.0):
+    """y = x W^T + scale (x A_a^T) B_a, a = adapter_of[s] (None: s) for the rows seq_offsets[s] .. seq_offsets[s + 1] - 1.
+
+    x (rows, dim_in), W (dim_out, dim_in), A (adapters, rank, dim_in), B (adapters, rank, dim_out): float32 or bfloat16, W, A
+    and B contiguous; seq_offsets (n_seqs + 1,) int64; adapter_of (n_seqs,) int32.  Returns y (rows, dim_out)."""
+    torch, p, ws = _adapter(x, W, A, B, seq_offsets, adapter_of, scale, 0)
+    y = torch.empty((x.shape[0], p.dim_out), dtype=x.dtype, device=x.device)
+    with torch.cuda.device(x.device):
+        _check(load_library().nugpr_adapter_forward(C.byref(p), x.data_ptr(), x.stride(0), y.data_ptr(),
+                                                    _stream(torch, x.device)))
+    return y
+
+
+def nugpr_adapter_backward(x, W, A, B, seq_offsets, d_y, adapter_of=None, scale=1.0):
+    """Gradients of nugpr_adapter_forward's x, A and B, in their type, from d_y; W is fixed."""
+    torch, p, ws = _adapter(x, W, A, B, seq_offsets, adapter_of, scale, 1)
+    _tensor(d_y, "d_y", x, (x.shape[0], p.dim_out), x.dtype)
+    _inner(d_y, "d_y")
+    dx = torch.empty((x.shape[0], p.dim_in), dtype=x.dtype, device=x.device)
+    dA, dB = torch.empty_like(A), torch.empty_like(B)
+    with torch.cuda.device(x.device):
+        _check(load_library().nugpr_adapter_backward(C.byref(p), x.data_ptr(), x.stride(0), d_y.data_ptr(), d_y.stride(0),
+                                                     dx.data_ptr(), dA.data_ptr(), dB.data_ptr(), _stream(torch, x.device)))
+    return dx, dA, dB
