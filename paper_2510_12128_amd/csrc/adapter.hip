@@ -243,14 +243,24 @@ __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
         Frag wf[NTL];
 #pragma unroll
         for (int n = 0; n < NTL; ++n) wf[n] = TR::col_frag(sB, LDN, 0, wn + 16 * n, i, kg);
+        // (an adapter may hold values that are not finite: they are for the rows of its own requests, where a zero row of h
+        // would make them NaN)
 #pragma unroll
-        for (int part = 0; part < TR::S_PARTS; ++part)
+        for (int m = 0; m < MT; ++m) {
+          const int row = wm + 16 * m + i;
+          const bool own = row >= rlo && row < rhi;
+          Frag xf[TR::S_PARTS];
 #pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            const Frag xf = TR::row_frag(sA + (wm + 16 * m + i) * LDA, part * KS, kg);
+          for (int part = 0; part < TR::S_PARTS; ++part) xf[part] = TR::row_frag(sA + (wm + 16 * m + i) * LDA, part * KS, kg);
 #pragma unroll
-            for (int n = 0; n < NTL; ++n) acc[n][m] = TR::mfma(wf[n], xf, acc[n][m]);
+          for (int n = 0; n < NTL; ++n) {
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int part = 0; part < TR::S_PARTS; ++part) v = TR::mfma(wf[n], xf[part], v);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[n][m][r] += own ? v[r] : 0.f;
           }
+        }
       }
     }
   }
