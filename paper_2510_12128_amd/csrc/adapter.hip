@@ -249,14 +249,14 @@ __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
         for (int m = 0; m < MT; ++m) {
           const int row = wm + 16 * m + i;
           const bool own = row >= rlo && row < rhi;
-          Frag xf[TR::S_PARTS];
+          Frag xf[TR::LOW_PARTS];
 #pragma unroll
-          for (int part = 0; part < TR::S_PARTS; ++part) xf[part] = TR::row_frag(sA + (wm + 16 * m + i) * LDA, part * KS, kg);
+          for (int part = 0; part < TR::LOW_PARTS; ++part) xf[part] = TR::row_frag(sA + (wm + 16 * m + i) * LDA, part * KS, kg);
 #pragma unroll
           for (int n = 0; n < NTL; ++n) {
             f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int part = 0; part < TR::S_PARTS; ++part) v = TR::mfma(wf[n], xf[part], v);
+            for (int part = 0; part < TR::LOW_PARTS; ++part) v = TR::mfma(wf[n], xf[part], v);
 #pragma unroll
             for (int r = 0; r < 4; ++r) acc[n][m][r] += own ? v[r] : 0.f;
           }
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(THREADS) void k_adapter_grad(const GradArgs a) {
   constexpr int KS = TR::KS, E = TR::E, PAD = 16 / sizeof(T), LDX = GRAD_COLS + PAD, LDJ = 16 * JT + PAD;
   constexpr int X = GRAD_ROWS * GRAD_COLS / E / THREADS;
   __shared__ __align__(16) T sX[GRAD_ROWS * LDX];
-  __shared__ __align__(16) T sL[TR::S_PARTS][GRAD_ROWS * LDJ];
+  __shared__ __align__(16) T sL[TR::LOW_PARTS][GRAD_ROWS * LDJ];
   const int side = (int)blockIdx.x < a.side[0].tiles ? 0 : 1;
   const GradSide& sd = a.side[side];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, kg = lane >> 4;
@@ -413,7 +413,7 @@ __global__ __launch_bounds__(THREADS) void k_adapter_grad(const GradArgs a) {
           if (row < rows && col < a.padded) w = *reinterpret_cast<const f32x4*>(sd.low + (r0 + row) * a.padded + col);
           if constexpr (E == 8) {
             *reinterpret_cast<u32x2*>(sL[0] + row * LDJ + col) = u32x2{two_upper(w[0], w[1]), two_upper(w[2], w[3])};
-            *reinterpret_cast<u32x2*>(sL[TR::S_PARTS - 1] + row * LDJ + col) =
+            *reinterpret_cast<u32x2*>(sL[TR::LOW_PARTS - 1] + row * LDJ + col) =
                 u32x2{two_bf16(w[0] - upper(w[0]), w[1] - upper(w[1])), two_bf16(w[2] - upper(w[2]), w[3] - upper(w[3]))};
           } else {
             *reinterpret_cast<f32x4*>(sL[0] + row * LDJ + col) = w;
@@ -426,7 +426,7 @@ __global__ __launch_bounds__(THREADS) void k_adapter_grad(const GradArgs a) {
 #pragma unroll
           for (int m = 0; m < 2; ++m) xf[m] = TR::col_frag(sX, LDX, k, 32 * wave + 16 * m, i, kg);
 #pragma unroll
-          for (int part = 0; part < TR::S_PARTS; ++part)
+          for (int part = 0; part < TR::LOW_PARTS; ++part)
 #pragma unroll
             for (int j = 0; j < JT; ++j) {
               const Frag lf = TR::col_frag(sL[part], LDJ, k, 16 * j, i, kg);

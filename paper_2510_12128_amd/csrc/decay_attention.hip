@@ -56,85 +56,123 @@ __device__ float log_of(const float* log_decay, int h) {
 }
 
 // lam^n as the sum of two float32: the powers of a block multiply up over a long sequence
-__device__ void power(float g, int n, float& hi, float& lo) {
+__device__ void power(float g, double n, float& hi, float& lo) {
   const double p = exp((double)g * n);
   hi = (float)p;
   lo = (float)(p - (double)hi);
 }
 
+// (a value that all lanes have, in a scalar register)
+__device__ inline double same_in_all(double x) {
+  const u32x2 v = __builtin_bit_cast(u32x2, x);
+  return __builtin_bit_cast(double, (u32x2{(uint32_t)__builtin_amdgcn_readfirstlane((int)v[0]), (uint32_t)__builtin_amdgcn_readfirstlane((int)v[1])}));
+}
+
 template <class TR, int D>
 struct Tile {
-  static constexpr int LD = D + (TR::E == 8 ? 8 : 4);       // 16 rows of a 16-byte column on different banks
+  static constexpr int NT = 1;                              // a wave's tiles of 16 of the state's columns
+  static constexpr int WAVES = D / 16 / NT;
   static constexpr int A_ROW = D / TR::E;                   // threads a row
-  static constexpr int PASS = THREADS / A_ROW;              // rows that one load of all threads covers
+  static constexpr int PASS = 64 * WAVES / A_ROW;           // rows that one load of all threads covers
   static constexpr int N = C / PASS;
 };
 
-// Rows first + dir r, r < cnt, of one head, `width` columns: 16 bytes a thread and pass; zero elsewhere.
-template <class TR, int D, bool AL>
-__device__ inline void fetch(u32x4* r, const void* base, int64_t stride, int64_t first, int dir, int cnt, int width) {
+// A block's rows in an array, cnt of them, as a buffer that begins at their lowest address and ends behind the last one: what lies
+// beyond reads as zero and is not stored.  `at`: the thread's byte offset from row 0 of the block (place_in); `pass`, in
+// bytes, is added for every further pass.  Only where AL; else everything by 64-bit pointers, value by value.
+template <class TR, int D>
+struct Window {
+  __amdgpu_buffer_rsrc_t rsrc;
+  uint32_t from, pass;
+  __device__ Window(const typename TR::T* base, int64_t stride, int dir, int cnt, int width) {
+    constexpr int S = sizeof(typename TR::T);
+    const int64_t below = dir > 0 ? 0 : (cnt - 1) * stride;
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<typename TR::T*>(base - below), 0, (int)(((cnt - 1) * stride + width) * S), 0x00027000);
+    from = (uint32_t)below * S;
+    pass = (uint32_t)(dir * Tile<TR, D>::PASS) * (uint32_t)stride * S;
+  }
+  __device__ u32x4 load(uint32_t at, int p) const {
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + (from + p * pass), 0, 0));
+  }
+  __device__ void store(uint32_t at, int p, u32x4 v) const { __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, at + (from + p * pass), 0, 0); }
+};
+
+template <class TR, int D>
+__device__ inline uint32_t place_in(int tid, int64_t stride, int dir, int width) {
   using L = Tile<TR, D>;
-  const int col = (threadIdx.x % L::A_ROW) * TR::E, row0 = threadIdx.x / L::A_ROW;
+  const int col = tid % L::A_ROW * TR::E;
+  // (columns beyond the width: beyond any buffer)
+  return col < width ? (uint32_t)(dir * (tid / L::A_ROW)) * (uint32_t)stride * (uint32_t)sizeof(typename TR::T) + col * (uint32_t)sizeof(typename TR::T)
+                     : 0x80000000u;
+}
+
+// Rows of a block, 16 bytes a thread and pass; zero from row cnt and column `width` on.
+template <class TR, int D, bool AL>
+__device__ inline void fetch(u32x4* r, int tid, const typename TR::T* base, int64_t stride, int dir, uint32_t at, int cnt, int width) {
+  using L = Tile<TR, D>;
+  if constexpr (AL) {
+    const Window<TR, D> w(base, stride, dir, cnt, width);
 #pragma unroll
-  for (int p = 0; p < L::N; ++p) {
-    const int row = row0 + p * L::PASS;
-    u32x4 v = {0, 0, 0, 0};
-    if (row < cnt && col < width) {
-      const typename TR::T* x = static_cast<const typename TR::T*>(base) + (first + (int64_t)dir * row) * stride + col;
-      if constexpr (AL) {
-        v = *reinterpret_cast<const u32x4*>(x);
-      } else if constexpr (TR::E == 8) {
+    for (int p = 0; p < L::N; ++p) r[p] = w.load(at, p);
+  } else {
+    const int col = (tid % L::A_ROW) * TR::E, row0 = tid / L::A_ROW;
+    const typename TR::T* x = base + (int64_t)dir * row0 * stride + col;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (col + j < width) v[j >> 1] |= (uint32_t)x[j] << (16 * (j & 1));
-      } else {
+    for (int p = 0; p < L::N; ++p, x += dir * L::PASS * stride) {
+      u32x4 v = {0, 0, 0, 0};
+      if (row0 + p * L::PASS < cnt) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (col + j < width) v[j] = __builtin_bit_cast(uint32_t, x[j]);
+        for (int j = 0; j < TR::E; ++j)
+          if (col + j < width) {
+            if constexpr (TR::E == 8) v[j >> 1] |= (uint32_t)x[j] << (16 * (j & 1));
+            else v[j] = __builtin_bit_cast(uint32_t, x[j]);
+          }
       }
+      r[p] = v;
     }
-    r[p] = v;
   }
 }
 
-template <class TR, int D, bool PLACED>
-__device__ inline void put(typename TR::T* tile, const u32x4* r) {
+// the block into a tile in LDS; `at`: the thread's byte offset in it for the first pass
+template <class TR, int D>
+__device__ inline void put(typename TR::T* tile, int at, const u32x4* r) {
   using L = Tile<TR, D>;
-  const int col = (threadIdx.x % L::A_ROW) * TR::E, row0 = threadIdx.x / L::A_ROW;
+  static_assert(L::PASS % 16 == 0, "rows of one thread are permuted alike");
 #pragma unroll
-  for (int p = 0; p < L::N; ++p) {
-    typename TR::T* row = tile + (row0 + p * L::PASS) * L::LD;
-    if constexpr (PLACED) TR::store_row(row, col, r[p]);
-    else *reinterpret_cast<u32x4*>(row + col) = r[p];
-  }
+  for (int p = 0; p < L::N; ++p)
+    *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(tile) + at + p * L::PASS * D * (int)sizeof(typename TR::T)) = r[p];
 }
 
 // One workgroup walks one span of one sequence and key / value head in blocks of C rows; the state stays in accumulator
-// registers, its columns split among the four waves.  WALK: writes o from given start states; else: what the span adds to
-// the state, for k_span_join.
-// Per block and head: P^T = K Q^T (each wave 16 rows of Q), masked and decayed, goes through LDS; o^T = S^T Q^T and V^T P^T with
-// the wave's columns of S and V; S += K^T (w V).  S is read as an operand where it lies (matrix_core.h).  In bfloat16 the state
-// takes part with 16 of its bits and P with 8; w V, which is summed into the float32 state, with all 24.
+// registers, 16 or 32 of its columns a wave.  WALK: writes o from given start states; else: what the span adds to
+// the state, for k_span_join.  SUM: some role's o is a sum over heads of k and v (gk > 1).
+// Per block and head: P^T = K Q^T (each wave tiles of 16 rows of Q), masked and decayed, goes through LDS; o^T = S^T Q^T and V^T P^T with
+// the wave's columns of S and V; S += K^T (w V).  S is read as an operand where it lies (matrix_core.h).  In bfloat16 P and
+// the operand that S is read as are rounded to it, as o is in the end: together that is 1.4 times the error of the last
+// rounding alone, where 16 bits of S would cost twice the products and six times the conversions; w V, which is summed into the
+// float32 state, keeps all 24 bits.
 // Values that are not finite: rows s > t must not touch o_t, but 0 x NaN in the masked part of P would; a block whose V
 // has such a value takes P V row by row.
-template <class TR, int D, bool AL, bool WALK>
-__global__ __launch_bounds__(THREADS, 2) void k_decay_scan(const ScanArgs a) {
+template <class TR, int D, bool AL, bool WALK, bool SUM>
+__global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) void k_decay_scan(const ScanArgs a) {
   using T = typename TR::T;
   using Frag = typename TR::Frag;
   using L = Tile<TR, D>;
   constexpr int KS = TR::KS, KT = KS / 16;       // accumulator tiles of a contraction step
-  constexpr int NT = D / 64;                     // tiles of a wave's columns
+  constexpr int NT = L::NT, THREADS = 64 * L::WAVES, HALVES = L::WAVES / 4;     // waves that share 16 rows of Q in K Q^T
   constexpr int PLD = C + (TR::E == 8 ? 8 : 4);
-  __shared__ __align__(16) T sK[C * L::LD];
-  __shared__ __align__(16) T sV[C * L::LD];
-  __shared__ __align__(16) T sQ[WALK ? C * L::LD : 8];
+  __shared__ __align__(16) T sK[C * D];
+  __shared__ __align__(16) T sV[C * D];
+  __shared__ __align__(16) T sQ[WALK ? C * D : 8];
   __shared__ __align__(16) T sP[WALK ? C * PLD : 8];
-  __shared__ __align__(16) float sLam[C + 4];    // lam^i
+  __shared__ __align__(16) float sLam[2 * C + 4];    // lam^n at C + n; zero before C
+  __shared__ __align__(16) float sPw[WALK ? 2 * C + 4 : 4];    // the same, as P is multiplied by it
   __shared__ __align__(16) float sW[C];          // weights of the block's rows in the state
   __shared__ int sOdd;
 
   const ScanRole& ro = a.role[blockIdx.y];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, kg = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int i = tid & 15, kg = (tid >> 4) & 3;
   const int h = blockIdx.x % a.kv, item = blockIdx.x / a.kv;
 
   if (WALK && item == a.items) {                 // rows that no sequence owns
@@ -159,14 +197,19 @@ __global__ __launch_bounds__(THREADS, 2) void k_decay_scan(const ScanArgs a) {
   const int e = ro.back;
 
   const float g = log_of(a.log_decay, h);
-  for (int n = tid; n <= C; n += THREADS) sLam[n] = (float)exp((double)g * n);
+  for (int n = tid; n <= 2 * C; n += THREADS) {
+    sLam[n] = n < C ? 0.f : (float)exp((double)g * (n - C));
+    if (WALK) sPw[n] = ro.wscale * ro.oscale * sLam[n];
+  }
   if (tid == 0) sOdd = 0;
-  float lam_hi, lam_lo;
-  power(g, C, lam_hi, lam_lo);
+  // lam^C in every block is rounded so that the product of them all stays within a rounding of its exact value: a block's
+  // rounding error would otherwise add up over the hundreds of blocks that a slowly decaying state remembers
+  const double lam_block = same_in_all(exp((double)g * C)), lam_inv = same_in_all(lam_block > 1e-30 ? 1.0 / lam_block : 0.0);
+  double drift = 1.0;
 
-  // the state: rows 16 m + 4 kg .., columns col0 + 16 n + i
+  // the state: rows acc_row(m, kg) .., columns col0 + 16 n + i
   f32x4 S[D / 16][NT];
-  const int col0 = wave * (D / 4);
+  const int col0 = wave * 16 * NT;
   const int64_t s_size = (int64_t)ro.dk * ro.dv;
   const int s_r = ro.s_trans ? 1 : ro.dv, s_c = ro.s_trans ? ro.dk : 1;
   const float* from = !WALK ? nullptr
@@ -179,50 +222,92 @@ __global__ __launch_bounds__(THREADS, 2) void k_decay_scan(const ScanArgs a) {
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int row = 16 * m + 4 * kg + r, col = col0 + 16 * n + i;
+        const int row = TR::acc_row(m, kg) + r, col = col0 + 16 * n + i;
         S[m][n][r] = have && row < ro.dk && col < ro.dv ? from[row * s_r + col * s_c] : 0.f;
       }
 
-  const int gq = WALK ? ro.gq : 1, gk = ro.gk, heads = max(gq, gk);
+  const int gq = WALK ? ro.gq : 1, gk = SUM ? ro.gk : 1, heads = max(gq, gk);
   const int blocks = (n_tok + C - 1) / C;
   const int64_t first = e ? hi - 1 - c0 : lo + c0;
   const int dir = e ? -1 : 1;
-  const T* qb = static_cast<const T*>(ro.q) + (int64_t)h * ro.gq * ro.q_head;
-  const T* kb = static_cast<const T*>(ro.k) + (int64_t)h * ro.gk * ro.k_head;
-  const T* vb = static_cast<const T*>(ro.v) + (int64_t)h * ro.gk * ro.v_head;
+  // row 0 of the block to load next in the arrays, and a thread's places
+  const int row0 = tid / L::A_ROW, col_in = tid % L::A_ROW * TR::E;
+  const T* q_at = static_cast<const T*>(ro.q) + (int64_t)h * ro.gq * ro.q_head + first * ro.q_row;
+  const T* k_at = static_cast<const T*>(ro.k) + (int64_t)h * ro.gk * ro.k_head + first * ro.k_row;
+  const T* v_at = static_cast<const T*>(ro.v) + (int64_t)h * ro.gk * ro.v_head + first * ro.v_row;
+  T* o_at = WALK ? static_cast<T*>(ro.o) + (int64_t)h * ro.gq * ro.o_head + first * ro.o_row : nullptr;
+  const uint32_t q_off = place_in<TR, D>(tid, ro.q_row, dir, ro.dk), k_off = place_in<TR, D>(tid, ro.k_row, dir, ro.dk),
+                 v_off = place_in<TR, D>(tid, ro.v_row, dir, ro.dv), o_off = place_in<TR, D>(tid, ro.o_row, dir, ro.dv);
+  // and in LDS
+  int put_at = TR::template unit<D>(row0, col_in), along_at = TR::template along_at<D>(i, kg);
+  int v_cols[TR::ACROSS], k_cols[TR::ACROSS];
+  TR::template columns_at<D>(v_cols, col0, i, kg);
+  TR::template acc_columns_at<D>(k_cols, i, kg);
   u32x4 rq[WALK ? L::N : 1], rk[L::N], rv[L::N];
   auto fetch_block = [&](int b, int m) {
-    const int64_t at = first + (int64_t)dir * b * C;
     const int cnt = min(C, n_tok - b * C);
     if (gk > 1 || m == 0) {
-      fetch<TR, D, AL>(rk, kb + m * ro.k_head, ro.k_row, at, dir, cnt, ro.dk);
-      fetch<TR, D, AL>(rv, vb + m * ro.v_head, ro.v_row, at, dir, cnt, ro.dv);
+      fetch<TR, D, AL>(rk, tid, k_at + m * ro.k_head, ro.k_row, dir, k_off, cnt, ro.dk);
+      fetch<TR, D, AL>(rv, tid, v_at + m * ro.v_head, ro.v_row, dir, v_off, cnt, ro.dv);
     }
     if constexpr (WALK)
-      if (gq > 1 || m == 0) fetch<TR, D, AL>(rq, qb + m * ro.q_head, ro.q_row, at, dir, cnt, ro.dk);
+      if (gq > 1 || m == 0) fetch<TR, D, AL>(rq, tid, q_at + m * ro.q_head, ro.q_row, dir, q_off, cnt, ro.dk);
+    if (m + 1 == heads) {
+      k_at += dir * C * ro.k_row;
+      v_at += dir * C * ro.v_row;
+      if constexpr (WALK) q_at += dir * C * ro.q_row;
+    }
   };
   f32x4 o[NT][C / 16];
+  // A block's o goes into Q's tile, which nobody reads any more by then, and on to memory at the beginning of the next step, by the
+  // threads that write the next rows of Q to the same places: whole lines, and ahead of that step's loads (who waits for loads
+  // waits for what was stored before them, too, and would wait for the stores' way to memory right behind them).
+  T* out_at = nullptr;
+  int out_cnt = 0;
+  auto flush = [&]() {
+    const char* tile = reinterpret_cast<const char*>(sQ) + put_at;
+    if constexpr (AL) {
+      const Window<TR, D> w(out_at, ro.o_row, dir, out_cnt, ro.dv);
+#pragma unroll
+      for (int p = 0; p < L::N; ++p) w.store(o_off, p, *reinterpret_cast<const u32x4*>(tile + p * L::PASS * D * (int)sizeof(T)));
+    } else {
+      T* x = out_at + (int64_t)dir * row0 * ro.o_row + col_in;
+#pragma unroll
+      for (int p = 0; p < L::N; ++p, x += dir * L::PASS * ro.o_row)
+        if (row0 + p * L::PASS < out_cnt)
+#pragma unroll
+          for (int j = 0; j < TR::E; ++j)
+            if (col_in + j < ro.dv) x[j] = reinterpret_cast<const T*>(tile + p * L::PASS * D * (int)sizeof(T))[j];
+    }
+    out_cnt = 0;
+  };
   if (blocks > 0) fetch_block(0, 0);
   int kv_step = 0;
   for (int b = 0; b < blocks; ++b) {
     const int cnt = min(C, n_tok - b * C);
     for (int m = 0; m < heads; ++m) {
+      // (what follows from these is cheaper made anew than kept in registers from step to step)
+      asm volatile("" : "+v"(i), "+v"(kg), "+v"(put_at), "+v"(along_at));
+#pragma unroll
+      for (int x = 0; x < TR::ACROSS; ++x) asm volatile("" : "+v"(v_cols[x]), "+v"(k_cols[x]));
       const bool kv_new = gk > 1 || m == 0, q_new = WALK && (gq > 1 || m == 0);
       __syncthreads();
+      if constexpr (WALK)
+        if (out_cnt > 0) flush();
       if (kv_new) {
         ++kv_step;
-        put<TR, D, true>(sK, rk);
-        put<TR, D, false>(sV, rv);
+        put<TR, D>(sK, put_at, rk);
+        put<TR, D>(sV, put_at, rv);
         if (WALK) {
-          bool odd = false;
+          uint32_t odd = 0;
 #pragma unroll
           for (int p = 0; p < L::N; ++p) odd |= TR::odd(rv[p]);
-          if (odd) sOdd = kv_step;
+          if (odd & TR::SIGN) sOdd = kv_step;
         }
-        if (tid < C) sW[tid] = tid < cnt ? ro.wscale * (float)sLam[cnt - 1 - tid + e] : 0.f;
+        if (tid < C) sW[tid] = tid < cnt ? ro.wscale * sLam[C + cnt - 1 - tid + e] : 0.f;
       }
       if constexpr (WALK)
-        if (q_new) put<TR, D, true>(sQ, rq);
+        if (q_new) put<TR, D>(sQ, put_at, rq);
       __syncthreads();
       if (m + 1 < heads) fetch_block(b, m + 1);
       else if (b + 1 < blocks) fetch_block(b + 1, 0);
@@ -230,22 +315,26 @@ __global__ __launch_bounds__(THREADS, 2) void k_decay_scan(const ScanArgs a) {
       const bool end = gq == 1 || m + 1 == heads;          // the state moves on
       const bool keep = !WALK || b + 1 < blocks || (last && ro.s_out);
       if constexpr (WALK) {
-        // P^T, rows of K x the wave's 16 rows of Q
-        const int t = 16 * wave + i;
+        // P^T, rows of K x 16 rows of Q
+        const int qt = wave / HALVES, t = 16 * qt + i;
         Frag qf[D / KS];
 #pragma unroll
-        for (int k = 0; k < D / KS; ++k) qf[k] = TR::row_frag(sQ + t * L::LD, k * KS, kg);
+        for (int k = 0; k < D / KS; ++k) qf[k] = TR::template along<D>(sQ, along_at, 16 * qt, k * KS);
 #pragma unroll
-        for (int st = 0; st < C / 16; ++st) {
-          if (st > (KT == 2 ? wave | 1 : wave)) break;     // (a product of 32 rows reads the masked tile too)
+        for (int x = 0; x < C / 16 / HALVES; ++x) {
+          const int st = wave % HALVES * (C / 16 / HALVES) + x;
+          if (st > (KT == 2 ? qt | 1 : qt)) break;         // (a product of 32 rows reads the masked tile too)
           f32x4 p = {0.f, 0.f, 0.f, 0.f};
-          if (st <= wave) {
+          if (st <= qt) {
 #pragma unroll
-            for (int k = 0; k < D / KS; ++k) p = TR::mfma(TR::row_frag(sK + (16 * st + i) * L::LD, k * KS, kg), qf[k], p);
+            for (int k = 0; k < D / KS; ++k) p = TR::mfma(TR::template along<D>(sK, along_at, 16 * st, k * KS), qf[k], p);
+            const int d = t - 16 * st - 4 * kg;            // rows apart, of the first of four
+            if (st == qt) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int d = t - (16 * st + 4 * kg + r);
-              p[r] = d >= 0 ? p[r] * (ro.wscale * sLam[max(d, 0)]) : 0.f;
+              for (int r = 0; r < 4; ++r) p[r] = d >= r ? p[r] * sPw[C + d - r] : 0.f;
+            } else {
+#pragma unroll
+              for (int r = 0; r < 4; ++r) p[r] *= sPw[C + d - r];
             }
           }
           T* to = sP + t * PLD + 16 * st + 4 * kg;
@@ -261,77 +350,84 @@ __global__ __launch_bounds__(THREADS, 2) void k_decay_scan(const ScanArgs a) {
           if (have) {
 #pragma unroll
             for (int k = 0; k < D / KS; ++k) {
-              Frag sf[NT][TR::S_PARTS];
+              __builtin_amdgcn_sched_barrier(0);
+              Frag sf[NT];
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
                 f32x4 part[KT];
 #pragma unroll
                 for (int x = 0; x < KT; ++x) part[x] = S[k * KT + x][n];
-                acc_frags(part, sf[n], TR{});
+                sf[n] = acc_frag(part, TR{});
               }
 #pragma unroll
               for (int tt = 0; tt < C / 16; ++tt) {
-                const Frag q = TR::row_frag(sQ + (16 * tt + i) * L::LD, k * KS, kg);
+                const Frag q = TR::template along<D>(sQ, along_at, 16 * tt, k * KS);
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                  for (int x = 0; x < TR::S_PARTS; ++x) o[n][tt] = TR::mfma(sf[n][x], q, o[n][tt]);
+                for (int n = 0; n < NT; ++n) o[n][tt] = TR::mfma(sf[n], q, o[n][tt]);
               }
             }
 #pragma unroll
             for (int tt = 0; tt < C / 16; ++tt) {
-              const float w = sLam[16 * tt + i + 1 - e];
+              const float w = ro.oscale * sLam[C + 16 * tt + i + 1 - e];
 #pragma unroll
               for (int n = 0; n < NT; ++n) o[n][tt] *= w;
             }
           }
         }
-        __syncthreads();
       }
-      const bool odd = WALK && sOdd == kv_step;
-      if (end && keep && (have || !WALK) && (gk == 1 || m == 0)) {
-        if (cnt < C) power(g, cnt, lam_hi, lam_lo);
+      // S moves on: its decay, then K^T (w V)
+      if (end && keep) {
+        if ((have || !WALK) && (gk == 1 || m == 0)) {
+          float lam = sLam[C + cnt];
+          if (cnt == C) {
+            const double want = lam_block * drift;
+            lam = (float)want;
+            drift = same_in_all(fma(want - (double)lam, lam_inv, 1.0));
+          }
 #pragma unroll
-        for (int mm = 0; mm < D / 16; ++mm)
+          for (int mm = 0; mm < D / 16; ++mm)
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[mm][n][r] = fmaf(S[mm][n][r], lam_hi, S[mm][n][r] * lam_lo);
-      }
-#pragma unroll
-      for (int k = 0; k < C / KS; ++k) {
-        Frag vf[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) vf[n] = TR::col_frag(sV, L::LD, k * KS, col0 + 16 * n, i, kg);
-        if (WALK && !odd) {
-#pragma unroll
-          for (int tt = 0; tt < C / 16; ++tt)
-            if (16 * tt + 15 >= k * KS) {
-              // (P lies in its natural order, as the transposing reads give V)
-              const Frag pf = TR::row_frag(sP + (16 * tt + i) * PLD, k * KS, kg);
-#pragma unroll
-              for (int n = 0; n < NT; ++n) o[n][tt] = TR::mfma(vf[n], pf, o[n][tt]);
-            }
+            for (int n = 0; n < NT; ++n) S[mm][n] *= lam;
         }
-        if (end && keep) {
+#pragma unroll
+        for (int k = 0; k < C / KS; ++k) {
+          __builtin_amdgcn_sched_barrier(0);
           float w[TR::E];
 #pragma unroll
           for (int j = 0; j < TR::E; ++j) w[j] = sW[k * KS + TR::col_k(j, kg)];
           Frag vw[NT][TR::PARTS];
 #pragma unroll
-          for (int n = 0; n < NT; ++n) weighted_frags(vf[n], w, vw[n], TR{});
+          for (int n = 0; n < NT; ++n) weighted_frags(TR::template columns<D>(sV, v_cols, k * KS, n), w, vw[n], TR{});
 #pragma unroll
           for (int mm = 0; mm < D / 16; ++mm) {
-            const Frag kf = TR::col_frag_placed(sK, L::LD, k * KS, 16 * mm, i, kg);
+            if (mm % 4 == 0) __builtin_amdgcn_sched_barrier(0);     // (operands read further ahead would not fit the registers)
+            const Frag kf = TR::template acc_columns<D>(sK, k_cols, k * KS, mm);
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int x = 0; x < TR::PARTS; ++x)
 #pragma unroll
-              for (int x = 0; x < TR::PARTS; ++x) S[mm][n] = TR::mfma(kf, vw[n][x], S[mm][n]);
+              for (int n = 0; n < NT; ++n) S[mm][n] = TR::mfma(kf, vw[n][x], S[mm][n]);
           }
         }
       }
       if constexpr (WALK) {
-        if (odd) {
+        __syncthreads();
+        // o^T += V^T P^T (P lies in its natural order, as the transposing reads give V)
+        const bool odd = sOdd == kv_step;
+        if (!odd) {
+#pragma unroll
+          for (int k = 0; k < C / KS; ++k) {
+            Frag vf[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) vf[n] = TR::template columns<D>(sV, v_cols, k * KS, n);
+#pragma unroll
+            for (int tt = 0; tt < C / 16; ++tt)
+              if (16 * tt + 15 >= k * KS) {
+                const Frag pf = TR::row_frag(sP + (16 * tt + i) * PLD, k * KS, kg);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) o[n][tt] = TR::mfma(vf[n], pf, o[n][tt]);
+              }
+          }
+        } else {
           for (int s = 0; s < cnt; ++s)
 #pragma unroll
             for (int tt = 0; tt < C / 16; ++tt) {
@@ -340,36 +436,30 @@ __global__ __launch_bounds__(THREADS, 2) void k_decay_scan(const ScanArgs a) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                  for (int r = 0; r < 4; ++r) o[n][tt][r] += p * TR::get(sV[s * L::LD + col0 + 16 * n + 4 * kg + r]);
+                  for (int r = 0; r < 4; ++r)
+                    o[n][tt][r] += p * TR::get(*reinterpret_cast<const T*>(reinterpret_cast<const char*>(sV) + TR::template unit<D>(s, col0 + 16 * n + 4 * kg + r)));
             }
         }
         if (gk == 1 || m + 1 == heads) {
-          T* ob = static_cast<T*>(ro.o) + (int64_t)(h * ro.gq + (gq > 1 ? m : 0)) * ro.o_head;
+          out_at = o_at + (gq > 1 ? m * ro.o_head : 0);
+          out_cnt = cnt;
 #pragma unroll
-          for (int tt = 0; tt < C / 16; ++tt) {
-            const int row = 16 * tt + i;
-            if (row >= cnt) continue;
-            T* orow = ob + (first + (int64_t)dir * (b * C + row)) * ro.o_row;
+          for (int tt = 0; tt < C / 16; ++tt)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              const int col = col0 + 16 * n + 4 * kg;
-              const f32x4 x = o[n][tt] * ro.oscale;
-              if constexpr (AL) {
-                if (col < ro.dv) {
-                  if constexpr (KT == 2) *reinterpret_cast<u32x2*>(orow + col) = u32x2{two_bf16(x[0], x[1]), two_bf16(x[2], x[3])};
-                  else *reinterpret_cast<f32x4*>(orow + col) = x;
-                }
-              } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                  if (col + r < ro.dv) orow[col + r] = TR::put(x[r]);
-              }
+              char* x = reinterpret_cast<char*>(sQ) + TR::template unit<D>(i, col0 + 16 * n + 4 * kg) + 16 * tt * D * (int)sizeof(T);
+              if constexpr (KT == 2) *reinterpret_cast<u32x2*>(x) = u32x2{two_bf16(o[n][tt][0], o[n][tt][1]), two_bf16(o[n][tt][2], o[n][tt][3])};
+              else *reinterpret_cast<f32x4*>(x) = o[n][tt];
             }
-          }
+          if (m + 1 == heads) o_at += dir * C * ro.o_row;
         }
       }
       if (end && (gk == 1 || m + 1 == heads)) have = true;
     }
+  }
+  if constexpr (WALK) {
+    __syncthreads();
+    if (out_cnt > 0) flush();
   }
   float* to = !WALK ? ro.spans + ((int64_t)item * a.kv + h) * s_size
               : last && ro.s_out ? ro.s_out + ((int64_t)seq * a.kv + h) * s_size : nullptr;
@@ -380,13 +470,14 @@ __global__ __launch_bounds__(THREADS, 2) void k_decay_scan(const ScanArgs a) {
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int row = 16 * m + 4 * kg + r, col = col0 + 16 * n + i;
+          const int row = TR::acc_row(m, kg) + r, col = col0 + 16 * n + i;
           if (row < ro.dk && col < ro.dv) to[row * s_r + col * s_c] = S[m][n][r];
         }
   }
 }
 
-// Sequences of several spans: what each span adds to the state becomes each span's start state.
+// Sequences of several spans: what each span adds to the state becomes each span's start state.  A wave takes 64 values of the
+// states and a quarter of 128 spans, which it has in registers at once; the quarters' sums meet in LDS.
 struct JoinArgs {
   float* spans[2];
   const float* s_in[2];
@@ -396,29 +487,50 @@ struct JoinArgs {
   int kv, span_log2, size;
 };
 
+constexpr int JOIN_EACH = 32;
 __global__ __launch_bounds__(THREADS) void k_span_join(const JoinArgs a) {
+  constexpr int PARTS = THREADS / 64;
+  __shared__ float sum[PARTS][64];
   const int h = blockIdx.x % a.kv, seq = blockIdx.x / a.kv;
   const int64_t lo = clamped(a.off[seq], 0, a.n_rows), hi = clamped(a.off[seq + 1], lo, a.n_rows);
   const int spans = (int)((hi - lo + ((int64_t)1 << a.span_log2) - 1) >> a.span_log2);
-  const int e = blockIdx.y * THREADS + threadIdx.x;
-  if (spans < 2 || e >= a.size) return;
-  float lam_hi, lam_lo;
-  power(log_of(a.log_decay, h), 1 << a.span_log2, lam_hi, lam_lo);
+  if (spans < 2) return;
+  const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
+  const float g = log_of(a.log_decay, h);
+  float lam_hi, lam_lo, far_hi, far_lo;
+  power(g, (double)((int64_t)1 << a.span_log2), lam_hi, lam_lo);
+  power(g, (double)((int64_t)JOIN_EACH << a.span_log2), far_hi, far_lo);
   const int64_t stride = (int64_t)a.kv * a.size;
   const float* s_in = a.s_in[blockIdx.z];
-  float* p = a.spans[blockIdx.z] + (((lo >> a.span_log2) + seq) * a.kv + h) * a.size + e;
-  float cur = s_in ? s_in[((int64_t)seq * a.kv + h) * a.size + e] : 0.f;
-  constexpr int AHEAD = 8;
-  for (int j = 0; j < spans; j += AHEAD) {
-    float add[AHEAD];
+  for (int e0 = blockIdx.y * 64; e0 < a.size; e0 += gridDim.y * 64) {
+    const int e = min(e0 + lane, a.size - 1);              // (lanes past the end repeat the last value and store nothing)
+    const bool live = e0 + lane < a.size;
+    float* p = a.spans[blockIdx.z] + (((lo >> a.span_log2) + seq) * a.kv + h) * a.size + e;
+    float start = s_in ? s_in[((int64_t)seq * a.kv + h) * a.size + e] : 0.f;
+    for (int j0 = 0; j0 < spans; j0 += PARTS * JOIN_EACH) {
+      const int j1 = j0 + part * JOIN_EACH, n = min(JOIN_EACH, spans - j1);
+      float add[JOIN_EACH], all = 0.f;
 #pragma unroll
-    for (int x = 0; x < AHEAD; ++x) add[x] = j + x + 1 < spans ? p[(j + x) * stride] : 0.f;
+      for (int x = 0; x < JOIN_EACH; ++x) add[x] = j1 + x + 1 < spans ? p[(j1 + x) * stride] : 0.f;
 #pragma unroll
-    for (int x = 0; x < AHEAD; ++x)
-      if (j + x < spans) {
-        p[(j + x) * stride] = cur;
-        cur = fmaf(cur, lam_hi, fmaf(cur, lam_lo, add[x]));
+      for (int x = 0; x < JOIN_EACH; ++x) all = fmaf(all, lam_hi, fmaf(all, lam_lo, add[x]));
+      __syncthreads();
+      sum[part][lane] = all;
+      __syncthreads();
+      float cur = start;
+      for (int k = 0; k < PARTS; ++k) {
+        if (k == part) {
+          float c = cur;
+#pragma unroll
+          for (int x = 0; x < JOIN_EACH; ++x) {
+            if (x < n && live) p[(j1 + x) * stride] = c;
+            c = fmaf(c, lam_hi, fmaf(c, lam_lo, add[x]));
+          }
+        }
+        cur = fmaf(cur, far_hi, fmaf(cur, far_lo, sum[k][lane]));
       }
+      start = cur;                                         // (used where all parts were full)
+    }
   }
 }
 
@@ -535,7 +647,8 @@ size_t value_size(const nugpr_decay_attention* p) { return p->dtype == NUGPR_BFL
 
 bool wide(const nugpr_heads* x, int width, size_t value) {
   const int64_t e = 16 / (int64_t)value;
-  return !(reinterpret_cast<uintptr_t>(x->data) & 15u) && x->row_stride % e == 0 && x->head_stride % e == 0 && width % e == 0;
+  return !(reinterpret_cast<uintptr_t>(x->data) & 15u) && x->row_stride % e == 0 && x->head_stride % e == 0 && width % e == 0 &&
+         x->row_stride >= width && x->row_stride < (int64_t)1 << 22;      // (rows one behind the other, a block of them within 31-bit offsets)
 }
 
 // Rows of a span: a power of two of blocks, so many that the scans of the call give about 512 workgroups (two on
@@ -556,14 +669,23 @@ constexpr int FORWARD_SCANS = 1, BACKWARD_SCANS = 3;
 template <class TR, int D>
 int launch_scans(const ScanArgs& adds, int n_adds, const JoinArgs& join, const ScanArgs& walk, int n_walk, bool al, hipStream_t s) {
   const unsigned x = (unsigned)walk.items * walk.kv;
+  const dim3 threads(64 * Tile<TR, D>::WAVES);
   // (a span that holds all rows: no sequence has several)
   if (((int64_t)1 << walk.span_log2) < walk.n_rows) {
-    if (al) hipLaunchKernelGGL((k_decay_scan<TR, D, true, false>), dim3(x, n_adds), dim3(THREADS), 0, s, adds);
-    else hipLaunchKernelGGL((k_decay_scan<TR, D, false, false>), dim3(x, n_adds), dim3(THREADS), 0, s, adds);
-    hipLaunchKernelGGL(k_span_join, dim3((unsigned)walk.n_seqs * walk.kv, (join.size + THREADS - 1) / THREADS, n_adds), dim3(THREADS), 0, s, join);
+    const dim3 grid(x, n_adds);
+    if (al) hipLaunchKernelGGL((k_decay_scan<TR, D, true, false, true>), grid, threads, 0, s, adds);
+    else hipLaunchKernelGGL((k_decay_scan<TR, D, false, false, true>), grid, threads, 0, s, adds);
+    // (workgroups to fill the card with few sequences, not so many with many, most of which have one span)
+    const int64_t pairs = (int64_t)walk.n_seqs * walk.kv, blocks = (join.size + 63) / 64;
+    const int64_t y = min(blocks, (16383 + pairs) / pairs);
+    hipLaunchKernelGGL(k_span_join, dim3((unsigned)pairs, (unsigned)y, n_adds), dim3(THREADS), 0, s, join);
   }
-  if (al) hipLaunchKernelGGL((k_decay_scan<TR, D, true, true>), dim3(x + walk.kv, n_walk), dim3(THREADS), 0, s, walk);
-  else hipLaunchKernelGGL((k_decay_scan<TR, D, false, true>), dim3(x + walk.kv, n_walk), dim3(THREADS), 0, s, walk);
+  const dim3 grid(x + walk.kv, n_walk);
+  const bool sum = n_walk > 1 && walk.role[1].gk > 1;
+  if (al && sum) hipLaunchKernelGGL((k_decay_scan<TR, D, true, true, true>), grid, threads, 0, s, walk);
+  else if (al) hipLaunchKernelGGL((k_decay_scan<TR, D, true, true, false>), grid, threads, 0, s, walk);
+  else if (sum) hipLaunchKernelGGL((k_decay_scan<TR, D, false, true, true>), grid, threads, 0, s, walk);
+  else hipLaunchKernelGGL((k_decay_scan<TR, D, false, true, false>), grid, threads, 0, s, walk);
   NUGPR_HIP(hipGetLastError());
   return NUGPR_OK;
 }

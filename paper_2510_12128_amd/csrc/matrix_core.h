@@ -5,7 +5,7 @@
 //   bfloat16  KS = 32, one 16x16x32 instruction, eight values a lane
 //   float32   KS = 16, four 16x16x4 instructions, four values a lane, one for each
 // Accumulator: column i, rows 4 kg .. 4 kg + 3.  An accumulator tile is therefore itself an operand whose contraction indexes
-// are the rows of 16 (float32) or of two times 16 rows (bfloat16: 4 kg .. of the first tile, then 4 kg .. of the second).
+// are the rows of one tile (float32) or of two (bfloat16: 4 kg .. of the first tile, then 4 kg .. of the second).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -22,51 +22,91 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // nearest bfloat16 (ties to even; NaN stays NaN)
 __device__ inline uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 __device__ inline float from_bf16(uint16_t x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
-__device__ inline uint32_t two_bf16(float lo, float hi) { return (uint32_t)to_bf16(lo) | (uint32_t)to_bf16(hi) << 16; }
+__device__ inline uint32_t two_bf16(float lo, float hi) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
+}
 // the upper halves of two float32: their first eight significant bits, the rest cut off
 __device__ inline uint32_t two_upper(float lo, float hi) {
   return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
 }
 __device__ inline float upper(float x) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u); }
 
-// a 16-byte run with a value that is not finite
-__device__ inline bool odd_bf16(u32x4 v) {
-  bool odd = false;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) odd |= (v[j] & 0x7f80u) == 0x7f80u || (v[j] & 0x7f800000u) == 0x7f800000u;
-  return odd;
-}
-__device__ inline bool odd_f32(u32x4 v) {
-  bool odd = false;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) odd |= (v[j] & 0x7f800000u) == 0x7f800000u;
-  return odd;
+// Bits that tell whether a 16-byte run holds a value that is not finite: `sign` of them, ored together (an exponent of ones carries
+// into the sign's place).
+__device__ inline uint32_t odd_bits(u32x4 v, uint32_t exponent, uint32_t one) {
+  return ((v[0] & exponent) + one) | ((v[1] & exponent) + one) | ((v[2] & exponent) + one) | ((v[3] & exponent) + one);
 }
 
+// A tile in LDS whose rows are read as operands both along the rows and across them has no padding; of every row the 16-byte
+// units are permuted (unit ^ swizzle(row)) so that the units that a wave's lanes want at one time lie on different banks: one unit
+// of 16 consecutive rows, or some units side by side of a few rows.
 struct Bf16 {
   typedef uint16_t T;
   typedef bf16x8 Frag;
   static constexpr int KS = 32;     // contraction indexes of a step
   static constexpr int E = 8;       // values in 16 bytes
   static constexpr int PARTS = 3;   // a float32 is exactly three bfloat16
-  static constexpr int S_PARTS = 2; // parts that a state is read with (16 of its bits)
+  static constexpr int LOW_PARTS = 2; // parts that a float32 factor beside a bfloat16 one is read with, where 16 of its bits are wanted
   static __device__ float get(T x) { return from_bf16(x); }
   static __device__ T put(float x) { return to_bf16(x); }
-  static __device__ bool odd(u32x4 v) { return odd_bf16(v); }
+  typedef u32x2 Four;               // four values
+  static __device__ T nth(Four v, int j) { return (T)(v[j >> 1] >> (16 * (j & 1))); }
+  static constexpr uint32_t SIGN = 0x80008000u;
+  static __device__ uint32_t odd(u32x4 v) { return odd_bits(v, 0x7f807f80u, 0x00800080u); }
   static __device__ f32x4 mfma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-  // Rows whose contraction runs along them lie in LDS with the columns of every 32 in the order in which accumulator
-  // tiles hold them: 4 kg .. 4 kg + 3 and 16 + 4 kg .. of group kg side by side.
-  static __device__ int place(int col) { return (col & ~31) + ((col & 15) >> 2) * 8 + ((col >> 4) & 1) * 4 + (col & 3); }
-  static __device__ void store_row(T* row, int col, u32x4 v) {        // col a multiple of 8
-    T* p = row + (col & ~31) + ((col >> 3) & 1) * 16 + ((col >> 4) & 1) * 4;
-    *reinterpret_cast<u32x2*>(p) = u32x2{v[0], v[1]};
-    *reinterpret_cast<u32x2*>(p + 8) = u32x2{v[2], v[3]};
+  // (Along: a 16-byte read serves lanes 0-3, 12-15, 20-23, 24-27 at one time, and three more such sets; so rows 0-3, 12-15
+  // of group kg and 4-11 of the next one must differ.  Across: four rows in a row, two units or half of four units of each.
+  // Measured, clocks a wave: along 4.2, against 8.0 for rows padded by 16 bytes or permuted by the row's bits exchanged.)
+  template <int D>
+  static __device__ int swizzle(int row) {
+    const int far = ((row >> 3 ^ row >> 2) & 1) << 1 | (row >> 3 & 1);
+    return (D == 128 ? (row & 3) << 2 : (row & 2) << 1) | far;
   }
+  // Byte offsets in a tile; a lane makes its own once, and a wave's tiles and steps are constants away from it (rows that differ by
+  // multiples of 16 are permuted alike).
+  template <int D>
+  static __device__ int unit(int row, int col) { return row * (2 * D) + (((col >> 3) ^ swizzle<D>(row)) << 4) + 2 * (col & 7); }
+  // rows m0 + i, indexes k0 .. k0 + 31; `at`: unit(i, 8 kg)
+  template <int D>
+  static __device__ int along_at(int i, int kg) { return unit<D>(i, 8 * kg); }
+  template <int D>
+  static __device__ Frag along(const T* tile, int at, int m0, int k0) {
+    return *reinterpret_cast<const Frag*>(reinterpret_cast<const char*>(tile) + (at ^ (2 * k0)) + m0 * 2 * D);
+  }
+  // rows k0 .. k0 + 31, 16 columns of which a lane's four-column run begins at `col`
+  static constexpr int ACROSS = 2;
+  template <int D>
+  static __device__ void across_at(int (&at)[ACROSS], int col, int i, int kg) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) at[x] = unit<D>(8 * kg + (i >> 2) + 4 * x, col);
+  }
+  template <int D>
+  static __device__ void columns_at(int (&at)[ACROSS], int m0, int i, int kg) { across_at<D>(at, m0 + 4 * (i & 3), i, kg); }
+  template <int D>
+  static __device__ Frag columns(const T* tile, const int (&at)[ACROSS], int k0, int n) {       // (16 n columns on, below 64)
+    const char* p = reinterpret_cast<const char*>(tile) + k0 * 2 * D;
+    return tr(p + (at[0] ^ (32 * n)), p + (at[1] ^ (32 * n)));
+  }
+  // the columns that accumulator tile m holds as rows (acc_row)
+  template <int D>
+  static __device__ void acc_columns_at(int (&at)[ACROSS], int i, int kg) { across_at<D>(at, 8 * (i & 3), i, kg); }
+  template <int D>
+  static __device__ Frag acc_columns(const T* tile, const int (&at)[ACROSS], int k0, int m) {
+    const char* p = reinterpret_cast<const char*>(tile) + k0 * 2 * D + (m & 1) * 8;
+    return tr(p + (at[0] ^ ((m >> 1) * 64)), p + (at[1] ^ ((m >> 1) * 64)));
+  }
+  // Index that row 4 kg of accumulator tile m stands for (4 kg + r: that plus r), so that two tiles, 2 x and 2 x + 1, are an operand
+  // with contraction indexes 32 x .. in their natural order.
+  static __device__ int acc_row(int m, int kg) { return (m >> 1) * 32 + 8 * kg + 4 * (m & 1); }
+  template <int D>
+  static __device__ float at(const T* tile, int row, int col) { return get(unit<D>(tile, row, col & ~7)[col & 7]); }
   static __device__ Frag row_frag(const T* row, int k0, int kg) { return *reinterpret_cast<const Frag*>(row + k0 + 8 * kg); }
   // operand whose contraction runs over the rows of a tile: columns m0 .. m0 + 15, rows k0 .. k0 + 31, by transposing reads (the
   // 16 lanes of a group read four rows of 16 columns, lane i gets column i)
-  static __device__ Frag tr(const T* p0, const T* p1) {
+  static __device__ Frag tr(const void* p0, const void* p1) {
     typedef __attribute__((address_space(3))) i16x4* Lds;
     const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p0));
     const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p1));
@@ -76,11 +116,6 @@ struct Bf16 {
   }
   static __device__ Frag col_frag(const T* tile, int ld, int k0, int m0, int i, int kg) {
     const T* p = tile + (k0 + 8 * kg + (i >> 2)) * ld + m0 + 4 * (i & 3);
-    return tr(p, p + 4 * ld);
-  }
-  // the same of rows stored by store_row
-  static __device__ Frag col_frag_placed(const T* tile, int ld, int k0, int m0, int i, int kg) {
-    const T* p = tile + (k0 + 8 * kg + (i >> 2)) * ld + (m0 & ~31) + (i & 3) * 8 + ((m0 >> 4) & 1) * 4;
     return tr(p, p + 4 * ld);
   }
   // contraction index (row of the tile) of a col_frag's value j
@@ -93,40 +128,61 @@ struct F32 {
   static constexpr int KS = 16;
   static constexpr int E = 4;
   static constexpr int PARTS = 1;
-  static constexpr int S_PARTS = 1;
+  static constexpr int LOW_PARTS = 1;
   static __device__ float get(T x) { return x; }
   static __device__ T put(float x) { return x; }
-  static __device__ bool odd(u32x4 v) { return odd_f32(v); }
+  typedef f32x4 Four;
+  static __device__ T nth(Four v, int j) { return v[j]; }
+  static constexpr uint32_t SIGN = 0x80000000u;
+  static __device__ uint32_t odd(u32x4 v) { return odd_bits(v, 0x7f800000u, 0x00800000u); }
   static __device__ f32x4 mfma(Frag a, Frag b, f32x4 c) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
     return c;
   }
-  static __device__ int place(int col) { return col; }
-  static __device__ void store_row(T* row, int col, u32x4 v) { *reinterpret_cast<u32x4*>(row + col) = v; }
+  // (Along: as above.  Across: four units of each of four rows, four rows apart.)
+  template <int D>
+  static __device__ int unit(int row, int col) { return row * (4 * D) + (((col >> 2) ^ (row & 15)) << 4) + 4 * (col & 3); }
+  template <int D>
+  static __device__ int along_at(int i, int kg) { return unit<D>(i, 4 * kg); }
+  template <int D>
+  static __device__ Frag along(const T* tile, int at, int m0, int k0) {
+    return *reinterpret_cast<const Frag*>(reinterpret_cast<const char*>(tile) + (at ^ (4 * k0)) + m0 * 4 * D);
+  }
+  static constexpr int ACROSS = 4;
+  template <int D>
+  static __device__ void columns_at(int (&at)[ACROSS], int m0, int i, int kg) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) at[j] = unit<D>(4 * kg + j, m0 + i);
+  }
+  template <int D>
+  static __device__ Frag columns(const T* tile, const int (&at)[ACROSS], int k0, int n) { return acc_columns<D>(tile, at, k0, n); }
+  template <int D>
+  static __device__ void acc_columns_at(int (&at)[ACROSS], int i, int kg) { columns_at<D>(at, 0, i, kg); }
+  template <int D>
+  static __device__ Frag acc_columns(const T* tile, const int (&at)[ACROSS], int k0, int m) {
+    Frag f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      f[j] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(tile) + k0 * 4 * D + (at[j] ^ (m * 64)));
+    return f;
+  }
+  static __device__ int acc_row(int m, int kg) { return 16 * m + 4 * kg; }
   static __device__ Frag row_frag(const T* row, int k0, int kg) { return *reinterpret_cast<const Frag*>(row + k0 + 4 * kg); }
   static __device__ Frag col_frag(const T* tile, int ld, int k0, int m0, int i, int kg) {
     const T* p = tile + (k0 + 4 * kg) * ld + m0 + i;
     return Frag{p[0], p[ld], p[2 * ld], p[3 * ld]};
   }
-  static __device__ Frag col_frag_placed(const T* tile, int ld, int k0, int m0, int i, int kg) {
-    return col_frag(tile, ld, k0, m0, i, kg);
-  }
   static __device__ int col_k(int j, int kg) { return 4 * kg + j; }
 };
 
-// Operand(s) of accumulator tiles: the KS / 16 tiles t[0 .. KS / 16 - 1], whose rows become the contraction index.
-__device__ inline void acc_frags(const f32x4* t, F32::Frag (&out)[1], F32) { out[0] = t[0]; }
-__device__ inline void acc_frags(const f32x4* t, Bf16::Frag (&out)[2], Bf16) {
-  u32x4 hi, lo;
+// Operand of the KS / 16 accumulator tiles t[0 .. KS / 16 - 1], whose rows become the contraction index (bfloat16: rounded).
+__device__ inline F32::Frag acc_frag(const f32x4* t, F32) { return t[0]; }
+__device__ inline Bf16::Frag acc_frag(const f32x4* t, Bf16) {
+  u32x4 v;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float a = t[j >> 1][2 * (j & 1)], b = t[j >> 1][2 * (j & 1) + 1];
-    hi[j] = two_upper(a, b);
-    lo[j] = two_bf16(a - upper(a), b - upper(b));
-  }
-  out[0] = __builtin_bit_cast(bf16x8, hi);
-  out[1] = __builtin_bit_cast(bf16x8, lo);
+  for (int j = 0; j < 4; ++j) v[j] = two_bf16(t[j >> 1][2 * (j & 1)], t[j >> 1][2 * (j & 1) + 1]);
+  return __builtin_bit_cast(bf16x8, v);
 }
 
 // Operand times one float32 weight a contraction index, without rounding to fewer than 24 bits: in bfloat16 the product is cut
