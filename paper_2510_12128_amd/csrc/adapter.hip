@@ -121,21 +121,124 @@ struct ProjectArgs {
   int k, n, rank, padded;
 };
 
-// 128-byte steps of the contraction through LDS, the next step's loads in registers meanwhile; the accumulators' rows are the columns of
-// y (four in a row a lane).  The adapters are further steps at the end: for every request with rows in the tile, its rows of h
-// (in bfloat16 as two numbers, 16 bits in all) and 32 rows of B_a at a time.
+// What the large products share.  The accumulators' rows are the columns of y, four in a row a lane: tile (n, m) of a wave stands for
+// columns wn + 16 n + 4 kg .. and row wm + 16 m + i of the workgroup's tile.
+//
+// The adapters are further steps of the contraction: for every request with rows in the tile, its rows of h (in bfloat16 as two
+// numbers, 16 bits in all) and KS rows of B_a at a time.  sA, sB: room for BM x 128 bytes and KS x BN.
+template <class TR, int BM, int BN, int MT, int NTL, int N_THREADS, bool AL>
+__device__ inline void add_adapters(const ProjectArgs& a, int64_t m0, int n0, int rows, int wm, int wn, typename TR::T* sA, typename TR::T* sB,
+                                    f32x4 (&acc)[NTL][MT]) {
+  using T = typename TR::T;
+  using Frag = typename TR::Frag;
+  constexpr int KS = TR::KS, E = TR::E, BK = 128 / sizeof(T);
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, kg = lane >> 4;
+  const int along_at = TR::template along_at<BK>(i, kg);
+  int cols_at[TR::ACROSS];
+  TR::template columns_at<BN>(cols_at, wn, i, kg);
+  for (int at = 0; at < a.q.n_seqs; at += 64) {
+    // which of 64 requests have rows here
+    const int mine = at + lane;
+    int64_t lo = 0, hi = 0;
+    int ad = -1;
+    if (mine < a.q.n_seqs) {
+      lo = clamped(a.q.off[mine], m0, m0 + rows);
+      hi = clamped(a.q.off[mine + 1], lo, m0 + rows);
+      ad = adapter(a.q, mine);
+    }
+    uint64_t some = __ballot(hi > lo && ad >= 0);
+    while (some) {
+      const int from = __builtin_ctzll(some);
+      some &= some - 1;
+      const int rlo = __shfl((int)(lo - m0), from), rhi = __shfl((int)(hi - m0), from), one = __shfl(ad, from);
+      const T* up = static_cast<const T*>(a.up) + (int64_t)one * a.rank * a.n;
+      for (int j0 = 0; j0 < a.rank; j0 += KS) {
+        __syncthreads();
+        for (int c = tid; c < BM * KS / 4; c += N_THREADS) {
+          const int row = c / (KS / 4), col = c % (KS / 4) * 4;
+          f32x4 v = {0.f, 0.f, 0.f, 0.f};
+          if (row >= rlo && row < rhi) v = *reinterpret_cast<const f32x4*>(a.low + (m0 + row) * a.padded + j0 + col);
+          char* to = reinterpret_cast<char*>(sA);
+          if constexpr (E == 8) {
+            *reinterpret_cast<u32x2*>(to + TR::template unit<BK>(row, col)) = u32x2{two_upper(v[0], v[1]), two_upper(v[2], v[3])};
+            *reinterpret_cast<u32x2*>(to + TR::template unit<BK>(row, KS + col)) =
+                u32x2{two_bf16(v[0] - upper(v[0]), v[1] - upper(v[1])), two_bf16(v[2] - upper(v[2]), v[3] - upper(v[3]))};
+          } else {
+            *reinterpret_cast<f32x4*>(to + TR::template unit<BK>(row, col)) = v;
+          }
+        }
+        for (int c = tid; c < KS * BN / E; c += N_THREADS) {
+          const int row = c / (BN / E), col = c % (BN / E) * E;
+          *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(sB) + TR::template unit<BN>(row, col)) =
+              j0 + row < a.rank ? run16<TR, AL>(up + (int64_t)(j0 + row) * a.n, n0 + col, a.n) : u32x4{0, 0, 0, 0};
+        }
+        __syncthreads();
+        Frag wf[NTL];
+#pragma unroll
+        for (int n = 0; n < NTL; ++n) wf[n] = TR::template columns<BN>(sB, cols_at, 0, n);
+        // (an adapter may hold values that are not finite: they are for the rows of its own requests, where a zero row of h
+        // would make them NaN)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const int row = wm + 16 * m + i;
+          const bool own = row >= rlo && row < rhi;
+          Frag xf[TR::LOW_PARTS];
+#pragma unroll
+          for (int part = 0; part < TR::LOW_PARTS; ++part) xf[part] = TR::template along<BK>(sA, along_at, wm + 16 * m, part * KS);
+#pragma unroll
+          for (int n = 0; n < NTL; ++n) {
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int part = 0; part < TR::LOW_PARTS; ++part) v = TR::mfma(wf[n], xf[part], v);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[n][m][r] += own ? v[r] : 0.f;
+          }
+        }
+      }
+    }
+  }
+}
+
+template <class TR, int MT, int NTL, bool AL>
+__device__ inline void store_rows(const ProjectArgs& a, int64_t m0, int n0, int rows, int wm, int wn, const f32x4 (&acc)[NTL][MT]) {
+  using T = typename TR::T;
+  constexpr int E = TR::E;
+  const int i = threadIdx.x & 15, kg = (threadIdx.x >> 4) & 3;
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int row = wm + 16 * m + i;
+    if (row >= rows) continue;
+    T* y = static_cast<T*>(a.y) + (m0 + row) * a.n;
+#pragma unroll
+    for (int n = 0; n < NTL; ++n) {
+      const int col = n0 + wn + 16 * n + 4 * kg;
+      const f32x4 v = acc[n][m];
+      if constexpr (AL) {
+        if (col < a.n) {
+          if constexpr (E == 8) *reinterpret_cast<u32x2*>(y + col) = u32x2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
+          else *reinterpret_cast<f32x4*>(y + col) = v;
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (col + r < a.n) y[col + r] = TR::put(v[r]);
+      }
+    }
+  }
+}
+
+// 128-byte steps of the contraction through LDS, the next step's loads in registers meanwhile.
 template <class TR, int BM, int BN, int WM, int WN, bool NN, bool AL>
 __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
   using T = typename TR::T;
   using Frag = typename TR::Frag;
-  constexpr int KS = TR::KS, E = TR::E, BK = 128 / sizeof(T), PAD = 16 / sizeof(T);
+  constexpr int KS = TR::KS, E = TR::E, BK = 128 / sizeof(T), S = sizeof(T);
   constexpr int MT = BM / WM / 16, NTL = BN / WN / 16;        // a wave's tiles
-  constexpr int LDA = BK + PAD, LDN = BN + PAD;
   constexpr int XA = BM * BK / E / THREADS, XB = (BN * BK / E + THREADS - 1) / THREADS;
   static_assert(WM * WN == 4 && 2 * KS <= BK, "");
-  __shared__ __align__(16) T sA[BM * LDA];
-  __shared__ __align__(16) T sB[NN ? BK * LDN : (BN * LDA > KS * LDN ? BN * LDA : KS * LDN)];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, kg = lane >> 4;
+  __shared__ __align__(16) T sA[BM * BK];
+  __shared__ __align__(16) T sB[BN * (NN || BK > KS ? BK : KS)];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, kg = lane >> 4;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   const int64_t m0 = (int64_t)blockIdx.y * BM;
   const int n0 = blockIdx.x * BN;
@@ -172,17 +275,21 @@ __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
 #pragma unroll
     for (int p = 0; p < XA; ++p) {
       const int c = tid + p * THREADS;
-      *reinterpret_cast<u32x4*>(sA + c / (BK / E) * LDA + c % (BK / E) * E) = ra[p];
+      *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(sA) + TR::template unit<BK>(c / (BK / E), c % (BK / E) * E)) = ra[p];
     }
 #pragma unroll
     for (int p = 0; p < XB; ++p) {
       const int c = tid + p * THREADS;
       if (c < BN * BK / E) {
-        if constexpr (NN) *reinterpret_cast<u32x4*>(sB + c / (BN / E) * LDN + c % (BN / E) * E) = rb[p];
-        else *reinterpret_cast<u32x4*>(sB + c / (BK / E) * LDA + c % (BK / E) * E) = rb[p];
+        char* to = reinterpret_cast<char*>(sB);
+        if constexpr (NN) *reinterpret_cast<u32x4*>(to + TR::template unit<BN>(c / (BN / E), c % (BN / E) * E)) = rb[p];
+        else *reinterpret_cast<u32x4*>(to + TR::template unit<BK>(c / (BK / E), c % (BK / E) * E)) = rb[p];
       }
     }
   };
+  const int along_at = TR::template along_at<BK>(i, kg);
+  int cols_at[TR::ACROSS];
+  TR::template columns_at<BN>(cols_at, wn, i, kg);
   load(0);
   for (int k0 = 0; k0 < a.k; k0 += BK) {
     __syncthreads();
@@ -193,98 +300,115 @@ __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
     for (int k = 0; k < BK; k += KS) {
       Frag xf[MT], wf[NTL];
 #pragma unroll
-      for (int m = 0; m < MT; ++m) xf[m] = TR::row_frag(sA + (wm + 16 * m + i) * LDA, k, kg);
+      for (int m = 0; m < MT; ++m) xf[m] = TR::template along<BK>(sA, along_at, wm + 16 * m, k);
 #pragma unroll
       for (int n = 0; n < NTL; ++n)
-        wf[n] = NN ? TR::col_frag(sB, LDN, k, wn + 16 * n, i, kg) : TR::row_frag(sB + (wn + 16 * n + i) * LDA, k, kg);
+        wf[n] = NN ? TR::template columns<BN>(sB, cols_at, k, n) : TR::template along<BK>(sB, along_at, wn + 16 * n, k);
 #pragma unroll
       for (int n = 0; n < NTL; ++n)
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[n][m] = TR::mfma(wf[n], xf[m], acc[n][m]);
     }
   }
-  // the adapters
-  for (int at = 0; at < a.q.n_seqs; at += 64) {
-    // which of 64 requests have rows here
-    const int mine = at + lane;
-    int64_t lo = 0, hi = 0;
-    int ad = -1;
-    if (mine < a.q.n_seqs) {
-      lo = clamped(a.q.off[mine], m0, m0 + rows);
-      hi = clamped(a.q.off[mine + 1], lo, m0 + rows);
-      ad = adapter(a.q, mine);
-    }
-    uint64_t some = __ballot(hi > lo && ad >= 0);
-    while (some) {
-      const int from = __builtin_ctzll(some);
-      some &= some - 1;
-      const int rlo = __shfl((int)(lo - m0), from), rhi = __shfl((int)(hi - m0), from), one = __shfl(ad, from);
-      const T* up = static_cast<const T*>(a.up) + (int64_t)one * a.rank * a.n;
-      for (int j0 = 0; j0 < a.rank; j0 += KS) {
-        __syncthreads();
-        for (int c = tid; c < BM * KS / 4; c += THREADS) {
-          const int row = c / (KS / 4), col = c % (KS / 4) * 4;
-          f32x4 v = {0.f, 0.f, 0.f, 0.f};
-          if (row >= rlo && row < rhi) v = *reinterpret_cast<const f32x4*>(a.low + (m0 + row) * a.padded + j0 + col);
-          if constexpr (E == 8) {
-            *reinterpret_cast<u32x2*>(sA + row * LDA + col) = u32x2{two_upper(v[0], v[1]), two_upper(v[2], v[3])};
-            *reinterpret_cast<u32x2*>(sA + row * LDA + KS + col) =
-                u32x2{two_bf16(v[0] - upper(v[0]), v[1] - upper(v[1])), two_bf16(v[2] - upper(v[2]), v[3] - upper(v[3]))};
-          } else {
-            *reinterpret_cast<f32x4*>(sA + row * LDA + col) = v;
-          }
-        }
-        for (int c = tid; c < KS * BN / E; c += THREADS) {
-          const int row = c / (BN / E), col = c % (BN / E) * E;
-          *reinterpret_cast<u32x4*>(sB + row * LDN + col) =
-              j0 + row < a.rank ? run16<TR, AL>(up + (int64_t)(j0 + row) * a.n, n0 + col, a.n) : u32x4{0, 0, 0, 0};
-        }
-        __syncthreads();
-        Frag wf[NTL];
+  add_adapters<TR, BM, BN, MT, NTL, THREADS, AL>(a, m0, n0, rows, wm, wn, sA, sB, acc);
+  store_rows<TR, MT, NTL, AL>(a, m0, n0, rows, wm, wn, acc);
+}
+
+// Many rows and columns in bfloat16: tiles of 256 x 256, eight waves of 128 x 64 each.  A step of 64 indexes goes from memory straight into
+// LDS (two buffers: the next step's loads run through a whole step's 64 products a wave), with one barrier a step.  A
+// load writes 16 bytes a lane side by side, so the permutation of a tile's units is made on the side of memory: lane l fetches the
+// unit that belongs at place l.  Rows and columns past the ends repeat the last ones and are not stored.
+constexpr int WIDE = 256, WIDE_THREADS = 512;
+template <bool NN>
+__global__ __launch_bounds__(WIDE_THREADS, 2) void k_project_wide(const ProjectArgs a, int tiles_m, int tiles_n) {
+  using TR = Bf16;
+  using T = TR::T;
+  constexpr int BK = 64, KS = 32, MT = 8, NTL = 4, PASSES = WIDE * BK / 8 / WIDE_THREADS;
+  __shared__ __align__(16) T sA0[WIDE * BK];
+  __shared__ __align__(16) T sB0[WIDE * BK];
+  __shared__ __align__(16) T sA1[WIDE * BK];
+  __shared__ __align__(16) T sB1[WIDE * BK];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, kg = lane >> 4;
+  const int wm = wave / 4 * 128, wn = wave % 4 * 64;
+  // a die (workgroup number modulo 8) takes tiles side by side: columns of eight tiles, so that what it reads stays in its L2
+  int bm, bn;
+  {
+    const int count = tiles_m * tiles_n, die = blockIdx.x % NUM_XCD, nth = blockIdx.x / NUM_XCD;
+    const int each = count / NUM_XCD, more = count % NUM_XCD;
+    const int tile = die * each + min(die, more) + nth;
+    const int group = tile / (8 * tiles_n), in = tile - group * 8 * tiles_n, high = min(8, tiles_m - 8 * group);
+    bm = 8 * group + in % high;
+    bn = in / high;
+  }
+  const int64_t m0 = (int64_t)bm * WIDE;
+  const int n0 = bn * WIDE;
+  const int rows = (int)min((int64_t)WIDE, a.q.n_rows - m0);
+  const T* x = static_cast<const T*>(a.x) + m0 * a.x_stride;
+  const T* W = static_cast<const T*>(a.W) + (NN ? (int64_t)0 : (int64_t)n0 * a.k);
+  const int cols = min(WIDE, a.n - n0);
+  const T *fa[PASSES], *fb[PASSES];
 #pragma unroll
-        for (int n = 0; n < NTL; ++n) wf[n] = TR::col_frag(sB, LDN, 0, wn + 16 * n, i, kg);
-        // (an adapter may hold values that are not finite: they are for the rows of its own requests, where a zero row of h
-        // would make them NaN)
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          const int row = wm + 16 * m + i;
-          const bool own = row >= rlo && row < rhi;
-          Frag xf[TR::LOW_PARTS];
-#pragma unroll
-          for (int part = 0; part < TR::LOW_PARTS; ++part) xf[part] = TR::row_frag(sA + (wm + 16 * m + i) * LDA, part * KS, kg);
-#pragma unroll
-          for (int n = 0; n < NTL; ++n) {
-            f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int part = 0; part < TR::LOW_PARTS; ++part) v = TR::mfma(wf[n], xf[part], v);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[n][m][r] += own ? v[r] : 0.f;
-          }
-        }
-      }
+  for (int p = 0; p < PASSES; ++p) {
+    const int c = tid + p * WIDE_THREADS, row = c / 8, unit = c % 8 ^ swizzle_bytes<128>(row);
+    fa[p] = x + (int64_t)min(row, rows - 1) * a.x_stride + 8 * unit;
+    if constexpr (NN) {
+      const int r = c / 32, u = c % 32 ^ swizzle_bytes<512>(r);
+      fb[p] = W + (int64_t)r * a.n + n0 + min(8 * u, cols - 8);
+    } else {
+      fb[p] = W + (int64_t)min(row, cols - 1) * a.k + 8 * unit;
     }
   }
+  const int64_t step_b = NN ? (int64_t)BK * a.n : BK;
+  typedef __attribute__((address_space(1))) const void* Global;
+  typedef __attribute__((address_space(3))) void* Lds;
+  auto stage = [&](T* sA, T* sB) {
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int row = wm + 16 * m + i;
-    if (row >= rows) continue;
-    T* y = static_cast<T*>(a.y) + (m0 + row) * a.n;
+    for (int p = 0; p < PASSES; ++p) {
+      __builtin_amdgcn_global_load_lds((Global)fa[p], (Lds)(sA + (p * WIDE_THREADS + wave * 64) * 8), 16, 0, 0);
+      fa[p] += BK;
+    }
 #pragma unroll
-    for (int n = 0; n < NTL; ++n) {
-      const int col = n0 + wn + 16 * n + 4 * kg;
-      const f32x4 v = acc[n][m];
-      if constexpr (AL) {
-        if (col < a.n) {
-          if constexpr (E == 8) *reinterpret_cast<u32x2*>(y + col) = u32x2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
-          else *reinterpret_cast<f32x4*>(y + col) = v;
-        }
-      } else {
+    for (int p = 0; p < PASSES; ++p) {
+      __builtin_amdgcn_global_load_lds((Global)fb[p], (Lds)(sB + (p * WIDE_THREADS + wave * 64) * 8), 16, 0, 0);
+      fb[p] += step_b;
+    }
+  };
+  f32x4 acc[NTL][MT];
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (col + r < a.n) y[col + r] = TR::put(v[r]);
-      }
+  for (int n = 0; n < NTL; ++n)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int along_at = TR::along_at<BK>(i, kg);
+  int cols_at[TR::ACROSS];
+  TR::columns_at<WIDE>(cols_at, wn, i, kg);
+  auto multiply = [&](const T* sA, const T* sB) {
+#pragma unroll
+    for (int k = 0; k < BK; k += KS) {
+      TR::Frag xf[MT], wf[NTL];
+#pragma unroll
+      for (int n = 0; n < NTL; ++n) wf[n] = NN ? TR::columns<WIDE>(sB, cols_at, k, n) : TR::along<BK>(sB, along_at, wn + 16 * n, k);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) xf[m] = TR::along<BK>(sA, along_at, wm + 16 * m, k);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NTL; ++n) acc[n][m] = TR::mfma(wf[n], xf[m], acc[n][m]);
+    }
+  };
+  const int steps = a.k / BK;
+  stage(sA0, sB0);
+  for (int s = 0; s < steps; s += 2) {
+    __syncthreads();                     // (waits for this step's loads, too)
+    if (s + 1 < steps) stage(sA1, sB1);
+    multiply(sA0, sB0);
+    if (s + 1 < steps) {
+      __syncthreads();
+      if (s + 2 < steps) stage(sA0, sB0);
+      multiply(sA1, sB1);
     }
   }
+  add_adapters<TR, WIDE, WIDE, MT, NTL, WIDE_THREADS, true>(a, m0, n0, rows, wm, wn, sA0, sB0, acc);
+  store_rows<TR, MT, NTL, true>(a, m0, n0, rows, wm, wn, acc);
 }
 
 // Few rows: W is read once, by 16 of its rows a workgroup whose eight waves split the contraction, and bounds the time.  Up to
@@ -559,6 +683,13 @@ void launch_project(const ProjectArgs& a, hipStream_t s) {
     else if (a.q.n_rows <= 32) hipLaunchKernelGGL((k_project_few<TR, 2, AL>), grid, dim3(FEW_THREADS), 0, s, a);
     else hipLaunchKernelGGL((k_project_few<TR, 4, AL>), grid, dim3(FEW_THREADS), 0, s, a);
     return;
+  }
+  if constexpr (TR::E == 8 && AL) {
+    const int64_t tm = (a.q.n_rows + WIDE - 1) / WIDE, tn = (a.n + WIDE - 1) / WIDE;
+    if (a.k % 64 == 0 && tm * tn >= 192 && tm * tn < 1 << 30) {
+      hipLaunchKernelGGL((k_project_wide<NN>), dim3((unsigned)(tm * tn)), dim3(WIDE_THREADS), 0, s, a, (int)tm, (int)tn);
+      return;
+    }
   }
   const int64_t large = ((a.q.n_rows + 127) / 128) * ((a.n + 127) / 128);
   if (a.n <= 32) launch_tiles<TR, 128, 32, 4, 1, NN, AL>(a, s);

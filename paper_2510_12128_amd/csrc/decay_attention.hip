@@ -497,16 +497,36 @@ __global__ __launch_bounds__(THREADS) void k_span_join(const JoinArgs a) {
   if (spans < 2) return;
   const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
   const float g = log_of(a.log_decay, h);
-  float lam_hi, lam_lo, far_hi, far_lo;
+  float lam_hi, lam_lo;
   power(g, (double)((int64_t)1 << a.span_log2), lam_hi, lam_lo);
-  power(g, (double)((int64_t)JOIN_EACH << a.span_log2), far_hi, far_lo);
   const int64_t stride = (int64_t)a.kv * a.size;
   const float* s_in = a.s_in[blockIdx.z];
+  s_in = s_in ? s_in + ((int64_t)seq * a.kv + h) * a.size : nullptr;
+  float* first = a.spans[blockIdx.z] + (((lo >> a.span_log2) + seq) * a.kv + h) * a.size;
+  if (spans <= JOIN_EACH) {                                // few: every thread its own value, all of its spans
+    for (int e = blockIdx.y * THREADS + threadIdx.x; e < a.size; e += gridDim.y * THREADS) {
+      float cur = s_in ? s_in[e] : 0.f;
+      for (int j0 = 0; j0 < spans; j0 += 8) {
+        float add[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) add[x] = j0 + x + 1 < spans ? first[(j0 + x) * stride + e] : 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          if (j0 + x < spans) {
+            first[(j0 + x) * stride + e] = cur;
+            cur = fmaf(cur, lam_hi, fmaf(cur, lam_lo, add[x]));
+          }
+      }
+    }
+    return;
+  }
+  float far_hi, far_lo;
+  power(g, (double)((int64_t)JOIN_EACH << a.span_log2), far_hi, far_lo);
   for (int e0 = blockIdx.y * 64; e0 < a.size; e0 += gridDim.y * 64) {
     const int e = min(e0 + lane, a.size - 1);              // (lanes past the end repeat the last value and store nothing)
     const bool live = e0 + lane < a.size;
-    float* p = a.spans[blockIdx.z] + (((lo >> a.span_log2) + seq) * a.kv + h) * a.size + e;
-    float start = s_in ? s_in[((int64_t)seq * a.kv + h) * a.size + e] : 0.f;
+    float* p = first + e;
+    float start = s_in ? s_in[e] : 0.f;
     for (int j0 = 0; j0 < spans; j0 += PARTS * JOIN_EACH) {
       const int j1 = j0 + part * JOIN_EACH, n = min(JOIN_EACH, spans - j1);
       float add[JOIN_EACH], all = 0.f;
@@ -677,7 +697,7 @@ int launch_scans(const ScanArgs& adds, int n_adds, const JoinArgs& join, const S
     else hipLaunchKernelGGL((k_decay_scan<TR, D, false, false, true>), grid, threads, 0, s, adds);
     // (workgroups to fill the card with few sequences, not so many with many, most of which have one span)
     const int64_t pairs = (int64_t)walk.n_seqs * walk.kv, blocks = (join.size + 63) / 64;
-    const int64_t y = min(blocks, (16383 + pairs) / pairs);
+    const int64_t y = min(blocks, (8191 + pairs) / pairs);
     hipLaunchKernelGGL(k_span_join, dim3((unsigned)pairs, (unsigned)y, n_adds), dim3(THREADS), 0, s, join);
   }
   const dim3 grid(x + walk.kv, n_walk);

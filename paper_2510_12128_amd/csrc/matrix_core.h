@@ -39,6 +39,13 @@ __device__ inline uint32_t odd_bits(u32x4 v, uint32_t exponent, uint32_t one) {
   return ((v[0] & exponent) + one) | ((v[1] & exponent) + one) | ((v[2] & exponent) + one) | ((v[3] & exponent) + one);
 }
 
+// The permutation below for rows of that many bytes.
+template <int BYTES>
+__device__ inline int swizzle_bytes(int row) {
+  const int far = ((row >> 3 ^ row >> 2) & 1) << 1 | (row >> 3 & 1);
+  return BYTES >= 256 ? (row & 3) << 2 | far : BYTES == 128 ? (row & 2) << 1 | far : far;
+}
+
 // A tile in LDS whose rows are read as operands both along the rows and across them has no padding; of every row the 16-byte
 // units are permuted (unit ^ swizzle(row)) so that the units that a wave's lanes want at one time lie on different banks: one unit
 // of 16 consecutive rows, or some units side by side of a few rows.
@@ -61,10 +68,7 @@ struct Bf16 {
   // of group kg and 4-11 of the next one must differ.  Across: four rows in a row, two units or half of four units of each.
   // Measured, clocks a wave: along 4.2, against 8.0 for rows padded by 16 bytes or permuted by the row's bits exchanged.)
   template <int D>
-  static __device__ int swizzle(int row) {
-    const int far = ((row >> 3 ^ row >> 2) & 1) << 1 | (row >> 3 & 1);
-    return (D == 128 ? (row & 3) << 2 : (row & 2) << 1) | far;
-  }
+  static __device__ int swizzle(int row) { return swizzle_bytes<2 * D>(row); }
   // Byte offsets in a tile; a lane makes its own once, and a wave's tiles and steps are constants away from it (rows that differ by
   // multiples of 16 are permuted alike).
   template <int D>
@@ -142,7 +146,9 @@ struct F32 {
   }
   // (Along: as above.  Across: four units of each of four rows, four rows apart.)
   template <int D>
-  static __device__ int unit(int row, int col) { return row * (4 * D) + (((col >> 2) ^ (row & 15)) << 4) + 4 * (col & 3); }
+  static __device__ int unit(int row, int col) {
+    return row * (4 * D) + (((col >> 2) ^ (D >= 64 ? row & 15 : swizzle_bytes<4 * D>(row))) << 4) + 4 * (col & 3);
+  }
   template <int D>
   static __device__ int along_at(int i, int kg) { return unit<D>(i, 4 * kg); }
   template <int D>

@@ -88,6 +88,25 @@ def test_large_product(lib, dtype):
         close(g, w.cpu(), TOL[dtype])
 
 
+@pytest.mark.parametrize("inp,out", [(192, 2104), (2104, 192)])
+def test_tiles_of_256(lib, inp, out):
+    """Enough rows and columns for the widest tiles, with both ends inside a tile, in either orientation of W; some requests
+    end inside a tile, one has no adapter, and rows before the first and behind the last have no request."""
+    n = 5700
+    x, W, A, B, _, _, _, _, dy = inputs([n], inp, out, 40, 3, BF16, seed=11)
+    off, which = np.array([3, 700, 700, 701, 2900, 5690]), [1, 0, 2, -1, 0]
+    dev_off, dev_which = torch.from_numpy(off).cuda(), torch.tensor(which, dtype=torch.int32, device="cuda")
+    x64, W64, A64, B64, dy64 = (t.double() for t in (x, W, A, B, dy))
+    y, dx = x64 @ W64.T, dy64 @ W64
+    for s, a in enumerate(which):
+        r = slice(int(off[s]), int(off[s + 1]))
+        if a >= 0:
+            y[r] += (x64[r] @ A64[a].T) @ B64[a]
+            dx[r] += (dy64[r] @ B64[a].T) @ A64[a]
+    close(lib.nugpr_adapter_forward(x, W, A, B, dev_off, adapter_of=dev_which), y.cpu(), TOL[BF16])
+    close(lib.nugpr_adapter_backward(x, W, A, B, dev_off, dy, adapter_of=dev_which)[0], dx.cpu(), TOL[BF16])
+
+
 def test_gradient_against_differences(lib):
     """y is linear in x and bilinear in A and B: central differences of the float64 reference are exact."""
     x, W, A, B, off, dev_off, which, dev_which, dy = inputs([9, 40, 3], 50, 30, 6, 2, F32, seed=3)
