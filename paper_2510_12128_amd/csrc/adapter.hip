@@ -6,6 +6,7 @@
 //
 // h and u (rows x rank, float32, in the workspace) are one kernel's work (k_low); the large products take them as a few
 // more steps of their contraction (k_project, or k_project_few where there are few rows), the sums over rows are k_adapter_grad's.
+#include <algorithm>
 #include <cmath>
 
 #include "matrix_core.h"
@@ -85,17 +86,23 @@ __global__ __launch_bounds__(1024) void k_low(const LowArgs a) {
   f32x4 acc[TILES];
 #pragma unroll
   for (int n = 0; n < TILES; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int k = wave * TR::KS; k < sd.width; k += waves * TR::KS) {
-    const int col = k + kg * TR::E;
-    u32x4 xv = {0, 0, 0, 0};
-    if (i < rows) xv = run16<TR, AL>(x, col, sd.width);
+  // (a wave takes RUN steps side by side, 256 bytes of a row, and has all their loads on the way at once)
+  constexpr int RUN = TILES > 4 ? 1 : TILES > 2 ? 2 : 4;
+  for (int k0 = wave * RUN * TR::KS; k0 < sd.width; k0 += waves * RUN * TR::KS) {
+    u32x4 xv[RUN], av[RUN][TILES];
 #pragma unroll
-    for (int n = 0; n < TILES; ++n) {
-      u32x4 av = {0, 0, 0, 0};
-      if (16 * n + i < a.rank) av = run16<TR, AL>(A + (int64_t)(16 * n + i) * sd.width, col, sd.width);
-      acc[n] = TR::mfma(__builtin_bit_cast(typename TR::Frag, xv), __builtin_bit_cast(typename TR::Frag, av), acc[n]);
+    for (int u = 0; u < RUN; ++u) {
+      const int col = k0 + u * TR::KS + kg * TR::E;
+      xv[u] = i < rows ? run16<TR, AL>(x, col, sd.width) : u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int n = 0; n < TILES; ++n)
+        av[u][n] = 16 * n + i < a.rank ? run16<TR, AL>(A + (int64_t)(16 * n + i) * sd.width, col, sd.width) : u32x4{0, 0, 0, 0};
     }
+#pragma unroll
+    for (int u = 0; u < RUN; ++u)
+#pragma unroll
+      for (int n = 0; n < TILES; ++n)
+        acc[n] = TR::mfma(__builtin_bit_cast(typename TR::Frag, xv[u]), __builtin_bit_cast(typename TR::Frag, av[u][n]), acc[n]);
   }
 #pragma unroll
   for (int n = 0; n < TILES; ++n)
@@ -314,22 +321,22 @@ __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
   store_rows<TR, MT, NTL, AL>(a, m0, n0, rows, wm, wn, acc);
 }
 
-// Many rows and columns in bfloat16: tiles of 256 x 256, eight waves of 128 x 64 each.  A step of 64 indexes goes from memory straight into
+// Many rows and columns in bfloat16: tiles of BM (256 or 128) x 256, eight waves of BM / 2 x 64 each.  A step of 64 indexes goes from memory straight into
 // LDS (two buffers: the next step's loads run through a whole step's 64 products a wave), with one barrier a step.  A
 // load writes 16 bytes a lane side by side, so the permutation of a tile's units is made on the side of memory: lane l fetches the
 // unit that belongs at place l.  Rows and columns past the ends repeat the last ones and are not stored.
 constexpr int WIDE = 256, WIDE_THREADS = 512;
-template <bool NN>
+template <int BM, bool NN>
 __global__ __launch_bounds__(WIDE_THREADS, 2) void k_project_wide(const ProjectArgs a, int tiles_m, int tiles_n) {
   using TR = Bf16;
   using T = TR::T;
-  constexpr int BK = 64, KS = 32, MT = 8, NTL = 4, PASSES = WIDE * BK / 8 / WIDE_THREADS;
-  __shared__ __align__(16) T sA0[WIDE * BK];
+  constexpr int BK = 64, KS = 32, MT = BM / 32, NTL = 4, PASSES_A = BM * BK / 8 / WIDE_THREADS, PASSES = WIDE * BK / 8 / WIDE_THREADS;
+  __shared__ __align__(16) T sA0[BM * BK];
   __shared__ __align__(16) T sB0[WIDE * BK];
-  __shared__ __align__(16) T sA1[WIDE * BK];
+  __shared__ __align__(16) T sA1[BM * BK];
   __shared__ __align__(16) T sB1[WIDE * BK];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, kg = lane >> 4;
-  const int wm = wave / 4 * 128, wn = wave % 4 * 64;
+  const int wm = wave / 4 * (BM / 2), wn = wave % 4 * 64;
   // a die (workgroup number modulo 8) takes tiles side by side: columns of eight tiles, so that what it reads stays in its L2
   int bm, bn;
   {
@@ -340,17 +347,17 @@ __global__ __launch_bounds__(WIDE_THREADS, 2) void k_project_wide(const ProjectA
     bm = 8 * group + in % high;
     bn = in / high;
   }
-  const int64_t m0 = (int64_t)bm * WIDE;
+  const int64_t m0 = (int64_t)bm * BM;
   const int n0 = bn * WIDE;
-  const int rows = (int)min((int64_t)WIDE, a.q.n_rows - m0);
+  const int rows = (int)min((int64_t)BM, a.q.n_rows - m0);
   const T* x = static_cast<const T*>(a.x) + m0 * a.x_stride;
   const T* W = static_cast<const T*>(a.W) + (NN ? (int64_t)0 : (int64_t)n0 * a.k);
   const int cols = min(WIDE, a.n - n0);
-  const T *fa[PASSES], *fb[PASSES];
+  const T *fa[PASSES_A], *fb[PASSES];
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     const int c = tid + p * WIDE_THREADS, row = c / 8, unit = c % 8 ^ swizzle_bytes<128>(row);
-    fa[p] = x + (int64_t)min(row, rows - 1) * a.x_stride + 8 * unit;
+    if (p < PASSES_A) fa[p] = x + (int64_t)min(row, rows - 1) * a.x_stride + 8 * unit;
     if constexpr (NN) {
       const int r = c / 32, u = c % 32 ^ swizzle_bytes<512>(r);
       fb[p] = W + (int64_t)r * a.n + n0 + min(8 * u, cols - 8);
@@ -363,7 +370,7 @@ __global__ __launch_bounds__(WIDE_THREADS, 2) void k_project_wide(const ProjectA
   typedef __attribute__((address_space(3))) void* Lds;
   auto stage = [&](T* sA, T* sB) {
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
+    for (int p = 0; p < PASSES_A; ++p) {
       __builtin_amdgcn_global_load_lds((Global)fa[p], (Lds)(sA + (p * WIDE_THREADS + wave * 64) * 8), 16, 0, 0);
       fa[p] += BK;
     }
@@ -407,7 +414,7 @@ __global__ __launch_bounds__(WIDE_THREADS, 2) void k_project_wide(const ProjectA
       multiply(sA1, sB1);
     }
   }
-  add_adapters<TR, WIDE, WIDE, MT, NTL, WIDE_THREADS, true>(a, m0, n0, rows, wm, wn, sA0, sB0, acc);
+  add_adapters<TR, BM, WIDE, MT, NTL, WIDE_THREADS, true>(a, m0, n0, rows, wm, wn, sA0, sB0, acc);
   store_rows<TR, MT, NTL, true>(a, m0, n0, rows, wm, wn, acc);
 }
 
@@ -431,19 +438,25 @@ __global__ __launch_bounds__(FEW_THREADS) void k_project_few(const ProjectArgs a
 #pragma unroll
   for (int r = 0; r < RT; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
   const u32x4 none = {0, 0, 0, 0};
-#pragma unroll 4
-  for (int k = wave * TR::KS; k < a.k; k += WAVES * TR::KS) {
-    const int col = k + kg * TR::E;
-    const u32x4 w = n0 + i < a.n ? run16<TR, AL>(W, col, a.k) : none;
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const u32x4 v = 16 * r + i < rows ? run16<TR, AL>(x + 16 * r * a.x_stride, col, a.k) : none;
-      acc[r] = TR::mfma(__builtin_bit_cast(Frag, w), __builtin_bit_cast(Frag, v), acc[r]);
-    }
-  }
+  // whose adapter a row has
   for (int r = wave; r < rows; r += WAVES) {
     const int s = owner_of(a.q.off, a.q.n_seqs, m0 + r);
     if (lane == 0) sAdapter[r] = s < 0 ? -1 : adapter(a.q, s);
+  }
+  constexpr int RUN = RT == 4 ? 4 : 8;          // steps side by side of a wave, whose loads are on the way at once
+  for (int k0 = wave * RUN * TR::KS; k0 < a.k; k0 += WAVES * RUN * TR::KS) {
+    u32x4 w[RUN], v[RUN][RT];
+#pragma unroll
+    for (int u = 0; u < RUN; ++u) {
+      const int col = k0 + u * TR::KS + kg * TR::E;
+      w[u] = n0 + i < a.n ? run16<TR, AL>(W, col, a.k) : none;
+#pragma unroll
+      for (int r = 0; r < RT; ++r) v[u][r] = 16 * r + i < rows ? run16<TR, AL>(x + 16 * r * a.x_stride, col, a.k) : none;
+    }
+#pragma unroll
+    for (int u = 0; u < RUN; ++u)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) acc[r] = TR::mfma(__builtin_bit_cast(Frag, w[u]), __builtin_bit_cast(Frag, v[u][r]), acc[r]);
   }
 #pragma unroll
   for (int r = 0; r < RT; ++r)
@@ -464,6 +477,104 @@ __global__ __launch_bounds__(FEW_THREADS) void k_project_few(const ProjectArgs a
       for (int j = 0; j < a.rank; ++j) sum = fmaf(low[j], TR::get(up[(int64_t)j * a.n]), sum);
     }
     static_cast<T*>(a.y)[(m0 + row) * a.n + n0 + col] = TR::put(sum);
+  }
+}
+
+// Few columns (up to 64) and a rank up to 32: both products with x in one pass over it.  A workgroup takes 32 rows; its waves split
+// the width as k_low's do, with W's rows and those of the adapter as operands side by side.  Further requests in the same rows
+// take further passes, for their adapters alone.
+constexpr int NARROW_ROWS = 32;
+template <class TR, bool AL, int WT, int JT>
+__global__ __launch_bounds__(THREADS) void k_project_narrow(const ProjectArgs a, const void* A_all, float scale) {
+  using T = typename TR::T;
+  using Frag = typename TR::Frag;
+  constexpr int WAVES = THREADS / 64, RT = NARROW_ROWS / 16, TT = WT + JT, RUN = TT > 3 ? 2 : 4;
+  __shared__ float red[WAVES][NARROW_ROWS][16 * TT + 1];
+  __shared__ float sH[NARROW_ROWS][16 * JT + 1], sY[NARROW_ROWS][16 * WT + 1];
+  __shared__ int sAdapter[NARROW_ROWS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, kg = lane >> 4;
+  const int64_t m0 = (int64_t)blockIdx.x * NARROW_ROWS;
+  const int rows = (int)min((int64_t)NARROW_ROWS, a.q.n_rows - m0);
+  const T* x = static_cast<const T*>(a.x) + (m0 + i) * a.x_stride;
+  const T* W = static_cast<const T*>(a.W) + (int64_t)i * a.k;
+  if (tid < NARROW_ROWS) sAdapter[tid] = -1;
+  const u32x4 none = {0, 0, 0, 0};
+  bool first = true;
+  auto pass = [&](int ad, int rlo, int rhi) {
+    const T* A = static_cast<const T*>(A_all) + ((int64_t)max(ad, 0) * a.rank + i) * a.k;
+    f32x4 acc[TT][RT];
+#pragma unroll
+    for (int n = 0; n < TT; ++n)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) acc[n][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k0 = wave * RUN * TR::KS; k0 < a.k; k0 += WAVES * RUN * TR::KS) {
+      u32x4 xv[RUN][RT], wv[RUN][TT];
+#pragma unroll
+      for (int u = 0; u < RUN; ++u) {
+        const int col = k0 + u * TR::KS + kg * TR::E;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) xv[u][r] = 16 * r + i < rows ? run16<TR, AL>(x + 16 * r * a.x_stride, col, a.k) : none;
+#pragma unroll
+        for (int n = 0; n < WT; ++n) wv[u][n] = first && 16 * n + i < a.n ? run16<TR, AL>(W + (int64_t)(16 * n) * a.k, col, a.k) : none;
+#pragma unroll
+        for (int n = 0; n < JT; ++n) wv[u][WT + n] = ad >= 0 && 16 * n + i < a.rank ? run16<TR, AL>(A + (int64_t)(16 * n) * a.k, col, a.k) : none;
+      }
+#pragma unroll
+      for (int u = 0; u < RUN; ++u)
+#pragma unroll
+        for (int n = 0; n < TT; ++n)
+#pragma unroll
+          for (int r = 0; r < RT; ++r) acc[n][r] = TR::mfma(__builtin_bit_cast(Frag, wv[u][n]), __builtin_bit_cast(Frag, xv[u][r]), acc[n][r]);
+    }
+    __syncthreads();                       // (what an earlier pass left in red has been read)
+#pragma unroll
+    for (int n = 0; n < TT; ++n)
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) red[wave][16 * r + i][16 * n + 4 * kg + j] = acc[n][r][j];
+    __syncthreads();
+    for (int e = tid; e < NARROW_ROWS * 16 * TT; e += THREADS) {
+      const int row = e / (16 * TT), col = e % (16 * TT);
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) sum += red[w][row][col];
+      if (col < 16 * WT) {
+        if (first) sY[row][col] = sum;
+      } else if (ad >= 0 && row >= rlo && row < rhi) {
+        sH[row][col - 16 * WT] = scale * sum;
+        if (col == 16 * WT) sAdapter[row] = ad;
+      }
+    }
+    first = false;
+  };
+  for (int at = 0; at < a.q.n_seqs; at += 64) {
+    const int mine = at + lane;
+    int64_t lo = 0, hi = 0;
+    int ad = -1;
+    if (mine < a.q.n_seqs) {
+      lo = clamped(a.q.off[mine], m0, m0 + rows);
+      hi = clamped(a.q.off[mine + 1], lo, m0 + rows);
+      ad = adapter(a.q, mine);
+    }
+    uint64_t some = __ballot(hi > lo && ad >= 0);
+    while (some) {
+      const int from = __builtin_ctzll(some);
+      some &= some - 1;
+      pass(__shfl(ad, from), __shfl((int)(lo - m0), from), __shfl((int)(hi - m0), from));
+    }
+  }
+  if (first) pass(-1, 0, 0);
+  __syncthreads();
+  for (int e = tid; e < rows * a.n; e += THREADS) {
+    const int row = e / a.n, col = e - row * a.n, ad = sAdapter[row];
+    float sum = sY[row][col];
+    if (ad >= 0) {
+      const T* up = static_cast<const T*>(a.up) + (int64_t)ad * a.rank * a.n + col;
+#pragma unroll 4
+      for (int j = 0; j < a.rank; ++j) sum = fmaf(sH[row][j], TR::get(up[(int64_t)j * a.n]), sum);
+    }
+    static_cast<T*>(a.y)[(m0 + row) * a.n + col] = TR::put(sum);
   }
 }
 
@@ -517,33 +628,42 @@ __global__ __launch_bounds__(THREADS) void k_adapter_grad(const GradArgs a) {
       const int from = __builtin_ctzll(some);
       some &= some - 1;
       const int64_t rlo = __shfl((long long)lo, from), rhi = __shfl((long long)hi, from);
-      for (int64_t r0 = rlo; r0 < rhi; r0 += GRAD_ROWS) {
+      u32x4 v[X];
+      f32x4 w[JT];
+      auto load = [&](int64_t r0) {
         const int rows = (int)min((int64_t)GRAD_ROWS, rhi - r0);
-        u32x4 v[X];
 #pragma unroll
         for (int p = 0; p < X; ++p) {
           const int c = tid + p * THREADS, row = c / (GRAD_COLS / E), col = c % (GRAD_COLS / E) * E;
           v[p] = row < rows ? run16<TR, AL>(x + (r0 + row) * sd.x_stride, n0 + col, sd.width) : u32x4{0, 0, 0, 0};
         }
+#pragma unroll
+        for (int p = 0; p < JT; ++p) {
+          const int c = tid + p * THREADS, row = c / (4 * JT), col = c % (4 * JT) * 4;
+          w[p] = row < rows && col < a.padded ? *reinterpret_cast<const f32x4*>(sd.low + (r0 + row) * a.padded + col) : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+      };
+      load(rlo);
+      for (int64_t r0 = rlo; r0 < rhi; r0 += GRAD_ROWS) {
         __syncthreads();
 #pragma unroll
         for (int p = 0; p < X; ++p) {
           const int c = tid + p * THREADS;
           *reinterpret_cast<u32x4*>(sX + c / (GRAD_COLS / E) * LDX + c % (GRAD_COLS / E) * E) = v[p];
         }
-        for (int c = tid; c < GRAD_ROWS * 4 * JT; c += THREADS) {
-          const int row = c / (4 * JT), col = c % (4 * JT) * 4;
-          f32x4 w = {0.f, 0.f, 0.f, 0.f};
-          if (row < rows && col < a.padded) w = *reinterpret_cast<const f32x4*>(sd.low + (r0 + row) * a.padded + col);
+#pragma unroll
+        for (int p = 0; p < JT; ++p) {
+          const int c = tid + p * THREADS, row = c / (4 * JT), col = c % (4 * JT) * 4;
           if constexpr (E == 8) {
-            *reinterpret_cast<u32x2*>(sL[0] + row * LDJ + col) = u32x2{two_upper(w[0], w[1]), two_upper(w[2], w[3])};
+            *reinterpret_cast<u32x2*>(sL[0] + row * LDJ + col) = u32x2{two_upper(w[p][0], w[p][1]), two_upper(w[p][2], w[p][3])};
             *reinterpret_cast<u32x2*>(sL[TR::LOW_PARTS - 1] + row * LDJ + col) =
-                u32x2{two_bf16(w[0] - upper(w[0]), w[1] - upper(w[1])), two_bf16(w[2] - upper(w[2]), w[3] - upper(w[3]))};
+                u32x2{two_bf16(w[p][0] - upper(w[p][0]), w[p][1] - upper(w[p][1])), two_bf16(w[p][2] - upper(w[p][2]), w[p][3] - upper(w[p][3]))};
           } else {
-            *reinterpret_cast<f32x4*>(sL[0] + row * LDJ + col) = w;
+            *reinterpret_cast<f32x4*>(sL[0] + row * LDJ + col) = w[p];
           }
         }
         __syncthreads();
+        if (r0 + GRAD_ROWS < rhi) load(r0 + GRAD_ROWS);
 #pragma unroll
         for (int k = 0; k < GRAD_ROWS; k += KS) {
           Frag xf[2];
@@ -659,8 +779,9 @@ template <class TR, bool AL>
 void launch_low(const LowArgs& a, int sides, hipStream_t s) {
   const unsigned items = (unsigned)((a.q.n_rows >> LOW_LOG2) + a.q.n_seqs);
   const int tiles = (a.rank + 15) / 16;
-  // (few pieces: more waves each, to share the width)
-  int waves = items * sides < 512 ? 16 : 4;
+  // (so many waves that each has about two runs of loads, 4 to 16; few pieces: 16)
+  const int width = sides > 1 ? max(a.side[0].width, a.side[1].width) : a.side[0].width, runs = width / (4 * TR::KS);
+  int waves = items * sides < 512 || runs >= 24 ? 16 : runs >= 12 ? 8 : 4;
   if (tiles > 2) waves = min(waves, 8);
   const dim3 grid(items, sides), threads(64 * waves);
   const size_t lds = (size_t)waves * 16 * 16 * (tiles <= 1 ? 1 : tiles <= 2 ? 2 : tiles <= 4 ? 4 : 8) * sizeof(float);
@@ -685,9 +806,14 @@ void launch_project(const ProjectArgs& a, hipStream_t s) {
     return;
   }
   if constexpr (TR::E == 8 && AL) {
-    const int64_t tm = (a.q.n_rows + WIDE - 1) / WIDE, tn = (a.n + WIDE - 1) / WIDE;
-    if (a.k % 64 == 0 && tm * tn >= 192 && tm * tn < 1 << 30) {
-      hipLaunchKernelGGL((k_project_wide<NN>), dim3((unsigned)(tm * tn)), dim3(WIDE_THREADS), 0, s, a, (int)tm, (int)tn);
+    // (from 192 tiles on, three quarters of the compute units)
+    const int64_t tn = (a.n + WIDE - 1) / WIDE, t256 = (a.q.n_rows + 255) / 256, t128 = (a.q.n_rows + 127) / 128;
+    if (a.k % 64 == 0 && t256 * tn >= 192) {
+      hipLaunchKernelGGL((k_project_wide<256, NN>), dim3((unsigned)(t256 * tn)), dim3(WIDE_THREADS), 0, s, a, (int)t256, (int)tn);
+      return;
+    }
+    if (a.k % 64 == 0 && t128 * tn >= 192) {
+      hipLaunchKernelGGL((k_project_wide<128, NN>), dim3((unsigned)(t128 * tn)), dim3(WIDE_THREADS), 0, s, a, (int)t128, (int)tn);
       return;
     }
   }
@@ -711,9 +837,24 @@ void launch_grad(const GradArgs& a, const SumArgs& sum, hipStream_t s) {
   }
 }
 
+template <class TR, bool AL, int WT>
+void launch_narrow(const ProjectArgs& a, const nugpr_adapter* p, hipStream_t s) {
+  const dim3 grid((unsigned)((a.q.n_rows + NARROW_ROWS - 1) / NARROW_ROWS));
+  if (p->rank <= 16) hipLaunchKernelGGL((k_project_narrow<TR, AL, WT, 1>), grid, dim3(THREADS), 0, s, a, p->A, (float)p->scale);
+  else hipLaunchKernelGGL((k_project_narrow<TR, AL, WT, 2>), grid, dim3(THREADS), 0, s, a, p->A, (float)p->scale);
+}
+
 template <class TR, bool AL>
 int run_forward(const nugpr_adapter* p, const void* x, int64_t x_stride, void* y, hipStream_t s) {
   const Requests q = requests(p);
+  if (p->dim_out <= 64 && p->rank <= 32 && q.n_rows > 64) {
+    const ProjectArgs a{x, p->W, p->B, nullptr, y, x_stride, q, p->dim_in, p->dim_out, p->rank, padded_rank(p)};
+    if (p->dim_out <= 16) launch_narrow<TR, AL, 1>(a, p, s);
+    else if (p->dim_out <= 32) launch_narrow<TR, AL, 2>(a, p, s);
+    else launch_narrow<TR, AL, 4>(a, p, s);
+    NUGPR_HIP(hipGetLastError());
+    return NUGPR_OK;
+  }
   LowArgs l{};
   l.q = q; l.scale = (float)p->scale; l.rank = p->rank; l.padded = padded_rank(p);
   l.side[0] = LowSide{x, p->A, static_cast<float*>(p->workspace), x_stride, p->dim_in};

@@ -88,13 +88,13 @@ def test_large_product(lib, dtype):
         close(g, w.cpu(), TOL[dtype])
 
 
+@pytest.mark.parametrize("n", [5700, 2900])
 @pytest.mark.parametrize("inp,out", [(192, 2104), (2104, 192)])
-def test_tiles_of_256(lib, inp, out):
-    """Enough rows and columns for the widest tiles, with both ends inside a tile, in either orientation of W; some requests
-    end inside a tile, one has no adapter, and rows before the first and behind the last have no request."""
-    n = 5700
+def test_tiles_of_256(lib, inp, out, n):
+    """Enough rows and columns for the widest tiles (of 256 and of 128 rows), with both ends inside a tile, in either orientation of
+    W; some requests end inside a tile, one has no adapter, and rows before the first and behind the last have no request."""
     x, W, A, B, _, _, _, _, dy = inputs([n], inp, out, 40, 3, BF16, seed=11)
-    off, which = np.array([3, 700, 700, 701, 2900, 5690]), [1, 0, 2, -1, 0]
+    off, which = np.array([3, 700, 700, 701, n // 2, n - 10]), [1, 0, 2, -1, 0]
     dev_off, dev_which = torch.from_numpy(off).cuda(), torch.tensor(which, dtype=torch.int32, device="cuda")
     x64, W64, A64, B64, dy64 = (t.double() for t in (x, W, A, B, dy))
     y, dx = x64 @ W64.T, dy64 @ W64
