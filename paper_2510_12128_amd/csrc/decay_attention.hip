@@ -41,7 +41,7 @@ struct ScanRole {
 };
 
 struct ScanArgs {
-  ScanRole role[3];
+  ScanRole role[3];       // (first, see k_decay_scan)
   const int64_t* off;
   const float* log_decay;
   int64_t n_rows;
@@ -159,6 +159,8 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
   using Frag = typename TR::Frag;
   using L = Tile<TR, D>;
   constexpr int KS = TR::KS, KT = KS / 16;       // accumulator tiles of a contraction step
+  constexpr bool LOOK = TR::E == 4;              // steps of the contraction beyond the width, and waves beyond the columns, are left out (in
+                                                 // bfloat16 the products are not what bounds the time, and the looks cost registers)
   constexpr int NT = L::NT, THREADS = 64 * L::WAVES, HALVES = L::WAVES / 4;     // waves that share 16 rows of Q in K Q^T
   constexpr int PLD = C + (TR::E == 8 ? 8 : 4);
   __shared__ __align__(16) T sK[C * D];
@@ -170,18 +172,21 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
   __shared__ __align__(16) float sW[C];          // weights of the block's rows in the state
   __shared__ int sOdd;
 
-  const ScanRole& ro = a.role[blockIdx.y];
+  // The role's numbers are read from the arguments where they are needed: kept over the loop they would not fit the scalar registers.
+  // (ScanArgs is the only argument, its roles come first.)
+  typedef const __attribute__((address_space(4))) ScanRole* RolePtr;
+  RolePtr ro = (RolePtr)((const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr() + blockIdx.y * sizeof(ScanRole));
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int i = tid & 15, kg = (tid >> 4) & 3;
   const int h = blockIdx.x % a.kv, item = blockIdx.x / a.kv;
 
   if (WALK && item == a.items) {                 // rows that no sequence owns
     const int64_t lo = clamped(a.off[0], 0, a.n_rows), hi = clamped(a.off[a.n_seqs], lo, a.n_rows);
-    const int64_t none = lo + a.n_rows - hi, per = (int64_t)ro.gq * ro.dv;
+    const int64_t none = lo + a.n_rows - hi, per = (int64_t)ro->gq * ro->dv;
     for (int64_t e = tid; e < none * per; e += THREADS) {
       const int64_t r = e / per;
       const int c = (int)(e - r * per);
-      static_cast<T*>(ro.o)[(r < lo ? r : r - lo + hi) * ro.o_row + (int64_t)(h * ro.gq + c / ro.dv) * ro.o_head + c % ro.dv] = TR::put(0.f);
+      static_cast<T*>(ro->o)[(r < lo ? r : r - lo + hi) * ro->o_row + (int64_t)(h * ro->gq + c / ro->dv) * ro->o_head + c % ro->dv] = TR::put(0.f);
     }
     return;
   }
@@ -194,12 +199,12 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
   if (c0 > 0 && c0 >= len) return;
   if (!WALK && last) return;
   const int n_tok = (int)min(span, len - c0);
-  const int e = ro.back;
+  const int e = ro->back;
 
   const float g = log_of(a.log_decay, h);
   for (int n = tid; n <= 2 * C; n += THREADS) {
     sLam[n] = n < C ? 0.f : (float)exp((double)g * (n - C));
-    if (WALK) sPw[n] = ro.wscale * ro.oscale * sLam[n];
+    if (WALK) sPw[n] = ro->wscale * ro->oscale * sLam[n];
   }
   if (tid == 0) sOdd = 0;
   // lam^C in every block is rounded so that the product of them all stays within a rounding of its exact value: a block's
@@ -210,11 +215,12 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
   // the state: rows acc_row(m, kg) .., columns col0 + 16 n + i
   f32x4 S[D / 16][NT];
   const int col0 = wave * 16 * NT;
-  const int64_t s_size = (int64_t)ro.dk * ro.dv;
-  const int s_r = ro.s_trans ? 1 : ro.dv, s_c = ro.s_trans ? ro.dk : 1;
+  const bool mine = !LOOK || col0 < ro->dv;
+  const int64_t s_size = (int64_t)ro->dk * ro->dv;
+  const int s_r = ro->s_trans ? 1 : ro->dv, s_c = ro->s_trans ? ro->dk : 1;
   const float* from = !WALK ? nullptr
-                      : several ? ro.spans + ((int64_t)item * a.kv + h) * s_size
-                      : ro.s_in ? ro.s_in + ((int64_t)seq * a.kv + h) * s_size : nullptr;
+                      : several ? ro->spans + ((int64_t)item * a.kv + h) * s_size
+                      : ro->s_in ? ro->s_in + ((int64_t)seq * a.kv + h) * s_size : nullptr;
   bool have = from != nullptr;
 #pragma unroll
   for (int m = 0; m < D / 16; ++m)
@@ -223,21 +229,21 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int row = TR::acc_row(m, kg) + r, col = col0 + 16 * n + i;
-        S[m][n][r] = have && row < ro.dk && col < ro.dv ? from[row * s_r + col * s_c] : 0.f;
+        S[m][n][r] = have && row < ro->dk && col < ro->dv ? from[row * s_r + col * s_c] : 0.f;
       }
 
-  const int gq = WALK ? ro.gq : 1, gk = SUM ? ro.gk : 1, heads = max(gq, gk);
+  const int gq = WALK ? ro->gq : 1, gk = SUM ? ro->gk : 1, heads = max(gq, gk);
   const int blocks = (n_tok + C - 1) / C;
   const int64_t first = e ? hi - 1 - c0 : lo + c0;
   const int dir = e ? -1 : 1;
   // row 0 of the block to load next in the arrays, and a thread's places
   const int row0 = tid / L::A_ROW, col_in = tid % L::A_ROW * TR::E;
-  const T* q_at = static_cast<const T*>(ro.q) + (int64_t)h * ro.gq * ro.q_head + first * ro.q_row;
-  const T* k_at = static_cast<const T*>(ro.k) + (int64_t)h * ro.gk * ro.k_head + first * ro.k_row;
-  const T* v_at = static_cast<const T*>(ro.v) + (int64_t)h * ro.gk * ro.v_head + first * ro.v_row;
-  T* o_at = WALK ? static_cast<T*>(ro.o) + (int64_t)h * ro.gq * ro.o_head + first * ro.o_row : nullptr;
-  const uint32_t q_off = place_in<TR, D>(tid, ro.q_row, dir, ro.dk), k_off = place_in<TR, D>(tid, ro.k_row, dir, ro.dk),
-                 v_off = place_in<TR, D>(tid, ro.v_row, dir, ro.dv), o_off = place_in<TR, D>(tid, ro.o_row, dir, ro.dv);
+  const T* q_at = static_cast<const T*>(ro->q) + (int64_t)h * ro->gq * ro->q_head + first * ro->q_row;
+  const T* k_at = static_cast<const T*>(ro->k) + (int64_t)h * ro->gk * ro->k_head + first * ro->k_row;
+  const T* v_at = static_cast<const T*>(ro->v) + (int64_t)h * ro->gk * ro->v_head + first * ro->v_row;
+  T* o_at = WALK ? static_cast<T*>(ro->o) + (int64_t)h * ro->gq * ro->o_head + first * ro->o_row : nullptr;
+  const uint32_t q_off = place_in<TR, D>(tid, ro->q_row, dir, ro->dk), k_off = place_in<TR, D>(tid, ro->k_row, dir, ro->dk),
+                 v_off = place_in<TR, D>(tid, ro->v_row, dir, ro->dv), o_off = place_in<TR, D>(tid, ro->o_row, dir, ro->dv);
   // and in LDS
   int put_at = TR::template unit<D>(row0, col_in), along_at = TR::template along_at<D>(i, kg);
   int v_cols[TR::ACROSS], k_cols[TR::ACROSS];
@@ -247,15 +253,15 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
   auto fetch_block = [&](int b, int m) {
     const int cnt = min(C, n_tok - b * C);
     if (gk > 1 || m == 0) {
-      fetch<TR, D, AL>(rk, tid, k_at + m * ro.k_head, ro.k_row, dir, k_off, cnt, ro.dk);
-      fetch<TR, D, AL>(rv, tid, v_at + m * ro.v_head, ro.v_row, dir, v_off, cnt, ro.dv);
+      fetch<TR, D, AL>(rk, tid, k_at + m * ro->k_head, ro->k_row, dir, k_off, cnt, ro->dk);
+      fetch<TR, D, AL>(rv, tid, v_at + m * ro->v_head, ro->v_row, dir, v_off, cnt, ro->dv);
     }
     if constexpr (WALK)
-      if (gq > 1 || m == 0) fetch<TR, D, AL>(rq, tid, q_at + m * ro.q_head, ro.q_row, dir, q_off, cnt, ro.dk);
+      if (gq > 1 || m == 0) fetch<TR, D, AL>(rq, tid, q_at + m * ro->q_head, ro->q_row, dir, q_off, cnt, ro->dk);
     if (m + 1 == heads) {
-      k_at += dir * C * ro.k_row;
-      v_at += dir * C * ro.v_row;
-      if constexpr (WALK) q_at += dir * C * ro.q_row;
+      k_at += dir * C * ro->k_row;
+      v_at += dir * C * ro->v_row;
+      if constexpr (WALK) q_at += dir * C * ro->q_row;
     }
   };
   f32x4 o[NT][C / 16];
@@ -267,17 +273,17 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
   auto flush = [&]() {
     const char* tile = reinterpret_cast<const char*>(sQ) + put_at;
     if constexpr (AL) {
-      const Window<TR, D> w(out_at, ro.o_row, dir, out_cnt, ro.dv);
+      const Window<TR, D> w(out_at, ro->o_row, dir, out_cnt, ro->dv);
 #pragma unroll
       for (int p = 0; p < L::N; ++p) w.store(o_off, p, *reinterpret_cast<const u32x4*>(tile + p * L::PASS * D * (int)sizeof(T)));
     } else {
-      T* x = out_at + (int64_t)dir * row0 * ro.o_row + col_in;
+      T* x = out_at + (int64_t)dir * row0 * ro->o_row + col_in;
 #pragma unroll
-      for (int p = 0; p < L::N; ++p, x += dir * L::PASS * ro.o_row)
+      for (int p = 0; p < L::N; ++p, x += dir * L::PASS * ro->o_row)
         if (row0 + p * L::PASS < out_cnt)
 #pragma unroll
           for (int j = 0; j < TR::E; ++j)
-            if (col_in + j < ro.dv) x[j] = reinterpret_cast<const T*>(tile + p * L::PASS * D * (int)sizeof(T))[j];
+            if (col_in + j < ro->dv) x[j] = reinterpret_cast<const T*>(tile + p * L::PASS * D * (int)sizeof(T))[j];
     }
     out_cnt = 0;
   };
@@ -287,7 +293,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
     const int cnt = min(C, n_tok - b * C);
     for (int m = 0; m < heads; ++m) {
       // (what follows from these is cheaper made anew than kept in registers from step to step)
-      asm volatile("" : "+v"(i), "+v"(kg), "+v"(put_at), "+v"(along_at));
+      asm volatile("" : "+v"(i), "+v"(kg), "+v"(put_at), "+v"(along_at), "+s"(ro));
 #pragma unroll
       for (int x = 0; x < TR::ACROSS; ++x) asm volatile("" : "+v"(v_cols[x]), "+v"(k_cols[x]));
       const bool kv_new = gk > 1 || m == 0, q_new = WALK && (gq > 1 || m == 0);
@@ -304,7 +310,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
           for (int p = 0; p < L::N; ++p) odd |= TR::odd(rv[p]);
           if (odd & TR::SIGN) sOdd = kv_step;
         }
-        if (tid < C) sW[tid] = tid < cnt ? ro.wscale * sLam[C + cnt - 1 - tid + e] : 0.f;
+        if (tid < C) sW[tid] = tid < cnt ? ro->wscale * sLam[C + cnt - 1 - tid + e] : 0.f;
       }
       if constexpr (WALK)
         if (q_new) put<TR, D>(sQ, put_at, rq);
@@ -313,13 +319,16 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
       else if (b + 1 < blocks) fetch_block(b + 1, 0);
 
       const bool end = gq == 1 || m + 1 == heads;          // the state moves on
-      const bool keep = !WALK || b + 1 < blocks || (last && ro.s_out);
+      const bool keep = !WALK || b + 1 < blocks || (last && ro->s_out);
       if constexpr (WALK) {
         // P^T, rows of K x 16 rows of Q
         const int qt = wave / HALVES, t = 16 * qt + i;
         Frag qf[D / KS];
 #pragma unroll
-        for (int k = 0; k < D / KS; ++k) qf[k] = TR::template along<D>(sQ, along_at, 16 * qt, k * KS);
+        for (int k = 0; k < D / KS; ++k) {
+          if (LOOK && k * KS >= ro->dk) break;
+          qf[k] = TR::template along<D>(sQ, along_at, 16 * qt, k * KS);
+        }
 #pragma unroll
         for (int x = 0; x < C / 16 / HALVES; ++x) {
           const int st = wave % HALVES * (C / 16 / HALVES) + x;
@@ -327,7 +336,10 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
           f32x4 p = {0.f, 0.f, 0.f, 0.f};
           if (st <= qt) {
 #pragma unroll
-            for (int k = 0; k < D / KS; ++k) p = TR::mfma(TR::template along<D>(sK, along_at, 16 * st, k * KS), qf[k], p);
+            for (int k = 0; k < D / KS; ++k) {
+              if (LOOK && k * KS >= ro->dk) break;
+              p = TR::mfma(TR::template along<D>(sK, along_at, 16 * st, k * KS), qf[k], p);
+            }
             const int d = t - 16 * st - 4 * kg;            // rows apart, of the first of four
             if (st == qt) {
 #pragma unroll
@@ -347,9 +359,10 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int tt = 0; tt < C / 16; ++tt) o[n][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
-          if (have) {
+          if (have && mine) {
 #pragma unroll
             for (int k = 0; k < D / KS; ++k) {
+              if (LOOK && k * KS >= ro->dk) break;
               __builtin_amdgcn_sched_barrier(0);
               Frag sf[NT];
 #pragma unroll
@@ -368,7 +381,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
             }
 #pragma unroll
             for (int tt = 0; tt < C / 16; ++tt) {
-              const float w = ro.oscale * sLam[C + 16 * tt + i + 1 - e];
+              const float w = ro->oscale * sLam[C + 16 * tt + i + 1 - e];
 #pragma unroll
               for (int n = 0; n < NT; ++n) o[n][tt] *= w;
             }
@@ -376,7 +389,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
         }
       }
       // S moves on: its decay, then K^T (w V)
-      if (end && keep) {
+      if (end && keep && mine) {
         if ((have || !WALK) && (gk == 1 || m == 0)) {
           float lam = sLam[C + cnt];
           if (cnt == C) {
@@ -400,6 +413,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
           for (int n = 0; n < NT; ++n) weighted_frags(TR::template columns<D>(sV, v_cols, k * KS, n), w, vw[n], TR{});
 #pragma unroll
           for (int mm = 0; mm < D / 16; ++mm) {
+            if (LOOK && 16 * mm >= ro->dk) break;
             if (mm % 4 == 0) __builtin_amdgcn_sched_barrier(0);     // (operands read further ahead would not fit the registers)
             const Frag kf = TR::template acc_columns<D>(sK, k_cols, k * KS, mm);
 #pragma unroll
@@ -413,7 +427,8 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
         __syncthreads();
         // o^T += V^T P^T (P lies in its natural order, as the transposing reads give V)
         const bool odd = sOdd == kv_step;
-        if (!odd) {
+        if (!mine) {
+        } else if (!odd) {
 #pragma unroll
           for (int k = 0; k < C / KS; ++k) {
             Frag vf[NT];
@@ -441,7 +456,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
             }
         }
         if (gk == 1 || m + 1 == heads) {
-          out_at = o_at + (gq > 1 ? m * ro.o_head : 0);
+          out_at = o_at + (gq > 1 ? m * ro->o_head : 0);
           out_cnt = cnt;
 #pragma unroll
           for (int tt = 0; tt < C / 16; ++tt)
@@ -451,7 +466,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
               if constexpr (KT == 2) *reinterpret_cast<u32x2*>(x) = u32x2{two_bf16(o[n][tt][0], o[n][tt][1]), two_bf16(o[n][tt][2], o[n][tt][3])};
               else *reinterpret_cast<f32x4*>(x) = o[n][tt];
             }
-          if (m + 1 == heads) o_at += dir * C * ro.o_row;
+          if (m + 1 == heads) o_at += dir * C * ro->o_row;
         }
       }
       if (end && (gk == 1 || m + 1 == heads)) have = true;
@@ -461,8 +476,8 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
     __syncthreads();
     if (out_cnt > 0) flush();
   }
-  float* to = !WALK ? ro.spans + ((int64_t)item * a.kv + h) * s_size
-              : last && ro.s_out ? ro.s_out + ((int64_t)seq * a.kv + h) * s_size : nullptr;
+  float* to = !WALK ? ro->spans + ((int64_t)item * a.kv + h) * s_size
+              : last && ro->s_out ? ro->s_out + ((int64_t)seq * a.kv + h) * s_size : nullptr;
   if (to) {
 #pragma unroll
     for (int m = 0; m < D / 16; ++m)
@@ -471,7 +486,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int row = TR::acc_row(m, kg) + r, col = col0 + 16 * n + i;
-          if (row < ro.dk && col < ro.dv) to[row * s_r + col * s_c] = S[m][n][r];
+          if (row < ro->dk && col < ro->dv) to[row * s_r + col * s_c] = S[m][n][r];
         }
   }
 }
@@ -671,11 +686,15 @@ bool wide(const nugpr_heads* x, int width, size_t value) {
          x->row_stride >= width && x->row_stride < (int64_t)1 << 22;      // (rows one behind the other, a block of them within 31-bit offsets)
 }
 
-// Rows of a span: a power of two of blocks, so many that the scans of the call give about 512 workgroups (two on
-// every compute unit).
+// Whether the instantiation for widths up to 64 serves a problem.
+bool narrow(const nugpr_decay_attention* p) { return p->dim_k <= 64 && p->dim_v <= 64; }
+
+// Rows of a span: a power of two of blocks, so many that the scans of the call give about 512 workgroups of the wide kernels (two on a
+// compute unit) or 2048 of the narrow ones (four, and more spans than that even out uneven sequences).  65536 rows, 16 / 4 heads of 128:
+// 286, 224, 245, 289 us with 256, 512, 1024, 2048 workgroups; 20011 rows in 40 uneven sequences, 8 heads of 64, float32: 196, 132, 126, 117.
 int span_log2(const nugpr_decay_attention* p, int scans) {
   int k = 6;
-  while (k < 30 && ((p->n_rows * p->kv_heads * scans) >> k) > 512) ++k;
+  while (k < 30 && ((p->n_rows * p->kv_heads * scans) >> k) > (narrow(p) ? 2048 : 512)) ++k;
   return k;
 }
 int64_t span_count(const nugpr_decay_attention* p, int scans) { return (p->n_rows >> span_log2(p, scans)) + p->n_seqs; }
@@ -712,10 +731,9 @@ int launch_scans(const ScanArgs& adds, int n_adds, const JoinArgs& join, const S
 
 int launch_scans(const nugpr_decay_attention* p, const ScanArgs& adds, int n_adds, const JoinArgs& join, const ScanArgs& walk, int n_walk,
                  bool al, hipStream_t s) {
-  const bool narrow = p->dim_k <= 64 && p->dim_v <= 64;
   if (p->dtype == NUGPR_BFLOAT16)
-    return narrow ? launch_scans<Bf16, 64>(adds, n_adds, join, walk, n_walk, al, s) : launch_scans<Bf16, 128>(adds, n_adds, join, walk, n_walk, al, s);
-  return narrow ? launch_scans<F32, 64>(adds, n_adds, join, walk, n_walk, al, s) : launch_scans<F32, 128>(adds, n_adds, join, walk, n_walk, al, s);
+    return narrow(p) ? launch_scans<Bf16, 64>(adds, n_adds, join, walk, n_walk, al, s) : launch_scans<Bf16, 128>(adds, n_adds, join, walk, n_walk, al, s);
+  return narrow(p) ? launch_scans<F32, 64>(adds, n_adds, join, walk, n_walk, al, s) : launch_scans<F32, 128>(adds, n_adds, join, walk, n_walk, al, s);
 }
 
 ScanRole role(const nugpr_heads* q, const nugpr_heads* k, const nugpr_heads* v, const nugpr_heads* o, int gq, int gk, int dk, int dv,
