@@ -74,9 +74,10 @@ __global__ __launch_bounds__(1024) void k_low(const LowArgs a) {
   const LowSide& sd = a.side[blockIdx.y];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6, i = lane & 15, kg = lane >> 4;
   const int item = blockIdx.x;
-  const int s = sequence_of(a.q.off, a.q.n_seqs, a.q.n_rows, LOW_LOG2, item);
+  const PieceOf piece = piece_of(a.q.off, a.q.n_seqs, a.q.n_rows, LOW_LOG2, item);
+  const int s = piece.seq;
   if (s < 0) return;
-  const int64_t lo = clamped(a.q.off[s], 0, a.q.n_rows), hi = clamped(a.q.off[s + 1], lo, a.q.n_rows);
+  const int64_t lo = piece.lo, hi = piece.hi;
   const int64_t row0 = lo + ((item - ((lo >> LOW_LOG2) + s)) << LOW_LOG2);
   const int ad = adapter(a.q, s);
   if (row0 >= hi || ad < 0) return;
@@ -234,7 +235,7 @@ __device__ inline void store_rows(const ProjectArgs& a, int64_t m0, int n0, int 
   }
 }
 
-// 128-byte steps of the contraction through LDS, the next step's loads in registers meanwhile.
+// 128-byte steps of the contraction through LDS, the loads of the two steps after it in registers meanwhile.
 template <class TR, int BM, int BN, int WM, int WN, bool NN, bool AL>
 __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
   using T = typename TR::T;
@@ -257,8 +258,8 @@ __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
   for (int n = 0; n < NTL; ++n)
 #pragma unroll
     for (int m = 0; m < MT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 ra[XA], rb[XB];
-  auto load = [&](int k0) {
+  u32x4 ra0[XA], rb0[XB], ra1[XA], rb1[XB];       // the next step and the one after it
+  auto load = [&](u32x4* ra, u32x4* rb, int k0) {
 #pragma unroll
     for (int p = 0; p < XA; ++p) {
       const int c = tid + p * THREADS, row = c / (BK / E), col = c % (BK / E) * E;
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
       rb[p] = v;
     }
   };
-  auto put = [&]() {
+  auto put = [&](const u32x4* ra, const u32x4* rb) {
 #pragma unroll
     for (int p = 0; p < XA; ++p) {
       const int c = tid + p * THREADS;
@@ -297,12 +298,7 @@ __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
   const int along_at = TR::template along_at<BK>(i, kg);
   int cols_at[TR::ACROSS];
   TR::template columns_at<BN>(cols_at, wn, i, kg);
-  load(0);
-  for (int k0 = 0; k0 < a.k; k0 += BK) {
-    __syncthreads();
-    put();
-    __syncthreads();
-    if (k0 + BK < a.k) load(k0 + BK);
+  auto multiply = [&]() {
 #pragma unroll
     for (int k = 0; k < BK; k += KS) {
       Frag xf[MT], wf[NTL];
@@ -315,6 +311,22 @@ __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
       for (int n = 0; n < NTL; ++n)
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[n][m] = TR::mfma(wf[n], xf[m], acc[n][m]);
+    }
+  };
+  load(ra0, rb0, 0);
+  if (BK < a.k) load(ra1, rb1, BK);
+  for (int k0 = 0; k0 < a.k; k0 += 2 * BK) {
+    __syncthreads();
+    put(ra0, rb0);
+    __syncthreads();
+    if (k0 + 2 * BK < a.k) load(ra0, rb0, k0 + 2 * BK);
+    multiply();
+    if (k0 + BK < a.k) {
+      __syncthreads();
+      put(ra1, rb1);
+      __syncthreads();
+      if (k0 + 3 * BK < a.k) load(ra1, rb1, k0 + 3 * BK);
+      multiply();
     }
   }
   add_adapters<TR, BM, BN, MT, NTL, THREADS, AL>(a, m0, n0, rows, wm, wn, sA, sB, acc);

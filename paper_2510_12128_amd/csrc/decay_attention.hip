@@ -190,9 +190,11 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
     }
     return;
   }
-  const int seq = sequence_of(a.off, a.n_seqs, a.n_rows, a.span_log2, item);
+  const float g = log_of(a.log_decay, h);
+  const PieceOf piece = piece_of(a.off, a.n_seqs, a.n_rows, a.span_log2, item);
+  const int seq = piece.seq;
   if (seq < 0) return;
-  const int64_t lo = clamped(a.off[seq], 0, a.n_rows), hi = clamped(a.off[seq + 1], lo, a.n_rows);
+  const int64_t lo = piece.lo, hi = piece.hi;
   const int64_t len = hi - lo, span = (int64_t)1 << a.span_log2;
   const int64_t c0 = (item - ((lo >> a.span_log2) + seq)) << a.span_log2;
   const bool last = c0 + span >= len, several = len > span;
@@ -201,7 +203,36 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
   const int n_tok = (int)min(span, len - c0);
   const int e = ro->back;
 
-  const float g = log_of(a.log_decay, h);
+  // the first loads are on their way while the rest is made ready
+  const int gq = WALK ? ro->gq : 1, gk = SUM ? ro->gk : 1, heads = max(gq, gk);
+  const int blocks = (n_tok + C - 1) / C;
+  const int64_t first = e ? hi - 1 - c0 : lo + c0;
+  const int dir = e ? -1 : 1;
+  // row 0 of the block to load next in the arrays, and a thread's places
+  const int row0 = tid / L::A_ROW, col_in = tid % L::A_ROW * TR::E;
+  const T* q_at = static_cast<const T*>(ro->q) + (int64_t)h * ro->gq * ro->q_head + first * ro->q_row;
+  const T* k_at = static_cast<const T*>(ro->k) + (int64_t)h * ro->gk * ro->k_head + first * ro->k_row;
+  const T* v_at = static_cast<const T*>(ro->v) + (int64_t)h * ro->gk * ro->v_head + first * ro->v_row;
+  T* o_at = WALK ? static_cast<T*>(ro->o) + (int64_t)h * ro->gq * ro->o_head + first * ro->o_row : nullptr;
+  const uint32_t q_off = place_in<TR, D>(tid, ro->q_row, dir, ro->dk), k_off = place_in<TR, D>(tid, ro->k_row, dir, ro->dk),
+                 v_off = place_in<TR, D>(tid, ro->v_row, dir, ro->dv), o_off = place_in<TR, D>(tid, ro->o_row, dir, ro->dv);
+  u32x4 rq[WALK ? L::N : 1], rk[L::N], rv[L::N];
+  auto fetch_block = [&](int b, int m) {
+    const int cnt = min(C, n_tok - b * C);
+    if (gk > 1 || m == 0) {
+      fetch<TR, D, AL>(rk, tid, k_at + m * ro->k_head, ro->k_row, dir, k_off, cnt, ro->dk);
+      fetch<TR, D, AL>(rv, tid, v_at + m * ro->v_head, ro->v_row, dir, v_off, cnt, ro->dv);
+    }
+    if constexpr (WALK)
+      if (gq > 1 || m == 0) fetch<TR, D, AL>(rq, tid, q_at + m * ro->q_head, ro->q_row, dir, q_off, cnt, ro->dk);
+    if (m + 1 == heads) {
+      k_at += dir * C * ro->k_row;
+      v_at += dir * C * ro->v_row;
+      if constexpr (WALK) q_at += dir * C * ro->q_row;
+    }
+  };
+  if (blocks > 0) fetch_block(0, 0);
+
   for (int n = tid; n <= 2 * C; n += THREADS) {
     sLam[n] = n < C ? 0.f : (float)exp((double)g * (n - C));
     if (WALK) sPw[n] = ro->wscale * ro->oscale * sLam[n];
@@ -232,38 +263,11 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
         S[m][n][r] = have && row < ro->dk && col < ro->dv ? from[row * s_r + col * s_c] : 0.f;
       }
 
-  const int gq = WALK ? ro->gq : 1, gk = SUM ? ro->gk : 1, heads = max(gq, gk);
-  const int blocks = (n_tok + C - 1) / C;
-  const int64_t first = e ? hi - 1 - c0 : lo + c0;
-  const int dir = e ? -1 : 1;
-  // row 0 of the block to load next in the arrays, and a thread's places
-  const int row0 = tid / L::A_ROW, col_in = tid % L::A_ROW * TR::E;
-  const T* q_at = static_cast<const T*>(ro->q) + (int64_t)h * ro->gq * ro->q_head + first * ro->q_row;
-  const T* k_at = static_cast<const T*>(ro->k) + (int64_t)h * ro->gk * ro->k_head + first * ro->k_row;
-  const T* v_at = static_cast<const T*>(ro->v) + (int64_t)h * ro->gk * ro->v_head + first * ro->v_row;
-  T* o_at = WALK ? static_cast<T*>(ro->o) + (int64_t)h * ro->gq * ro->o_head + first * ro->o_row : nullptr;
-  const uint32_t q_off = place_in<TR, D>(tid, ro->q_row, dir, ro->dk), k_off = place_in<TR, D>(tid, ro->k_row, dir, ro->dk),
-                 v_off = place_in<TR, D>(tid, ro->v_row, dir, ro->dv), o_off = place_in<TR, D>(tid, ro->o_row, dir, ro->dv);
   // and in LDS
   int put_at = TR::template unit<D>(row0, col_in), along_at = TR::template along_at<D>(i, kg);
   int v_cols[TR::ACROSS], k_cols[TR::ACROSS];
   TR::template columns_at<D>(v_cols, col0, i, kg);
   TR::template acc_columns_at<D>(k_cols, i, kg);
-  u32x4 rq[WALK ? L::N : 1], rk[L::N], rv[L::N];
-  auto fetch_block = [&](int b, int m) {
-    const int cnt = min(C, n_tok - b * C);
-    if (gk > 1 || m == 0) {
-      fetch<TR, D, AL>(rk, tid, k_at + m * ro->k_head, ro->k_row, dir, k_off, cnt, ro->dk);
-      fetch<TR, D, AL>(rv, tid, v_at + m * ro->v_head, ro->v_row, dir, v_off, cnt, ro->dv);
-    }
-    if constexpr (WALK)
-      if (gq > 1 || m == 0) fetch<TR, D, AL>(rq, tid, q_at + m * ro->q_head, ro->q_row, dir, q_off, cnt, ro->dk);
-    if (m + 1 == heads) {
-      k_at += dir * C * ro->k_row;
-      v_at += dir * C * ro->v_row;
-      if constexpr (WALK) q_at += dir * C * ro->q_row;
-    }
-  };
   f32x4 o[NT][C / 16];
   // A block's o goes into Q's tile, which nobody reads any more by then, and on to memory at the beginning of the next step, by the
   // threads that write the next rows of Q to the same places: whole lines, and ahead of that step's loads (who waits for loads
@@ -287,7 +291,6 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
     }
     out_cnt = 0;
   };
-  if (blocks > 0) fetch_block(0, 0);
   int kv_step = 0;
   for (int b = 0; b < blocks; ++b) {
     const int cnt = min(C, n_tok - b * C);

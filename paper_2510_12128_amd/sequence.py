@@ -63,12 +63,16 @@ def _first(t, name, dims):
     return t.device, t.dtype
 
 
+# (address of a device's current stream; without it through a Stream object, 1.7 us slower)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _call(function, device, *args):
     """The call on the current stream of `device`, which is made current for it."""
     if device.index == torch.cuda.current_device():
-        return _check(function(*args, torch.cuda.current_stream(device).cuda_stream))
+        return _check(function(*args, _raw_stream(device.index)))
     with torch.cuda.device(device):
-        return _check(function(*args, torch.cuda.current_stream(device).cuda_stream))
+        return _check(function(*args, _raw_stream(device.index)))
 
 
 def _scratch(lib, size, p, backward, device):
