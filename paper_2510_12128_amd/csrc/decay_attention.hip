@@ -21,7 +21,6 @@ namespace nugpr {
 
 namespace {
 
-constexpr int C = 64;             // rows of a block
 constexpr int THREADS = 256;
 constexpr float LOWEST_LOG = -1e4f;   // lam^0 = 1, any other power zero: log_decay = -infinity
 
@@ -68,7 +67,8 @@ __device__ inline double same_in_all(double x) {
   return __builtin_bit_cast(double, (u32x2{(uint32_t)__builtin_amdgcn_readfirstlane((int)v[0]), (uint32_t)__builtin_amdgcn_readfirstlane((int)v[1])}));
 }
 
-template <class TR, int D>
+// Blocks of C rows, widths up to D.
+template <class TR, int D, int C>
 struct Tile {
   static constexpr int NT = 1;                              // a wave's tiles of 16 of the state's columns
   static constexpr int WAVES = D / 16 / NT;
@@ -80,7 +80,7 @@ struct Tile {
 // A block's rows in an array, cnt of them, as a buffer that begins at their lowest address and ends behind the last one: what lies
 // beyond reads as zero and is not stored.  `at`: the thread's byte offset from row 0 of the block (place_in); `pass`, in
 // bytes, is added for every further pass.  Only where AL; else everything by 64-bit pointers, value by value.
-template <class TR, int D>
+template <class TR, int D, int C>
 struct Window {
   __amdgpu_buffer_rsrc_t rsrc;
   uint32_t from, pass;
@@ -89,7 +89,7 @@ struct Window {
     const int64_t below = dir > 0 ? 0 : (cnt - 1) * stride;
     rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<typename TR::T*>(base - below), 0, (int)(((cnt - 1) * stride + width) * S), 0x00027000);
     from = (uint32_t)below * S;
-    pass = (uint32_t)(dir * Tile<TR, D>::PASS) * (uint32_t)stride * S;
+    pass = (uint32_t)(dir * Tile<TR, D, C>::PASS) * (uint32_t)stride * S;
   }
   __device__ u32x4 load(uint32_t at, int p) const {
     return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + (from + p * pass), 0, 0));
@@ -97,9 +97,9 @@ struct Window {
   __device__ void store(uint32_t at, int p, u32x4 v) const { __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, at + (from + p * pass), 0, 0); }
 };
 
-template <class TR, int D>
+template <class TR, int D, int C>
 __device__ inline uint32_t place_in(int tid, int64_t stride, int dir, int width) {
-  using L = Tile<TR, D>;
+  using L = Tile<TR, D, C>;
   const int col = tid % L::A_ROW * TR::E;
   // (columns beyond the width: beyond any buffer)
   return col < width ? (uint32_t)(dir * (tid / L::A_ROW)) * (uint32_t)stride * (uint32_t)sizeof(typename TR::T) + col * (uint32_t)sizeof(typename TR::T)
@@ -107,11 +107,11 @@ __device__ inline uint32_t place_in(int tid, int64_t stride, int dir, int width)
 }
 
 // Rows of a block, 16 bytes a thread and pass; zero from row cnt and column `width` on.
-template <class TR, int D, bool AL>
+template <class TR, int D, int C, bool AL>
 __device__ inline void fetch(u32x4* r, int tid, const typename TR::T* base, int64_t stride, int dir, uint32_t at, int cnt, int width) {
-  using L = Tile<TR, D>;
+  using L = Tile<TR, D, C>;
   if constexpr (AL) {
-    const Window<TR, D> w(base, stride, dir, cnt, width);
+    const Window<TR, D, C> w(base, stride, dir, cnt, width);
 #pragma unroll
     for (int p = 0; p < L::N; ++p) r[p] = w.load(at, p);
   } else {
@@ -134,9 +134,9 @@ __device__ inline void fetch(u32x4* r, int tid, const typename TR::T* base, int6
 }
 
 // the block into a tile in LDS; `at`: the thread's byte offset in it for the first pass
-template <class TR, int D>
+template <class TR, int D, int C>
 __device__ inline void put(typename TR::T* tile, int at, const u32x4* r) {
-  using L = Tile<TR, D>;
+  using L = Tile<TR, D, C>;
   static_assert(L::PASS % 16 == 0, "rows of one thread are permuted alike");
 #pragma unroll
   for (int p = 0; p < L::N; ++p)
@@ -153,15 +153,17 @@ __device__ inline void put(typename TR::T* tile, int at, const u32x4* r) {
 // float32 state, keeps all 24 bits.
 // Values that are not finite: rows s > t must not touch o_t, but 0 x NaN in the masked part of P would; a block whose V
 // has such a value takes P V row by row.
-template <class TR, int D, bool AL, bool WALK, bool SUM>
-__global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) void k_decay_scan(const ScanArgs a) {
+template <class TR, int D, int C, bool AL, bool WALK, bool SUM>
+__global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), (TR::E == 8 || D == 64 ? 4 : 2)) void k_decay_scan(const ScanArgs a) {
   using T = typename TR::T;
   using Frag = typename TR::Frag;
-  using L = Tile<TR, D>;
+  using L = Tile<TR, D, C>;
   constexpr int KS = TR::KS, KT = KS / 16;       // accumulator tiles of a contraction step
   constexpr bool LOOK = TR::E == 4;              // steps of the contraction beyond the width, and waves beyond the columns, are left out (in
                                                  // bfloat16 the products are not what bounds the time, and the looks cost registers)
-  constexpr int NT = L::NT, THREADS = 64 * L::WAVES, HALVES = L::WAVES / 4;     // waves that share 16 rows of Q in K Q^T
+  constexpr int NT = L::NT, THREADS = 64 * L::WAVES;
+  constexpr int SHARE = L::WAVES / (C / 16);      // waves that share 16 rows of Q in K Q^T
+  constexpr int EACH = SHARE < C / 16 ? C / 16 / SHARE : 1;     // tiles of rows of K for each of them
   constexpr int PLD = C + (TR::E == 8 ? 8 : 4);
   __shared__ __align__(16) T sK[C * D];
   __shared__ __align__(16) T sV[C * D];
@@ -214,17 +216,17 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
   const T* k_at = static_cast<const T*>(ro->k) + (int64_t)h * ro->gk * ro->k_head + first * ro->k_row;
   const T* v_at = static_cast<const T*>(ro->v) + (int64_t)h * ro->gk * ro->v_head + first * ro->v_row;
   T* o_at = WALK ? static_cast<T*>(ro->o) + (int64_t)h * ro->gq * ro->o_head + first * ro->o_row : nullptr;
-  const uint32_t q_off = place_in<TR, D>(tid, ro->q_row, dir, ro->dk), k_off = place_in<TR, D>(tid, ro->k_row, dir, ro->dk),
-                 v_off = place_in<TR, D>(tid, ro->v_row, dir, ro->dv), o_off = place_in<TR, D>(tid, ro->o_row, dir, ro->dv);
+  const uint32_t q_off = place_in<TR, D, C>(tid, ro->q_row, dir, ro->dk), k_off = place_in<TR, D, C>(tid, ro->k_row, dir, ro->dk),
+                 v_off = place_in<TR, D, C>(tid, ro->v_row, dir, ro->dv), o_off = place_in<TR, D, C>(tid, ro->o_row, dir, ro->dv);
   u32x4 rq[WALK ? L::N : 1], rk[L::N], rv[L::N];
   auto fetch_block = [&](int b, int m) {
     const int cnt = min(C, n_tok - b * C);
     if (gk > 1 || m == 0) {
-      fetch<TR, D, AL>(rk, tid, k_at + m * ro->k_head, ro->k_row, dir, k_off, cnt, ro->dk);
-      fetch<TR, D, AL>(rv, tid, v_at + m * ro->v_head, ro->v_row, dir, v_off, cnt, ro->dv);
+      fetch<TR, D, C, AL>(rk, tid, k_at + m * ro->k_head, ro->k_row, dir, k_off, cnt, ro->dk);
+      fetch<TR, D, C, AL>(rv, tid, v_at + m * ro->v_head, ro->v_row, dir, v_off, cnt, ro->dv);
     }
     if constexpr (WALK)
-      if (gq > 1 || m == 0) fetch<TR, D, AL>(rq, tid, q_at + m * ro->q_head, ro->q_row, dir, q_off, cnt, ro->dk);
+      if (gq > 1 || m == 0) fetch<TR, D, C, AL>(rq, tid, q_at + m * ro->q_head, ro->q_row, dir, q_off, cnt, ro->dk);
     if (m + 1 == heads) {
       k_at += dir * C * ro->k_row;
       v_at += dir * C * ro->v_row;
@@ -277,7 +279,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
   auto flush = [&]() {
     const char* tile = reinterpret_cast<const char*>(sQ) + put_at;
     if constexpr (AL) {
-      const Window<TR, D> w(out_at, ro->o_row, dir, out_cnt, ro->dv);
+      const Window<TR, D, C> w(out_at, ro->o_row, dir, out_cnt, ro->dv);
 #pragma unroll
       for (int p = 0; p < L::N; ++p) w.store(o_off, p, *reinterpret_cast<const u32x4*>(tile + p * L::PASS * D * (int)sizeof(T)));
     } else {
@@ -305,8 +307,8 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
         if (out_cnt > 0) flush();
       if (kv_new) {
         ++kv_step;
-        put<TR, D>(sK, put_at, rk);
-        put<TR, D>(sV, put_at, rv);
+        put<TR, D, C>(sK, put_at, rk);
+        put<TR, D, C>(sV, put_at, rv);
         if (WALK) {
           uint32_t odd = 0;
 #pragma unroll
@@ -316,7 +318,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
         if (tid < C) sW[tid] = tid < cnt ? ro->wscale * sLam[C + cnt - 1 - tid + e] : 0.f;
       }
       if constexpr (WALK)
-        if (q_new) put<TR, D>(sQ, put_at, rq);
+        if (q_new) put<TR, D, C>(sQ, put_at, rq);
       __syncthreads();
       if (m + 1 < heads) fetch_block(b, m + 1);
       else if (b + 1 < blocks) fetch_block(b + 1, 0);
@@ -325,7 +327,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
       const bool keep = !WALK || b + 1 < blocks || (last && ro->s_out);
       if constexpr (WALK) {
         // P^T, rows of K x 16 rows of Q
-        const int qt = wave / HALVES, t = 16 * qt + i;
+        const int qt = wave / SHARE, t = 16 * qt + i;
         Frag qf[D / KS];
 #pragma unroll
         for (int k = 0; k < D / KS; ++k) {
@@ -333,8 +335,8 @@ __global__ __launch_bounds__((64 * Tile<TR, D>::WAVES), (TR::E == 8 ? 4 : 2)) vo
           qf[k] = TR::template along<D>(sQ, along_at, 16 * qt, k * KS);
         }
 #pragma unroll
-        for (int x = 0; x < C / 16 / HALVES; ++x) {
-          const int st = wave % HALVES * (C / 16 / HALVES) + x;
+        for (int x = 0; x < EACH; ++x) {
+          const int st = wave % SHARE * EACH + x;
           if (st > (KT == 2 ? qt | 1 : qt)) break;         // (a product of 32 rows reads the masked tile too)
           f32x4 p = {0.f, 0.f, 0.f, 0.f};
           if (st <= qt) {
@@ -708,26 +710,38 @@ size_t span_bytes(const nugpr_decay_attention* p, int scans) {
 
 constexpr int FORWARD_SCANS = 1, BACKWARD_SCANS = 3;
 
+template <class TR, int D, int C>
+void launch_adds(const ScanArgs& adds, int n_adds, bool al, hipStream_t s) {
+  const dim3 grid((unsigned)adds.items * adds.kv, n_adds), threads(64 * Tile<TR, D, C>::WAVES);
+  if (al) hipLaunchKernelGGL((k_decay_scan<TR, D, C, true, false, true>), grid, threads, 0, s, adds);
+  else hipLaunchKernelGGL((k_decay_scan<TR, D, C, false, false, true>), grid, threads, 0, s, adds);
+}
+
+template <class TR, int D, int C, bool SUM>
+void launch_walk(const ScanArgs& walk, int n_walk, bool al, hipStream_t s) {
+  const dim3 grid((unsigned)walk.items * walk.kv + walk.kv, n_walk), threads(64 * Tile<TR, D, C>::WAVES);
+  if (al) hipLaunchKernelGGL((k_decay_scan<TR, D, C, true, true, SUM>), grid, threads, 0, s, walk);
+  else hipLaunchKernelGGL((k_decay_scan<TR, D, C, false, true, SUM>), grid, threads, 0, s, walk);
+}
+
+// Blocks of 64 rows, or of 32 where that measured better: the narrow kernels in float32 (whose tiles leave room for twice the
+// workgroups then; 20011 rows, 8 heads of 64: 110 against 122 us; the wide ones 91 against 87), and the gradients in bfloat16 (16 x 1024
+// rows, 16 heads of 128: 206 against 236 us; forwards, 65536 rows, 16 / 4 heads: 236 against 227).
 template <class TR, int D>
 int launch_scans(const ScanArgs& adds, int n_adds, const JoinArgs& join, const ScanArgs& walk, int n_walk, bool al, hipStream_t s) {
-  const unsigned x = (unsigned)walk.items * walk.kv;
-  const dim3 threads(64 * Tile<TR, D>::WAVES);
+  constexpr bool small = TR::E == 4 && D == 64;
   // (a span that holds all rows: no sequence has several)
   if (((int64_t)1 << walk.span_log2) < walk.n_rows) {
-    const dim3 grid(x, n_adds);
-    if (al) hipLaunchKernelGGL((k_decay_scan<TR, D, true, false, true>), grid, threads, 0, s, adds);
-    else hipLaunchKernelGGL((k_decay_scan<TR, D, false, false, true>), grid, threads, 0, s, adds);
+    launch_adds<TR, D, small ? 32 : 64>(adds, n_adds, al, s);
     // (workgroups to fill the card with few sequences, not so many with many, most of which have one span)
     const int64_t pairs = (int64_t)walk.n_seqs * walk.kv, blocks = (join.size + 63) / 64;
     const int64_t y = min(blocks, (8191 + pairs) / pairs);
     hipLaunchKernelGGL(k_span_join, dim3((unsigned)pairs, (unsigned)y, n_adds), dim3(THREADS), 0, s, join);
   }
-  const dim3 grid(x + walk.kv, n_walk);
-  const bool sum = n_walk > 1 && walk.role[1].gk > 1;
-  if (al && sum) hipLaunchKernelGGL((k_decay_scan<TR, D, true, true, true>), grid, threads, 0, s, walk);
-  else if (al) hipLaunchKernelGGL((k_decay_scan<TR, D, true, true, false>), grid, threads, 0, s, walk);
-  else if (sum) hipLaunchKernelGGL((k_decay_scan<TR, D, false, true, true>), grid, threads, 0, s, walk);
-  else hipLaunchKernelGGL((k_decay_scan<TR, D, false, true, false>), grid, threads, 0, s, walk);
+  constexpr int BACK = small || TR::E == 8 ? 32 : 64;
+  if (n_walk == 1) launch_walk<TR, D, small ? 32 : 64, false>(walk, n_walk, al, s);
+  else if (walk.role[1].gk > 1) launch_walk<TR, D, BACK, true>(walk, n_walk, al, s);
+  else launch_walk<TR, D, BACK, false>(walk, n_walk, al, s);
   NUGPR_HIP(hipGetLastError());
   return NUGPR_OK;
 }
