@@ -154,7 +154,7 @@ __device__ inline void put(typename TR::T* tile, int at, const u32x4* r) {
 // Values that are not finite: rows s > t must not touch o_t, but 0 x NaN in the masked part of P would; a block whose V
 // has such a value takes P V row by row.
 template <class TR, int D, int C, bool AL, bool WALK, bool SUM>
-__global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), (TR::E == 8 || D == 64 ? 4 : 2)) void k_decay_scan(const ScanArgs a) {
+__global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(const ScanArgs a) {
   using T = typename TR::T;
   using Frag = typename TR::Frag;
   using L = Tile<TR, D, C>;
@@ -694,12 +694,14 @@ bool wide(const nugpr_heads* x, int width, size_t value) {
 // Whether the instantiation for widths up to 64 serves a problem.
 bool narrow(const nugpr_decay_attention* p) { return p->dim_k <= 64 && p->dim_v <= 64; }
 
-// Rows of a span: a power of two of blocks, so many that the scans of the call give about 512 workgroups of the wide kernels (two on a
-// compute unit) or 2048 of the narrow ones (four, and more spans than that even out uneven sequences).  65536 rows, 16 / 4 heads of 128:
-// 286, 224, 245, 289 us with 256, 512, 1024, 2048 workgroups; 20011 rows in 40 uneven sequences, 8 heads of 64, float32: 196, 132, 126, 117.
+// Rows of a span: a power of two, no less than a block, so large that the scans of the call give about 512 workgroups, or more (2048 at
+// most) the smaller their states, whose way through memory is what a span costs.  65536 rows, 16 / 4 heads of 128: 286, 224, 245,
+// 289 us with 256, 512, 1024, 2048 workgroups; 20011 rows in 40 uneven sequences, 8 heads of 64, float32: 220, 116, 110, 119 with
+// 512, 1024, 2048, 4096.
 int span_log2(const nugpr_decay_attention* p, int scans) {
-  int k = 6;
-  while (k < 30 && ((p->n_rows * p->kv_heads * scans) >> k) > (narrow(p) ? 2048 : 512)) ++k;
+  const int64_t groups = min((int64_t)2048, (int64_t)512 * 128 * 128 / (p->dim_k * p->dim_v));
+  int k = p->dtype == NUGPR_BFLOAT16 ? 6 : 5;
+  while (k < 30 && ((p->n_rows * p->kv_heads * scans) >> k) > groups) ++k;
   return k;
 }
 int64_t span_count(const nugpr_decay_attention* p, int scans) { return (p->n_rows >> span_log2(p, scans)) + p->n_seqs; }
@@ -724,22 +726,22 @@ void launch_walk(const ScanArgs& walk, int n_walk, bool al, hipStream_t s) {
   else hipLaunchKernelGGL((k_decay_scan<TR, D, C, false, true, SUM>), grid, threads, 0, s, walk);
 }
 
-// Blocks of 64 rows, or of 32 where that measured better: the narrow kernels in float32 (whose tiles leave room for twice the
-// workgroups then; 20011 rows, 8 heads of 64: 110 against 122 us; the wide ones 91 against 87), and the gradients in bfloat16 (16 x 1024
-// rows, 16 heads of 128: 206 against 236 us; forwards, 65536 rows, 16 / 4 heads: 236 against 227).
+// Rows of a block.  In float32 32: tiles and operands of 64 leave room for one workgroup of the wide kernels on a compute unit instead of two
+// (16384 rows, 8 heads of 128: 237 against 216 us) and for half the narrow ones (20011 rows, 8 heads of 64: 122 against 110).
+// In bfloat16 64 forwards, 32 for the gradients (65536 rows, 16 / 4 heads of 128, forwards: 227 with 64, 236 with 32; 16 x 1024 rows,
+// 16 heads of 128, gradients: 236 and 206).
 template <class TR, int D>
 int launch_scans(const ScanArgs& adds, int n_adds, const JoinArgs& join, const ScanArgs& walk, int n_walk, bool al, hipStream_t s) {
-  constexpr bool small = TR::E == 4 && D == 64;
+  constexpr int AHEAD = TR::E == 8 ? 64 : 32, BACK = 32;
   // (a span that holds all rows: no sequence has several)
   if (((int64_t)1 << walk.span_log2) < walk.n_rows) {
-    launch_adds<TR, D, small ? 32 : 64>(adds, n_adds, al, s);
+    launch_adds<TR, D, AHEAD>(adds, n_adds, al, s);
     // (workgroups to fill the card with few sequences, not so many with many, most of which have one span)
     const int64_t pairs = (int64_t)walk.n_seqs * walk.kv, blocks = (join.size + 63) / 64;
-    const int64_t y = min(blocks, (8191 + pairs) / pairs);
+    const int64_t y = min(blocks, (2047 + pairs) / pairs);
     hipLaunchKernelGGL(k_span_join, dim3((unsigned)pairs, (unsigned)y, n_adds), dim3(THREADS), 0, s, join);
   }
-  constexpr int BACK = small || TR::E == 8 ? 32 : 64;
-  if (n_walk == 1) launch_walk<TR, D, small ? 32 : 64, false>(walk, n_walk, al, s);
+  if (n_walk == 1) launch_walk<TR, D, AHEAD, false>(walk, n_walk, al, s);
   else if (walk.role[1].gk > 1) launch_walk<TR, D, BACK, true>(walk, n_walk, al, s);
   else launch_walk<TR, D, BACK, false>(walk, n_walk, al, s);
   NUGPR_HIP(hipGetLastError());
