@@ -429,8 +429,9 @@ int nugpr_decay_attention_forward(const nugpr_decay_attention* problem, const nu
                                   const nugpr_heads* v, const float* initial_state, const nugpr_heads* o, float* final_state,
                                   void* stream);
 
-/* Gradients, given d_o and (or NULL = zero) d_final_state; d_initial_state: out, or NULL; it may be d_final_state.  Those of
- * key / value heads are sums over the query heads that read them.  Nothing of the forward pass is needed but its inputs. */
+/* Gradients, given d_o and (or NULL = zero) d_final_state; d_initial_state: out, or NULL; refused where it overlaps
+ * d_final_state.  Gradients of key / value heads are sums over the query heads that read them.  Nothing of the forward
+ * pass is needed but its inputs. */
 int nugpr_decay_attention_backward(const nugpr_decay_attention* problem, const nugpr_heads* q, const nugpr_heads* k,
                                    const nugpr_heads* v, const float* initial_state, const nugpr_heads* d_o,
                                    const float* d_final_state, const nugpr_heads* dq, const nugpr_heads* dk,

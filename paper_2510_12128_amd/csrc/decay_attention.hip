@@ -859,6 +859,10 @@ int nugpr_decay_attention_backward(const nugpr_decay_attention* p, const nugpr_h
     al = al && wide(every[x], x == 2 || x == 3 || x == 6 ? p->dim_v : p->dim_k, z);
   }
   const int g = p->heads / p->kv_heads, wk = p->dim_k, wv = p->dim_v;
+  // (two roles read d_final_state, one of them writes d_initial_state)
+  const uintptr_t from = reinterpret_cast<uintptr_t>(d_final_state), to = reinterpret_cast<uintptr_t>(d_initial_state);
+  const size_t states = (size_t)p->n_seqs * p->kv_heads * wk * wv * sizeof(float);
+  if (from && to && from < to + states && to < from + states) { set_error("d_initial_state overlaps d_final_state"); return NUGPR_ERR_INVALID; }
   const float scale = (float)p->scale;
   float* s_spans = static_cast<float*>(p->workspace);                       // states S, dim_k x dim_v
   float* u_spans = reinterpret_cast<float*>(static_cast<char*>(p->workspace) + each);     // gradients U, dim_k x dim_v

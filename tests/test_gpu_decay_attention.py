@@ -261,6 +261,26 @@ def test_states_may_share_memory_and_streams(lib):
     close(S[0], end[0].double().cpu(), TOL[F32])
 
 
+def test_end_states_may_be_written_over_the_start_states(lib):
+    """Through the C entry point: sequences of no span, of one and of many."""
+    import ctypes as C
+
+    from paper_2510_12128_amd import binding as B
+
+    q, k, v, _, g, off, dev_off, S0, _ = inputs([0, 30, 3000], 4, 2, 48, 32, BF16, seed=13)
+    want_o, want_S = lib.nugpr_decay_attention_forward(q, k, v, g, dev_off, initial_state=S0)
+    c, o, S = B.load_library(), torch.empty_like(want_o), S0.clone()
+    p = B.DecayAttention(B.NUGPR_BFLOAT16, 4, 2, 48, 32, q.shape[0], 3, dev_off.data_ptr(), g.data_ptr(), 1.0, None, 0)
+    need = c.nugpr_decay_attention_workspace_bytes(C.byref(p), 0)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    p.workspace, p.workspace_bytes = ws.data_ptr(), need
+    heads = [C.byref(B.Heads(x.data_ptr(), x.stride(0), x.stride(1))) for x in (q, k, v, o)]
+    code = c.nugpr_decay_attention_forward(C.byref(p), *heads[:3], S.data_ptr(), heads[3], S.data_ptr(),
+                                           torch.cuda.current_stream().cuda_stream)
+    assert code == B.NUGPR_OK
+    assert torch.equal(o, want_o) and torch.equal(S, want_S)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("h,kv,dk,dv", [(2, 2, 64, 64), (8, 2, 128, 128), (3, 3, 5, 17), (6, 1, 72, 36)])
 def test_steps_continue_a_prompt(lib, h, kv, dk, dv, dtype):

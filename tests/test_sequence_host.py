@@ -60,6 +60,19 @@ def test_bad_attention_problems(lib, kw):
     assert lib.nugpr_decay_attention_step(C.byref(p), h, h, h, 4096, None, h, None) == B.NUGPR_ERR_INVALID
 
 
+def test_gradients_of_states_that_overlap_are_refused(lib):
+    h, p = B.Heads(4096, 64, 64), attention(workspace_bytes=1 << 40)
+    size = 3 * 2 * 64 * 32 * 4
+
+    def backward(d_final, d_initial):
+        return lib.nugpr_decay_attention_backward(C.byref(p), h, h, h, None, h, d_final, h, h, h, d_initial, None)
+
+    for apart in (0, 4, size - 4):
+        assert backward(1 << 20, (1 << 20) + apart) == B.NUGPR_ERR_INVALID
+        assert backward((1 << 20) + apart, 1 << 20) == B.NUGPR_ERR_INVALID
+        assert b"overlaps" in lib.nugpr_last_error_string()
+
+
 def test_bad_attention_calls(lib):
     h, null, odd, back = B.Heads(4096, 64, 64), B.Heads(None, 64, 64), B.Heads(4098, 64, 64), B.Heads(4096, -64, 64)
 
