@@ -33,13 +33,15 @@ __device__ inline int adapter(const Requests& q, int s) {
   return a >= 0 && a < q.n_adapters ? a : -1;
 }
 
-// 16 bytes of a row from column `col` on, zero past `width`
+// 16 bytes of a row from column `col` on, zero past `width`; AL: aligned, and the width a multiple of them
 template <class TR, bool AL>
 __device__ inline u32x4 run16(const typename TR::T* row, int64_t col, int64_t width) {
   u32x4 v = {0, 0, 0, 0};
   if constexpr (AL) {
     if (col < width) v = *reinterpret_cast<const u32x4*>(row + col);
-  } else {
+  } else if (col + TR::E <= width) {
+    v = load16(row + col);
+  } else if (col < width) {
 #pragma unroll
     for (int j = 0; j < TR::E; ++j)
       if (col + j < width) {
@@ -226,6 +228,9 @@ __device__ inline void store_rows(const ProjectArgs& a, int64_t m0, int n0, int 
           if constexpr (E == 8) *reinterpret_cast<u32x2*>(y + col) = u32x2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
           else *reinterpret_cast<f32x4*>(y + col) = v;
         }
+      } else if (col + 4 <= a.n) {
+        if constexpr (E == 8) store_any(y + col, u32x2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])});
+        else store_any(y + col, v);
       } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -235,18 +240,21 @@ __device__ inline void store_rows(const ProjectArgs& a, int64_t m0, int n0, int 
   }
 }
 
-// 128-byte steps of the contraction through LDS, the loads of the two steps after it in registers meanwhile.
-template <class TR, int BM, int BN, int WM, int WN, bool NN, bool AL>
-__global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
+// 128-byte steps of the contraction through LDS, the loads of the two steps after it in registers meanwhile.  G: groups of four waves
+// that share the contraction, each a run of its steps in tiles of its own; the first one adds the others' sums to its own.
+template <class TR, int BM, int BN, int WM, int WN, int G, bool NN, bool AL>
+__global__ __launch_bounds__(THREADS * G) void k_project(const ProjectArgs a) {
   using T = typename TR::T;
   using Frag = typename TR::Frag;
   constexpr int KS = TR::KS, E = TR::E, BK = 128 / sizeof(T), S = sizeof(T);
   constexpr int MT = BM / WM / 16, NTL = BN / WN / 16;        // a wave's tiles
   constexpr int XA = BM * BK / E / THREADS, XB = (BN * BK / E + THREADS - 1) / THREADS;
   static_assert(WM * WN == 4 && 2 * KS <= BK, "");
-  __shared__ __align__(16) T sA[BM * BK];
-  __shared__ __align__(16) T sB[BN * (NN || BK > KS ? BK : KS)];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, kg = lane >> 4;
+  __shared__ __align__(16) T tiles[G * (BM + BN) * BK];
+  const int tid = threadIdx.x % THREADS, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, kg = lane >> 4;
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
+  T *sA = tiles + group * (BM + BN) * BK, *sB = sA + BM * BK;
+  const int each = ((a.k + BK - 1) / BK + G - 1) / G * BK, k_end = min(a.k, (group + 1) * each);
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   const int64_t m0 = (int64_t)blockIdx.y * BM;
   const int n0 = blockIdx.x * BN;
@@ -263,7 +271,7 @@ __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
 #pragma unroll
     for (int p = 0; p < XA; ++p) {
       const int c = tid + p * THREADS, row = c / (BK / E), col = c % (BK / E) * E;
-      ra[p] = row < rows ? run16<TR, AL>(x + (int64_t)row * a.x_stride, k0 + col, a.k) : u32x4{0, 0, 0, 0};
+      ra[p] = row < rows ? run16<TR, AL>(x + (int64_t)row * a.x_stride, k0 + col, k_end) : u32x4{0, 0, 0, 0};
     }
 #pragma unroll
     for (int p = 0; p < XB; ++p) {
@@ -271,10 +279,10 @@ __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
       u32x4 v = {0, 0, 0, 0};
       if constexpr (NN) {
         const int row = c / (BN / E), col = c % (BN / E) * E;
-        if (row < BK && k0 + row < a.k) v = run16<TR, AL>(W + (int64_t)(k0 + row) * a.n, n0 + col, a.n);
+        if (row < BK && k0 + row < k_end) v = run16<TR, AL>(W + (int64_t)(k0 + row) * a.n, n0 + col, a.n);
       } else {
         const int row = c / (BK / E), col = c % (BK / E) * E;
-        if (row < BN && n0 + row < a.n) v = run16<TR, AL>(W + (int64_t)(n0 + row) * a.k, k0 + col, a.k);
+        if (row < BN && n0 + row < a.n) v = run16<TR, AL>(W + (int64_t)(n0 + row) * a.k, k0 + col, k_end);
       }
       rb[p] = v;
     }
@@ -313,24 +321,44 @@ __global__ __launch_bounds__(THREADS) void k_project(const ProjectArgs a) {
         for (int m = 0; m < MT; ++m) acc[n][m] = TR::mfma(wf[n], xf[m], acc[n][m]);
     }
   };
-  load(ra0, rb0, 0);
-  if (BK < a.k) load(ra1, rb1, BK);
-  for (int k0 = 0; k0 < a.k; k0 += 2 * BK) {
+  // (all groups take the same number of steps, with zeros past the end)
+  const int from = group * each, steps = min(a.k, each);
+  load(ra0, rb0, from);
+  if (BK < steps) load(ra1, rb1, from + BK);
+  for (int k0 = 0; k0 < steps; k0 += 2 * BK) {
     __syncthreads();
     put(ra0, rb0);
     __syncthreads();
-    if (k0 + 2 * BK < a.k) load(ra0, rb0, k0 + 2 * BK);
+    if (k0 + 2 * BK < steps) load(ra0, rb0, from + k0 + 2 * BK);
     multiply();
-    if (k0 + BK < a.k) {
+    if (k0 + BK < steps) {
       __syncthreads();
       put(ra1, rb1);
       __syncthreads();
-      if (k0 + 3 * BK < a.k) load(ra1, rb1, k0 + 3 * BK);
+      if (k0 + 3 * BK < steps) load(ra1, rb1, from + k0 + 3 * BK);
       multiply();
     }
   }
-  add_adapters<TR, BM, BN, MT, NTL, THREADS, AL>(a, m0, n0, rows, wm, wn, sA, sB, acc);
-  store_rows<TR, MT, NTL, AL>(a, m0, n0, rows, wm, wn, acc);
+  if constexpr (G > 1) {
+    static_assert((BM + BN) * BK * S >= NTL * MT * THREADS * 16, "a group's sums fit its tiles");
+    __syncthreads();
+    if (group > 0)
+#pragma unroll
+      for (int n = 0; n < NTL; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) reinterpret_cast<f32x4*>(sA)[(n * MT + m) * THREADS + tid] = acc[n][m];
+    __syncthreads();
+    if (group == 0)
+#pragma unroll
+      for (int other = 1; other < G; ++other)
+#pragma unroll
+        for (int n = 0; n < NTL; ++n)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) acc[n][m] += reinterpret_cast<const f32x4*>(sA + other * (BM + BN) * BK)[(n * MT + m) * THREADS + tid];
+  }
+  // (what the other groups do from here on only helps the first one's loads)
+  add_adapters<TR, BM, BN, MT, NTL, THREADS * G, AL>(a, m0, n0, rows, wm, wn, tiles, tiles + BM * BK, acc);
+  if (group == 0) store_rows<TR, MT, NTL, AL>(a, m0, n0, rows, wm, wn, acc);
 }
 
 // Many rows and columns in bfloat16: tiles of BM (256 or 128) x 256, eight waves of BM / 2 x 64 each.  A step of 64 indexes goes from memory straight into
@@ -803,9 +831,9 @@ void launch_low(const LowArgs& a, int sides, hipStream_t s) {
   else hipLaunchKernelGGL((k_low<TR, AL, 8>), grid, threads, lds, s, a);
 }
 
-template <class TR, int BM, int BN, int WM, int WN, bool NN, bool AL>
+template <class TR, int BM, int BN, int WM, int WN, int G, bool NN, bool AL>
 void launch_tiles(const ProjectArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((k_project<TR, BM, BN, WM, WN, NN, AL>), dim3((a.n + BN - 1) / BN, (unsigned)((a.q.n_rows + BM - 1) / BM)), dim3(THREADS), 0, s, a);
+  hipLaunchKernelGGL((k_project<TR, BM, BN, WM, WN, G, NN, AL>), dim3((a.n + BN - 1) / BN, (unsigned)((a.q.n_rows + BM - 1) / BM)), dim3(THREADS * G), 0, s, a);
 }
 
 template <class TR, bool NN, bool AL>
@@ -829,10 +857,21 @@ void launch_project(const ProjectArgs& a, hipStream_t s) {
       return;
     }
   }
-  const int64_t large = ((a.q.n_rows + 127) / 128) * ((a.n + 127) / 128);
-  if (a.n <= 32) launch_tiles<TR, 128, 32, 4, 1, NN, AL>(a, s);
-  else if (large < 256) launch_tiles<TR, 64, 64, 2, 2, NN, AL>(a, s);
-  else launch_tiles<TR, 128, 128, 2, 2, NN, AL>(a, s);
+  // The fewer tiles there are, the smaller they are and the more groups share their contraction.  128 x 4096 rows and columns, contraction
+  // 4096, 128 tiles of 64 x 64: 52 us with these, 36 with four groups, 31 with tiles of 32 x 32 as well; 512 x 2048, 2048 (256):
+  // 29, 22, 30; with two groups 24; 2048 x 1024, 2048 (512): 31, 34, 48; 28.  In float32, whose products last longer, smaller tiles rather
+  // than groups: 1501 x 500, 301 (192): 51, 51, 49; tiles of 32 x 32 with one group 43.
+  const int64_t large = ((a.q.n_rows + 127) / 128) * ((a.n + 127) / 128), small = ((a.q.n_rows + 63) / 64) * ((a.n + 63) / 64);
+  if (large >= 256) return launch_tiles<TR, 128, 128, 2, 2, 1, NN, AL>(a, s);
+  if (small <= 128) return launch_tiles<TR, 32, 32, 2, 2, 4, NN, AL>(a, s);
+  if constexpr (TR::E == 8) {
+    if (small <= 256) return launch_tiles<TR, 64, 64, 2, 2, 4, NN, AL>(a, s);
+    if (small <= 512) return launch_tiles<TR, 64, 64, 2, 2, 2, NN, AL>(a, s);
+  } else {
+    if (small <= 256) return launch_tiles<TR, 32, 32, 2, 2, 1, NN, AL>(a, s);
+  }
+  if (a.n <= 32) launch_tiles<TR, 128, 32, 4, 1, 1, NN, AL>(a, s);
+  else launch_tiles<TR, 64, 64, 2, 2, 1, NN, AL>(a, s);
 }
 
 template <class TR, bool AL>

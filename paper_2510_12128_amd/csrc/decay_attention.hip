@@ -120,7 +120,9 @@ __device__ inline void fetch(u32x4* r, int tid, const typename TR::T* base, int6
 #pragma unroll
     for (int p = 0; p < L::N; ++p, x += dir * L::PASS * stride) {
       u32x4 v = {0, 0, 0, 0};
-      if (row0 + p * L::PASS < cnt) {
+      if (row0 + p * L::PASS < cnt && col + TR::E <= width) {
+        v = load16(x);
+      } else if (row0 + p * L::PASS < cnt) {
 #pragma unroll
         for (int j = 0; j < TR::E; ++j)
           if (col + j < width) {
@@ -286,7 +288,8 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
       T* x = out_at + (int64_t)dir * row0 * ro->o_row + col_in;
 #pragma unroll
       for (int p = 0; p < L::N; ++p, x += dir * L::PASS * ro->o_row)
-        if (row0 + p * L::PASS < out_cnt)
+        if (row0 + p * L::PASS < out_cnt && col_in + TR::E <= ro->dv) store_any(x, *reinterpret_cast<const u32x4*>(tile + p * L::PASS * D * (int)sizeof(T)));
+        else if (row0 + p * L::PASS < out_cnt)
 #pragma unroll
           for (int j = 0; j < TR::E; ++j)
             if (col_in + j < ro->dv) x[j] = reinterpret_cast<const T*>(tile + p * L::PASS * D * (int)sizeof(T))[j];

@@ -49,6 +49,17 @@ __device__ inline int swizzle_bytes(int row) {
 // A tile in LDS whose rows are read as operands both along the rows and across them has no padding; of every row the 16-byte
 // units are permuted (unit ^ swizzle(row)) so that the units that a wave's lanes want at one time lie on different banks: one unit
 // of 16 consecutive rows, or some units side by side of a few rows.
+// 16 bytes, or 8, at any address that the values themselves are aligned at
+__device__ inline u32x4 load16(const void* p) {
+  u32x4 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+template <class V>
+__device__ inline void store_any(void* p, V v) {
+  __builtin_memcpy(p, &v, sizeof(V));
+}
+
 struct Bf16 {
   typedef uint16_t T;
   typedef bf16x8 Frag;
