@@ -68,7 +68,8 @@ struct LowArgs {
 };
 
 // A workgroup takes 16 rows of one request and all of the rank; its waves split the width, operands go from memory straight
-// into registers (nothing is read twice but A, from L2), the waves' sums meet in LDS.
+// into registers (nothing is read twice but A, from L2), the waves' sums meet in LDS.  The way from L2 bounds it, as a
+// workgroup reads as much of A as of x: 8192 rows of 4096, rank 16, bfloat16: 25 us (67 MB, 2.7 TB/s).
 template <class TR, bool AL, int TILES>
 __global__ __launch_bounds__(1024) void k_low(const LowArgs a) {
   using T = typename TR::T;
@@ -241,7 +242,9 @@ __device__ inline void store_rows(const ProjectArgs& a, int64_t m0, int n0, int 
 }
 
 // 128-byte steps of the contraction through LDS, the loads of the two steps after it in registers meanwhile.  G: groups of four waves
-// that share the contraction, each a run of its steps in tiles of its own; the first one adds the others' sums to its own.
+// that share the contraction, each a run of its steps in tiles of its own; the first one adds the others' sums to its own.  For what the wide
+// tiles are not for: odd sizes, float32, few tiles, where the wait of a step and the number of steps bound it: 1501 rows, 301 to 500
+// columns, float32: 14 us; 1888 rows, 620 to 142, bfloat16: 11.
 template <class TR, int BM, int BN, int WM, int WN, int G, bool NN, bool AL>
 __global__ __launch_bounds__(THREADS * G) void k_project(const ProjectArgs a) {
   using T = typename TR::T;
@@ -364,7 +367,8 @@ __global__ __launch_bounds__(THREADS * G) void k_project(const ProjectArgs a) {
 // Many rows and columns in bfloat16: tiles of BM (256 or 128) x 256, eight waves of BM / 2 x 64 each.  A step of 64 indexes goes from memory straight into
 // LDS (two buffers: the next step's loads run through a whole step's 64 products a wave), with one barrier a step.  A
 // load writes 16 bytes a lane side by side, so the permutation of a tile's units is made on the side of memory: lane l fetches the
-// unit that belongs at place l.  Rows and columns past the ends repeat the last ones and are not stored.
+// unit that belongs at place l.  Rows and columns past the ends repeat the last ones and are not stored.  The matrix cores bound it: 8192
+// rows, 4096 x 4096: 250 us with the adapters (1.10 PFLOP/s); 4096 rows, 2048 x 2048, tiles of 128: 43 us (0.80).
 constexpr int WIDE = 256, WIDE_THREADS = 512;
 template <int BM, bool NN>
 __global__ __launch_bounds__(WIDE_THREADS, 2) void k_project_wide(const ProjectArgs a, int tiles_m, int tiles_n) {
@@ -458,8 +462,8 @@ __global__ __launch_bounds__(WIDE_THREADS, 2) void k_project_wide(const ProjectA
   store_rows<TR, MT, NTL, true>(a, m0, n0, rows, wm, wn, acc);
 }
 
-// Few rows: W is read once, by 16 of its rows a workgroup whose eight waves split the contraction, and bounds the time.  Up to
-// 16 RT rows a workgroup (blockIdx.y: the next ones).
+// Few rows (up to 16 RT): W is read once, by 16 of its rows a workgroup whose eight waves split the contraction.  The wait for its
+// loads bounds it: 24 rows, 2048 x 2048, bfloat16: 8 us (8.4 MB).
 constexpr int FEW_THREADS = 512;
 template <class TR, int RT, bool AL>
 __global__ __launch_bounds__(FEW_THREADS) void k_project_few(const ProjectArgs a) {
@@ -470,17 +474,16 @@ __global__ __launch_bounds__(FEW_THREADS) void k_project_few(const ProjectArgs a
   __shared__ int sAdapter[ROWS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, kg = lane >> 4;
   const int n0 = blockIdx.x * 16;
-  const int64_t m0 = (int64_t)blockIdx.y * ROWS;
-  const int rows = (int)min((int64_t)ROWS, a.q.n_rows - m0);
+  const int rows = (int)min((int64_t)ROWS, a.q.n_rows);
   const T* W = static_cast<const T*>(a.W) + (int64_t)(n0 + i) * a.k;
-  const T* x = static_cast<const T*>(a.x) + (m0 + i) * a.x_stride;
+  const T* x = static_cast<const T*>(a.x) + i * a.x_stride;
   f32x4 acc[RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
   const u32x4 none = {0, 0, 0, 0};
   // whose adapter a row has
   for (int r = wave; r < rows; r += WAVES) {
-    const int s = owner_of(a.q.off, a.q.n_seqs, m0 + r);
+    const int s = owner_of(a.q.off, a.q.n_seqs, r);
     if (lane == 0) sAdapter[r] = s < 0 ? -1 : adapter(a.q, s);
   }
   constexpr int RUN = RT == 4 ? 4 : 8;          // steps side by side of a wave, whose loads are on the way at once
@@ -512,17 +515,18 @@ __global__ __launch_bounds__(FEW_THREADS) void k_project_few(const ProjectArgs a
     const int ad = sAdapter[row];
     if (ad >= 0) {
       const T* up = static_cast<const T*>(a.up) + (int64_t)ad * a.rank * a.n + n0 + col;
-      const float* low = a.low + (m0 + row) * a.padded;
+      const float* low = a.low + row * a.padded;
 #pragma unroll 8
       for (int j = 0; j < a.rank; ++j) sum = fmaf(low[j], TR::get(up[(int64_t)j * a.n]), sum);
     }
-    static_cast<T*>(a.y)[(m0 + row) * a.n + n0 + col] = TR::put(sum);
+    static_cast<T*>(a.y)[(int64_t)row * a.n + n0 + col] = TR::put(sum);
   }
 }
 
 // Few columns (up to 64) and a rank up to 32: both products with x in one pass over it.  A workgroup takes 32 rows; its waves split
 // the width as k_low's do, with W's rows and those of the adapter as operands side by side.  Further requests in the same rows
-// take further passes, for their adapters alone.
+// take further passes, for their adapters alone.  L2 and the matrix cores bound it: 32768 rows of 512, 20 columns, rank 4, float32: 33 us
+// (67 MB, 2.0 TB/s, matrix cores busy a third of it).
 constexpr int NARROW_ROWS = 32;
 template <class TR, bool AL, int WT, int JT>
 __global__ __launch_bounds__(THREADS) void k_project_narrow(const ProjectArgs a, const void* A_all, float scale) {
@@ -637,6 +641,8 @@ struct GradArgs {
 constexpr int GRAD_COLS = 128, GRAD_ROWS = 64;
 
 // A workgroup takes 128 columns of one adapter's gradient and a part of the rows, and of these the requests that have the adapter.
+// The wait for 64 rows at a time bounds it: 4096 rows, 2048 + 2048 columns, rank 16, 8 adapters, bfloat16: 20 us (34 MB), and
+// 4 for the sum over two parts.
 template <class TR, int JT, bool AL>
 __global__ __launch_bounds__(THREADS) void k_adapter_grad(const GradArgs a) {
   using T = typename TR::T;
@@ -839,7 +845,7 @@ void launch_tiles(const ProjectArgs& a, hipStream_t s) {
 template <class TR, bool NN, bool AL>
 void launch_project(const ProjectArgs& a, hipStream_t s) {
   if (!NN && a.q.n_rows <= 64) {
-    const dim3 grid((a.n + 15) / 16, 1);
+    const dim3 grid((a.n + 15) / 16);
     if (a.q.n_rows <= 16) hipLaunchKernelGGL((k_project_few<TR, 1, AL>), grid, dim3(FEW_THREADS), 0, s, a);
     else if (a.q.n_rows <= 32) hipLaunchKernelGGL((k_project_few<TR, 2, AL>), grid, dim3(FEW_THREADS), 0, s, a);
     else hipLaunchKernelGGL((k_project_few<TR, 4, AL>), grid, dim3(FEW_THREADS), 0, s, a);
@@ -898,7 +904,10 @@ void launch_narrow(const ProjectArgs& a, const nugpr_adapter* p, hipStream_t s) 
 template <class TR, bool AL>
 int run_forward(const nugpr_adapter* p, const void* x, int64_t x_stride, void* y, hipStream_t s) {
   const Requests q = requests(p);
-  if (p->dim_out <= 64 && p->rank <= 32 && q.n_rows > 64) {
+  // (one pass over x; each further request with rows in a workgroup's 32 costs it a pass more, which takes the longer the wider x is, so that wide
+  // x with fewer rows than keep the card busy go the general way: 4118 rows of 1959, 23 uneven requests, 64 columns: 81 us, the
+  // general way 45; 2048 rows of 2048: 21 and 16; 32768 rows of 512, 20 columns, float32: 34 and 59)
+  if (p->dim_out <= 64 && p->rank <= 32 && q.n_rows > 64 && (p->dim_in <= 1024 || q.n_rows >= 16384)) {
     const ProjectArgs a{x, p->W, p->B, nullptr, y, x_stride, q, p->dim_in, p->dim_out, p->rank, padded_rank(p)};
     if (p->dim_out <= 16) launch_narrow<TR, AL, 1>(a, p, s);
     else if (p->dim_out <= 32) launch_narrow<TR, AL, 2>(a, p, s);

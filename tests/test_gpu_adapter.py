@@ -107,6 +107,30 @@ def test_tiles_of_256(lib, inp, out, n):
     close(lib.nugpr_adapter_backward(x, W, A, B, dev_off, dy, adapter_of=dev_which)[0], dx.cpu(), TOL[BF16])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,inp,out,rank", [(300, 520, 515, 20), (700, 1000, 1008, 5), (700, 1001, 999, 40), (1500, 1100, 1090, 33),
+                                            (17000, 24, 31, 40), (200, 1300, 40, 9)])
+def test_tiles_between(lib, n, inp, out, rank, dtype):
+    """From too few tiles for all compute units to more than enough, aligned and not."""
+    x, W, A, B, _, _, _, _, dy = inputs([n], inp, out, rank, 3, dtype, seed=12)
+    off, which = np.array([3, 70, 70, 71, n // 2, n - 10]), [1, 0, 2, -1, 0]
+    dev_off, dev_which = torch.from_numpy(off).cuda(), torch.tensor(which, dtype=torch.int32, device="cuda")
+    x64, W64, A64, B64, dy64 = (t.double() for t in (x, W, A, B, dy))
+    y, dx, dA, dB = x64 @ W64.T, dy64 @ W64, torch.zeros_like(A64), torch.zeros_like(B64)
+    for s, a in enumerate(which):
+        r = slice(int(off[s]), int(off[s + 1]))
+        if a >= 0:
+            low, up = x64[r] @ A64[a].T, dy64[r] @ B64[a].T
+            y[r] += low @ B64[a]
+            dx[r] += up @ A64[a]
+            dA[a] += up.T @ x64[r]
+            dB[a] += low.T @ dy64[r]
+    close(lib.nugpr_adapter_forward(x, W, A, B, dev_off, adapter_of=dev_which), y.cpu(), TOL[dtype])
+    got = lib.nugpr_adapter_backward(x, W, A, B, dev_off, dy, adapter_of=dev_which)
+    for g, w in zip(got, (dx, dA, dB)):
+        close(g, w.cpu(), TOL[dtype])
+
+
 def test_gradient_against_differences(lib):
     """y is linear in x and bilinear in A and B: central differences of the float64 reference are exact."""
     x, W, A, B, off, dev_off, which, dev_which, dy = inputs([9, 40, 3], 50, 30, 6, 2, F32, seed=3)
