@@ -137,6 +137,11 @@ struct ProjectArgs {
 //
 // The adapters are further steps of the contraction: for every request with rows in the tile, its rows of h (in bfloat16 as two
 // numbers, 16 bits in all) and KS rows of B_a at a time.  sA, sB: room for BM x 128 bytes and KS x BN.
+// A step waits for its loads, about a microsecond, so that with more than OWN_LANES steps in a small tile every lane works on its own
+// rows and columns instead, in float32: 36 requests of one row, rank 64, 547 to 171 columns and back, bfloat16: 80 us with steps only, 46
+// so; 256 requests of four rows, rank 8, 1000 columns: 36 and 20.  (2: 8 requests of 32 rows 19 us instead of 17; 8: 128 of 8 rows 25
+// instead of 19.)
+constexpr int OWN_LANES = 4;
 template <class TR, int BM, int BN, int MT, int NTL, int N_THREADS, bool AL>
 __device__ inline void add_adapters(const ProjectArgs& a, int64_t m0, int n0, int rows, int wm, int wn, typename TR::T* sA, typename TR::T* sB,
                                     f32x4 (&acc)[NTL][MT]) {
@@ -144,6 +149,60 @@ __device__ inline void add_adapters(const ProjectArgs& a, int64_t m0, int n0, in
   using Frag = typename TR::Frag;
   constexpr int KS = TR::KS, E = TR::E, BK = 128 / sizeof(T);
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, kg = lane >> 4;
+  if constexpr (MT * NTL <= 4) {
+    int own[MT], count = 0;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) own[m] = -1;
+    for (int at = 0; at < a.q.n_seqs; at += 64) {
+      const int mine = at + lane;
+      int64_t lo = 0, hi = 0;
+      int ad = -1;
+      if (mine < a.q.n_seqs) {
+        lo = clamped(a.q.off[mine], m0, m0 + rows);
+        hi = clamped(a.q.off[mine + 1], lo, m0 + rows);
+        ad = adapter(a.q, mine);
+      }
+      uint64_t some = __ballot(hi > lo && ad >= 0);
+      while (some) {
+        const int from = __builtin_ctzll(some);
+        some &= some - 1;
+        ++count;
+        const int rlo = __shfl((int)(lo - m0), from), rhi = __shfl((int)(hi - m0), from), one = __shfl(ad, from);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+          if (wm + 16 * m + i >= rlo && wm + 16 * m + i < rhi) own[m] = one;
+      }
+    }
+    if (count * ((a.rank + KS - 1) / KS) > OWN_LANES) {
+      if (tid >= THREADS) return;          // (further groups of the same tile)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        if (own[m] < 0) continue;
+        const float* low = a.low + (m0 + wm + 16 * m + i) * a.padded;
+#pragma unroll
+        for (int n = 0; n < NTL; ++n) {
+          const int col = n0 + wn + 16 * n + 4 * kg;
+          const T* up = static_cast<const T*>(a.up) + (int64_t)own[m] * a.rank * a.n + col;
+          if (col + 4 <= a.n) {
+#pragma unroll 8
+            for (int j = 0; j < a.rank; ++j) {
+              T b[4];
+              __builtin_memcpy(b, up + (int64_t)j * a.n, sizeof(b));
+              const float h = low[j];
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[n][m][r] = fmaf(h, TR::get(b[r]), acc[n][m][r]);
+            }
+          } else {
+            for (int j = 0; j < a.rank; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (col + r < a.n) acc[n][m][r] = fmaf(low[j], TR::get(up[(int64_t)j * a.n + r]), acc[n][m][r]);
+          }
+        }
+      }
+      return;
+    }
+  }
   const int along_at = TR::template along_at<BK>(i, kg);
   int cols_at[TR::ACROSS];
   TR::template columns_at<BN>(cols_at, wn, i, kg);

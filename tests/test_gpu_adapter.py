@@ -131,6 +131,26 @@ def test_tiles_between(lib, n, inp, out, rank, dtype):
         close(g, w.cpu(), TOL[dtype])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("inp,out,rank", [(200, 136, 8), (131, 203, 40), (70, 1200, 3)])
+def test_many_requests_in_a_tile(lib, inp, out, rank, dtype):
+    """Requests of none to four rows, one in seven without an adapter, one adapter with a value that is not finite."""
+    lens = [s * 3 % 5 for s in range(70)]
+    x, W, A, B, off, dev_off, _, _, dy = inputs(lens, inp, out, rank, 5, dtype, seed=13)
+    which = [-1 if s % 7 == 3 else s % 5 for s in range(70)]
+    dev_which = torch.tensor(which, dtype=torch.int32, device="cuda")
+    bad_A, bad_B = A.clone(), B.clone()
+    bad_A[2, rank - 1, inp - 1], bad_B[2, 0, 1] = float("nan"), float("inf")
+    hit = torch.zeros(x.shape[0], dtype=torch.bool)
+    for s, a in enumerate(which):
+        hit[off[s]:off[s + 1]] = a == 2
+    for AA, BB, rows in ((A, B, slice(None)), (bad_A, bad_B, ~hit)):
+        close(lib.nugpr_adapter_forward(x, W, AA, BB, dev_off, adapter_of=dev_which, scale=1.5)[rows],
+              reference(x, W, A, B, off, which, 1.5)[rows], TOL[dtype])
+        dx = lib.nugpr_adapter_backward(x, W, AA, BB, dev_off, dy, adapter_of=dev_which, scale=1.5)[0]
+        close(dx[rows], reference(x, W, A, B, off, which, 1.5, dy)[0][rows], TOL[dtype])
+
+
 def test_gradient_against_differences(lib):
     """y is linear in x and bilinear in A and B: central differences of the float64 reference are exact."""
     x, W, A, B, off, dev_off, which, dev_which, dy = inputs([9, 40, 3], 50, 30, 6, 2, F32, seed=3)
