@@ -33,14 +33,15 @@ __device__ inline int adapter(const Requests& q, int s) {
   return a >= 0 && a < q.n_adapters ? a : -1;
 }
 
-// 16 bytes of a row from column `col` on, zero past `width`; AL: aligned, and the width a multiple of them
-template <class TR, bool AL>
+// 16 bytes of a row from column `col` on, zero past `width`; AL: aligned, and the width a multiple of them;
+// NOW: nothing else is done while it is on its way
+template <class TR, bool AL, bool NOW = false>
 __device__ inline u32x4 run16(const typename TR::T* row, int64_t col, int64_t width) {
   u32x4 v = {0, 0, 0, 0};
   if constexpr (AL) {
     if (col < width) v = *reinterpret_cast<const u32x4*>(row + col);
   } else if (col + TR::E <= width) {
-    v = load16(row + col);
+    v = NOW ? load16_now(row + col) : load16(row + col);
   } else if (col < width) {
 #pragma unroll
     for (int j = 0; j < TR::E; ++j)
@@ -97,10 +98,10 @@ __global__ __launch_bounds__(1024) void k_low(const LowArgs a) {
 #pragma unroll
     for (int u = 0; u < RUN; ++u) {
       const int col = k0 + u * TR::KS + kg * TR::E;
-      xv[u] = i < rows ? run16<TR, AL>(x, col, sd.width) : u32x4{0, 0, 0, 0};
+      xv[u] = i < rows ? run16<TR, AL, true>(x, col, sd.width) : u32x4{0, 0, 0, 0};
 #pragma unroll
       for (int n = 0; n < TILES; ++n)
-        av[u][n] = 16 * n + i < a.rank ? run16<TR, AL>(A + (int64_t)(16 * n + i) * sd.width, col, sd.width) : u32x4{0, 0, 0, 0};
+        av[u][n] = 16 * n + i < a.rank ? run16<TR, AL, true>(A + (int64_t)(16 * n + i) * sd.width, col, sd.width) : u32x4{0, 0, 0, 0};
     }
 #pragma unroll
     for (int u = 0; u < RUN; ++u)
@@ -240,7 +241,7 @@ __device__ inline void add_adapters(const ProjectArgs& a, int64_t m0, int n0, in
         for (int c = tid; c < KS * BN / E; c += N_THREADS) {
           const int row = c / (BN / E), col = c % (BN / E) * E;
           *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(sB) + TR::template unit<BN>(row, col)) =
-              j0 + row < a.rank ? run16<TR, AL>(up + (int64_t)(j0 + row) * a.n, n0 + col, a.n) : u32x4{0, 0, 0, 0};
+              j0 + row < a.rank ? run16<TR, AL, true>(up + (int64_t)(j0 + row) * a.n, n0 + col, a.n) : u32x4{0, 0, 0, 0};
         }
         __syncthreads();
         Frag wf[NTL];
@@ -551,9 +552,9 @@ __global__ __launch_bounds__(FEW_THREADS) void k_project_few(const ProjectArgs a
 #pragma unroll
     for (int u = 0; u < RUN; ++u) {
       const int col = k0 + u * TR::KS + kg * TR::E;
-      w[u] = n0 + i < a.n ? run16<TR, AL>(W, col, a.k) : none;
+      w[u] = n0 + i < a.n ? run16<TR, AL, true>(W, col, a.k) : none;
 #pragma unroll
-      for (int r = 0; r < RT; ++r) v[u][r] = 16 * r + i < rows ? run16<TR, AL>(x + 16 * r * a.x_stride, col, a.k) : none;
+      for (int r = 0; r < RT; ++r) v[u][r] = 16 * r + i < rows ? run16<TR, AL, true>(x + 16 * r * a.x_stride, col, a.k) : none;
     }
 #pragma unroll
     for (int u = 0; u < RUN; ++u)
@@ -616,11 +617,11 @@ __global__ __launch_bounds__(THREADS) void k_project_narrow(const ProjectArgs a,
       for (int u = 0; u < RUN; ++u) {
         const int col = k0 + u * TR::KS + kg * TR::E;
 #pragma unroll
-        for (int r = 0; r < RT; ++r) xv[u][r] = 16 * r + i < rows ? run16<TR, AL>(x + 16 * r * a.x_stride, col, a.k) : none;
+        for (int r = 0; r < RT; ++r) xv[u][r] = 16 * r + i < rows ? run16<TR, AL, true>(x + 16 * r * a.x_stride, col, a.k) : none;
 #pragma unroll
-        for (int n = 0; n < WT; ++n) wv[u][n] = first && 16 * n + i < a.n ? run16<TR, AL>(W + (int64_t)(16 * n) * a.k, col, a.k) : none;
+        for (int n = 0; n < WT; ++n) wv[u][n] = first && 16 * n + i < a.n ? run16<TR, AL, true>(W + (int64_t)(16 * n) * a.k, col, a.k) : none;
 #pragma unroll
-        for (int n = 0; n < JT; ++n) wv[u][WT + n] = ad >= 0 && 16 * n + i < a.rank ? run16<TR, AL>(A + (int64_t)(16 * n) * a.k, col, a.k) : none;
+        for (int n = 0; n < JT; ++n) wv[u][WT + n] = ad >= 0 && 16 * n + i < a.rank ? run16<TR, AL, true>(A + (int64_t)(16 * n) * a.k, col, a.k) : none;
       }
 #pragma unroll
       for (int u = 0; u < RUN; ++u)
@@ -964,8 +965,7 @@ template <class TR, bool AL>
 int run_forward(const nugpr_adapter* p, const void* x, int64_t x_stride, void* y, hipStream_t s) {
   const Requests q = requests(p);
   // (one pass over x; each further request with rows in a workgroup's 32 costs it a pass more, which takes the longer the wider x is, so that wide
-  // x with fewer rows than keep the card busy go the general way: 4118 rows of 1959, 23 uneven requests, 64 columns: 81 us, the
-  // general way 45; 2048 rows of 2048: 21 and 16; 32768 rows of 512, 20 columns, float32: 34 and 59)
+  // x with fewer rows than keep the card busy go the general way: 2048 rows of 2048, 64 columns: 21 us, the general way 16; 32768 rows of 512, 20 columns, float32: 34 and 59)
   if (p->dim_out <= 64 && p->rank <= 32 && q.n_rows > 64 && (p->dim_in <= 1024 || q.n_rows >= 16384)) {
     const ProjectArgs a{x, p->W, p->B, nullptr, y, x_stride, q, p->dim_in, p->dim_out, p->rank, padded_rank(p)};
     if (p->dim_out <= 16) launch_narrow<TR, AL, 1>(a, p, s);

@@ -49,12 +49,29 @@ __device__ inline int swizzle_bytes(int row) {
 // A tile in LDS whose rows are read as operands both along the rows and across them has no padding; of every row the 16-byte
 // units are permuted (unit ^ swizzle(row)) so that the units that a wave's lanes want at one time lie on different banks: one unit
 // of 16 consecutive rows, or some units side by side of a few rows.
-// 16 bytes, or 8, at any address that the values themselves are aligned at
+// 16 bytes at any address that the values themselves are aligned at
 __device__ inline u32x4 load16(const void* p) {
   u32x4 v;
   __builtin_memcpy(&v, p, 16);
   return v;
 }
+// The same for loads that are waited for at once.  Those of two-byte values that are not on four bytes take a multiple of the others' time: they
+// come in the five words that hold them (and no word more), shifted.
+__device__ inline u32x4 load16_now(const float* p) { return load16(p); }
+__device__ inline u32x4 load16_now(const uint16_t* p) {
+  const uint32_t odd = (uint32_t)reinterpret_cast<uintptr_t>(p) & 2u;
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(p) - odd);
+  u32x4 v;
+  __builtin_memcpy(&v, words, 16);
+  if (odd) {
+    uint32_t last;
+    __builtin_memcpy(&last, words + 4, 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_alignbit(j < 3 ? v[j + 1] : last, v[j], 16);
+  }
+  return v;
+}
+// 16 bytes, or 8
 template <class V>
 __device__ inline void store_any(void* p, V v) {
   __builtin_memcpy(p, &v, sizeof(V));
