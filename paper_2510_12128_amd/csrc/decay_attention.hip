@@ -150,9 +150,9 @@ __device__ inline void put(typename TR::T* tile, int at, const u32x4* r) {
 // the state, for k_span_join.  SUM: some role's o is a sum over heads of k and v (gk > 1).
 // Per block and head: P^T = K Q^T (each wave tiles of 16 rows of Q), masked and decayed, goes through LDS; o^T = S^T Q^T and V^T P^T with
 // the wave's columns of S and V; S += K^T (w V).  S is read as an operand where it lies (matrix_core.h).  In bfloat16 P and
-// the operand that S is read as are rounded to it, as o is in the end: together that is 1.4 times the error of the last
-// rounding alone, where 16 bits of S would cost twice the products and six times the conversions; w V, which is summed into the
-// float32 state, keeps all 24 bits.
+// S are each read as two bfloat16, 17 bits of them: no more than the float32 sums' own error, so that o is rounded once.  (With one bfloat16 of
+// each o had 1.4 times the error of its last rounding; it took 217 us instead of 250 for 65536 rows, 16 / 4 heads of 128, 197 instead of 229 for the
+// gradients of 16 x 1024 rows, 16 heads.)  w V, which is summed into the float32 state, keeps all 24 bits.
 // Values that are not finite: rows s > t must not touch o_t, but 0 x NaN in the masked part of P would; a block whose V
 // has such a value takes P V row by row.
 // What bounds it: memory in bfloat16, the matrix cores and LDS together in float32, the length of the chain where there are few rows.
@@ -174,7 +174,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
   __shared__ __align__(16) T sK[C * D];
   __shared__ __align__(16) T sV[C * D];
   __shared__ __align__(16) T sQ[WALK ? C * D : 8];
-  __shared__ __align__(16) T sP[WALK ? C * PLD : 8];
+  __shared__ __align__(16) T sP[WALK ? TR::SPLIT * C * PLD : 8];
   __shared__ __align__(16) float sLam[2 * C + 4];    // lam^n at C + n; zero before C
   __shared__ __align__(16) float sPw[WALK ? 2 * C + 4 : 4];    // the same, as P is multiplied by it
   __shared__ __align__(16) float sW[C];          // weights of the block's rows in the state
@@ -362,8 +362,19 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
             }
           }
           T* to = sP + t * PLD + 16 * st + 4 * kg;
-          if constexpr (KT == 2) *reinterpret_cast<u32x2*>(to) = u32x2{two_bf16(p[0], p[1]), two_bf16(p[2], p[3])};
-          else *reinterpret_cast<f32x4*>(to) = p;
+          if constexpr (KT == 2) {
+            const u32x2 near = {two_bf16(p[0], p[1]), two_bf16(p[2], p[3])};
+            float rest[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              rest[r] = p[r] - from_two(near[r >> 1], r & 1);
+              rest[r] = rest[r] == rest[r] ? rest[r] : 0.f;      // (an infinity has none)
+            }
+            *reinterpret_cast<u32x2*>(to) = near;
+            *reinterpret_cast<u32x2*>(to + C * PLD) = u32x2{two_bf16(rest[0], rest[1]), two_bf16(rest[2], rest[3])};
+          } else {
+            *reinterpret_cast<f32x4*>(to) = p;
+          }
         }
         // o^T = S^T Q^T, rows of the state's columns
         if (gk == 1 || m == 0) {
@@ -376,19 +387,21 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
             for (int k = 0; k < D / KS; ++k) {
               if (LOOK && k * KS >= ro->dk) break;
               __builtin_amdgcn_sched_barrier(0);
-              Frag sf[NT];
+              Frag sf[NT][TR::SPLIT];
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
                 f32x4 part[KT];
 #pragma unroll
                 for (int x = 0; x < KT; ++x) part[x] = S[k * KT + x][n];
-                sf[n] = acc_frag(part, TR{});
+                acc_frags(part, sf[n], TR{});
               }
 #pragma unroll
               for (int tt = 0; tt < C / 16; ++tt) {
                 const Frag q = TR::template along<D>(sQ, along_at, 16 * tt, k * KS);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) o[n][tt] = TR::mfma(sf[n], q, o[n][tt]);
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                  for (int x = 0; x < TR::SPLIT; ++x) o[n][tt] = TR::mfma(sf[n][x], q, o[n][tt]);
               }
             }
 #pragma unroll
@@ -449,16 +462,21 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
 #pragma unroll
             for (int tt = 0; tt < C / 16; ++tt)
               if (16 * tt + 15 >= k * KS) {
-                const Frag pf = TR::row_frag(sP + (16 * tt + i) * PLD, k * KS, kg);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) o[n][tt] = TR::mfma(vf[n], pf, o[n][tt]);
+                for (int x = 0; x < TR::SPLIT; ++x) {
+                  const Frag pf = TR::row_frag(sP + (x * C + 16 * tt + i) * PLD, k * KS, kg);
+#pragma unroll
+                  for (int n = 0; n < NT; ++n) o[n][tt] = TR::mfma(vf[n], pf, o[n][tt]);
+                }
               }
           }
         } else {
           for (int s = 0; s < cnt; ++s)
 #pragma unroll
             for (int tt = 0; tt < C / 16; ++tt) {
-              const float p = TR::get(sP[(16 * tt + i) * PLD + s]);
+              float p = 0.f;
+#pragma unroll
+              for (int x = 0; x < TR::SPLIT; ++x) p += TR::get(sP[(x * C + 16 * tt + i) * PLD + s]);
               if (s <= 16 * tt + i)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)

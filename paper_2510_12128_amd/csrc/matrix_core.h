@@ -27,6 +27,7 @@ __device__ inline uint32_t two_bf16(float lo, float hi) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
 }
+__device__ inline float from_two(uint32_t two, int nth) { return __builtin_bit_cast(float, nth ? two & 0xffff0000u : two << 16); }
 // the upper halves of two float32: their first eight significant bits, the rest cut off
 __device__ inline uint32_t two_upper(float lo, float hi) {
   return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
@@ -83,6 +84,7 @@ struct Bf16 {
   static constexpr int KS = 32;     // contraction indexes of a step
   static constexpr int E = 8;       // values in 16 bytes
   static constexpr int PARTS = 3;   // a float32 is exactly three bfloat16
+  static constexpr int SPLIT = 2;   // bfloat16 that a float32 factor beside bfloat16 ones is read as, each the nearest: 17 bits of it
   static constexpr int LOW_PARTS = 2; // parts that a float32 factor beside a bfloat16 one is read with, where 16 of its bits are wanted
   static __device__ float get(T x) { return from_bf16(x); }
   static __device__ T put(float x) { return to_bf16(x); }
@@ -160,6 +162,7 @@ struct F32 {
   static constexpr int KS = 16;
   static constexpr int E = 4;
   static constexpr int PARTS = 1;
+  static constexpr int SPLIT = 1;
   static constexpr int LOW_PARTS = 1;
   static __device__ float get(T x) { return x; }
   static __device__ T put(float x) { return x; }
@@ -210,13 +213,18 @@ struct F32 {
   static __device__ int col_k(int j, int kg) { return 4 * kg + j; }
 };
 
-// Operand of the KS / 16 accumulator tiles t[0 .. KS / 16 - 1], whose rows become the contraction index (bfloat16: rounded).
-__device__ inline F32::Frag acc_frag(const f32x4* t, F32) { return t[0]; }
-__device__ inline Bf16::Frag acc_frag(const f32x4* t, Bf16) {
-  u32x4 v;
+// Operands of the KS / 16 accumulator tiles t[0 .. KS / 16 - 1], whose rows become the contraction index.
+__device__ inline void acc_frags(const f32x4* t, F32::Frag (&out)[1], F32) { out[0] = t[0]; }
+__device__ inline void acc_frags(const f32x4* t, Bf16::Frag (&out)[2], Bf16) {
+  u32x4 near, rest;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = two_bf16(t[j >> 1][2 * (j & 1)], t[j >> 1][2 * (j & 1) + 1]);
-  return __builtin_bit_cast(bf16x8, v);
+  for (int j = 0; j < 4; ++j) {
+    const float a = t[j >> 1][2 * (j & 1)], b = t[j >> 1][2 * (j & 1) + 1];
+    near[j] = two_bf16(a, b);
+    rest[j] = two_bf16(a - from_two(near[j], 0), b - from_two(near[j], 1));
+  }
+  out[0] = __builtin_bit_cast(bf16x8, near);
+  out[1] = __builtin_bit_cast(bf16x8, rest);
 }
 
 // Operand times one float32 weight a contraction index, without rounding to fewer than 24 bits: in bfloat16 the product is cut
