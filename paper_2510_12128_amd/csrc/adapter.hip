@@ -935,9 +935,9 @@ void launch_project(const ProjectArgs& a, hipStream_t s) {
     if (small <= 512) return launch_tiles<TR, 64, 64, 2, 2, 2, NN, AL>(a, s);
   } else {
     if (small <= 256) return launch_tiles<TR, 32, 32, 2, 2, 1, NN, AL>(a, s);
+    if (a.n <= 32) return launch_tiles<TR, 128, 32, 4, 1, 1, NN, AL>(a, s);
   }
-  if (a.n <= 32) launch_tiles<TR, 128, 32, 4, 1, 1, NN, AL>(a, s);
-  else launch_tiles<TR, 64, 64, 2, 2, 1, NN, AL>(a, s);
+  launch_tiles<TR, 64, 64, 2, 2, 1, NN, AL>(a, s);
 }
 
 template <class TR, bool AL>

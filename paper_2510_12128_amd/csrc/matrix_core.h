@@ -40,16 +40,16 @@ __device__ inline uint32_t odd_bits(u32x4 v, uint32_t exponent, uint32_t one) {
   return ((v[0] & exponent) + one) | ((v[1] & exponent) + one) | ((v[2] & exponent) + one) | ((v[3] & exponent) + one);
 }
 
-// The permutation below for rows of that many bytes.
+// A tile in LDS whose rows are read as operands both along the rows and across them has no padding; of every row the 16-byte
+// units are permuted (unit ^ swizzle(row)) so that the units that a wave's lanes want at one time lie on different banks: one unit
+// of 16 consecutive rows, or some units side by side of a few rows.  Here for
+// rows of that many bytes.
 template <int BYTES>
 __device__ inline int swizzle_bytes(int row) {
   const int far = ((row >> 3 ^ row >> 2) & 1) << 1 | (row >> 3 & 1);
   return BYTES >= 256 ? (row & 3) << 2 | far : BYTES == 128 ? (row & 2) << 1 | far : far;
 }
 
-// A tile in LDS whose rows are read as operands both along the rows and across them has no padding; of every row the 16-byte
-// units are permuted (unit ^ swizzle(row)) so that the units that a wave's lanes want at one time lie on different banks: one unit
-// of 16 consecutive rows, or some units side by side of a few rows.
 // 16 bytes at any address that the values themselves are aligned at
 __device__ inline u32x4 load16(const void* p) {
   u32x4 v;
@@ -88,8 +88,6 @@ struct Bf16 {
   static constexpr int LOW_PARTS = 2; // parts that a float32 factor beside a bfloat16 one is read with, where 16 of its bits are wanted
   static __device__ float get(T x) { return from_bf16(x); }
   static __device__ T put(float x) { return to_bf16(x); }
-  typedef u32x2 Four;               // four values
-  static __device__ T nth(Four v, int j) { return (T)(v[j >> 1] >> (16 * (j & 1))); }
   static constexpr uint32_t SIGN = 0x80008000u;
   static __device__ uint32_t odd(u32x4 v) { return odd_bits(v, 0x7f807f80u, 0x00800080u); }
   static __device__ f32x4 mfma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -135,8 +133,6 @@ struct Bf16 {
   // Index that row 4 kg of accumulator tile m stands for (4 kg + r: that plus r), so that two tiles, 2 x and 2 x + 1, are an operand
   // with contraction indexes 32 x .. in their natural order.
   static __device__ int acc_row(int m, int kg) { return (m >> 1) * 32 + 8 * kg + 4 * (m & 1); }
-  template <int D>
-  static __device__ float at(const T* tile, int row, int col) { return get(unit<D>(tile, row, col & ~7)[col & 7]); }
   static __device__ Frag row_frag(const T* row, int k0, int kg) { return *reinterpret_cast<const Frag*>(row + k0 + 8 * kg); }
   // operand whose contraction runs over the rows of a tile: columns m0 .. m0 + 15, rows k0 .. k0 + 31, by transposing reads (the
   // 16 lanes of a group read four rows of 16 columns, lane i gets column i)
@@ -166,8 +162,6 @@ struct F32 {
   static constexpr int LOW_PARTS = 1;
   static __device__ float get(T x) { return x; }
   static __device__ T put(float x) { return x; }
-  typedef f32x4 Four;
-  static __device__ T nth(Four v, int j) { return v[j]; }
   static constexpr uint32_t SIGN = 0x80000000u;
   static __device__ uint32_t odd(u32x4 v) { return odd_bits(v, 0x7f800000u, 0x00800000u); }
   static __device__ f32x4 mfma(Frag a, Frag b, f32x4 c) {
