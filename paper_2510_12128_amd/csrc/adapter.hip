@@ -136,8 +136,8 @@ struct ProjectArgs {
 // What the large products share.  The accumulators' rows are the columns of y, four in a row a lane: tile (n, m) of a wave stands for
 // columns wn + 16 n + 4 kg .. and row wm + 16 m + i of the workgroup's tile.
 //
-// The adapters are further steps of the contraction: for every request with rows in the tile, its rows of h (in bfloat16 as two
-// numbers, 16 bits in all) and KS rows of B_a at a time.  sA, sB: room for BM x 128 bytes and KS x BN.
+// The adapters are further steps of the contraction: for every request with rows in the tile, its rows of h (in bfloat16 as three
+// numbers, exactly) and KS rows of B_a at a time.  sA, sB: room for BM x 128 bytes and BN x 128 bytes.
 // A step waits for its loads, about a microsecond, so that with more than OWN_LANES steps in a small tile every lane works on its own
 // rows and columns instead, in float32: 36 requests of one row, rank 64, 547 to 171 columns and back, bfloat16: 80 us with steps only, 46
 // so; 256 requests of four rows, rank 8, 1000 columns: 36 and 20.  (2: 8 requests of 32 rows 19 us instead of 17; 8: 128 of 8 rows 25
@@ -204,7 +204,9 @@ __device__ inline void add_adapters(const ProjectArgs& a, int64_t m0, int n0, in
       return;
     }
   }
-  const int along_at = TR::template along_at<BK>(i, kg);
+  static_assert(TR::PARTS == 1 || BM <= BN, "the third part of h lies beside B_a in sB");
+  const int along_at = TR::template along_at<BK>(i, kg), third_at = TR::template along_at<KS>(i, kg);
+  T* sThird = sB + KS * BN;
   int cols_at[TR::ACROSS];
   TR::template columns_at<BN>(cols_at, wn, i, kg);
   for (int at = 0; at < a.q.n_seqs; at += 64) {
@@ -229,14 +231,12 @@ __device__ inline void add_adapters(const ProjectArgs& a, int64_t m0, int n0, in
           const int row = c / (KS / 4), col = c % (KS / 4) * 4;
           f32x4 v = {0.f, 0.f, 0.f, 0.f};
           if (row >= rlo && row < rhi) v = *reinterpret_cast<const f32x4*>(a.low + (m0 + row) * a.padded + j0 + col);
-          char* to = reinterpret_cast<char*>(sA);
-          if constexpr (E == 8) {
-            *reinterpret_cast<u32x2*>(to + TR::template unit<BK>(row, col)) = u32x2{two_upper(v[0], v[1]), two_upper(v[2], v[3])};
-            *reinterpret_cast<u32x2*>(to + TR::template unit<BK>(row, KS + col)) =
-                u32x2{two_bf16(v[0] - upper(v[0]), v[1] - upper(v[1])), two_bf16(v[2] - upper(v[2]), v[3] - upper(v[3]))};
-          } else {
-            *reinterpret_cast<f32x4*>(to + TR::template unit<BK>(row, col)) = v;
-          }
+          typename TR::Four parts[TR::PARTS];
+          exact_parts(v, parts, TR{});
+#pragma unroll
+          for (int x = 0; x < TR::PARTS; ++x)
+            *reinterpret_cast<typename TR::Four*>(x < 2 ? reinterpret_cast<char*>(sA) + TR::template unit<BK>(row, x * KS + col)
+                                                        : reinterpret_cast<char*>(sThird) + TR::template unit<KS>(row, col)) = parts[x];
         }
         for (int c = tid; c < KS * BN / E; c += N_THREADS) {
           const int row = c / (BN / E), col = c % (BN / E) * E;
@@ -253,14 +253,15 @@ __device__ inline void add_adapters(const ProjectArgs& a, int64_t m0, int n0, in
         for (int m = 0; m < MT; ++m) {
           const int row = wm + 16 * m + i;
           const bool own = row >= rlo && row < rhi;
-          Frag xf[TR::LOW_PARTS];
+          Frag xf[TR::PARTS];
 #pragma unroll
-          for (int part = 0; part < TR::LOW_PARTS; ++part) xf[part] = TR::template along<BK>(sA, along_at, wm + 16 * m, part * KS);
+          for (int part = 0; part < TR::PARTS; ++part)
+            xf[part] = part < 2 ? TR::template along<BK>(sA, along_at, wm + 16 * m, part * KS) : TR::template along<KS>(sThird, third_at, wm + 16 * m, 0);
 #pragma unroll
           for (int n = 0; n < NTL; ++n) {
             f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int part = 0; part < TR::LOW_PARTS; ++part) v = TR::mfma(wf[n], xf[part], v);
+            for (int part = 0; part < TR::PARTS; ++part) v = TR::mfma(wf[n], xf[part], v);
 #pragma unroll
             for (int r = 0; r < 4; ++r) acc[n][m][r] += own ? v[r] : 0.f;
           }
@@ -710,7 +711,7 @@ __global__ __launch_bounds__(THREADS) void k_adapter_grad(const GradArgs a) {
   constexpr int KS = TR::KS, E = TR::E, PAD = 16 / sizeof(T), LDX = GRAD_COLS + PAD, LDJ = 16 * JT + PAD;
   constexpr int X = GRAD_ROWS * GRAD_COLS / E / THREADS;
   __shared__ __align__(16) T sX[GRAD_ROWS * LDX];
-  __shared__ __align__(16) T sL[TR::LOW_PARTS][GRAD_ROWS * LDJ];
+  __shared__ __align__(16) T sL[TR::PARTS][GRAD_ROWS * LDJ];
   const int side = (int)blockIdx.x < a.side[0].tiles ? 0 : 1;
   const GradSide& sd = a.side[side];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, kg = lane >> 4;
@@ -760,13 +761,10 @@ __global__ __launch_bounds__(THREADS) void k_adapter_grad(const GradArgs a) {
 #pragma unroll
         for (int p = 0; p < JT; ++p) {
           const int c = tid + p * THREADS, row = c / (4 * JT), col = c % (4 * JT) * 4;
-          if constexpr (E == 8) {
-            *reinterpret_cast<u32x2*>(sL[0] + row * LDJ + col) = u32x2{two_upper(w[p][0], w[p][1]), two_upper(w[p][2], w[p][3])};
-            *reinterpret_cast<u32x2*>(sL[TR::LOW_PARTS - 1] + row * LDJ + col) =
-                u32x2{two_bf16(w[p][0] - upper(w[p][0]), w[p][1] - upper(w[p][1])), two_bf16(w[p][2] - upper(w[p][2]), w[p][3] - upper(w[p][3]))};
-          } else {
-            *reinterpret_cast<f32x4*>(sL[0] + row * LDJ + col) = w[p];
-          }
+          typename TR::Four parts[TR::PARTS];
+          exact_parts(w[p], parts, TR{});
+#pragma unroll
+          for (int x = 0; x < TR::PARTS; ++x) *reinterpret_cast<typename TR::Four*>(sL[x] + row * LDJ + col) = parts[x];
         }
         __syncthreads();
         if (r0 + GRAD_ROWS < rhi) load(r0 + GRAD_ROWS);
@@ -776,7 +774,7 @@ __global__ __launch_bounds__(THREADS) void k_adapter_grad(const GradArgs a) {
 #pragma unroll
           for (int m = 0; m < 2; ++m) xf[m] = TR::col_frag(sX, LDX, k, 32 * wave + 16 * m, i, kg);
 #pragma unroll
-          for (int part = 0; part < TR::LOW_PARTS; ++part)
+          for (int part = 0; part < TR::PARTS; ++part)
 #pragma unroll
             for (int j = 0; j < JT; ++j) {
               const Frag lf = TR::col_frag(sL[part], LDJ, k, 16 * j, i, kg);

@@ -84,8 +84,8 @@ struct Bf16 {
   static constexpr int KS = 32;     // contraction indexes of a step
   static constexpr int E = 8;       // values in 16 bytes
   static constexpr int PARTS = 3;   // a float32 is exactly three bfloat16
+  typedef u32x2 Four;               // four values
   static constexpr int SPLIT = 2;   // bfloat16 that a float32 factor beside bfloat16 ones is read as, each the nearest: 17 bits of it
-  static constexpr int LOW_PARTS = 2; // parts that a float32 factor beside a bfloat16 one is read with, where 16 of its bits are wanted
   static __device__ float get(T x) { return from_bf16(x); }
   static __device__ T put(float x) { return to_bf16(x); }
   static constexpr uint32_t SIGN = 0x80008000u;
@@ -158,8 +158,8 @@ struct F32 {
   static constexpr int KS = 16;
   static constexpr int E = 4;
   static constexpr int PARTS = 1;
+  typedef f32x4 Four;
   static constexpr int SPLIT = 1;
-  static constexpr int LOW_PARTS = 1;
   static __device__ float get(T x) { return x; }
   static __device__ T put(float x) { return x; }
   static constexpr uint32_t SIGN = 0x80000000u;
@@ -219,6 +219,17 @@ __device__ inline void acc_frags(const f32x4* t, Bf16::Frag (&out)[2], Bf16) {
   }
   out[0] = __builtin_bit_cast(bf16x8, near);
   out[1] = __builtin_bit_cast(bf16x8, rest);
+}
+
+// Four float32 as the operand type's numbers whose sum they are: themselves, or three bfloat16 of eight significant bits each.
+__device__ inline void exact_parts(f32x4 v, f32x4 (&out)[1], F32) { out[0] = v; }
+__device__ inline void exact_parts(f32x4 v, u32x2 (&out)[3], Bf16) {
+#pragma unroll
+  for (int x = 0; x < 3; ++x) {
+    out[x] = u32x2{two_upper(v[0], v[1]), two_upper(v[2], v[3])};
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] -= upper(v[r]);
+  }
 }
 
 // Operand times one float32 weight a contraction index, without rounding to fewer than 24 bits: in bfloat16 the product is cut
