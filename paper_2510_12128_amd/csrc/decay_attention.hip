@@ -61,6 +61,9 @@ __device__ void power(float g, double n, float& hi, float& lo) {
   lo = (float)(p - (double)hi);
 }
 
+// x lam + add, lam as the sum of two float32 (an infinite x keeps its sign beside the smaller one)
+__device__ inline float decayed(float x, float hi, float lo, float add) { return fmaf(x, hi, fmaf(__builtin_isinf(x) ? 0.f : x, lo, add)); }
+
 // (a value that all lanes have, in a scalar register)
 __device__ inline double same_in_all(double x) {
   const u32x2 v = __builtin_bit_cast(u32x2, x);
@@ -145,6 +148,95 @@ __device__ inline void put(typename TR::T* tile, int at, const u32x4* r) {
     *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(tile) + at + p * L::PASS * D * (int)sizeof(typename TR::T)) = r[p];
 }
 
+// (ScanArgs is k_decay_scan's only argument, its roles come first)
+typedef const __attribute__((address_space(4))) ScanRole* RolePtr;
+
+// A workgroup's span.
+struct Span {
+  int seq;                  // < 0: there is none
+  int64_t lo, len, from;    // rows of the sequence; the span's first one, counted along the scan
+};
+__device__ inline Span span_of(const ScanArgs& a, int item) {
+  const PieceOf piece = piece_of(a.off, a.n_seqs, a.n_rows, a.span_log2, item);
+  return Span{piece.seq, piece.lo, piece.hi - piece.lo, (int64_t)(item - ((piece.lo >> a.span_log2) + piece.seq)) << a.span_log2};
+}
+
+// Where the state of a span comes from and goes to, or null.
+template <bool WALK>
+__device__ inline const float* start_of(const ScanArgs& a, RolePtr ro, const Span& sp, int item, int h) {
+  if (!WALK) return nullptr;
+  const int64_t size = (int64_t)ro->dk * ro->dv;
+  if (sp.len > (int64_t)1 << a.span_log2) return ro->spans + ((int64_t)item * a.kv + h) * size;
+  return ro->s_in ? ro->s_in + ((int64_t)sp.seq * a.kv + h) * size : nullptr;
+}
+template <bool WALK>
+__device__ inline float* end_of(const ScanArgs& a, RolePtr ro, const Span& sp, int item, int h) {
+  const int64_t size = (int64_t)ro->dk * ro->dv;
+  if (!WALK) return ro->spans + ((int64_t)item * a.kv + h) * size;
+  return sp.from + ((int64_t)1 << a.span_log2) >= sp.len && ro->s_out ? ro->s_out + ((int64_t)sp.seq * a.kv + h) * size : nullptr;
+}
+
+// A span by the recurrence itself, token by token in float32, without LDS or barriers: a wave has 16 columns of the state, a lane every
+// fourth row of one of them.
+template <class TR, int D, bool WALK, bool SUM>
+__device__ inline void walk_tokens(const ScanArgs& a, RolePtr ro, int tid, int block) {
+  using T = typename TR::T;
+  constexpr int EACH = D / 4;
+  const int h = block % a.kv, item = block / a.kv;
+  const float g = log_of(a.log_decay, h);
+  const Span sp = span_of(a, item);
+  const int n_tok = (int)min((int64_t)1 << a.span_log2, sp.len - sp.from);
+  const int col = tid / 64 * 16 + (tid & 15), e = ro->back, dk = ro->dk, dir = e ? -1 : 1, gq = WALK ? ro->gq : 0, gk = SUM ? ro->gk : 1;
+  const int64_t first = e ? sp.lo + sp.len - 1 - sp.from : sp.lo + sp.from;
+  const bool live = col < ro->dv;
+  const int s_r = ro->s_trans ? 1 : ro->dv, s_c = ro->s_trans ? dk : 1;
+  const float* from = start_of<WALK>(a, ro, sp, item, h);
+  float* to = end_of<WALK>(a, ro, sp, item, h);
+  int row0 = tid >> 4 & 3;
+  float S[EACH], lam_hi, lam_lo;
+  power(g, 1.0, lam_hi, lam_lo);
+#pragma unroll
+  for (int x = 0; x < EACH; ++x) S[x] = from && live && row0 + 4 * x < dk ? from[(row0 + 4 * x) * s_r + col * s_c] : 0.f;
+#pragma unroll 1
+  for (int t = 0; t < n_tok; ++t) {
+    const int64_t at = first + (int64_t)dir * t;
+    asm volatile("" : "+v"(row0));                         // (which rows there are is not kept ready, lane by lane)
+    if (!e)
+#pragma unroll
+      for (int x = 0; x < EACH; ++x) S[x] = decayed(S[x], lam_hi, lam_lo, 0.f);
+#pragma unroll 1
+    for (int m = 0; m < gk; ++m) {
+      const T* k = static_cast<const T*>(ro->k) + at * ro->k_row + ((int64_t)h * ro->gk + m) * ro->k_head;
+      const float v = live ? ro->wscale * TR::get((static_cast<const T*>(ro->v) + at * ro->v_row + ((int64_t)h * ro->gk + m) * ro->v_head)[col]) : 0.f;
+#pragma unroll
+      for (int x = 0; x < EACH; ++x) {
+        if (x % 8 == 0) __builtin_amdgcn_sched_barrier(0);
+        if (row0 + 4 * x < dk) S[x] = fmaf(TR::get(k[row0 + 4 * x]), v, S[x]);
+      }
+    }
+#pragma unroll 1
+    for (int m = 0; m < gq; ++m) {
+      const T* q = static_cast<const T*>(ro->q) + at * ro->q_row + ((int64_t)h * ro->gq + m) * ro->q_head;
+      float o = 0.f;
+#pragma unroll
+      for (int x = 0; x < EACH; ++x) {
+        if (x % 8 == 0) __builtin_amdgcn_sched_barrier(0);
+        if (row0 + 4 * x < dk) o = fmaf(TR::get(q[row0 + 4 * x]), S[x], o);
+      }
+      o += __shfl_xor(o, 16);
+      o += __shfl_xor(o, 32);
+      if (live && row0 == 0) (static_cast<T*>(ro->o) + at * ro->o_row + ((int64_t)h * ro->gq + m) * ro->o_head)[col] = TR::put(ro->oscale * o);
+    }
+    if (e)
+#pragma unroll
+      for (int x = 0; x < EACH; ++x) S[x] = decayed(S[x], lam_hi, lam_lo, 0.f);
+  }
+  if (to && live)
+#pragma unroll
+    for (int x = 0; x < EACH; ++x)
+      if (row0 + 4 * x < dk) to[(row0 + 4 * x) * s_r + col * s_c] = S[x];
+}
+
 // One workgroup walks one span of one sequence and key / value head in blocks of C rows; the state stays in accumulator
 // registers, 16 of its columns a wave.  WALK: writes o from given start states; else: what the span adds to
 // the state, for k_span_join.  SUM: some role's o is a sum over heads of k and v (gk > 1).
@@ -153,8 +245,9 @@ __device__ inline void put(typename TR::T* tile, int at, const u32x4* r) {
 // S are each read as two bfloat16, 17 bits of them: no more than the float32 sums' own error, so that o is rounded once.  (With one bfloat16 of
 // each o had 1.4 times the error of its last rounding; it took 217 us instead of 250 for 65536 rows, 16 / 4 heads of 128, 197 instead of 229 for the
 // gradients of 16 x 1024 rows, 16 heads.)  w V, which is summed into the float32 state, keeps all 24 bits.
-// Values that are not finite: rows s > t must not touch o_t, but 0 x NaN in the masked part of P would; a block whose V
-// has such a value takes P V row by row.
+// Values that are not finite: rows s > t must not touch o_t, but 0 x NaN in the masked part of P would, nor may an infinity meet the
+// zeros beside a width or the difference of two infinities between the parts of a factor.  So a span whose results are not all finite is
+// walked once more, by walk_tokens.
 // What bounds it: memory in bfloat16, the matrix cores and LDS together in float32, the length of the chain where there are few rows.
 // Measured: 65536 rows, 16 / 4 heads of 128, bfloat16: 168 us to walk (671 MB, 4.0 TB/s) after 40 to add up; without loads
 // and stores the walk takes 127.  16 x 1024 rows, 16 heads, gradients: 205 us (three roles, 805 MB, 3.9 TB/s).  20011 rows, 8 heads of
@@ -178,11 +271,8 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
   __shared__ __align__(16) float sLam[2 * C + 4];    // lam^n at C + n; zero before C
   __shared__ __align__(16) float sPw[WALK ? 2 * C + 4 : 4];    // the same, as P is multiplied by it
   __shared__ __align__(16) float sW[C];          // weights of the block's rows in the state
-  __shared__ int sOdd;
 
   // The role's numbers are read from the arguments where they are needed: kept over the loop they would not fit the scalar registers.
-  // (ScanArgs is the only argument, its roles come first.)
-  typedef const __attribute__((address_space(4))) ScanRole* RolePtr;
   RolePtr ro = (RolePtr)((const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr() + blockIdx.y * sizeof(ScanRole));
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int i = tid & 15, kg = (tid >> 4) & 3;
@@ -199,13 +289,10 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
     return;
   }
   const float g = log_of(a.log_decay, h);
-  const PieceOf piece = piece_of(a.off, a.n_seqs, a.n_rows, a.span_log2, item);
-  const int seq = piece.seq;
-  if (seq < 0) return;
-  const int64_t lo = piece.lo, hi = piece.hi;
-  const int64_t len = hi - lo, span = (int64_t)1 << a.span_log2;
-  const int64_t c0 = (item - ((lo >> a.span_log2) + seq)) << a.span_log2;
-  const bool last = c0 + span >= len, several = len > span;
+  const Span sp = span_of(a, item);
+  if (sp.seq < 0) return;
+  const int64_t len = sp.len, span = (int64_t)1 << a.span_log2, c0 = sp.from;
+  const bool last = c0 + span >= len;
   if (c0 > 0 && c0 >= len) return;
   if (!WALK && last) return;
   const int n_tok = (int)min(span, len - c0);
@@ -214,7 +301,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
   // the first loads are on their way while the rest is made ready
   const int gq = WALK ? ro->gq : 1, gk = SUM ? ro->gk : 1, heads = max(gq, gk);
   const int blocks = (n_tok + C - 1) / C;
-  const int64_t first = e ? hi - 1 - c0 : lo + c0;
+  const int64_t first = e ? sp.lo + len - 1 - c0 : sp.lo + c0;
   const int dir = e ? -1 : 1;
   // row 0 of the block to load next in the arrays, and a thread's places
   const int row0 = tid / L::A_ROW, col_in = tid % L::A_ROW * TR::E;
@@ -245,7 +332,6 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
     sLam[n] = n < C ? 0.f : (float)exp((double)g * (n - C));
     if (WALK) sPw[n] = ro->wscale * ro->oscale * sLam[n];
   }
-  if (tid == 0) sOdd = 0;
   // lam^C in every block is rounded so that the product of them all stays within a rounding of its exact value: a block's
   // rounding error would otherwise add up over the hundreds of blocks that a slowly decaying state remembers
   const double lam_block = same_in_all(exp((double)g * C)), lam_inv = same_in_all(lam_block > 1e-30 ? 1.0 / lam_block : 0.0);
@@ -255,11 +341,8 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
   f32x4 S[D / 16][NT];
   const int col0 = wave * 16 * NT;
   const bool mine = !LOOK || col0 < ro->dv;
-  const int64_t s_size = (int64_t)ro->dk * ro->dv;
   const int s_r = ro->s_trans ? 1 : ro->dv, s_c = ro->s_trans ? ro->dk : 1;
-  const float* from = !WALK ? nullptr
-                      : several ? ro->spans + ((int64_t)item * a.kv + h) * s_size
-                      : ro->s_in ? ro->s_in + ((int64_t)seq * a.kv + h) * s_size : nullptr;
+  const float* from = start_of<WALK>(a, ro, sp, item, h);
   bool have = from != nullptr;
 #pragma unroll
   for (int m = 0; m < D / 16; ++m)
@@ -270,6 +353,8 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
         const int row = TR::acc_row(m, kg) + r, col = col0 + 16 * n + i;
         S[m][n][r] = have && row < ro->dk && col < ro->dv ? from[row * s_r + col * s_c] : 0.f;
       }
+
+  float odd = 0.f;      // NaN: a result was not finite
 
   // and in LDS
   int put_at = TR::template unit<D>(row0, col_in), along_at = TR::template along_at<D>(i, kg);
@@ -300,7 +385,6 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
     }
     out_cnt = 0;
   };
-  int kv_step = 0;
   for (int b = 0; b < blocks; ++b) {
     const int cnt = min(C, n_tok - b * C);
     for (int m = 0; m < heads; ++m) {
@@ -313,15 +397,8 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
       if constexpr (WALK)
         if (out_cnt > 0) flush();
       if (kv_new) {
-        ++kv_step;
         put<TR, D, C>(sK, put_at, rk);
         put<TR, D, C>(sV, put_at, rv);
-        if (WALK) {
-          uint32_t odd = 0;
-#pragma unroll
-          for (int p = 0; p < L::N; ++p) odd |= TR::odd(rv[p]);
-          if (odd & TR::SIGN) sOdd = kv_step;
-        }
         if (tid < C) sW[tid] = tid < cnt ? ro->wscale * sLam[C + cnt - 1 - tid + e] : 0.f;
       }
       if constexpr (WALK)
@@ -451,11 +528,10 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
       if constexpr (WALK) {
         __syncthreads();
         // o^T += V^T P^T (P lies in its natural order, as the transposing reads give V)
-        const bool odd = sOdd == kv_step;
-        if (!mine) {
-        } else if (!odd) {
+        if (mine) {
 #pragma unroll
           for (int k = 0; k < C / KS; ++k) {
+            __builtin_amdgcn_sched_barrier(0);
             Frag vf[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) vf[n] = TR::template columns<D>(sV, v_cols, k * KS, n);
@@ -470,22 +546,16 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
                 }
               }
           }
-        } else {
-          for (int s = 0; s < cnt; ++s)
-#pragma unroll
-            for (int tt = 0; tt < C / 16; ++tt) {
-              float p = 0.f;
-#pragma unroll
-              for (int x = 0; x < TR::SPLIT; ++x) p += TR::get(sP[(x * C + 16 * tt + i) * PLD + s]);
-              if (s <= 16 * tt + i)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                  for (int r = 0; r < 4; ++r)
-                    o[n][tt][r] += p * TR::get(*reinterpret_cast<const T*>(reinterpret_cast<const char*>(sV) + TR::template unit<D>(s, col0 + 16 * n + 4 * kg + r)));
-            }
+          __builtin_amdgcn_sched_barrier(0);
         }
         if (gk == 1 || m + 1 == heads) {
+#pragma unroll
+          for (int tt = 0; tt < C / 16; ++tt)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) odd = fmaf(o[n][tt][r], 0.f, odd);
+          asm volatile("" : "+v"(odd));
           out_at = o_at + (gq > 1 ? m * ro->o_head : 0);
           out_cnt = cnt;
 #pragma unroll
@@ -506,9 +576,21 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
     __syncthreads();
     if (out_cnt > 0) flush();
   }
-  float* to = !WALK ? ro->spans + ((int64_t)item * a.kv + h) * s_size
-              : last && ro->s_out ? ro->s_out + ((int64_t)seq * a.kv + h) * s_size : nullptr;
-  if (to) {
+#pragma unroll
+  for (int m = 0; m < D / 16; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) odd = fmaf(S[m][n][r], 0.f, odd);
+  if (__syncthreads_or(odd != 0.f)) {
+    __threadfence();                             // (rows of o that are written once more)
+    __syncthreads();
+    int block = blockIdx.x;
+    asm volatile("" : "+s"(block));              // (it finds its span anew: kept so far, that would not fit the registers)
+    walk_tokens<TR, D, WALK, SUM>(a, ro, tid, block);
+    return;
+  }
+  if (float* to = end_of<WALK>(a, ro, sp, item, h)) {
 #pragma unroll
     for (int m = 0; m < D / 16; ++m)
 #pragma unroll
@@ -560,7 +642,7 @@ __global__ __launch_bounds__(THREADS) void k_span_join(const JoinArgs a) {
         for (int x = 0; x < 8; ++x)
           if (j0 + x < spans) {
             first[(j0 + x) * stride + e] = cur;
-            cur = fmaf(cur, lam_hi, fmaf(cur, lam_lo, add[x]));
+            cur = decayed(cur, lam_hi, lam_lo, add[x]);
           }
       }
     }
@@ -579,7 +661,7 @@ __global__ __launch_bounds__(THREADS) void k_span_join(const JoinArgs a) {
 #pragma unroll
       for (int x = 0; x < JOIN_EACH; ++x) add[x] = j1 + x + 1 < spans ? p[(j1 + x) * stride] : 0.f;
 #pragma unroll
-      for (int x = 0; x < JOIN_EACH; ++x) all = fmaf(all, lam_hi, fmaf(all, lam_lo, add[x]));
+      for (int x = 0; x < JOIN_EACH; ++x) all = decayed(all, lam_hi, lam_lo, add[x]);
       __syncthreads();
       sum[part][lane] = all;
       __syncthreads();
@@ -590,10 +672,10 @@ __global__ __launch_bounds__(THREADS) void k_span_join(const JoinArgs a) {
 #pragma unroll
           for (int x = 0; x < JOIN_EACH; ++x) {
             if (x < n && live) p[(j1 + x) * stride] = c;
-            c = fmaf(c, lam_hi, fmaf(c, lam_lo, add[x]));
+            c = decayed(c, lam_hi, lam_lo, add[x]);
           }
         }
-        cur = fmaf(cur, far_hi, fmaf(cur, far_lo, sum[k][lane]));
+        cur = decayed(cur, far_hi, far_lo, sum[k][lane]);
       }
       start = cur;                                         // (used where all parts were full)
     }
