@@ -244,9 +244,12 @@ __device__ inline void add_adapters(const ProjectArgs& a, int64_t m0, int n0, in
               j0 + row < a.rank ? run16<TR, AL, true>(up + (int64_t)(j0 + row) * a.n, n0 + col, a.n) : u32x4{0, 0, 0, 0};
         }
         __syncthreads();
-        Frag wf[NTL];
+        Frag wf[NTL], finite[NTL];
 #pragma unroll
-        for (int n = 0; n < NTL; ++n) wf[n] = TR::template columns<BN>(sB, cols_at, 0, n);
+        for (int n = 0; n < NTL; ++n) {
+          wf[n] = TR::template columns<BN>(sB, cols_at, 0, n);
+          finite[n] = finite_frag(wf[n], TR{});
+        }
         // (an adapter may hold values that are not finite: they are for the rows of its own requests, where a zero row of h
         // would make them NaN)
 #pragma unroll
@@ -261,7 +264,7 @@ __device__ inline void add_adapters(const ProjectArgs& a, int64_t m0, int n0, in
           for (int n = 0; n < NTL; ++n) {
             f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int part = 0; part < TR::PARTS; ++part) v = TR::mfma(wf[n], xf[part], v);
+            for (int part = 0; part < TR::PARTS; ++part) v = TR::mfma(part ? finite[n] : wf[n], xf[part], v);
 #pragma unroll
             for (int r = 0; r < 4; ++r) acc[n][m][r] += own ? v[r] : 0.f;
           }
@@ -770,16 +773,19 @@ __global__ __launch_bounds__(THREADS) void k_adapter_grad(const GradArgs a) {
         if (r0 + GRAD_ROWS < rhi) load(r0 + GRAD_ROWS);
 #pragma unroll
         for (int k = 0; k < GRAD_ROWS; k += KS) {
-          Frag xf[2];
+          Frag xf[2], finite[2];
 #pragma unroll
-          for (int m = 0; m < 2; ++m) xf[m] = TR::col_frag(sX, LDX, k, 32 * wave + 16 * m, i, kg);
+          for (int m = 0; m < 2; ++m) {
+            xf[m] = TR::col_frag(sX, LDX, k, 32 * wave + 16 * m, i, kg);
+            finite[m] = finite_frag(xf[m], TR{});
+          }
 #pragma unroll
           for (int part = 0; part < TR::PARTS; ++part)
 #pragma unroll
             for (int j = 0; j < JT; ++j) {
               const Frag lf = TR::col_frag(sL[part], LDJ, k, 16 * j, i, kg);
 #pragma unroll
-              for (int m = 0; m < 2; ++m) acc[m][j] = TR::mfma(xf[m], lf, acc[m][j]);
+              for (int m = 0; m < 2; ++m) acc[m][j] = TR::mfma(part ? finite[m] : xf[m], lf, acc[m][j]);
             }
         }
       }

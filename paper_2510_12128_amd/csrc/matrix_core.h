@@ -34,10 +34,10 @@ __device__ inline uint32_t two_upper(float lo, float hi) {
 }
 __device__ inline float upper(float x) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u); }
 
-// Bits that tell whether a 16-byte run holds a value that is not finite: `sign` of them, ored together (an exponent of ones carries
-// into the sign's place).
-__device__ inline uint32_t odd_bits(u32x4 v, uint32_t exponent, uint32_t one) {
-  return ((v[0] & exponent) + one) | ((v[1] & exponent) + one) | ((v[2] & exponent) + one) | ((v[3] & exponent) + one);
+// Two bfloat16 with zeros for those that are not finite (an exponent of ones carries into the sign's place).
+__device__ inline uint32_t finite_two(uint32_t x) {
+  const uint32_t odd = ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  return x & ~(odd | (odd - (odd >> 15)));
 }
 
 // A tile in LDS whose rows are read as operands both along the rows and across them has no padding; of every row the 16-byte
@@ -88,8 +88,6 @@ struct Bf16 {
   static constexpr int SPLIT = 2;   // bfloat16 that a float32 factor beside bfloat16 ones is read as, each the nearest: 17 bits of it
   static __device__ float get(T x) { return from_bf16(x); }
   static __device__ T put(float x) { return to_bf16(x); }
-  static constexpr uint32_t SIGN = 0x80008000u;
-  static __device__ uint32_t odd(u32x4 v) { return odd_bits(v, 0x7f807f80u, 0x00800080u); }
   static __device__ f32x4 mfma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
   // (Along: a 16-byte read serves lanes 0-3, 12-15, 20-23, 24-27 at one time, and three more such sets; so rows 0-3, 12-15
@@ -162,8 +160,6 @@ struct F32 {
   static constexpr int SPLIT = 1;
   static __device__ float get(T x) { return x; }
   static __device__ T put(float x) { return x; }
-  static constexpr uint32_t SIGN = 0x80000000u;
-  static __device__ uint32_t odd(u32x4 v) { return odd_bits(v, 0x7f800000u, 0x00800000u); }
   static __device__ f32x4 mfma(Frag a, Frag b, f32x4 c) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
@@ -221,15 +217,29 @@ __device__ inline void acc_frags(const f32x4* t, Bf16::Frag (&out)[2], Bf16) {
   out[1] = __builtin_bit_cast(bf16x8, rest);
 }
 
-// Four float32 as the operand type's numbers whose sum they are: themselves, or three bfloat16 of eight significant bits each.
+// Four float32 as the operand type's numbers whose sum they are: themselves, or three bfloat16 of eight significant bits each (of an
+// infinity: itself and zeros).
 __device__ inline void exact_parts(f32x4 v, f32x4 (&out)[1], F32) { out[0] = v; }
 __device__ inline void exact_parts(f32x4 v, u32x2 (&out)[3], Bf16) {
 #pragma unroll
   for (int x = 0; x < 3; ++x) {
     out[x] = u32x2{two_upper(v[0], v[1]), two_upper(v[2], v[3])};
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] -= upper(v[r]);
+    for (int r = 0; r < 4; ++r) {
+      v[r] -= upper(v[r]);
+      v[r] = v[r] == v[r] ? v[r] : 0.f;
+    }
   }
+}
+
+// The operand that the second and third parts of a factor are multiplied by: one that is not finite has its product with the first part, and the
+// others may be zero.
+__device__ inline F32::Frag finite_frag(F32::Frag v, F32) { return v; }
+__device__ inline Bf16::Frag finite_frag(Bf16::Frag v, Bf16) {
+  u32x4 x = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = finite_two(x[j]);
+  return __builtin_bit_cast(bf16x8, x);
 }
 
 // Operand times one float32 weight a contraction index, without rounding to fewer than 24 bits: in bfloat16 the product is cut

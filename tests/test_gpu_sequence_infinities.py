@@ -117,3 +117,48 @@ def test_a_step_keeps_an_infinite_state(lib, dtype):
     want_o, want_S = recurrence(q, k, v, g, [0, 1, 2, 3], S0)
     alike(S, want_S, TOL[F32], "state")
     alike(o, want_o, TOL[dtype], "o")
+
+
+def adapted(x, W, A, B, off, which, dy):
+    x, W, A, B, dy = (t.double().cpu() for t in (x, W, A, B, dy))
+    y, dx, dA, dB = x @ W.T, dy @ W, torch.zeros_like(A), torch.zeros_like(B)
+    for s, a in enumerate(which):
+        r = slice(int(off[s]), int(off[s + 1]))
+        low, up = x[r] @ A[a].T, dy[r] @ B[a].T
+        y[r] += low @ B[a]
+        dx[r] += up @ A[a]
+        dA[a] += up.T @ x[r]
+        dB[a] += low.T @ dy[r]
+    return y, dx, dA, dB
+
+
+@pytest.mark.parametrize("whole", [False, True], ids=["spread", "ones"])     # (ones: low parts of h are zero)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("where", ["x", "dy", "A", "B", "W"])
+@pytest.mark.parametrize("lens,inp,out,rank", [
+    ([5, 9, 30], 64, 80, 4), ([5, 9, 400], 64, 80, 33), ([5, 90, 400], 256, 40, 8), ([4] * 70, 130, 203, 20), ([700, 20, 800], 256, 1088, 3),
+    ([1, 300, 5400], 192, 2104, 2), ([1, 300, 2600], 192, 2104, 40)], ids=lambda x: str(sum(x)) if isinstance(x, list) else str(x))
+def test_adapters(lib, lens, inp, out, rank, where, dtype, whole):
+    gen = torch.Generator().manual_seed(inp + rank)
+    off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+    n, which = int(off[-1]), [s % 3 for s in range(len(lens))]
+
+    def some(*shape):
+        return (torch.ones(*shape) if whole else positive(gen, *shape)).to(dtype)
+
+    x, W, A, B, dy = some(n, inp), some(out, inp), some(3, rank, inp), some(3, rank, out), some(n, out)
+    if where == "x":
+        x[2, 7], x[n - 3, 0] = INF, -INF
+    elif where == "dy":
+        dy[2, 7], dy[n - 3, 0] = INF, -INF
+    elif where == "A":
+        A[1, rank - 1, 5] = INF
+    elif where == "B":
+        B[1, 0, 5] = -INF
+    else:
+        W[3, 4] = INF
+    args = [t.cuda() for t in (x, W, A, B, torch.from_numpy(off))]
+    dev_which = torch.tensor(which, dtype=torch.int32, device="cuda")
+    got = (lib.nugpr_adapter_forward(*args, adapter_of=dev_which), *lib.nugpr_adapter_backward(*args, dy.cuda(), adapter_of=dev_which))
+    for g, w, name in zip(got, adapted(x, W, A, B, off, which, dy), ("y", "dx", "dA", "dB")):
+        alike(g, w, TOL[dtype], name)
