@@ -176,56 +176,125 @@ __device__ inline float* end_of(const ScanArgs& a, RolePtr ro, const Span& sp, i
   return sp.from + ((int64_t)1 << a.span_log2) >= sp.len && ro->s_out ? ro->s_out + ((int64_t)sp.seq * a.kv + h) * size : nullptr;
 }
 
-// A span by the recurrence itself, token by token in float32, without LDS or barriers: a wave has 16 columns of the state, a lane every
-// fourth row of one of them.
+// N values of a row that has `left` more; zero past its end.
+template <class TR, int N>
+__device__ inline void row_part(const typename TR::T* row, int left, float (&v)[N]) {
+  constexpr int E = TR::E;
+  static_assert(N % E == 0, "");
+#pragma unroll
+  for (int c = 0; c < N / E; ++c) {
+    typename TR::T part[E] = {};
+    if (c * E + E <= left) {
+      const u32x4 x = load16(row + c * E);
+      __builtin_memcpy(part, &x, 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j)
+        if (c * E + j < left) part[j] = row[c * E + j];
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j) v[c * E + j] = TR::get(part[j]);
+  }
+}
+
+// A workgroup's span for the rare ways that find it anew.
+template <class TR, bool WALK, bool SUM>
+struct SpanRows {
+  using T = typename TR::T;
+  RolePtr ro;
+  Span sp;
+  int h, item, n_tok, dir, gq, gk;
+  int64_t first;
+  __device__ SpanRows(const ScanArgs& a, RolePtr ro, int block) : ro(ro), sp(span_of(a, block / a.kv)), h(block % a.kv), item(block / a.kv) {
+    n_tok = (int)min((int64_t)1 << a.span_log2, sp.len - sp.from);
+    dir = ro->back ? -1 : 1;
+    gq = WALK ? ro->gq : 0;
+    gk = SUM ? ro->gk : 1;
+    first = ro->back ? sp.lo + sp.len - 1 - sp.from : sp.lo + sp.from;
+  }
+  __device__ const T* q(int t, int m) const { return static_cast<const T*>(ro->q) + (first + (int64_t)dir * t) * ro->q_row + ((int64_t)h * ro->gq + m) * ro->q_head; }
+  __device__ const T* k(int t, int m) const { return static_cast<const T*>(ro->k) + (first + (int64_t)dir * t) * ro->k_row + ((int64_t)h * ro->gk + m) * ro->k_head; }
+  __device__ const T* v(int t, int m) const { return static_cast<const T*>(ro->v) + (first + (int64_t)dir * t) * ro->v_row + ((int64_t)h * ro->gk + m) * ro->v_head; }
+  __device__ T* o(int t, int m) const { return static_cast<T*>(ro->o) + (first + (int64_t)dir * t) * ro->o_row + ((int64_t)h * ro->gq + m) * ro->o_head; }
+};
+
+// Whether a span whose results are not all finite may have them wrong: with an infinity among its rows or in its start state, or, where o is
+// written, a NaN in a column of v whose state was none before.  (Any other NaN goes where it belongs.)  A thread's share; the span has it if one does.
+template <class TR, int D, bool WALK, bool SUM>
+__device__ inline bool needs_tokens(const ScanArgs& a, RolePtr ro, int tid, int block) {
+  const SpanRows<TR, WALK, SUM> rows(a, ro, block);
+  constexpr int E = TR::E, A_ROW = D / E;
+  const int col = tid % A_ROW * E, s_c = ro->s_trans ? ro->dk : 1;
+  const float* from = start_of<WALK>(a, ro, rows.sp, rows.item, rows.h);
+  bool found = false, was[E];          // (v makes a column of the state NaN, or none of it)
+#pragma unroll
+  for (int j = 0; j < E; ++j) was[j] = !WALK || (from && col + j < ro->dv && __builtin_isnan(from[(col + j) * s_c]));
+#pragma unroll 1
+  for (int t = tid / A_ROW; t < rows.n_tok; t += blockDim.x / A_ROW) {
+    float x[E];
+#pragma unroll 1
+    for (int m = 0; m < rows.gk; ++m) {
+      row_part<TR>(rows.k(t, m) + col, ro->dk - col, x);
+#pragma unroll
+      for (int j = 0; j < E; ++j) found |= __builtin_isinf(x[j]);
+      row_part<TR>(rows.v(t, m) + col, ro->dv - col, x);
+#pragma unroll
+      for (int j = 0; j < E; ++j) found |= __builtin_isinf(x[j]) || (__builtin_isnan(x[j]) && !was[j]);
+    }
+#pragma unroll 1
+    for (int m = 0; m < rows.gq; ++m) {
+      row_part<TR>(rows.q(t, m) + col, ro->dk - col, x);
+#pragma unroll
+      for (int j = 0; j < E; ++j) found |= __builtin_isinf(x[j]);
+    }
+  }
+  if (from)
+    for (int e = tid; e < ro->dk * ro->dv; e += blockDim.x) found |= __builtin_isinf(from[e]);
+  return found;
+}
+
+// A span by the recurrence itself, token by token in float32, without LDS or barriers: a wave has 16 columns of the state, a lane D / 4 rows
+// of one of them.  The wait for a row's loads bounds it, about a microsecond each: 65536 rows, 16 / 4 heads of 128, bfloat16, with one infinity:
+// 2.7 ms instead of 0.25.
 template <class TR, int D, bool WALK, bool SUM>
 __device__ inline void walk_tokens(const ScanArgs& a, RolePtr ro, int tid, int block) {
-  using T = typename TR::T;
   constexpr int EACH = D / 4;
-  const int h = block % a.kv, item = block / a.kv;
-  const float g = log_of(a.log_decay, h);
-  const Span sp = span_of(a, item);
-  const int n_tok = (int)min((int64_t)1 << a.span_log2, sp.len - sp.from);
-  const int col = tid / 64 * 16 + (tid & 15), e = ro->back, dk = ro->dk, dir = e ? -1 : 1, gq = WALK ? ro->gq : 0, gk = SUM ? ro->gk : 1;
-  const int64_t first = e ? sp.lo + sp.len - 1 - sp.from : sp.lo + sp.from;
+  const SpanRows<TR, WALK, SUM> span(a, ro, block);
+  const float g = log_of(a.log_decay, span.h);
+  const int col = tid / 64 * 16 + (tid & 15), e = ro->back, dk = ro->dk, n_tok = span.n_tok, gq = span.gq, gk = span.gk;
   const bool live = col < ro->dv;
   const int s_r = ro->s_trans ? 1 : ro->dv, s_c = ro->s_trans ? dk : 1;
-  const float* from = start_of<WALK>(a, ro, sp, item, h);
-  float* to = end_of<WALK>(a, ro, sp, item, h);
-  int row0 = tid >> 4 & 3;
+  const float* from = start_of<WALK>(a, ro, span.sp, span.item, span.h);
+  float* to = end_of<WALK>(a, ro, span.sp, span.item, span.h);
+  const int row0 = (tid >> 4 & 3) * EACH;
+  int rows = dk - row0;
   float S[EACH], lam_hi, lam_lo;
   power(g, 1.0, lam_hi, lam_lo);
 #pragma unroll
-  for (int x = 0; x < EACH; ++x) S[x] = from && live && row0 + 4 * x < dk ? from[(row0 + 4 * x) * s_r + col * s_c] : 0.f;
+  for (int x = 0; x < EACH; ++x) S[x] = from && live && x < rows ? from[(row0 + x) * s_r + col * s_c] : 0.f;
 #pragma unroll 1
   for (int t = 0; t < n_tok; ++t) {
-    const int64_t at = first + (int64_t)dir * t;
-    asm volatile("" : "+v"(row0));                         // (which rows there are is not kept ready, lane by lane)
+    asm volatile("" : "+v"(rows));                         // (which rows there are is not kept ready, lane by lane)
     if (!e)
 #pragma unroll
       for (int x = 0; x < EACH; ++x) S[x] = decayed(S[x], lam_hi, lam_lo, 0.f);
 #pragma unroll 1
     for (int m = 0; m < gk; ++m) {
-      const T* k = static_cast<const T*>(ro->k) + at * ro->k_row + ((int64_t)h * ro->gk + m) * ro->k_head;
-      const float v = live ? ro->wscale * TR::get((static_cast<const T*>(ro->v) + at * ro->v_row + ((int64_t)h * ro->gk + m) * ro->v_head)[col]) : 0.f;
+      float k[EACH];
+      row_part<TR>(span.k(t, m) + row0, rows, k);
+      const float v = live ? ro->wscale * TR::get(span.v(t, m)[col]) : 0.f;
 #pragma unroll
-      for (int x = 0; x < EACH; ++x) {
-        if (x % 8 == 0) __builtin_amdgcn_sched_barrier(0);
-        if (row0 + 4 * x < dk) S[x] = fmaf(TR::get(k[row0 + 4 * x]), v, S[x]);
-      }
+      for (int x = 0; x < EACH; ++x) S[x] = fmaf(k[x], v, S[x]);
     }
 #pragma unroll 1
     for (int m = 0; m < gq; ++m) {
-      const T* q = static_cast<const T*>(ro->q) + at * ro->q_row + ((int64_t)h * ro->gq + m) * ro->q_head;
-      float o = 0.f;
+      float q[EACH], o = 0.f;
+      row_part<TR>(span.q(t, m) + row0, rows, q);
 #pragma unroll
-      for (int x = 0; x < EACH; ++x) {
-        if (x % 8 == 0) __builtin_amdgcn_sched_barrier(0);
-        if (row0 + 4 * x < dk) o = fmaf(TR::get(q[row0 + 4 * x]), S[x], o);
-      }
+      for (int x = 0; x < EACH; ++x) o = x < rows ? fmaf(q[x], S[x], o) : o;      // (rows beyond the width may hold zero times an infinity)
       o += __shfl_xor(o, 16);
       o += __shfl_xor(o, 32);
-      if (live && row0 == 0) (static_cast<T*>(ro->o) + at * ro->o_row + ((int64_t)h * ro->gq + m) * ro->o_head)[col] = TR::put(ro->oscale * o);
+      if (live && row0 == 0) span.o(t, m)[col] = TR::put(ro->oscale * o);
     }
     if (e)
 #pragma unroll
@@ -234,7 +303,7 @@ __device__ inline void walk_tokens(const ScanArgs& a, RolePtr ro, int tid, int b
   if (to && live)
 #pragma unroll
     for (int x = 0; x < EACH; ++x)
-      if (row0 + 4 * x < dk) to[(row0 + 4 * x) * s_r + col * s_c] = S[x];
+      if (x < rows) to[(row0 + x) * s_r + col * s_c] = S[x];
 }
 
 // One workgroup walks one span of one sequence and key / value head in blocks of C rows; the state stays in accumulator
@@ -247,7 +316,7 @@ __device__ inline void walk_tokens(const ScanArgs& a, RolePtr ro, int tid, int b
 // gradients of 16 x 1024 rows, 16 heads.)  w V, which is summed into the float32 state, keeps all 24 bits.
 // Values that are not finite: rows s > t must not touch o_t, but 0 x NaN in the masked part of P would, nor may an infinity meet the
 // zeros beside a width or the difference of two infinities between the parts of a factor.  So a span whose results are not all finite is
-// walked once more, by walk_tokens.
+// looked through for them (needs_tokens) and, with them, walked once more (walk_tokens).
 // What bounds it: memory in bfloat16, the matrix cores and LDS together in float32, the length of the chain where there are few rows.
 // Measured: 65536 rows, 16 / 4 heads of 128, bfloat16: 168 us to walk (671 MB, 4.0 TB/s) after 40 to add up; without loads
 // and stores the walk takes 127.  16 x 1024 rows, 16 heads, gradients: 205 us (three roles, 805 MB, 3.9 TB/s).  20011 rows, 8 heads of
@@ -582,15 +651,19 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int r = 0; r < 4; ++r) odd = fmaf(S[m][n][r], 0.f, odd);
-  if (__syncthreads_or(odd != 0.f)) {
-    __threadfence();                             // (rows of o that are written once more)
-    __syncthreads();
+  bool anew = __syncthreads_or(odd != 0.f);
+  if (anew) {
     int block = blockIdx.x;
     asm volatile("" : "+s"(block));              // (it finds its span anew: kept so far, that would not fit the registers)
-    walk_tokens<TR, D, WALK, SUM>(a, ro, tid, block);
-    return;
+    anew = __syncthreads_or(needs_tokens<TR, D, WALK, SUM>(a, ro, tid, block));
+    if (anew) {
+      __threadfence();                           // (rows of o that are written once more)
+      __syncthreads();
+      walk_tokens<TR, D, WALK, SUM>(a, ro, tid, block);
+    }
   }
-  if (float* to = end_of<WALK>(a, ro, sp, item, h)) {
+  float* to = anew ? nullptr : end_of<WALK>(a, ro, sp, item, h);
+  if (to) {
 #pragma unroll
     for (int m = 0; m < D / 16; ++m)
 #pragma unroll

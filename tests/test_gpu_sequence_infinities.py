@@ -1,4 +1,4 @@
-"""An infinite value among the inputs of the sequence operators (GPU) makes the results that the formulas give it, infinities and NaN alike,
+"""An infinite value, or a NaN, among the inputs of the sequence operators (GPU) makes the results that the formulas give it, infinities and NaN alike,
 by the definitions in float64; what it does not reach stays as it is.  Inputs are positive, so that infinities of one sign do not
 cancel by the order of a sum.
 
@@ -57,9 +57,10 @@ def positive(gen, *shape):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("bad", [INF, float("nan")])
 @pytest.mark.parametrize("where", ["k", "v", "q", "initial_state"])
 @pytest.mark.parametrize("h,kv,dk,dv", [(2, 2, 64, 64), (6, 3, 40, 72), (4, 2, 128, 128), (3, 3, 5, 17), (96, 96, 20, 24)])      # (many heads: spans of several blocks)
-def test_attention(lib, h, kv, dk, dv, where, dtype):
+def test_attention(lib, h, kv, dk, dv, where, bad, dtype):
     lens = [40, 0, 2300, 1, 90]                       # one block, none, many spans, one token, two blocks
     off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
     gen = torch.Generator().manual_seed(dk)
@@ -68,14 +69,14 @@ def test_attention(lib, h, kv, dk, dv, where, dtype):
     S0 = positive(gen, len(lens), kv, dk, dv)
     for t in (10, 50, 1500, int(off[4]) + 70):
         if where == "k":
-            k[t, ::2, t % dk] = INF
+            k[t, ::2, t % dk] = bad
         elif where == "v":
-            v[t, ::2, t % dv] = INF
-            v[t + 3, 1::2, (t + 1) % dv] = -INF
+            v[t, ::2, t % dv] = bad
+            v[t + 3, 1::2, (t + 1) % dv] = -bad
         elif where == "q":
-            q[t, h - 1, t % dk] = INF
+            q[t, h - 1, t % dk] = bad
     if where == "initial_state":
-        S0[0, 0, 1, 2], S0[2, kv - 1, 3, 1], S0[3, 0, 2, 2] = INF, -INF, INF
+        S0[0, 0, 1, 2], S0[2, kv - 1, 3, 1], S0[3, 0, 2, 2] = bad, -bad, bad
     g = torch.log1p(-2.0 ** -torch.linspace(7, 10, kv))
     args = [x.cuda() for x in (q, k, v, g, torch.from_numpy(off))]
     o, S = lib.nugpr_decay_attention_forward(*args, initial_state=S0.cuda())
@@ -85,9 +86,10 @@ def test_attention(lib, h, kv, dk, dv, where, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("bad", [INF, float("nan")])
 @pytest.mark.parametrize("where", ["k", "v", "do"])
 @pytest.mark.parametrize("h,kv,dk,dv", [(2, 2, 64, 64), (6, 3, 40, 72), (4, 2, 128, 128)])
-def test_attention_gradients(lib, h, kv, dk, dv, where, dtype):
+def test_attention_gradients(lib, h, kv, dk, dv, where, bad, dtype):
     lens = [40, 0, 500, 1, 90]
     off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
     gen = torch.Generator().manual_seed(dk + 1)
@@ -95,7 +97,7 @@ def test_attention_gradients(lib, h, kv, dk, dv, where, dtype):
     q, k, v, do = (positive(gen, n, x, w).to(dtype) for x, w in ((h, dk), (kv, dk), (kv, dv), (h, dv)))
     S0, R = positive(gen, len(lens), kv, dk, dv), positive(gen, len(lens), kv, dk, dv)
     for t in (10, 250, int(off[4]) + 70):
-        {"k": k, "v": v, "do": do}[where][t, 0, t % min(dk, dv)] = INF
+        {"k": k, "v": v, "do": do}[where][t, 0, t % min(dk, dv)] = bad
     g = torch.log1p(-2.0 ** -torch.linspace(7, 10, kv))
     args = [x.cuda() for x in (q, k, v, g, torch.from_numpy(off), do)]
     got = lib.nugpr_decay_attention_backward(*args, initial_state=S0.cuda(), d_final_state=R.cuda())
