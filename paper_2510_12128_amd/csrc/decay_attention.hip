@@ -784,7 +784,9 @@ __global__ __launch_bounds__(THREADS) void k_decay_step(const StepArgs a) {
       if (slice * COLS + x % COLS < a.dv) ob[(x / COLS) * a.o_head + slice * COLS + x % COLS] = TR::put(0.f);
     return;
   }
-  const float lam = expf(log_of(a.log_decay, h));
+  // (the rounding of one float32 would be the same at every token, and add up over all that the state remembers)
+  float lam_hi, lam_lo;
+  power(log_of(a.log_decay, h), 1.0, lam_hi, lam_lo);
   const T* qb = static_cast<const T*>(a.q) + b * a.q_row + (int64_t)h * a.g * a.q_head;
   const T* kb = static_cast<const T*>(a.k) + b * a.k_row + h * a.k_head;
   const T* vb = static_cast<const T*>(a.v) + b * a.v_row + h * a.v_head;
@@ -812,7 +814,7 @@ __global__ __launch_bounds__(THREADS) void k_decay_step(const StepArgs a) {
     if (live && row < a.dk) {
       const float k = TR::get(kb[row]);
 #pragma unroll
-      for (int j = 0; j < V; ++j) S[s][j] = fmaf(S[s][j], lam, k * v[j]);
+      for (int j = 0; j < V; ++j) S[s][j] = decayed(S[s][j], lam_hi, lam_lo, k * v[j]);
       if constexpr (V == 4) *reinterpret_cast<f32x4*>(sb + row * a.dv + col) = f32x4{S[s][0], S[s][1], S[s][2], S[s][3]};
       else sb[row * a.dv + col] = S[s][0];
     }
