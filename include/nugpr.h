@@ -387,8 +387,8 @@ int nugpr_copy_probe(void* dst /*DEVICE*/, const void* src /*DEVICE*/, size_t by
  *   - Their arrays are float32 or bfloat16 (dtype, the same for all that are not said to be float); sums, states and
  *     decays are float32 in either case.
  *   - Offsets are DEVICE int64 arrays (no call waits for them): sequence s owns rows offsets[s] .. offsets[s+1]-1; ascending,
- *     empty sequences allowed, within 0 .. n_rows (offsets outside are taken as the nearest end: no access is out
- *     of bounds).  Output rows that no sequence owns are set to zero unless said otherwise.
+ *     empty sequences allowed, within 0 .. n_rows (offsets outside are taken as the nearest end; where they do not ascend, results are
+ *     undefined; no access is out of bounds).  Output rows that no sequence owns are set to zero unless said otherwise.
  *   - The calls only enqueue, on the given stream and on the device that is current.  Those that need scratch memory take
  *     a 256-byte aligned DEVICE workspace of the size that the call before them in this file gives; it must not
  *     be used by other work until the call's kernels have ended.  Results do not depend on the order in which workgroups

@@ -10,8 +10,8 @@ namespace nugpr {
 __device__ inline int64_t clamped(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
 // Sequence s has the piece numbers from (offsets[s] >> piece_log2) + s on: with ceil(rows / piece) pieces it ends before the next
-// one's, so no table of them is needed.  The sequence of a piece is the last one that begins at or before it (seq < 0: none);
-// lo, hi: its rows.
+// one's, so no table of them is needed.  The sequence of a piece is the last one that begins at or before it (seq < 0: none; where offsets do
+// not ascend the search may end at one that begins later, which has no such piece); lo, hi: its rows.
 struct PieceOf {
   int seq;
   int64_t lo, hi;
@@ -40,7 +40,8 @@ __device__ inline PieceOf piece_of(const int64_t* off, int n_seqs, int64_t n_row
   }
   const int n = __popcll(__ballot(at < to && (lo >> piece_log2) + at <= item)) - 1;
   if (n < 0) return PieceOf{-1, 0, 0};
-  return PieceOf{from + n, of_lane(lo, n), of_lane(hi, n)};
+  const PieceOf p{from + n, of_lane(lo, n), of_lane(hi, n)};
+  return (p.lo >> piece_log2) + p.seq <= item ? p : PieceOf{-1, 0, 0};
 }
 
 // The sequence that owns a row: the last one that begins at or before it, if it reaches that far; else -1.  (All lanes of a wave
