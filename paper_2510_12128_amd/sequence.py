@@ -1,7 +1,8 @@
 """Operators of sequence models (include/nugpr.h has their definitions): same names as the C entry points, argument checks and
 marshalling only.  Arrays are CUDA tensors, float32 or bfloat16, of any strides with the last dimension contiguous; offsets,
 slots and the like stay on the device, and no call waits for the GPU.  Outputs and scratch memory are torch tensors on
-the current stream of the tensors' device."""
+the current stream of the tensors' device.  Autograd does not record the calls (their gradients are the _backward calls, for a
+torch.autograd.Function or by hand): inputs that require gradients are refused where it would."""
 from __future__ import annotations
 
 import ctypes as C
@@ -36,6 +37,17 @@ def _dense(t, name, device, dtype, shape):
     if not t.is_contiguous():
         _refuse(f"{name} must be contiguous")
     return t.data_ptr()
+
+
+def _refuse_recorded(**tensors):
+    """Refuses the tensor whose gradient autograd expects to follow through the call."""
+    for name, t in tensors.items():
+        if t is not None and t.requires_grad:
+            _refuse(f"{name} requires a gradient, which autograd does not get through this call: use torch.no_grad(), and "
+                    "the _backward calls")
+
+
+_recording, _written = torch.is_grad_enabled, torch.autograd.graph.increment_version
 
 
 def _heads(t, name):
@@ -113,6 +125,9 @@ def nugpr_decay_attention_forward(q, k, v, log_decay, seq_offsets, scale=1.0, in
     float32, <= 0; seq_offsets (n_seqs + 1,) int64; initial_state (n_seqs, kv_heads, dim_k, dim_v) float32 or None.
     Returns o (rows, heads, dim_v) and the sequences' end states, float32."""
     lib = load_library()
+    if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad or log_decay.requires_grad or
+                         (initial_state is not None and initial_state.requires_grad)):
+        _refuse_recorded(q=q, k=k, v=v, log_decay=log_decay, initial_state=initial_state)
     p, device, dtype, shape = _attention(q, k, v, log_decay, scale, *_offsets(seq_offsets, q.device))
     ws = _scratch(lib, lib.nugpr_decay_attention_workspace_bytes, p, 0, device)  # noqa: F841
     s0 = None if initial_state is None else _dense(initial_state, "initial_state", device, torch.float32, shape)
@@ -128,6 +143,11 @@ def nugpr_decay_attention_backward(q, k, v, log_decay, seq_offsets, d_o, scale=1
     """Gradients of nugpr_decay_attention_forward's q, k, v (in their type) and initial state (float32), from d_o and, unless
     None, d_final_state."""
     lib = load_library()
+    if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad or log_decay.requires_grad or
+                         d_o.requires_grad or (initial_state is not None and initial_state.requires_grad) or
+                         (d_final_state is not None and d_final_state.requires_grad)):
+        _refuse_recorded(q=q, k=k, v=v, log_decay=log_decay, d_o=d_o, initial_state=initial_state,
+                         d_final_state=d_final_state)
     p, device, dtype, shape = _attention(q, k, v, log_decay, scale, *_offsets(seq_offsets, q.device))
     ws = _scratch(lib, lib.nugpr_decay_attention_workspace_bytes, p, 1, device)  # noqa: F841
     s0 = None if initial_state is None else _dense(initial_state, "initial_state", device, torch.float32, shape)
@@ -144,12 +164,15 @@ def nugpr_decay_attention_step(q, k, v, log_decay, state, slots=None, scale=1.0)
     """One token for each request: q (requests, heads, dim_k), k, v alike; state (n_states, kv_heads, dim_k, dim_v) float32 is
     advanced in place, request b's at slots[b] (int32; None: b).  Returns o (requests, heads, dim_v)."""
     lib = load_library()
+    if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad or log_decay.requires_grad or state.requires_grad):
+        _refuse_recorded(q=q, k=k, v=v, log_decay=log_decay, state=state)
     p, device, dtype, shape = _attention(q, k, v, log_decay, scale, state.shape[0] if state.dim() else 0, None)
     st = _dense(state, "state", device, torch.float32, shape)
     at = None if slots is None else _dense(slots, "slots", device, torch.int32, (q.shape[0],))
     o = torch.empty((q.shape[0], q.shape[1], v.shape[2]), dtype=dtype, device=device)
     _call(lib.nugpr_decay_attention_step, device, _byref(p), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), st, at,
           _heads(o, "o"))
+    _written(state)                                                # (whoever saved it for a backward pass is told)
     return o
 
 
@@ -176,6 +199,8 @@ def nugpr_adapter_forward(x, W, A, B, seq_offsets, adapter_of=None, scale=1.0):
     x (rows, dim_in), W (dim_out, dim_in), A (adapters, rank, dim_in), B (adapters, rank, dim_out): float32 or bfloat16, W, A
     and B contiguous; seq_offsets (n_seqs + 1,) int64; adapter_of (n_seqs,) int32.  Returns y (rows, dim_out)."""
     lib = load_library()
+    if _recording() and (x.requires_grad or W.requires_grad or A.requires_grad or B.requires_grad):
+        _refuse_recorded(x=x, W=W, A=A, B=B)
     p, ws, device, dtype = _adapter(lib, x, W, A, B, seq_offsets, adapter_of, scale, 0)
     y = torch.empty((x.shape[0], W.shape[0]), dtype=dtype, device=device)
     _call(lib.nugpr_adapter_forward, device, _byref(p), x.data_ptr(), _rows(x, "x"), y.data_ptr())
@@ -185,6 +210,8 @@ def nugpr_adapter_forward(x, W, A, B, seq_offsets, adapter_of=None, scale=1.0):
 def nugpr_adapter_backward(x, W, A, B, seq_offsets, d_y, adapter_of=None, scale=1.0):
     """Gradients of nugpr_adapter_forward's x, A and B, in their type, from d_y; W is fixed."""
     lib = load_library()
+    if _recording() and (x.requires_grad or W.requires_grad or A.requires_grad or B.requires_grad or d_y.requires_grad):
+        _refuse_recorded(x=x, W=W, A=A, B=B, d_y=d_y)
     p, ws, device, dtype = _adapter(lib, x, W, A, B, seq_offsets, adapter_of, scale, 1)
     _like(d_y, "d_y", device, dtype, (x.shape[0], W.shape[0]))
     dx = torch.empty(x.shape, dtype=dtype, device=device)
