@@ -892,7 +892,7 @@ void launch_low(const LowArgs& a, int sides, hipStream_t s) {
   // (so many waves that each has about two runs of loads, 4 to 16; few pieces: 16)
   const int width = sides > 1 ? max(a.side[0].width, a.side[1].width) : a.side[0].width, runs = width / (4 * TR::KS);
   int waves = items * sides < 512 || runs >= 24 ? 16 : runs >= 12 ? 8 : 4;
-  if (tiles > 2) waves = min(waves, 8);
+  if (tiles > 2 || items > 0xffffffffu / 1024) waves = min(waves, 8);      // (the threads of a launch are counted in 32 bits)
   const dim3 grid(items, sides), threads(64 * waves);
   const size_t lds = (size_t)waves * 16 * 16 * (tiles <= 1 ? 1 : tiles <= 2 ? 2 : tiles <= 4 ? 4 : 8) * sizeof(float);
   if (tiles <= 1) hipLaunchKernelGGL((k_low<TR, AL, 1>), grid, threads, lds, s, a);

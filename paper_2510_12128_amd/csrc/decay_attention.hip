@@ -959,7 +959,8 @@ int check_scan(const nugpr_decay_attention* p, int scans, size_t need, bool* don
   if (!std::isfinite(p->scale)) { set_error("scale must be finite"); return NUGPR_ERR_INVALID; }
   if (p->n_rows == 0 && p->n_seqs == 0) { *done = true; return NUGPR_OK; }
   if (p->n_seqs < 1 || !p->seq_offsets || !p->log_decay) { set_error("seq_offsets or log_decay is null, or there is no sequence"); return NUGPR_ERR_INVALID; }
-  if ((span_count(p, scans) + 1) * p->kv_heads > (int64_t)0x7fffffff) { set_error("too many rows, sequences and heads for one call"); return NUGPR_ERR_INVALID; }
+  // (the threads of a launch are counted in 32 bits)
+  if ((span_count(p, scans) + 1) * p->kv_heads > (int64_t)0xffffffff / (narrow(p) ? 256 : 512)) { set_error("too many rows, sequences and heads for one call"); return NUGPR_ERR_INVALID; }
   if (need && (!p->workspace || (reinterpret_cast<uintptr_t>(p->workspace) & 255u))) { set_error("workspace is null or not 256-byte aligned"); return NUGPR_ERR_WORKSPACE; }
   if (p->workspace_bytes < need) { set_error("workspace smaller than nugpr_decay_attention_workspace_bytes()"); return NUGPR_ERR_WORKSPACE; }
   return NUGPR_OK;
@@ -1085,7 +1086,7 @@ int nugpr_decay_attention_step(const nugpr_decay_attention* p, const nugpr_heads
   a.n_states = p->n_seqs; a.kv = p->kv_heads; a.g = p->heads / p->kv_heads; a.dk = p->dim_k; a.dv = p->dim_v;
   a.slices = (p->dim_v + 31) / 32;
   const int64_t groups = p->n_rows * a.kv * a.slices;
-  if (groups > 0x7fffffff) { set_error("too many requests and heads for one call"); return NUGPR_ERR_INVALID; }
+  if (groups > (int64_t)0xffffffff / THREADS) { set_error("too many requests and heads for one call"); return NUGPR_ERR_INVALID; }
   const bool four = p->dim_v % 4 == 0 && !(reinterpret_cast<uintptr_t>(state) & 15u);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)groups), threads(THREADS);
