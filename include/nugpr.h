@@ -414,7 +414,7 @@ typedef struct {
   int32_t n_seqs;             /* sequences; nugpr_decay_attention_step: states that `state` holds   */
   const int64_t* seq_offsets; /* DEVICE, n_seqs+1; not read by nugpr_decay_attention_step           */
   const float* log_decay;     /* DEVICE, kv_heads                                                   */
-  double scale;               /* finite                                                             */
+  double scale;               /* finite, in float32 too                                             */
   void* workspace;            /* DEVICE; not used by nugpr_decay_attention_step                     */
   size_t workspace_bytes;
 } nugpr_decay_attention;
@@ -459,7 +459,7 @@ typedef struct {
   const void* W;              /* DEVICE, dim_out x dim_in row-major                                 */
   const void* A;              /* DEVICE, n_adapters x rank x dim_in                                 */
   const void* B;              /* DEVICE, n_adapters x rank x dim_out                                */
-  double scale;               /* finite                                                             */
+  double scale;               /* finite, in float32 too                                             */
   void* workspace;            /* DEVICE                                                             */
   size_t workspace_bytes;
 } nugpr_adapter;

@@ -861,7 +861,7 @@ bool wide(const void* x, int64_t stride, size_t value) {
 }
 
 int check_call(const nugpr_adapter* p, size_t need) {
-  if (!std::isfinite(p->scale)) { set_error("scale must be finite"); return NUGPR_ERR_INVALID; }
+  if (!std::isfinite((float)p->scale)) { set_error("scale must be finite in float32"); return NUGPR_ERR_INVALID; }
   const size_t z = value_size(p);
   if (p->n_seqs > 0 && !p->seq_offsets) { set_error("seq_offsets is null"); return NUGPR_ERR_INVALID; }
   if (!p->W || (p->n_adapters > 0 && (!p->A || !p->B))) { set_error("W, A or B is null"); return NUGPR_ERR_INVALID; }

@@ -956,7 +956,7 @@ ScanRole role(const nugpr_heads* q, const nugpr_heads* k, const nugpr_heads* v, 
 // what both scanning calls check; *done: nothing is left to do
 int check_scan(const nugpr_decay_attention* p, int scans, size_t need, bool* done) {
   *done = false;
-  if (!std::isfinite(p->scale)) { set_error("scale must be finite"); return NUGPR_ERR_INVALID; }
+  if (!std::isfinite((float)p->scale)) { set_error("scale must be finite in float32"); return NUGPR_ERR_INVALID; }
   if (p->n_rows == 0 && p->n_seqs == 0) { *done = true; return NUGPR_OK; }
   if (p->n_seqs < 1 || !p->seq_offsets || !p->log_decay) { set_error("seq_offsets or log_decay is null, or there is no sequence"); return NUGPR_ERR_INVALID; }
   // (the threads of a launch are counted in 32 bits)
@@ -1067,7 +1067,7 @@ int nugpr_decay_attention_backward(const nugpr_decay_attention* p, const nugpr_h
 int nugpr_decay_attention_step(const nugpr_decay_attention* p, const nugpr_heads* q, const nugpr_heads* k, const nugpr_heads* v, float* state,
                                const int32_t* slots, const nugpr_heads* o, void* stream) {
   NUGPR_TRY(check(p));
-  if (!std::isfinite(p->scale)) { set_error("scale must be finite"); return NUGPR_ERR_INVALID; }
+  if (!std::isfinite((float)p->scale)) { set_error("scale must be finite in float32"); return NUGPR_ERR_INVALID; }
   if (p->n_rows == 0) return NUGPR_OK;
   const size_t z = value_size(p);
   NUGPR_TRY(check_heads(q, "q", z));
