@@ -385,7 +385,10 @@ int nugpr_copy_probe(void* dst /*DEVICE*/, const void* src /*DEVICE*/, size_t by
  * between runs) and a projection with low-rank adapters (one adapter a request, or a cluster).  They need no context.
  *
  *   - Their arrays are float32 or bfloat16 (dtype, the same for all that are not said to be float); sums, states and
- *     decays are float32 in either case.
+ *     decays are float32 in either case, and results are rounded to dtype once.  (Attention in bfloat16 reads the decayed products of q and
+ *     k, and the state, with 17 bits.)
+ *   - Values that are not finite go where the formulas send them.  (Between far rows of a sequence, where a power of lam is zero in
+ *     float32, an infinity becomes NaN.)
  *   - Offsets are DEVICE int64 arrays (no call waits for them): sequence s owns rows offsets[s] .. offsets[s+1]-1; ascending,
  *     empty sequences allowed, within 0 .. n_rows (offsets outside are taken as the nearest end; where they do not ascend, results are
  *     undefined; no access is out of bounds).  Output rows that no sequence owns are set to zero unless said otherwise.
@@ -411,7 +414,8 @@ typedef struct {
   int32_t heads, kv_heads;    /* kv_heads divides heads                                             */
   int32_t dim_k, dim_v;       /* 1..128                                                             */
   int64_t n_rows;             /* rows (tokens) in all; nugpr_decay_attention_step: requests         */
-  int32_t n_seqs;             /* sequences; nugpr_decay_attention_step: states that `state` holds   */
+  int32_t n_seqs;             /* sequences, at least one where there are rows;
+                                 nugpr_decay_attention_step: states that `state` holds              */
   const int64_t* seq_offsets; /* DEVICE, n_seqs+1; not read by nugpr_decay_attention_step           */
   const float* log_decay;     /* DEVICE, kv_heads                                                   */
   double scale;               /* finite, in float32 too                                             */
