@@ -879,8 +879,8 @@ bool wide(const nugpr_heads* x, int width, size_t value) {
 bool narrow(const nugpr_decay_attention* p) { return p->dim_k <= 64 && p->dim_v <= 64; }
 
 // Rows of a span: a power of two, no less than a block, so large that the scans of the call give about 512 workgroups, or more (2048 at
-// most) the smaller their states, whose way through memory is what a span costs.  65536 rows, 16 / 4 heads of 128: 286, 224, 245,
-// 289 us with 256, 512, 1024, 2048 workgroups; 20011 rows in 40 uneven sequences, 8 heads of 64, float32: 220, 116, 110, 119 with
+// most) the smaller their states, whose way through memory is what a span costs.  65536 rows, 16 / 4 heads of 128: 310, 250, 274,
+// 313 us with 256, 512, 1024, 2048 workgroups; 20011 rows in 40 uneven sequences, 8 heads of 64, float32: 145, 112, 108, 132 with
 // 512, 1024, 2048, 4096.
 int span_log2(const nugpr_decay_attention* p, int scans) {
   const int64_t groups = min((int64_t)2048, (int64_t)512 * 128 * 128 / (p->dim_k * p->dim_v));
@@ -910,25 +910,26 @@ void launch_walk(const ScanArgs& walk, int n_walk, bool al, hipStream_t s) {
   else hipLaunchKernelGGL((k_decay_scan<TR, D, C, false, true, SUM>), grid, threads, 0, s, walk);
 }
 
-// Rows of a block.  In float32 32: tiles and operands of 64 leave room for one workgroup of the wide kernels on a compute unit instead of two
-// (16384 rows, 8 heads of 128: 237 against 216 us) and for half the narrow ones (20011 rows, 8 heads of 64: 122 against 110).
-// In bfloat16 64 forwards, 32 for the gradients (65536 rows, 16 / 4 heads of 128, forwards: 227 with 64, 236 with 32; 16 x 1024 rows,
-// 16 heads of 128, gradients: 236 and 206).
+// Rows of a block: 64 in bfloat16 for widths beyond 64, else 32.  In float32, tiles and operands of 64 leave room for one workgroup of the wide
+// kernels on a compute unit instead of two (16384 rows, 8 heads of 128: 223 against 189 us), and for fewer of the narrow ones (20011 rows, 8
+// heads of 64: 125 against 108), as they do in narrow bfloat16 (30000 rows, 16 / 4 heads of 64: 94 against 83; 2048 rows, 8 heads: 22.5 and 23).
+// Wide bfloat16 has the state's operand to make once a block (65536 rows, 16 / 4 heads of 128: 282 with 32, 258 with 64; gradients of 16 x 1024
+// rows, 16 heads: 236 and 223).
 template <class TR, int D>
 int launch_scans(const ScanArgs& adds, int n_adds, const JoinArgs& join, const ScanArgs& walk, int n_walk, bool al, hipStream_t s) {
-  constexpr int AHEAD = TR::E == 8 ? 64 : 32, BACK = 32;
+  constexpr int C = TR::E == 8 && D > 64 ? 64 : 32;
   // (a span that holds all rows: no sequence has several)
   if (((int64_t)1 << walk.span_log2) < walk.n_rows) {
-    launch_adds<TR, D, AHEAD>(adds, n_adds, al, s);
-    // (workgroups to fill the card with few sequences, not so many with many, most of which have one span: four times as many make 205 us of
-    // gradients 212, 16 x 1024 rows, 16 heads of 128, and 112 us 110, 20011 rows in 40 uneven sequences, 8 heads of 64, float32)
+    launch_adds<TR, D, C>(adds, n_adds, al, s);
+    // (workgroups to fill the card with few sequences, not so many with many, most of which have one span: four times as many make 218 us of
+    // gradients 221, 16 x 1024 rows, 16 heads of 128, and 108.6 us 107.5, 20011 rows in 40 uneven sequences, 8 heads of 64, float32)
     const int64_t pairs = (int64_t)walk.n_seqs * walk.kv, blocks = (join.size + 63) / 64;
     const int64_t y = min(blocks, (2047 + pairs) / pairs);
     hipLaunchKernelGGL(k_span_join, dim3((unsigned)pairs, (unsigned)y, n_adds), dim3(THREADS), 0, s, join);
   }
-  if (n_walk == 1) launch_walk<TR, D, AHEAD, false>(walk, n_walk, al, s);
-  else if (walk.role[1].gk > 1) launch_walk<TR, D, BACK, true>(walk, n_walk, al, s);
-  else launch_walk<TR, D, BACK, false>(walk, n_walk, al, s);
+  if (n_walk == 1) launch_walk<TR, D, C, false>(walk, n_walk, al, s);
+  else if (walk.role[1].gk > 1) launch_walk<TR, D, C, true>(walk, n_walk, al, s);
+  else launch_walk<TR, D, C, false>(walk, n_walk, al, s);
   NUGPR_HIP(hipGetLastError());
   return NUGPR_OK;
 }
