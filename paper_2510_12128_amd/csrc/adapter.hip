@@ -70,7 +70,7 @@ struct LowArgs {
 
 // A workgroup takes 16 rows of one request and all of the rank; its waves split the width, operands go from memory straight
 // into registers (nothing is read twice but A, from L2), the waves' sums meet in LDS.  The way from L2 bounds it, as a
-// workgroup reads as much of A as of x: 8192 rows of 4096, rank 16, bfloat16: 25 us (67 MB, 2.7 TB/s).
+// workgroup reads as much of A as of x: 8192 rows of 4096, rank 16, bfloat16: 25 to 27 us (67 MB, 2.6 TB/s).
 template <class TR, bool AL, int TILES>
 __global__ __launch_bounds__(1024) void k_low(const LowArgs a) {
   using T = typename TR::T;
@@ -139,9 +139,9 @@ struct ProjectArgs {
 // The adapters are further steps of the contraction: for every request with rows in the tile, its rows of h (in bfloat16 as three
 // numbers, exactly) and KS rows of B_a at a time.  sA, sB: room for BM x 128 bytes and BN x 128 bytes.
 // A step waits for its loads, about a microsecond, so that with more than OWN_LANES steps in a small tile every lane works on its own
-// rows and columns instead, in float32: 36 requests of one row, rank 64, 547 to 171 columns and back, bfloat16: 80 us with steps only, 46
-// so; 256 requests of four rows, rank 8, 1000 columns: 36 and 20.  (2: 8 requests of 32 rows 19 us instead of 17; 8: 128 of 8 rows 25
-// instead of 19.)
+// rows and columns instead, in float32: gradients of 36 requests of one row, rank 64, 547 to 171 columns, bfloat16: 97 us with steps only, 52
+// so; 256 requests of four rows, rank 8, 1000 columns: 43 and 21.  (8: 128 of 8 rows 28 instead of 19; 2: as 4.)  Larger tiles take their requests in
+// steps however many there are: 4096 rows, 4096 x 4096, rank 16, 385 us in 1024 requests, 130 in 16.
 constexpr int OWN_LANES = 4;
 template <class TR, int BM, int BN, int MT, int NTL, int N_THREADS, bool AL>
 __device__ inline void add_adapters(const ProjectArgs& a, int64_t m0, int n0, int rows, int wm, int wn, typename TR::T* sA, typename TR::T* sB,
@@ -432,7 +432,8 @@ __global__ __launch_bounds__(THREADS * G) void k_project(const ProjectArgs a) {
 // LDS (two buffers: the next step's loads run through a whole step's 64 products a wave), with one barrier a step.  A
 // load writes 16 bytes a lane side by side, so the permutation of a tile's units is made on the side of memory: lane l fetches the
 // unit that belongs at place l.  Rows and columns past the ends repeat the last ones and are not stored.  The matrix cores bound it: 8192
-// rows, 4096 x 4096: 250 us with the adapters (1.10 PFLOP/s); 4096 rows, 2048 x 2048, tiles of 128: 43 us (0.80).
+// rows, 4096 x 4096, with the adapters, under the profiler: 269 us at least, 284 in the median (1.02 and 0.97 PFLOP/s); 4096 rows, 2048 x 2048,
+// tiles of 128: 42 us (0.81).
 constexpr int WIDE = 256, WIDE_THREADS = 512;
 template <int BM, bool NN>
 __global__ __launch_bounds__(WIDE_THREADS, 2) void k_project_wide(const ProjectArgs a, int tiles_m, int tiles_n) {
@@ -589,8 +590,9 @@ __global__ __launch_bounds__(FEW_THREADS) void k_project_few(const ProjectArgs a
 
 // Few columns (up to 64) and a rank up to 32: both products with x in one pass over it.  A workgroup takes 32 rows; its waves split
 // the width as k_low's do, with W's rows and those of the adapter as operands side by side.  Further requests in the same rows
-// take further passes, for their adapters alone.  L2 and the matrix cores bound it: 32768 rows of 512, 20 columns, rank 4, float32: 33 us
-// (67 MB, 2.0 TB/s, matrix cores busy a third of it).
+// take further passes, for their adapters alone.  L2 and the matrix cores bound it: 32768 rows of 512, 20 columns, rank 4, float32: 32 to 37 us
+// (67 MB, 2.0 TB/s, matrix cores busy a third of it).  With many short requests the passes are what counts: 256 rows of 512, 64 columns,
+// 118 us in 256 requests, 15 in 16.
 constexpr int NARROW_ROWS = 32;
 template <class TR, bool AL, int WT, int JT>
 __global__ __launch_bounds__(THREADS) void k_project_narrow(const ProjectArgs a, const void* A_all, float scale) {
@@ -705,7 +707,7 @@ struct GradArgs {
 constexpr int GRAD_COLS = 128, GRAD_ROWS = 64;
 
 // A workgroup takes 128 columns of one adapter's gradient and a part of the rows, and of these the requests that have the adapter.
-// The wait for 64 rows at a time bounds it: 4096 rows, 2048 + 2048 columns, rank 16, 8 adapters, bfloat16: 20 us (34 MB), and
+// The wait for 64 rows at a time bounds it: 4096 rows, 2048 + 2048 columns, rank 16, 8 adapters, bfloat16: 22 us (34 MB), and
 // 4 for the sum over two parts.
 template <class TR, int JT, bool AL>
 __global__ __launch_bounds__(THREADS) void k_adapter_grad(const GradArgs a) {

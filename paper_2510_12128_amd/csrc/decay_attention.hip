@@ -312,15 +312,17 @@ __device__ inline void walk_tokens(const ScanArgs& a, RolePtr ro, int tid, int b
 // Per block and head: P^T = K Q^T (each wave tiles of 16 rows of Q), masked and decayed, goes through LDS; o^T = S^T Q^T and V^T P^T with
 // the wave's columns of S and V; S += K^T (w V).  S is read as an operand where it lies (matrix_core.h).  In bfloat16 P and
 // S are each read as two bfloat16, 17 bits of them: no more than the float32 sums' own error, so that o is rounded once.  (With one bfloat16 of
-// each o had 1.4 times the error of its last rounding; it took 217 us instead of 250 for 65536 rows, 16 / 4 heads of 128, 197 instead of 229 for the
+// each o had 1.4 times the error of its last rounding; it took 217 us instead of 250 for 65536 rows, 16 / 4 heads of 128, 197 instead of 220 for the
 // gradients of 16 x 1024 rows, 16 heads.)  w V, which is summed into the float32 state, keeps all 24 bits.
 // Values that are not finite: rows s > t must not touch o_t, but 0 x NaN in the masked part of P would, nor may an infinity meet the
 // zeros beside a width or the difference of two infinities between the parts of a factor.  So a span whose results are not all finite is
 // looked through for them (needs_tokens) and, with them, walked once more (walk_tokens).
-// What bounds it: memory in bfloat16, the matrix cores and LDS together in float32, the length of the chain where there are few rows.
-// Measured: 65536 rows, 16 / 4 heads of 128, bfloat16: 168 us to walk (671 MB, 4.0 TB/s) after 40 to add up; without loads
-// and stores the walk takes 127.  16 x 1024 rows, 16 heads, gradients: 205 us (three roles, 805 MB, 3.9 TB/s).  20011 rows, 8 heads of
-// 64, float32: 64 after 26 us (matrix cores busy 37 % of it).
+// What bounds it: in bfloat16 the way of the rows together with the work between (of 65536 rows, 16 / 4 heads of 128: vector pipe 45 % of the
+// time, LDS 40 %, matrix cores 27 %); in float32 the waits of a block's steps, which few waves hide (matrix cores busy a third of the time, LDS 13 %,
+// waves waiting 36 % of it); the length of the chain where there are few rows.
+// Measured under the profiler, median and least: those 65536 rows: 247 and 202 us to walk (671 MB, 2.7 and 3.3 TB/s) after 47 and 40 to add
+// up; 16 x 1024 rows, 16 heads, gradients: 230 and 211 (three roles, 805 MB, 3.5 and 3.8 TB/s); 20011 rows, 8 heads of 64, float32: 62 after 26.
+// 128 registers a lane do not hold it all for widths beyond 64: in float32 the walks spill 17 to 50 of them, in bfloat16 none to 14.
 template <class TR, int D, int C, bool AL, bool WALK, bool SUM>
 __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(const ScanArgs a) {
   using T = typename TR::T;
@@ -347,7 +349,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
   int i = tid & 15, kg = (tid >> 4) & 3;
   const int h = blockIdx.x % a.kv, item = blockIdx.x / a.kv;
 
-  if (WALK && item == a.items) {                 // rows that no sequence owns
+  if (WALK && item == a.items) {                 // rows that no sequence owns (one workgroup a head: for few of them; half of 65536 rows, 16 heads of 128: 9 ms)
     const int64_t lo = clamped(a.off[0], 0, a.n_rows), hi = clamped(a.off[a.n_seqs], lo, a.n_rows);
     const int64_t none = lo + a.n_rows - hi, per = (int64_t)ro->gq * ro->dv;
     for (int64_t e = tid; e < none * per; e += THREADS) {
@@ -678,7 +680,7 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
 
 // Sequences of several spans: what each span adds to the state becomes each span's start state.  A wave takes 64 values of the
 // states and a quarter of 128 spans, which it has in registers at once; the quarters' sums meet in LDS.  The wait for these loads bounds it:
-// 13 us for 128 spans x 4 heads of 128 x 128 (67 MB), 7 for 32 spans x 8 heads of 64 x 64.
+// 13 to 15 us for 128 spans x 4 heads of 128 x 128 (67 MB), 7 to 8 for 32 spans x 8 heads of 64 x 64.
 struct JoinArgs {
   float* spans[2];
   const float* s_in[2];
@@ -757,7 +759,7 @@ __global__ __launch_bounds__(THREADS) void k_span_join(const JoinArgs a) {
 
 // One token a request: the state is read and written once, which bounds it.  A workgroup takes 32 columns of one state (V of
 // them a thread and row), all of them in registers: each load is on its way before the first is waited for.  256 requests, 16 heads of
-// 128 x 128: 537 MB in 96 to 120 us (5.6 to 4.5 TB/s); one request, 8 heads of 64: 4 us.
+// 128 x 128: 537 MB in 97 to 118 us (5.5 to 4.6 TB/s); one request, 8 heads of 64: 4 us.
 struct StepArgs {
   const void *q, *k, *v;
   void* o;

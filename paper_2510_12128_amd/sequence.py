@@ -122,8 +122,9 @@ def nugpr_decay_attention_forward(q, k, v, log_decay, seq_offsets, scale=1.0, in
     """Linear attention with a decay for each head over packed sequences.
 
     q (rows, heads, dim_k), k (rows, kv_heads, dim_k), v (rows, kv_heads, dim_v): float32 or bfloat16; log_decay (kv_heads,)
-    float32, <= 0; seq_offsets (n_seqs + 1,) int64, n_seqs at least 1 where there are rows; initial_state (n_seqs, kv_heads, dim_k, dim_v) float32 or None.
-    Returns o (rows, heads, dim_v) and the sequences' end states, float32."""
+    float32, <= 0; seq_offsets (n_seqs + 1,) int64, n_seqs at least 1 where there are rows; initial_state (n_seqs, kv_heads,
+    dim_k, dim_v) float32 or None.  Returns o (rows, heads, dim_v) and the sequences' end states,
+    float32."""
     lib = load_library()
     if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad or log_decay.requires_grad or
                          (initial_state is not None and initial_state.requires_grad)):
