@@ -218,15 +218,18 @@ struct SpanRows {
   __device__ T* o(int t, int m) const { return static_cast<T*>(ro->o) + (first + (int64_t)dir * t) * ro->o_row + ((int64_t)h * ro->gq + m) * ro->o_head; }
 };
 
-// Whether a span whose results are not all finite may have them wrong: with an infinity among its rows or in its start state, or, where o is
-// written, a NaN in a column of v whose state was none before.  (Any other NaN goes where it belongs.)  A thread's share; the span has it if one does.
+// What makes a span's results not finite.  MUST: something that they may be wrong for: an infinity among the rows or in the start state, or, where o
+// is written, a NaN in a column of v whose state was none before.  HAS_NAN: any other NaN, which goes where it belongs.  A thread's share; the span has what one
+// thread has.
+constexpr int MUST = 2, HAS_NAN = 1;
 template <class TR, int D, bool WALK, bool SUM>
-__device__ inline bool needs_tokens(const ScanArgs& a, RolePtr ro, int tid, int block) {
+__device__ inline int needs_tokens(const ScanArgs& a, RolePtr ro, int tid, int block) {
   const SpanRows<TR, WALK, SUM> rows(a, ro, block);
   constexpr int E = TR::E, A_ROW = D / E;
   const int col = tid % A_ROW * E, s_c = ro->s_trans ? ro->dk : 1;
   const float* from = start_of<WALK>(a, ro, rows.sp, rows.item, rows.h);
-  bool found = false, was[E];          // (v makes a column of the state NaN, or none of it)
+  int found = 0;
+  bool was[E];                         // (v makes a column of the state NaN, or none of it)
 #pragma unroll
   for (int j = 0; j < E; ++j) was[j] = !WALK || (from && col + j < ro->dv && __builtin_isnan(from[(col + j) * s_c]));
 #pragma unroll 1
@@ -236,20 +239,20 @@ __device__ inline bool needs_tokens(const ScanArgs& a, RolePtr ro, int tid, int 
     for (int m = 0; m < rows.gk; ++m) {
       row_part<TR>(rows.k(t, m) + col, ro->dk - col, x);
 #pragma unroll
-      for (int j = 0; j < E; ++j) found |= __builtin_isinf(x[j]);
+      for (int j = 0; j < E; ++j) found |= __builtin_isinf(x[j]) ? MUST : __builtin_isnan(x[j]) ? HAS_NAN : 0;
       row_part<TR>(rows.v(t, m) + col, ro->dv - col, x);
 #pragma unroll
-      for (int j = 0; j < E; ++j) found |= __builtin_isinf(x[j]) || (__builtin_isnan(x[j]) && !was[j]);
+      for (int j = 0; j < E; ++j) found |= __builtin_isinf(x[j]) || (__builtin_isnan(x[j]) && !was[j]) ? MUST : __builtin_isnan(x[j]) ? HAS_NAN : 0;
     }
 #pragma unroll 1
     for (int m = 0; m < rows.gq; ++m) {
       row_part<TR>(rows.q(t, m) + col, ro->dk - col, x);
 #pragma unroll
-      for (int j = 0; j < E; ++j) found |= __builtin_isinf(x[j]);
+      for (int j = 0; j < E; ++j) found |= __builtin_isinf(x[j]) ? MUST : __builtin_isnan(x[j]) ? HAS_NAN : 0;
     }
   }
   if (from)
-    for (int e = tid; e < ro->dk * ro->dv; e += blockDim.x) found |= __builtin_isinf(from[e]);
+    for (int e = tid; e < ro->dk * ro->dv; e += blockDim.x) found |= __builtin_isinf(from[e]) ? MUST : __builtin_isnan(from[e]) ? HAS_NAN : 0;
   return found;
 }
 
@@ -315,8 +318,8 @@ __device__ inline void walk_tokens(const ScanArgs& a, RolePtr ro, int tid, int b
 // each o had 1.4 times the error of its last rounding; it took 217 us instead of 250 for 65536 rows, 16 / 4 heads of 128, 197 instead of 220 for the
 // gradients of 16 x 1024 rows, 16 heads.)  w V, which is summed into the float32 state, keeps all 24 bits.
 // Values that are not finite: rows s > t must not touch o_t, but 0 x NaN in the masked part of P would, nor may an infinity meet the
-// zeros beside a width or the difference of two infinities between the parts of a factor.  So a span whose results are not all finite is
-// looked through for them (needs_tokens) and, with them, walked once more (walk_tokens).
+// zeros beside a width or the difference of two infinities between the parts of a factor, as where a product leaves float32's range.  So a span
+// whose results are not all finite is looked through for what made them so (needs_tokens) and, if need be, walked once more (walk_tokens).
 // What bounds it: in bfloat16 the way of the rows together with the work between (of 65536 rows, 16 / 4 heads of 128: vector pipe 45 % of the
 // time, LDS 40 %, matrix cores 27 %); in float32 the waits of a block's steps, which few waves hide (matrix cores busy a third of the time, LDS 13 %,
 // waves waiting 36 % of it); the length of the chain where there are few rows.
@@ -657,7 +660,9 @@ __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(
   if (anew) {
     int block = blockIdx.x;
     asm volatile("" : "+s"(block));              // (it finds its span anew: kept so far, that would not fit the registers)
-    anew = __syncthreads_or(needs_tokens<TR, D, WALK, SUM>(a, ro, tid, block));
+    const int what = needs_tokens<TR, D, WALK, SUM>(a, ro, tid, block);          // (by all lanes: they search for the span together)
+    const bool must = __syncthreads_or(what & MUST), nan = __syncthreads_or(what & HAS_NAN);
+    anew = must || !nan;                         // (finite throughout: something has left float32's range, where the parts of a factor may cancel)
     if (anew) {
       __threadfence();                           // (rows of o that are written once more)
       __syncthreads();

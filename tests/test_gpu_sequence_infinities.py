@@ -107,6 +107,31 @@ def test_attention_gradients(lib, h, kv, dk, dv, where, bad, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (40, 128)])
+def test_what_leaves_the_range_of_float32_is_infinite(lib, dk, dv, dtype):
+    """Finite keys and values whose product is not, and a finite query whose product with the state is not."""
+    lens = [50, 400, 3]
+    gen, off = torch.Generator().manual_seed(5), np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+    q, k, v = (positive(gen, 453, 2, w).to(dtype) for w in (dk, dk, dv))
+    k[60, 0], v[60, 0, 3:] = 1e25, 1e25
+    q[200, 1], q[449, 1] = 1e38, 1e38
+    g, S0 = torch.tensor([-0.001, -0.002]), positive(gen, 3, 2, dk, dv)
+    o, S = lib.nugpr_decay_attention_forward(q.cuda(), k.cuda(), v.cuda(), g.cuda(), torch.from_numpy(off).cuda(), initial_state=S0.cuda())
+    want_o, want_S = recurrence(q, k, v, g, off, S0)
+    want_o, want_S = want_o.cpu(), want_S.cpu()                            # (1e50 and 1e42 in float64)
+    want_o[want_o > 3.5e38], want_S[want_S > 3.5e38] = INF, INF
+    assert int(want_S.isinf().sum()) == dk * (dv - 3) and int(want_o.isinf().sum()) == 390 * (dv - 3) + 2 * dv
+    # (row 60 of the first three columns has a key of 1e25: of another size than all other results, so it is compared alone)
+    far = want_o > 1e20
+    far &= want_o.isfinite()
+    alike(torch.where(far, torch.zeros(()), o.cpu().double()), torch.where(far, torch.zeros(()), want_o), TOL[dtype], "o")
+    assert torch.allclose(o.cpu().double()[far], want_o[far], rtol=TOL[dtype], atol=0)
+    small = want_S < 1e20
+    alike(torch.where(small, S.cpu().double(), torch.zeros(())), torch.where(small, want_S, torch.zeros(())), TOL[F32], "state")
+    assert torch.equal(S.cpu().isinf(), want_S.isinf())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_a_step_keeps_an_infinite_state(lib, dtype):
     gen = torch.Generator().manual_seed(3)
     q, k, v = (positive(gen, 3, 2, 16).to(dtype) for _ in range(3))
