@@ -325,7 +325,7 @@ __device__ inline void walk_tokens(const ScanArgs& a, RolePtr ro, int tid, int b
 // waves waiting 36 % of it); the length of the chain where there are few rows.
 // Measured under the profiler, median and least: those 65536 rows: 247 and 202 us to walk (671 MB, 2.7 and 3.3 TB/s) after 47 and 40 to add
 // up; 16 x 1024 rows, 16 heads, gradients: 230 and 211 (three roles, 805 MB, 3.5 and 3.8 TB/s); 20011 rows, 8 heads of 64, float32: 62 after 26.
-// 128 registers a lane do not hold it all for widths beyond 64: in float32 the walks spill 17 to 50 of them, in bfloat16 none to 14.
+// 128 registers a lane do not hold it all for widths beyond 64: in float32 the walks spill 17 to 50 of them, in bfloat16 none to 11.
 template <class TR, int D, int C, bool AL, bool WALK, bool SUM>
 __global__ __launch_bounds__((64 * Tile<TR, D, C>::WAVES), 4) void k_decay_scan(const ScanArgs a) {
   using T = typename TR::T;
