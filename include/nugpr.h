@@ -382,7 +382,9 @@ int nugpr_copy_probe(void* dst /*DEVICE*/, const void* src /*DEVICE*/, size_t by
  * A point of the regression may be a sequence, its coordinates what a layer makes of that sequence.  Two operators of such
  * a layer have the structure of the covariance above, dense blocks plus terms of low rank over rows stored one after the
  * other with an array of offsets: linear attention with decay (a dense block inside a run of rows, a dim_k x dim_v state
- * between runs) and a projection with low-rank adapters (one adapter a request, or a cluster).  They need no context.
+ * between runs) and a projection with low-rank adapters (one adapter a request, or a cluster).  Two more mix along the rows
+ * channel by channel: a short causal convolution, and a state space scan whose decay the tokens choose.  The norm of a
+ * layer's gradients, and their clipping, go with its training.  They need no context.
  *
  *   - Their arrays are float32 or bfloat16 (dtype, the same for all that are not said to be float); sums, states and
  *     decays are float32 in either case, and results are rounded to dtype once.  (Attention in bfloat16 reads the decayed products of q and
@@ -479,6 +481,122 @@ int nugpr_adapter_forward(const nugpr_adapter* problem, const void* x, int64_t x
  * dy_stride.  W is fixed, as it is while adapters are trained: it gets none.  dx may be NULL. */
 int nugpr_adapter_backward(const nugpr_adapter* problem, const void* x, int64_t x_stride, const void* d_y, int64_t dy_stride,
                            void* dx, void* dA, void* dB, void* stream);
+
+/* Rows x width array: value (row, j) at data[row * row_stride + j] (the stride in values, not negative). */
+typedef struct {
+  void* data;          /* DEVICE */
+  int64_t row_stride;
+} nugpr_rows;
+
+/* Causal convolution along each sequence, of every channel by itself: with x_{t-k} before the sequence's begin taken from its
+ * window (zero without one),
+ *   p_t[c] = bias[c] + sum_{k < width} weight[c][width-1-k] x_{t-k}[c],      y = p, or p / (1 + e^-p) where silu.
+ * A window holds a sequence's width - 1 rows before the next one, oldest first; of dtype, as they were given. */
+typedef struct {
+  int32_t dtype;              /* of x, y, weight, bias, windows and their gradients                 */
+  int32_t dim;                /* channels, 1..65536                                                 */
+  int32_t width;              /* 1..8                                                               */
+  int32_t silu;               /* 0 or 1                                                             */
+  int64_t n_rows;             /* rows (tokens) in all; nugpr_short_conv_step: requests              */
+  int32_t n_seqs;             /* sequences; nugpr_short_conv_step: windows that `window` holds      */
+  const int64_t* seq_offsets; /* DEVICE, n_seqs+1; not read by nugpr_short_conv_step                */
+  const void* weight;         /* DEVICE, dim x width                                                */
+  const void* bias;           /* DEVICE, dim, or NULL: none                                         */
+  void* workspace;            /* DEVICE; used by nugpr_short_conv_backward only                     */
+  size_t workspace_bytes;
+} nugpr_short_conv;
+
+/* Bytes of workspace that nugpr_short_conv_backward needs.  Only dtype, dim, width, n_rows and n_seqs are read; 0 on invalid input. */
+size_t nugpr_short_conv_workspace_bytes(const nugpr_short_conv* problem);
+
+/* initial_window: DEVICE n_seqs x (width-1) x dim, or NULL = zero.  final_window: the same, out, or NULL; refused where it
+ * overlaps initial_window. */
+int nugpr_short_conv_forward(const nugpr_short_conv* problem, const nugpr_rows* x, const void* initial_window, const nugpr_rows* y,
+                             void* final_window, void* stream);
+
+/* Gradients, given d_y and (or NULL = zero) d_final_window; dbias (NULL where there is no bias) and d_initial_window (or NULL) are out;
+ * refused where d_initial_window overlaps d_final_window.  Nothing of the forward pass is needed but its inputs. */
+int nugpr_short_conv_backward(const nugpr_short_conv* problem, const nugpr_rows* x, const void* initial_window, const nugpr_rows* d_y,
+                              const void* d_final_window, const nugpr_rows* dx, void* dweight, void* dbias, void* d_initial_window,
+                              void* stream);
+
+/* One token for each of n_rows requests: row b goes behind window slots[b] (DEVICE int32; NULL: window b) of `window`, DEVICE n_seqs x
+ * (width-1) x dim, which moves on by a row, in place.  A slot outside 0 .. n_seqs-1 stands for no request: its output is
+ * zero.  No two rows may name one window. */
+int nugpr_short_conv_step(const nugpr_short_conv* problem, const nugpr_rows* x, void* window, const int32_t* slots, const nugpr_rows* y,
+                          void* stream);
+
+/* State space layer whose decay depends on the token.  Channel c reads B and C of group c / (dim / groups); within a sequence, with
+ * h[c][n] its dim_state states,
+ *   d_t = softplus(dt_t[c] + dt_bias[c]), or dt_t[c] + dt_bias[c] without softplus,
+ *   h_t[c][n] = e^(d_t A[c][n]) h_{t-1}[c][n] + d_t x_t[c] B_t[n],
+ *   y_t[c] = (sum_n C_t[n] h_t[c][n] + D[c] x_t[c]) silu(z_t[c])       (without D: no such term; without z: no such factor).
+ * d_t A is meant to be <= 0; exponents below -87 are a factor of zero.  (An infinite state that such a factor meets becomes NaN.) */
+typedef struct {
+  int32_t dtype;              /* of x, dt, B, C, z, y and their gradients                           */
+  int32_t dim;                /* channels, 1..65536                                                 */
+  int32_t groups;             /* divides dim                                                        */
+  int32_t dim_state;          /* 1..64                                                              */
+  int32_t softplus;           /* 0 or 1                                                             */
+  int64_t n_rows;             /* rows (tokens) in all; nugpr_selective_scan_step: requests          */
+  int32_t n_seqs;             /* sequences, at least one where there are rows;
+                                 nugpr_selective_scan_step: states that `state` holds               */
+  const int64_t* seq_offsets; /* DEVICE, n_seqs+1; not read by nugpr_selective_scan_step            */
+  const float* A;             /* DEVICE, dim x dim_state                                            */
+  const float* D;             /* DEVICE, dim, or NULL                                               */
+  const float* dt_bias;       /* DEVICE, dim, or NULL: zero                                         */
+  void* workspace;            /* DEVICE; not used by nugpr_selective_scan_step                      */
+  size_t workspace_bytes;
+} nugpr_selective_scan;
+
+/* Bytes of workspace that the two calls below need (backward != 0: the second one).  Only dtype, dim, groups, dim_state, n_rows and
+ * n_seqs are read; 0 on invalid input. */
+size_t nugpr_selective_scan_workspace_bytes(const nugpr_selective_scan* problem, int32_t backward);
+
+/* x, dt, z, y: dim wide; B, C: `groups` heads of width dim_state; z may be NULL.  initial_state: DEVICE float n_seqs x dim x
+ * dim_state, or NULL = zero.  final_state: the same, out, or NULL; refused where it overlaps initial_state. */
+int nugpr_selective_scan_forward(const nugpr_selective_scan* problem, const nugpr_rows* x, const nugpr_rows* dt, const nugpr_heads* B,
+                                 const nugpr_heads* C, const nugpr_rows* z, const float* initial_state, const nugpr_rows* y,
+                                 float* final_state, void* stream);
+
+/* Gradients, given d_y and (or NULL = zero) d_final_state, of everything that is read: of B and C summed over the channels of a
+ * group, of A (dim x dim_state), D and dt_bias (dim; NULL where there is none) summed over the rows, in float.  dz: NULL where z is.
+ * d_initial_state: out, or NULL; refused where it overlaps d_final_state.  Nothing of the forward pass is needed but its inputs. */
+int nugpr_selective_scan_backward(const nugpr_selective_scan* problem, const nugpr_rows* x, const nugpr_rows* dt, const nugpr_heads* B,
+                                  const nugpr_heads* C, const nugpr_rows* z, const float* initial_state, const nugpr_rows* d_y,
+                                  const float* d_final_state, const nugpr_rows* dx, const nugpr_rows* ddt, const nugpr_heads* dB,
+                                  const nugpr_heads* dC, const nugpr_rows* dz, float* dA, float* dD, float* ddt_bias,
+                                  float* d_initial_state, void* stream);
+
+/* One token for each of n_rows requests: row b advances state slots[b] (DEVICE int32; NULL: state b) of `state`, DEVICE float n_seqs x
+ * dim x dim_state, in place, and reads it.  A slot outside 0 .. n_seqs-1 stands for no request: its output is zero.  No
+ * two rows may name one state. */
+int nugpr_selective_scan_step(const nugpr_selective_scan* problem, const nugpr_rows* x, const nugpr_rows* dt, const nugpr_heads* B,
+                              const nugpr_heads* C, const nugpr_rows* z, float* state, const int32_t* slots, const nugpr_rows* y,
+                              void* stream);
+
+/* A tensor of a model's gradients: `count` values, in any order. */
+typedef struct {
+  void* data;          /* DEVICE                                                                    */
+  void* out;           /* DEVICE, where the clipped values go, or NULL: in place                    */
+  int64_t count;
+  int32_t dtype;       /* NUGPR_FLOAT32 or NUGPR_BFLOAT16                                           */
+  int32_t out_dtype;   /* of `out`; not read where that is NULL                                     */
+} nugpr_gradient;
+
+/* Bytes of workspace that the two calls below need for so many tensors; 0 on invalid input.  `gradients` is a HOST array, here and
+ * below, and is read before the calls return. */
+size_t nugpr_gradient_norm_workspace_bytes(const nugpr_gradient* gradients, int32_t n_gradients);
+
+/* *norm (DEVICE float) = the 2-norm of all values of all tensors, their squares summed in 64 bits.  `out` is not read. */
+int nugpr_gradient_norm(const nugpr_gradient* gradients, int32_t n_gradients, float* norm, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/* The same, and every value is multiplied by min(1, max_norm / norm): out = data x factor, multiplied in 64 bits.  In place,
+ * nothing is written where norm <= max_norm.  A norm that is infinite makes the factor zero, a NaN NaN.  max_norm >= 0, infinity
+ * allowed.  Tensors that are written must not overlap any other. */
+int nugpr_clip_gradients(const nugpr_gradient* gradients, int32_t n_gradients, double max_norm, float* norm, void* workspace,
+                         size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

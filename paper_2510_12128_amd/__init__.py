@@ -13,6 +13,8 @@ from .binding import (  # noqa: F401
     NUGPR_ERR_INVALID, NUGPR_ERR_WORKSPACE, NUGPR_ERR_HIP, NUGPR_ERR_STATE, NUGPR_ISOTROPIC,
 )
 from .sequence import (  # noqa: F401
-    nugpr_adapter_backward, nugpr_adapter_forward, nugpr_decay_attention_backward, nugpr_decay_attention_forward,
-    nugpr_decay_attention_step,
+    nugpr_adapter_backward, nugpr_adapter_forward, nugpr_clip_gradients, nugpr_decay_attention_backward,
+    nugpr_decay_attention_forward, nugpr_decay_attention_step, nugpr_gradient_norm, nugpr_selective_scan_backward,
+    nugpr_selective_scan_forward, nugpr_selective_scan_step, nugpr_short_conv_backward, nugpr_short_conv_forward,
+    nugpr_short_conv_step,
 )

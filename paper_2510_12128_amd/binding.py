@@ -79,6 +79,28 @@ class Adapter(C.Structure):
                 ("scale", C.c_double), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64)]
+
+
+class ShortConv(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("dim", C.c_int32), ("width", C.c_int32), ("silu", C.c_int32), ("n_rows", C.c_int64),
+                ("n_seqs", C.c_int32), ("seq_offsets", C.c_void_p), ("weight", C.c_void_p), ("bias", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class SelectiveScan(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("dim", C.c_int32), ("groups", C.c_int32), ("dim_state", C.c_int32),
+                ("softplus", C.c_int32), ("n_rows", C.c_int64), ("n_seqs", C.c_int32), ("seq_offsets", C.c_void_p),
+                ("A", C.c_void_p), ("D", C.c_void_p), ("dt_bias", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
+class Gradient(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64), ("dtype", C.c_int32),
+                ("out_dtype", C.c_int32)]
+
+
 _LIB = None
 
 
@@ -175,6 +197,30 @@ def load_library():
     lib.nugpr_adapter_forward.argtypes = [ad, vp, C.c_int64, vp, vp]
     lib.nugpr_adapter_backward.restype = C.c_int
     lib.nugpr_adapter_backward.argtypes = [ad, vp, C.c_int64, vp, C.c_int64, vp, vp, vp, vp]
+    sc, rw = C.POINTER(ShortConv), C.POINTER(Rows)
+    lib.nugpr_short_conv_workspace_bytes.restype = C.c_size_t
+    lib.nugpr_short_conv_workspace_bytes.argtypes = [sc]
+    lib.nugpr_short_conv_forward.restype = C.c_int
+    lib.nugpr_short_conv_forward.argtypes = [sc, rw, vp, rw, vp, vp]
+    lib.nugpr_short_conv_backward.restype = C.c_int
+    lib.nugpr_short_conv_backward.argtypes = [sc, rw, vp, rw, vp, rw, vp, vp, vp, vp]
+    lib.nugpr_short_conv_step.restype = C.c_int
+    lib.nugpr_short_conv_step.argtypes = [sc, rw, vp, vp, rw, vp]
+    ss = C.POINTER(SelectiveScan)
+    lib.nugpr_selective_scan_workspace_bytes.restype = C.c_size_t
+    lib.nugpr_selective_scan_workspace_bytes.argtypes = [ss, C.c_int32]
+    lib.nugpr_selective_scan_forward.restype = C.c_int
+    lib.nugpr_selective_scan_forward.argtypes = [ss, rw, rw, hd, hd, rw, vp, rw, vp, vp]
+    lib.nugpr_selective_scan_backward.restype = C.c_int
+    lib.nugpr_selective_scan_backward.argtypes = [ss, rw, rw, hd, hd, rw, vp, rw, vp, rw, rw, hd, hd, rw, vp, vp, vp, vp, vp]
+    lib.nugpr_selective_scan_step.restype = C.c_int
+    lib.nugpr_selective_scan_step.argtypes = [ss, rw, rw, hd, hd, rw, vp, vp, rw, vp]
+    lib.nugpr_gradient_norm_workspace_bytes.restype = C.c_size_t
+    lib.nugpr_gradient_norm_workspace_bytes.argtypes = [vp, C.c_int32]
+    lib.nugpr_gradient_norm.restype = C.c_int
+    lib.nugpr_gradient_norm.argtypes = [vp, C.c_int32, vp, vp, C.c_size_t, vp]
+    lib.nugpr_clip_gradients.restype = C.c_int
+    lib.nugpr_clip_gradients.argtypes = [vp, C.c_int32, C.c_double, vp, vp, C.c_size_t, vp]
     _LIB = lib
     return lib
 

@@ -1,0 +1,1125 @@
+// State space layer whose decay depends on the token, over packed sequences: forward, gradients, and one token at a time.
+//
+//   d_t = softplus(dt_t + bias),  h_t[n] = a_t[n] h_{t-1}[n] + u_t B_t[n],  a_t[n] = e^(d_t A[n]),  u_t = d_t x_t
+//   y_t = (sum_n C_t[n] h_t[n] + D x_t) silu(z_t)                                       (every channel by itself)
+//
+// With e_t = dy_t silu(z_t) and g_t[n] the gradient by h_t[n]
+//   g_t = a_{t+1} g_{t+1} + e_t C_t,   dB_t = sum_c u_t g_t,   dC_t = sum_c e_t h_t,   du_t = sum_n g_t B_t
+//   q_t[n] = g_t a_t h_{t-1},   dd_t = x_t du_t + sum_n q_t A,   dA = sum_t q_t d_t,   dx_t = d_t du_t + D e_t
+//
+// The vector pipe bounds it: of a state and row the exponential takes four times the time of another instruction, and there
+// are four of those forward (d A, u B, and two multiply-adds).
+//
+// A workgroup has 64 channels, a lane one of them, a wave four of the states; rows go by in tiles of 16.  A tile's d and u are made once,
+// by all threads, and lie in LDS, as do B and C, of which a lane reads one value for every four rows: the instructions that use
+// them fetch the value from the lane that has it.  The waves' parts of y meet in LDS, where all threads take them up again.
+//
+// A sequence is cut into spans where there are too few workgroups otherwise: a first pass finds what each span adds to the state, a
+// small one the spans' start states, and the last walks through the spans.
+#include <algorithm>
+#include <type_traits>
+#include <utility>
+
+#include "nugpr_internal.h"
+#include "packed_rows.h"
+#include "row_values.h"
+
+namespace nugpr {
+
+namespace {
+
+constexpr int TILE_ROWS = 16;
+constexpr int CH = 64;               // channels of a workgroup
+constexpr int PER = 4;               // states of a wave
+constexpr int ZERO_GROUPS = 128;     // workgroups that clear the rows without a sequence
+
+struct ScanArgs {
+  const void *x, *dt, *z, *B, *C, *dy;
+  void *y, *dx, *ddt, *dz;
+  int64_t x_row, dt_row, z_row, y_row, dy_row, dx_row, ddt_row, dz_row;
+  int64_t B_row, B_head, C_row, C_head;
+  const float *A, *D, *bias;
+  const float *s_in, *ds_end;        // states at the sequences' begin; gradients of those at their end
+  float *s_out, *ds_in;
+  const int64_t* off;
+  int64_t n_rows;
+  int n_seqs, dim, groups, each, blocks, states, softplus;     // each: channels of a group; blocks: of CH channels, all groups
+  int span_log2, items;
+  float* adds;                       // items x dim x states: what a span adds to the state, then its start state
+  float* steps;                      // items x dim: sum of a span's d
+  float* back;                       // the same as adds, of the gradients
+  float* tiles;                      // tiles x dim x states: states at the tiles' begin (from zero, but in a sequence's first span)
+  float* tile_steps;                 // tiles x dim: sum of the span's d before the tile
+  float *dB, *dC;                    // blocks of a group x n_rows x groups x states
+  float *dA, *dD, *dbias;            // items x dim (x states)
+};
+
+// Value I of those that 16 consecutive lanes hold.  (No instruction of its own: the one that uses it reads its operand so.)
+template <int I>
+__device__ inline float from_lane(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x150 + I, 0xf, 0xf, true));
+}
+
+// Where a workgroup stands.
+struct Place {
+  int group, channel, valid;         // its first channel, and how many it has
+  PieceOf piece;
+  int64_t from, to;                  // its rows
+  int span;                          // of the sequence
+  bool last;                         // the sequence ends with it
+};
+
+__device__ inline bool find(const ScanArgs& a, int item, int block, Place& p) {
+  const int of_group = a.blocks / a.groups, b = block % of_group;
+  p.group = block / of_group;
+  p.channel = p.group * a.each + b * CH;
+  p.valid = min(CH, a.each - b * CH);
+  p.piece = piece_of(a.off, a.n_seqs, a.n_rows, a.span_log2, item);
+  if (p.piece.seq < 0) return false;
+  p.span = item - (int)((p.piece.lo >> a.span_log2) + p.piece.seq);
+  p.from = p.piece.lo + ((int64_t)p.span << a.span_log2);
+  if (p.span > 0 && p.from >= p.piece.hi) return false;
+  p.to = min(p.piece.hi, p.from + ((int64_t)1 << a.span_log2));
+  p.last = p.to == p.piece.hi;
+  return true;
+}
+
+// The tile's rows as memory has them: a thread holds V channels of one row, and one value of B and C.
+template <class TR, int WAVES, int CHUNKS, bool GRADIENT>
+struct Incoming {
+  static constexpr int V = TILE_ROWS / WAVES;
+  Values<TR, V> x, dt, z, dy;
+  float b[CHUNKS], c[CHUNKS];
+  __device__ void load(const ScanArgs& a, const Place& p, int64_t row0, int n_rows, bool live) {
+    typedef typename TR::T T;
+    const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
+    const int64_t row = row0 + r;
+    const int valid = r < n_rows && live ? p.valid - col : 0;
+    x.load(static_cast<const T*>(a.x) + row * a.x_row + p.channel + col, valid);
+    dt.load(static_cast<const T*>(a.dt) + row * a.dt_row + p.channel + col, valid);
+    if (a.z) z.load(static_cast<const T*>(a.z) + row * a.z_row + p.channel + col, valid);
+    if constexpr (GRADIENT) dy.load(static_cast<const T*>(a.dy) + row * a.dy_row + p.channel + col, valid);
+    const int br = threadIdx.x / (PER * WAVES);
+#pragma unroll
+    for (int k = 0; k < CHUNKS; ++k) {
+      const int n = k * PER * WAVES + threadIdx.x % (PER * WAVES);
+      b[k] = c[k] = 0.f;
+      if (live && br < n_rows && n < a.states) {
+        b[k] = TR::get(static_cast<const T*>(a.B)[(row0 + br) * a.B_row + p.group * a.B_head + n]);
+        c[k] = TR::get(static_cast<const T*>(a.C)[(row0 + br) * a.C_row + p.group * a.C_head + n]);
+      }
+    }
+  }
+};
+
+// f(0), f(1), ..: with the number as a constant
+template <class F, int... I>
+__device__ inline void repeat_all(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ inline void repeat(F f) { repeat_all(f, std::make_integer_sequence<int, N>{}); }
+
+// Sum over the waves' parts.
+template <int V>
+__device__ inline void gather(const float (*part)[TILE_ROWS][CH], int waves, int r, int col, float (&out)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) out[j] = part[0][r][col + j];
+  for (int w = 1; w < waves; ++w)
+#pragma unroll
+    for (int j = 0; j < V; ++j) out[j] += part[w][r][col + j];
+}
+
+__device__ inline void load_states(float (&h)[PER], const float* from, int n) {
+#pragma unroll
+  for (int s = 0; s < PER; ++s) h[s] = s < n ? from[s] : 0.f;
+}
+__device__ inline void store_states(const float (&h)[PER], float* to, int n) {
+#pragma unroll
+  for (int s = 0; s < PER; ++s)
+    if (s < n) to[s] = h[s];
+}
+
+// A lane's states: four for each chunk of those that the waves share out.
+template <int WAVES, int CHUNKS>
+struct States {
+  float v[CHUNKS][PER];
+  // the wave's number of chunk k's
+  static __device__ int count(const ScanArgs& a, int wave, int k) { return min(PER, a.states - (k * WAVES + wave) * PER); }
+  // from (or to) those of the lane's channel in an array channels x states, where live
+  __device__ void load(const ScanArgs& a, const float* from, int wave, bool live) {
+#pragma unroll
+    for (int k = 0; k < CHUNKS; ++k) load_states(v[k], from + (k * WAVES + wave) * PER, live ? count(a, wave, k) : 0);
+  }
+  __device__ void store(const ScanArgs& a, float* to, int wave, bool live) const {
+    if (!live) return;
+#pragma unroll
+    for (int k = 0; k < CHUNKS; ++k) store_states(v[k], to + (k * WAVES + wave) * PER, count(a, wave, k));
+  }
+  __device__ void fill(float x) {
+#pragma unroll
+    for (int k = 0; k < CHUNKS; ++k)
+#pragma unroll
+      for (int s = 0; s < PER; ++s) v[k][s] = x;
+  }
+  __device__ void scale(float x) {
+#pragma unroll
+    for (int k = 0; k < CHUNKS; ++k)
+#pragma unroll
+      for (int s = 0; s < PER; ++s) v[k][s] *= x;
+  }
+};
+
+// One number a channel for the V channels of a thread.
+template <int V>
+__device__ inline void load_channels(float (&v)[V], const float* p, int channel, int col, int valid) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] = p && col + j < valid ? p[channel + col + j] : 0.f;
+}
+
+// What a tile's rows are read from, while its states are walked through.
+template <int WAVES, int CHUNKS, bool GRADIENT>
+struct Tile {
+  float2 du[TILE_ROWS][CH];                        // d and u
+  float B[CHUNKS][TILE_ROWS][PER * WAVES], C[CHUNKS][TILE_ROWS][PER * WAVES];
+  float e[GRADIENT ? TILE_ROWS : 1][CH];
+};
+
+// Makes a tile's rows from what came in.  Rows and channels that there are not: d = u = 0, which leaves a state as it is.  steps: sums
+// of d, a row of every tile a thread.
+template <class TR, int WAVES, int CHUNKS, bool GRADIENT>
+__device__ inline void fill_tile(Tile<WAVES, CHUNKS, GRADIENT>& tile, const ScanArgs& a, const Incoming<TR, WAVES, CHUNKS, GRADIENT>& in, int n_rows,
+                                 int valid, const float (&bias)[TILE_ROWS / WAVES], float (&steps)[TILE_ROWS / WAVES]) {
+  constexpr int V = TILE_ROWS / WAVES;
+  const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    float d = in.dt.get(j) + bias[j];
+    if (a.softplus) d = softplus_of(d);
+    if (r >= n_rows || col + j >= valid) d = 0.f;
+    steps[j] += d;
+    tile.du[r][col + j] = float2{d, d * in.x.get(j)};
+    if constexpr (GRADIENT) {
+      const float dy = in.dy.get(j), z = a.z ? in.z.get(j) : 0.f;
+      tile.e[r][col + j] = a.z ? dy * (z * sigmoid_of(z)) : dy;
+    }
+  }
+  const int br = threadIdx.x / (PER * WAVES), n = threadIdx.x % (PER * WAVES);
+#pragma unroll
+  for (int k = 0; k < CHUNKS; ++k) {
+    tile.B[k][br][n] = in.b[k];
+    tile.C[k][br][n] = in.c[k];
+  }
+}
+
+// Sum over the rows of a tile's threads, of `steps` and the like; out[CH] in LDS.  (All threads.)
+template <int V>
+__device__ inline void sum_rows(float (&v)[V], float (*part)[CH], float* to, int valid) {
+  const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < V; ++j) part[r][col + j] = v[j];
+  __syncthreads();
+  if ((int)threadIdx.x < valid) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < TILE_ROWS; ++k) s += part[k][threadIdx.x];
+    to[threadIdx.x] = s;
+  }
+}
+
+// A wave's N states of chunk `k` over one tile; its part of y is stored where OUT, beside that of the chunks before.
+template <int N, bool OUT, class T>
+__device__ inline void walk_tile(float (&h)[PER], const float (&a2)[PER], const T& tile, int k, int wave, int lane, float (*part)[CH]) {
+  const int row = (lane & 15) / PER, n = wave * PER + lane % PER;
+  repeat<TILE_ROWS / 4>([&](auto q) {
+    const float vb = tile.B[k][4 * q + row][n], vc = OUT ? tile.C[k][4 * q + row][n] : 0.f;
+    repeat<4>([&](auto i) {
+      constexpr int t = 4 * q + i;
+      const float2 du = tile.du[t][lane];
+      float y = 0.f;
+      repeat<N>([&](auto s) {
+        constexpr int at = PER * i + s;
+        h[s] = fmaf(exp2_of(du.x * a2[s]), h[s], du.y * from_lane<at>(vb));
+        if constexpr (OUT) y = s == 0 ? from_lane<at>(vc) * h[s] : fmaf(from_lane<at>(vc), h[s], y);
+      });
+      if constexpr (OUT) part[t][lane] = k ? part[t][lane] + y : y;
+    });
+  });
+}
+
+// The same without output, and the product of the factors so far, and what e C adds to the gradient by the state before the tile's rows.
+template <int N, class T>
+__device__ inline void walk_tile_back(float (&h)[PER], float (&product)[PER], float (&g)[PER], const float (&a2)[PER], const T& tile, int k, int wave,
+                                      int lane) {
+  const int row = (lane & 15) / PER, n = wave * PER + lane % PER;
+  repeat<TILE_ROWS / 4>([&](auto q) {
+    const float vb = tile.B[k][4 * q + row][n], vc = tile.C[k][4 * q + row][n];
+    repeat<4>([&](auto i) {
+      constexpr int t = 4 * q + i;
+      const float2 du = tile.du[t][lane];
+      const float e = tile.e[t][lane];
+      repeat<N>([&](auto s) {
+        constexpr int at = PER * i + s;
+        const float f = exp2_of(du.x * a2[s]);
+        h[s] = fmaf(f, h[s], du.y * from_lane<at>(vb));
+        product[s] *= f;
+        g[s] = fmaf(product[s] * e, from_lane<at>(vc), g[s]);
+      });
+    });
+  });
+}
+
+// For every chunk: f(the chunk, the number of the wave's states in it, as a constant); full: all have PER.
+template <int WAVES, int CHUNKS, bool FULL, class F>
+__device__ inline void with_states(const ScanArgs& a, int wave, F f) {
+  repeat<CHUNKS>([&](auto k) {
+    if constexpr (FULL) {
+      f(k, std::integral_constant<int, PER>{});
+    } else {
+      const int n = States<WAVES, CHUNKS>::count(a, wave, k);
+      if (n == 4) f(k, std::integral_constant<int, 4>{});
+      else if (n == 3) f(k, std::integral_constant<int, 3>{});
+      else if (n == 2) f(k, std::integral_constant<int, 2>{});
+      else if (n == 1) f(k, std::integral_constant<int, 1>{});
+    }
+  });
+}
+
+// Rows before the first sequence and behind the last are cleared by workgroups of their own.
+template <class TR>
+__device__ void clear_rows(const ScanArgs& a, int who, void* to, int64_t stride) {
+  if (!to) return;
+  const int64_t first = clamped(a.off[0], 0, a.n_rows), last = clamped(a.off[a.n_seqs], first, a.n_rows);
+  Values<TR, 4> zero;
+  zero.clear();
+  for (int64_t row = who; row < a.n_rows - (last - first); row += ZERO_GROUPS) {
+    typename TR::T* p = static_cast<typename TR::T*>(to) + (row < first ? row : row + (last - first)) * stride;
+    for (int col = threadIdx.x * 4; col < a.dim; col += blockDim.x * 4) zero.store(p + col, a.dim - col);
+  }
+}
+
+// ADDS: what a span adds to the state, and the sum of its d; else the walk that writes y.
+template <class TR, int WAVES, int CHUNKS, bool FULL, bool ADDS>
+__global__ __launch_bounds__(64 * WAVES) void k_scan(const ScanArgs a) {
+  typedef typename TR::T T;
+  constexpr int V = TILE_ROWS / WAVES;
+  __shared__ Tile<WAVES, CHUNKS, false> tile;
+  __shared__ float part[ADDS ? 1 : WAVES][TILE_ROWS][CH];
+  const int item = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
+  if (!ADDS && item >= a.items) {
+    clear_rows<TR>(a, blockIdx.x - a.items * a.blocks, a.y, a.y_row);
+    return;
+  }
+  Place p;
+  if (!find(a, item, block, p) || (ADDS && p.last)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int waves = min(WAVES, (a.states + PER - 1) / PER);      // (those that have states)
+  const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
+  const bool live = lane < p.valid;
+  const int64_t of_lane = (int64_t)(p.channel + lane) * a.states, each = (int64_t)a.dim * a.states;
+  States<WAVES, CHUNKS> h, a2;
+  float bias[V], D[V], steps[V];
+  a2.load(a, a.A + of_lane, wave, live);
+  a2.scale(LOG2_E);
+  const float* start = p.span == 0 ? (a.s_in ? a.s_in + p.piece.seq * each : nullptr) : ADDS ? nullptr : a.adds + item * each;
+  h.load(a, start + of_lane, wave, live && start);
+  load_channels(bias, a.bias, p.channel, col, p.valid);
+  load_channels(D, a.D, p.channel, col, p.valid);
+#pragma unroll
+  for (int j = 0; j < V; ++j) steps[j] = 0.f;
+  Incoming<TR, WAVES, CHUNKS, false> in;
+  in.load(a, p, p.from, (int)min((int64_t)TILE_ROWS, p.to - p.from), true);
+  for (int64_t t0 = p.from; t0 < p.to; t0 += TILE_ROWS) {
+    const int rows = (int)min((int64_t)TILE_ROWS, p.to - t0);
+    if (ADDS) __syncthreads();                     // (the walk's second one has this effect)
+    fill_tile(tile, a, in, rows, p.valid, bias, steps);
+    const auto now = in;
+    __syncthreads();
+    const int64_t next = t0 + TILE_ROWS;
+    in.load(a, p, next, (int)min((int64_t)TILE_ROWS, p.to - next), next < p.to);
+    with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) {
+      walk_tile<decltype(n)::value, !ADDS>(h.v[k], a2.v[k], tile, k, wave, lane, part[ADDS ? 0 : wave]);
+    });
+    if constexpr (!ADDS) {
+      __syncthreads();
+      float y[V];
+      gather(part, waves, r, col, y);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        y[j] = a.D ? fmaf(D[j], now.x.get(j), y[j]) : y[j];
+        if (a.z) y[j] *= now.z.get(j) * sigmoid_of(now.z.get(j));
+      }
+      Values<TR, V> o;
+      o.put(y);
+      if (r < rows) o.store(static_cast<T*>(a.y) + (t0 + r) * a.y_row + p.channel + col, p.valid - col);
+    }
+  }
+  if constexpr (ADDS) {
+    h.store(a, a.adds + item * each + of_lane, wave, live);
+    sum_rows(steps, part[0], a.steps + (int64_t)item * a.dim + p.channel, p.valid);
+  } else {
+    if (a.s_out) h.store(a, a.s_out + p.piece.seq * each + of_lane, wave, live && p.last);
+  }
+}
+
+// Start states of a sequence's spans, in the place of what the spans add; the second half of the grid: gradients at their end, against time.
+__global__ __launch_bounds__(256) void k_scan_join(const ScanArgs a) {
+  const int64_t each = (int64_t)a.dim * a.states, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= each) return;
+  for (int seq = blockIdx.y; seq < a.n_seqs; seq += gridDim.y) {
+    const int64_t lo = clamped(a.off[seq], 0, a.n_rows), hi = clamped(a.off[seq + 1], lo, a.n_rows);
+    const int spans = (int)((hi - lo + ((int64_t)1 << a.span_log2) - 1) >> a.span_log2);
+    if (spans < 2) continue;
+    const int64_t first = (lo >> a.span_log2) + seq;
+    const int c = (int)(at / a.states);
+    const float a2 = a.A[at] * LOG2_E;
+    constexpr int STEP = 8;
+    if (blockIdx.z == 0) {
+      float* adds = a.adds + first * each + at;
+      const float* steps = a.steps + first * a.dim + c;
+      float h = adds[0];
+      for (int k = 1; k < spans; k += STEP) {
+        float add[STEP], d[STEP];
+  #pragma unroll
+        for (int j = 0; j < STEP; ++j) {
+          const bool there = k + j < spans - 1;      // (the last span adds to none)
+          add[j] = there ? adds[(k + j) * each] : 0.f;
+          d[j] = there ? steps[(int64_t)(k + j) * a.dim] : 0.f;
+        }
+  #pragma unroll
+        for (int j = 0; j < STEP; ++j) {
+          if (k + j >= spans) break;
+          adds[(k + j) * each] = h;
+          const float f = exp2_of(a2 * d[j]);
+          h = h == 0.f || (f == 0.f && __builtin_isinf(h)) ? h + add[j] : fmaf(f, h, add[j]);
+        }
+      }
+    } else {
+      float* back = a.back + first * each + at;
+      const float* steps = a.steps + first * a.dim + c;
+      float g = a.ds_end ? a.ds_end[seq * each + at] : 0.f;
+      for (int k = spans - 1; k >= 0; k -= STEP) {
+        float add[STEP], d[STEP];
+  #pragma unroll
+        for (int j = 0; j < STEP; ++j) {
+          const bool there = k - j > 0;
+          add[j] = there ? back[(k - j) * each] : 0.f;
+          d[j] = there ? steps[(int64_t)(k - j) * a.dim] : 0.f;
+        }
+  #pragma unroll
+        for (int j = 0; j < STEP; ++j) {
+          if (k - j < 0) break;
+          back[(k - j) * each] = g;
+          const float f = exp2_of(a2 * d[j]);
+          g = g == 0.f || (f == 0.f && __builtin_isinf(g)) ? g + add[j] : fmaf(f, g, add[j]);
+        }
+      }
+    }
+  }
+}
+
+// ---- gradients ------------------------------------------------------------------------------------------------------------
+__device__ inline int64_t first_tile(const Place& p) { return p.piece.lo / TILE_ROWS + p.piece.seq + (p.from - p.piece.lo) / TILE_ROWS; }
+
+// The states at the begin of every tile, what a span adds, and what it adds to the gradient by the state before it.
+template <class TR, int WAVES, int CHUNKS, bool FULL>
+__global__ __launch_bounds__(64 * WAVES) void k_scan_tiles(const ScanArgs a) {
+  constexpr int V = TILE_ROWS / WAVES;
+  __shared__ Tile<WAVES, CHUNKS, true> tile;
+  __shared__ float part[TILE_ROWS][CH];
+  const int item = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
+  Place p;
+  if (!find(a, item, block, p)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int col = threadIdx.x % (CH / V) * V;
+  const bool live = lane < p.valid;
+  const int64_t of_lane = (int64_t)(p.channel + lane) * a.states, each = (int64_t)a.dim * a.states;
+  States<WAVES, CHUNKS> h, a2, product, g;
+  float bias[V], steps[V];
+  a2.load(a, a.A + of_lane, wave, live);
+  a2.scale(LOG2_E);
+  product.fill(1.f);
+  g.fill(0.f);
+  const float* start = p.span == 0 && a.s_in ? a.s_in + p.piece.seq * each : nullptr;
+  h.load(a, start + of_lane, wave, live && start);
+  load_channels(bias, a.bias, p.channel, col, p.valid);
+#pragma unroll
+  for (int j = 0; j < V; ++j) steps[j] = 0.f;
+  int64_t number = first_tile(p);
+  float passed = 0.f;                              // sum of d before the tile (first wave)
+  Incoming<TR, WAVES, CHUNKS, true> in;
+  in.load(a, p, p.from, (int)min((int64_t)TILE_ROWS, p.to - p.from), true);
+  for (int64_t t0 = p.from; t0 < p.to; t0 += TILE_ROWS, ++number) {
+    const int rows = (int)min((int64_t)TILE_ROWS, p.to - t0);
+    h.store(a, a.tiles + number * each + of_lane, wave, live);
+    __syncthreads();
+    fill_tile(tile, a, in, rows, p.valid, bias, steps);
+    __syncthreads();
+    const int64_t next = t0 + TILE_ROWS;
+    in.load(a, p, next, (int)min((int64_t)TILE_ROWS, p.to - next), next < p.to);
+    if (p.span > 0) {
+      if (wave == 0 && live) {
+        a.tile_steps[number * a.dim + p.channel + lane] = passed;
+        for (int t = 0; t < TILE_ROWS; ++t) passed += tile.du[t][lane].x;
+      }
+      with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) {
+        walk_tile_back<decltype(n)::value>(h.v[k], product.v[k], g.v[k], a2.v[k], tile, k, wave, lane);
+      });
+    } else {
+      with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) {
+        walk_tile<decltype(n)::value, false>(h.v[k], a2.v[k], tile, k, wave, lane, part);
+      });
+    }
+  }
+  if (p.span == 0 && p.last) return;
+  h.store(a, a.adds + item * each + of_lane, wave, live && !p.last);
+  g.store(a, a.back + item * each + of_lane, wave, live && p.span > 0);
+  sum_rows(steps, part, a.steps + (int64_t)item * a.dim + p.channel, p.valid);
+}
+
+__device__ inline void swap_halves(float& x, float& y) {
+  const auto v = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
+  x = __builtin_bit_cast(float, (uint32_t)v[0]);
+  y = __builtin_bit_cast(float, (uint32_t)v[1]);
+}
+__device__ inline void swap_rows(float& x, float& y) {
+  const auto v = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
+  x = __builtin_bit_cast(float, (uint32_t)v[0]);
+  y = __builtin_bit_cast(float, (uint32_t)v[1]);
+}
+template <int CTRL>
+__device__ inline float moved(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+
+// Sums over the wave's lanes of four rows x four states: lane l gets the one of row l / 16, state l % 16 / 4.  Two numbers are joined in one
+// register at each step, so that 16 sums take 35 instructions instead of 96.
+__device__ inline float lane_sums(float (&v)[4][PER], int lane) {
+  float w[2][PER], z[PER];
+#pragma unroll
+  for (int s = 0; s < PER; ++s) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      swap_halves(v[i][s], v[i + 2][s]);
+      w[i][s] = v[i][s] + v[i + 2][s];
+    }
+    swap_rows(w[0][s], w[1][s]);
+    z[s] = w[0][s] + w[1][s];
+  }
+  const bool upper8 = lane & 8, upper4 = lane & 4;
+  float k[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) k[s] = (upper8 ? z[s + 2] : z[s]) + moved<0x128>(upper8 ? z[s] : z[s + 2]);     // eight lanes on
+  float x = (upper4 ? k[1] : k[0]) + moved<0x141>(upper4 ? k[0] : k[1]);                                     // mirrored among eight
+  x += moved<0xb1>(x);
+  x += moved<0x4e>(x);
+  return x;
+}
+
+// A wave's N states of chunk k over one tile: forward from its first states, then back.  The parts stand beside those of the chunks before;
+// dB, dC: of the tile's first row and the wave's first state, rows `stride` apart.
+template <int N, class T>
+__device__ inline void back_tile(float (&g)[PER], float (&dA)[PER], const float (&h0)[PER], const float (&a2)[PER], const T& tile, int k, int wave,
+                                 int lane, float (*part_u)[CH], float (*part_d)[CH], float (*part_y)[CH], float* dB, float* dC, int64_t stride,
+                                 int rows) {
+  const int row = (lane & 15) / PER, n = wave * PER + lane % PER;
+  float h[TILE_ROWS + 1][PER], f[TILE_ROWS][PER];
+#pragma unroll
+  for (int s = 0; s < PER; ++s) h[0][s] = h0[s];
+  repeat<TILE_ROWS / 4>([&](auto q) {
+    const float vb = tile.B[k][4 * q + row][n], vc = tile.C[k][4 * q + row][n];
+    repeat<4>([&](auto i) {
+      constexpr int t = 4 * q + i;
+      const float2 du = tile.du[t][lane];
+      float y = 0.f;
+      repeat<N>([&](auto s) {
+        constexpr int at = PER * i + s;
+        f[t][s] = exp2_of(du.x * a2[s]);
+        h[t + 1][s] = fmaf(f[t][s], h[t][s], du.y * from_lane<at>(vb));
+        y = s == 0 ? from_lane<at>(vc) * h[t + 1][s] : fmaf(from_lane<at>(vc), h[t + 1][s], y);
+      });
+      part_y[t][lane] = k ? part_y[t][lane] + y : y;
+    });
+    __builtin_amdgcn_sched_barrier(0);             // (what comes later is not read earlier: its registers are needed)
+  });
+  repeat<TILE_ROWS / 4>([&](auto back) {
+    constexpr int q = TILE_ROWS / 4 - 1 - back;
+    const float vb = tile.B[k][4 * q + row][n], vc = tile.C[k][4 * q + row][n];
+    float sb[4][PER], sc[4][PER];
+    repeat<4>([&](auto j) {
+      constexpr int i = 3 - j, t = 4 * q + i;
+      const float2 du = tile.du[t][lane];
+      const float e = tile.e[t][lane];
+      float by_u = 0.f, by_d = 0.f;
+#pragma unroll
+      for (int s = N; s < PER; ++s) sb[i][s] = sc[i][s] = 0.f;
+      repeat<N>([&](auto s) {
+        constexpr int at = PER * i + s;
+        g[s] = fmaf(e, from_lane<at>(vc), g[s]);
+        sb[i][s] = g[s] * du.y;
+        sc[i][s] = e * h[t + 1][s];
+        by_u = s == 0 ? from_lane<at>(vb) * g[s] : fmaf(from_lane<at>(vb), g[s], by_u);
+        g[s] *= f[t][s];
+        const float x = g[s] * h[t][s];
+        dA[s] = fmaf(x, du.x, dA[s]);
+        by_d = s == 0 ? x * a2[s] : fmaf(x, a2[s], by_d);
+      });
+      part_u[t][lane] = k ? part_u[t][lane] + by_u : by_u;
+      part_d[t][lane] = k ? part_d[t][lane] + by_d : by_d;
+    });
+    const float b = lane_sums(sb, lane), c = lane_sums(sc, lane);
+    const int at = 4 * q + lane / 16, s = lane % 16 / 4;
+    if (at < rows && s < N) {
+      if (lane % 4 == 0) dB[at * stride + s] = b;
+      if (lane % 4 == 1) dC[at * stride + s] = c;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  });
+}
+
+template <class TR, int WAVES, int CHUNKS, bool FULL>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_scan_backward(const ScanArgs a) {
+  typedef typename TR::T T;
+  constexpr int V = TILE_ROWS / WAVES;
+  __shared__ Tile<WAVES, CHUNKS, true> tile;
+  __shared__ float part[3][WAVES][TILE_ROWS][CH];
+  const int item = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
+  if (item >= a.items) {
+    const int who = blockIdx.x - a.items * a.blocks;
+    clear_rows<TR>(a, who, a.dx, a.dx_row);
+    clear_rows<TR>(a, who, a.ddt, a.ddt_row);
+    clear_rows<TR>(a, who, a.dz, a.dz_row);
+    return;
+  }
+  Place p;
+  const bool found = find(a, item, block, p);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int waves = min(WAVES, (a.states + PER - 1) / PER);
+  const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
+  const bool live = lane < p.valid;
+  const int64_t of_lane = (int64_t)(p.channel + lane) * a.states, each = (int64_t)a.dim * a.states;
+  States<WAVES, CHUNKS> dA;
+  float dD[V], dbias[V];
+  dA.fill(0.f);
+#pragma unroll
+  for (int j = 0; j < V; ++j) dD[j] = dbias[j] = 0.f;
+  if (found) {
+    States<WAVES, CHUNKS> g, a2;
+    float bias[V], D[V], steps[V];
+    a2.load(a, a.A + of_lane, wave, live);
+    a2.scale(LOG2_E);
+    const float* end = p.last && p.span == 0 ? (a.ds_end ? a.ds_end + p.piece.seq * each : nullptr) : a.back + item * each;
+    g.load(a, end + of_lane, wave, live && end);
+    load_channels(bias, a.bias, p.channel, col, p.valid);
+    load_channels(D, a.D, p.channel, col, p.valid);
+    const int tiles = (int)((p.to - p.from + TILE_ROWS - 1) / TILE_ROWS);
+    const int64_t number = first_tile(p), stride = (int64_t)a.groups * a.states;
+    // (of the group's blocks this one's parts of dB and dC)
+    const int64_t part_at = (int64_t)(block % (a.blocks / a.groups)) * a.n_rows * stride + p.group * a.states;
+    Incoming<TR, WAVES, CHUNKS, true> in;
+    if (tiles > 0) in.load(a, p, p.from + (int64_t)(tiles - 1) * TILE_ROWS, (int)(p.to - p.from - (int64_t)(tiles - 1) * TILE_ROWS), true);
+    for (int k = tiles - 1; k >= 0; --k) {
+      const int64_t t0 = p.from + (int64_t)k * TILE_ROWS;
+      const int rows = (int)min((int64_t)TILE_ROWS, p.to - t0);
+      States<WAVES, CHUNKS> h0;
+      h0.load(a, a.tiles + (number + k) * each + of_lane, wave, live);
+      if (p.span > 0 && live) {
+        States<WAVES, CHUNKS> start;
+        start.load(a, a.adds + item * each + of_lane, wave, true);
+        const float d = a.tile_steps[(number + k) * a.dim + p.channel + lane];
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+          for (int s = 0; s < PER; ++s)
+            h0.v[c][s] = start.v[c][s] == 0.f ? h0.v[c][s] : fmaf(exp2_of(a2.v[c][s] * d), start.v[c][s], h0.v[c][s]);
+      }
+      fill_tile(tile, a, in, rows, p.valid, bias, steps);
+      const auto now = in;
+      __syncthreads();
+      if (k > 0) in.load(a, p, t0 - TILE_ROWS, TILE_ROWS, true);
+      with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto c, auto n) {
+        const int64_t at = part_at + t0 * stride + (c * WAVES + wave) * PER;
+        back_tile<decltype(n)::value>(g.v[c], dA.v[c], h0.v[c], a2.v[c], tile, c, wave, lane, part[0][wave], part[1][wave], part[2][wave], a.dB + at,
+                                      a.dC + at, stride, rows);
+      });
+      __syncthreads();
+      float du[V], dd[V], y[V], dx[V], ddt[V], dz[V];
+      gather(part[0], waves, r, col, du);
+      gather(part[1], waves, r, col, dd);
+      gather(part[2], waves, r, col, y);
+      const bool there = r < rows;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float d = tile.du[r][col + j].x, e = tile.e[r][col + j], x = now.x.get(j), raw = now.dt.get(j) + bias[j];
+        dx[j] = a.D ? fmaf(D[j], e, d * du[j]) : d * du[j];
+        ddt[j] = fmaf(x, du[j], LN_2 * dd[j]);
+        if (a.softplus) ddt[j] *= sigmoid_of(raw);
+        if (there && col + j < p.valid) {
+          dD[j] = fmaf(e, x, dD[j]);
+          dbias[j] += ddt[j];
+        }
+        dz[j] = 0.f;
+        if (a.z) {
+          const float z = now.z.get(j), s = sigmoid_of(z);
+          dz[j] = now.dy.get(j) * (a.D ? fmaf(D[j], x, y[j]) : y[j]) * s * fmaf(z, 1.f - s, 1.f);
+        }
+      }
+      if (there) {
+        Values<TR, V> o;
+        o.put(dx);
+        o.store(static_cast<T*>(a.dx) + (t0 + r) * a.dx_row + p.channel + col, p.valid - col);
+        o.put(ddt);
+        o.store(static_cast<T*>(a.ddt) + (t0 + r) * a.ddt_row + p.channel + col, p.valid - col);
+        if (a.z) {
+          o.put(dz);
+          o.store(static_cast<T*>(a.dz) + (t0 + r) * a.dz_row + p.channel + col, p.valid - col);
+        }
+      }
+      __syncthreads();                             // (the tile is read above)
+    }
+    if (p.span == 0 && a.ds_in) g.store(a, a.ds_in + p.piece.seq * each + of_lane, wave, live);
+  }
+  // (items that are no span have sums too: zero)
+  dA.store(a, a.dA + item * each + of_lane, wave, live);
+  if (a.D) sum_rows(dD, part[0][0], a.dD + (int64_t)item * a.dim + p.channel, p.valid);
+  if (a.bias) sum_rows(dbias, part[0][0], a.dbias + (int64_t)item * a.dim + p.channel, p.valid);
+}
+
+// dB and dC from the channel blocks' parts, in their order; zero where no sequence owns the row.
+template <class TR>
+__global__ __launch_bounds__(256) void k_scan_sum_blocks(const ScanArgs a, void* dB, int64_t dB_row, int64_t dB_head, void* dC, int64_t dC_row,
+                                                         int64_t dC_head) {
+  typedef typename TR::T T;
+  const int64_t stride = (int64_t)a.groups * a.states, total = a.n_rows * stride, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= total) return;
+  const int64_t row = at / stride;
+  const int group = (int)(at % stride) / a.states, n = (int)(at % stride) % a.states, parts = a.blocks / a.groups;
+  const int64_t first = clamped(a.off[0], 0, a.n_rows), last = clamped(a.off[a.n_seqs], first, a.n_rows);
+  const float* from = (blockIdx.y ? a.dC : a.dB) + at;
+  float s = 0.f;
+  if (row >= first && row < last)
+    for (int k = 0; k < parts; ++k) s += from[k * total];
+  if (blockIdx.y) static_cast<T*>(dC)[row * dC_row + group * dC_head + n] = TR::put(s);
+  else static_cast<T*>(dB)[row * dB_row + group * dB_head + n] = TR::put(s);
+}
+
+// dA, dD and dbias from the spans' parts, in their order: each wave of a workgroup a quarter of them.
+__global__ __launch_bounds__(256) void k_scan_sum_items(const ScanArgs a, float* dA, float* dD, float* dbias) {
+  __shared__ float part[4][64];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const float* from = blockIdx.y == 0 ? a.dA : blockIdx.y == 1 ? a.dD : a.dbias;
+  float* to = blockIdx.y == 0 ? dA : blockIdx.y == 1 ? dD : dbias;
+  const int64_t size = (int64_t)a.dim * (blockIdx.y == 0 ? a.states : 1), at = (int64_t)blockIdx.x * 64 + lane;
+  if (!to || (int64_t)blockIdx.x * 64 >= size) return;
+  const int each = (a.items + 3) / 4, end = min(a.items, (wave + 1) * each);
+  float s = 0.f;
+  if (at < size)
+    for (int k = wave * each; k < end; ++k) s += from[k * size + at];
+  part[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && at < size) to[at] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+}
+
+// ---- single tokens --------------------------------------------------------------------------------------------------------
+struct ScanStepArgs {
+  const void *x, *dt, *z, *B, *C;
+  void* y;
+  int64_t x_row, dt_row, z_row, y_row, B_row, B_head, C_row, C_head;
+  const float *A, *D, *bias;
+  float* state;
+  const int32_t* slots;
+  int n_states, dim, each, states, softplus, col_blocks;
+};
+
+// LANES lanes a channel, each with four of its states.  The states' way from memory and back bounds it.
+template <class TR, int LANES, bool WIDE>
+__global__ __launch_bounds__(256) void k_scan_step(const ScanStepArgs a) {
+  typedef typename TR::T T;
+  const int64_t row = blockIdx.x / a.col_blocks;
+  const int c = (int)(blockIdx.x % a.col_blocks) * (256 / LANES) + threadIdx.x / LANES, n0 = threadIdx.x % LANES * PER;
+  const bool live = c < a.dim;
+  const int64_t slot = a.slots ? a.slots[row] : row;
+  T* y = static_cast<T*>(a.y) + row * a.y_row + c;
+  if (slot < 0 || slot >= a.n_states) {
+    if (live && n0 == 0) *y = TR::put(0.f);
+    return;
+  }
+  float out = 0.f, x = 0.f;
+  if (live) {
+    const int64_t at = (int64_t)c * a.states + n0;
+    float* state = a.state + slot * a.dim * a.states + at;
+    const int n = min(PER, a.states - n0), group = c / a.each;
+    float h[PER], f[PER];
+    if constexpr (WIDE) {
+      if (n > 0) {
+        __builtin_memcpy(h, state, sizeof h);
+        __builtin_memcpy(f, a.A + at, sizeof f);
+      }
+    } else {
+      load_states(h, state, n);
+      load_states(f, a.A + at, n);
+    }
+    x = TR::get(static_cast<const T*>(a.x)[row * a.x_row + c]);
+    float d = TR::get(static_cast<const T*>(a.dt)[row * a.dt_row + c]) + (a.bias ? a.bias[c] : 0.f);
+    if (a.softplus) d = softplus_of(d);
+    const float u = d * x;
+#pragma unroll
+    for (int s = 0; s < PER; ++s) {
+      if (s >= n) continue;
+      const float b = TR::get(static_cast<const T*>(a.B)[row * a.B_row + group * a.B_head + n0 + s]);
+      const float w = TR::get(static_cast<const T*>(a.C)[row * a.C_row + group * a.C_head + n0 + s]);
+      h[s] = fmaf(exp_of(d * f[s]), h[s], u * b);
+      out = fmaf(w, h[s], out);
+    }
+    if constexpr (WIDE) {
+      if (n > 0) __builtin_memcpy(state, h, sizeof h);
+    } else {
+      store_states(h, state, n);
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < LANES; d *= 2) out += __shfl_xor(out, d);
+  if (!live || n0) return;
+  if (a.D) out = fmaf(a.D[c], x, out);
+  if (a.z) {
+    const float z = TR::get(static_cast<const T*>(a.z)[row * a.z_row + c]);
+    out *= z * sigmoid_of(z);
+  }
+  *y = TR::put(out);
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------------
+int invalid(const std::string& what) {
+  set_error(what);
+  return NUGPR_ERR_INVALID;
+}
+
+int check(const nugpr_selective_scan* p) {
+  if (!p) return invalid("problem is null");
+  if (p->dtype != NUGPR_FLOAT32 && p->dtype != NUGPR_BFLOAT16) return invalid("dtype must be NUGPR_FLOAT32 or NUGPR_BFLOAT16");
+  if (p->dim < 1 || p->dim > 65536) return invalid("dim must be 1..65536");
+  if (p->groups < 1 || p->dim % p->groups) return invalid("groups must divide dim");
+  if (p->dim_state < 1 || p->dim_state > 64) return invalid("dim_state must be 1..64");
+  if (p->n_rows < 0 || p->n_rows > (int64_t)1 << 40) return invalid("n_rows must be 0..2^40");
+  if (p->n_seqs < 0) return invalid("n_seqs must be >= 0");
+  return NUGPR_OK;
+}
+
+size_t value_size(const nugpr_selective_scan* p) { return p->dtype == NUGPR_BFLOAT16 ? 2 : 4; }
+
+int check_array(const void* data, int64_t stride, int64_t more, const char* name, size_t value) {
+  if (!data) return invalid(std::string(name) + " is null");
+  if (stride < 0 || more < 0) return invalid(std::string(name) + ": negative stride");
+  if (reinterpret_cast<uintptr_t>(data) % value) return invalid(std::string(name) + " misaligned");
+  return NUGPR_OK;
+}
+int check_rows(const nugpr_rows* x, const char* name, size_t value) { return check_array(x ? x->data : nullptr, x ? x->row_stride : 0, 0, name, value); }
+int check_heads(const nugpr_heads* x, const char* name, size_t value) {
+  return check_array(x ? x->data : nullptr, x ? x->row_stride : 0, x ? x->head_stride : 0, name, value);
+}
+int check_floats(const float* x, const char* name, bool needed) {
+  if (!x && needed) return invalid(std::string(name) + " is null");
+  if (reinterpret_cast<uintptr_t>(x) % 4) return invalid(std::string(name) + " misaligned");
+  return NUGPR_OK;
+}
+
+bool overlap(const void* a, const void* b, size_t bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x && y && x < y + bytes && y < x + bytes;
+}
+
+int waves_of(const nugpr_selective_scan* p) {
+  int w = 1;
+  while (w < 8 && w * PER < p->dim_state) w *= 2;
+  return w;
+}
+
+int blocks_of(const nugpr_selective_scan* p) { return p->groups * ((p->dim / p->groups + CH - 1) / CH); }
+
+// Rows of a span: a power of two, a few tiles at least, so large that the spans of the rows give about that many waves.
+constexpr int64_t WAVES_WANTED = 2048;
+int span_log2(const nugpr_selective_scan* p) {
+  int k = 6;
+  while (k < 40 && ((p->n_rows * blocks_of(p) * waves_of(p)) >> k) > WAVES_WANTED) ++k;
+  return k;
+}
+bool one_span(const nugpr_selective_scan* p) { return p->n_rows <= (int64_t)1 << span_log2(p); }
+int64_t items_of(const nugpr_selective_scan* p) { return (p->n_rows >> span_log2(p)) + p->n_seqs; }
+int64_t tiles_of(const nugpr_selective_scan* p) { return p->n_rows / TILE_ROWS + p->n_seqs; }
+
+// Where the parts of the workspace begin.
+struct Workspace {
+  size_t bytes = 0;
+  char* base;
+  explicit Workspace(void* ws) : base(static_cast<char*>(ws)) {}
+  float* take(size_t floats) {
+    float* p = reinterpret_cast<float*>(base + bytes);
+    bytes += (floats * sizeof(float) + 255) / 256 * 256;
+    return p;
+  }
+};
+
+size_t lay_out(const nugpr_selective_scan* p, bool backward, void* ws, ScanArgs* a) {
+  Workspace w(ws);
+  ScanArgs none;
+  if (!a) a = &none;
+  const size_t items = (size_t)items_of(p), tiles = (size_t)tiles_of(p), states = (size_t)p->dim * p->dim_state;
+  const bool spans = !one_span(p);
+  a->adds = w.take(spans ? items * states : 0);
+  a->steps = w.take(spans ? items * p->dim : 0);
+  if (backward) {
+    const size_t parts = (size_t)(blocks_of(p) / p->groups) * p->n_rows * p->groups * p->dim_state;
+    a->back = w.take(spans ? items * states : 0);
+    a->tiles = w.take(tiles * states);
+    a->tile_steps = w.take(spans ? tiles * p->dim : 0);
+    a->dB = w.take(parts);
+    a->dC = w.take(parts);
+    a->dA = w.take(items * states);
+    a->dD = w.take(items * p->dim);
+    a->dbias = w.take(items * p->dim);
+  }
+  return w.bytes;
+}
+
+#define NUGPR_TRY(call)                 \
+  do {                                  \
+    const int c__ = (call);             \
+    if (c__ != NUGPR_OK) return c__;    \
+  } while (0)
+
+// What both calls over sequences check; *done: nothing is left to do.
+int check_call(const nugpr_selective_scan* p, bool backward, bool* done) {
+  *done = p->n_rows == 0 && p->n_seqs == 0;
+  NUGPR_TRY(check_floats(p->A, "A", true));
+  NUGPR_TRY(check_floats(p->D, "D", false));
+  NUGPR_TRY(check_floats(p->dt_bias, "dt_bias", false));
+  if (*done) return NUGPR_OK;
+  if (p->n_seqs < 1 || !p->seq_offsets) return invalid("seq_offsets is null, or there is no sequence");
+  // (the threads of a launch are counted in 32 bits)
+  if (items_of(p) * blocks_of(p) + ZERO_GROUPS > (int64_t)0xffffffff / (64 * waves_of(p)) ||
+      (backward && p->n_rows * p->groups * p->dim_state > (int64_t)0xffffffff - 256))
+    return invalid("too many rows, sequences and channels for one call");
+  const size_t need = lay_out(p, backward, nullptr, nullptr);
+  if (need && (!p->workspace || (reinterpret_cast<uintptr_t>(p->workspace) & 255u))) { set_error("workspace is null or not 256-byte aligned"); return NUGPR_ERR_WORKSPACE; }
+  if (p->workspace_bytes < need) { set_error("workspace smaller than nugpr_selective_scan_workspace_bytes()"); return NUGPR_ERR_WORKSPACE; }
+  return NUGPR_OK;
+}
+
+ScanArgs scan_args(const nugpr_selective_scan* p) {
+  ScanArgs a{};
+  a.A = p->A; a.D = p->D; a.bias = p->dt_bias; a.off = p->seq_offsets; a.n_rows = p->n_rows; a.n_seqs = p->n_seqs;
+  a.dim = p->dim; a.groups = p->groups; a.each = p->dim / p->groups; a.blocks = blocks_of(p); a.states = p->dim_state;
+  a.softplus = p->softplus != 0; a.span_log2 = span_log2(p); a.items = (int)items_of(p);
+  return a;
+}
+
+// f(waves, chunks, whether all of them have four states), as constants
+template <class F>
+void with_waves(const nugpr_selective_scan* p, F f) {
+  auto with = [&](auto waves, auto chunks) {
+    if (p->dim_state == decltype(waves)::value * decltype(chunks)::value * PER) f(waves, chunks, std::true_type{});
+    else f(waves, chunks, std::false_type{});
+  };
+  constexpr std::integral_constant<int, 1> one{};
+  if (p->dim_state > 8 * PER) return with(std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
+  switch (waves_of(p)) {
+    case 1: return with(one, one);
+    case 2: return with(std::integral_constant<int, 2>{}, one);
+    case 4: return with(std::integral_constant<int, 4>{}, one);
+    default: return with(std::integral_constant<int, 8>{}, one);
+  }
+}
+
+void launch_join(const ScanArgs& a, bool backward, hipStream_t s) {
+  const int64_t each = (int64_t)a.dim * a.states;
+  const int64_t x = (each + 255) / 256, y = std::min<int64_t>(a.n_seqs, std::max<int64_t>(1, 8192 / x));
+  hipLaunchKernelGGL(k_scan_join, dim3((unsigned)x, (unsigned)y, backward ? 2 : 1), dim3(256), 0, s, a);
+}
+
+template <class TR>
+void launch_forward(const nugpr_selective_scan* p, const ScanArgs& a, hipStream_t s) {
+  with_waves(p, [&](auto w, auto chunks, auto full) {
+    constexpr int W = decltype(w)::value, K = decltype(chunks)::value;
+    constexpr bool FULL = decltype(full)::value;
+    const dim3 spans((unsigned)(a.items * a.blocks)), all((unsigned)(a.items * a.blocks + ZERO_GROUPS)), threads(64 * W);
+    if (!one_span(p)) {
+      hipLaunchKernelGGL((k_scan<TR, W, K, FULL, true>), spans, threads, 0, s, a);
+      launch_join(a, false, s);
+    }
+    hipLaunchKernelGGL((k_scan<TR, W, K, FULL, false>), all, threads, 0, s, a);
+  });
+}
+
+template <class TR>
+void launch_backward(const nugpr_selective_scan* p, const ScanArgs& a, const nugpr_heads* dB, const nugpr_heads* dC, float* dA, float* dD, float* dbias,
+                     hipStream_t s) {
+  with_waves(p, [&](auto w, auto chunks, auto full) {
+    constexpr int W = decltype(w)::value, K = decltype(chunks)::value;
+    constexpr bool FULL = decltype(full)::value;
+    const dim3 spans((unsigned)(a.items * a.blocks)), all((unsigned)(a.items * a.blocks + ZERO_GROUPS)), threads(64 * W);
+    hipLaunchKernelGGL((k_scan_tiles<TR, W, K, FULL>), spans, threads, 0, s, a);
+    if (!one_span(p)) launch_join(a, true, s);
+    hipLaunchKernelGGL((k_scan_backward<TR, W, K, FULL>), all, threads, 0, s, a);
+  });
+  const int64_t values = a.n_rows * a.groups * a.states, each = (int64_t)a.dim * a.states;
+  if (values)
+    hipLaunchKernelGGL(k_scan_sum_blocks<TR>, dim3((unsigned)((values + 255) / 256), 2), dim3(256), 0, s, a, dB->data, dB->row_stride, dB->head_stride,
+                       dC->data, dC->row_stride, dC->head_stride);
+  hipLaunchKernelGGL(k_scan_sum_items, dim3((unsigned)((each + 63) / 64), 3), dim3(256), 0, s, a, dA, a.D ? dD : nullptr, a.bias ? dbias : nullptr);
+}
+
+}  // namespace
+
+}  // namespace nugpr
+
+using namespace nugpr;
+
+extern "C" {
+
+size_t nugpr_selective_scan_workspace_bytes(const nugpr_selective_scan* p, int32_t backward) {
+  if (check(p) != NUGPR_OK) return 0;
+  return 256 + lay_out(p, backward != 0, nullptr, nullptr);
+}
+
+int nugpr_selective_scan_forward(const nugpr_selective_scan* p, const nugpr_rows* x, const nugpr_rows* dt, const nugpr_heads* B, const nugpr_heads* C,
+                                 const nugpr_rows* z, const float* initial_state, const nugpr_rows* y, float* final_state, void* stream) {
+  NUGPR_TRY(check(p));
+  bool done;
+  NUGPR_TRY(check_call(p, false, &done));
+  if (done) return NUGPR_OK;
+  const size_t v = value_size(p);
+  ScanArgs a = scan_args(p);
+  if (p->n_rows > 0) {
+    NUGPR_TRY(check_rows(x, "x", v));
+    NUGPR_TRY(check_rows(dt, "dt", v));
+    NUGPR_TRY(check_heads(B, "B", v));
+    NUGPR_TRY(check_heads(C, "C", v));
+    if (z) NUGPR_TRY(check_rows(z, "z", v));
+    NUGPR_TRY(check_rows(y, "y", v));
+    a.x = x->data; a.x_row = x->row_stride;
+    a.dt = dt->data; a.dt_row = dt->row_stride;
+    a.B = B->data; a.B_row = B->row_stride; a.B_head = B->head_stride;
+    a.C = C->data; a.C_row = C->row_stride; a.C_head = C->head_stride;
+    if (z) { a.z = z->data; a.z_row = z->row_stride; }
+    a.y = y->data; a.y_row = y->row_stride;
+  }
+  NUGPR_TRY(check_floats(initial_state, "initial_state", false));
+  NUGPR_TRY(check_floats(final_state, "final_state", false));
+  if (overlap(initial_state, final_state, (size_t)p->n_seqs * p->dim * p->dim_state * sizeof(float))) return invalid("final_state overlaps initial_state");
+  a.s_in = initial_state; a.s_out = final_state;
+  lay_out(p, false, p->workspace, &a);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (p->dtype == NUGPR_BFLOAT16) launch_forward<Bf16>(p, a, s);
+  else launch_forward<F32>(p, a, s);
+  NUGPR_HIP(hipGetLastError());
+  return NUGPR_OK;
+}
+
+int nugpr_selective_scan_backward(const nugpr_selective_scan* p, const nugpr_rows* x, const nugpr_rows* dt, const nugpr_heads* B, const nugpr_heads* C,
+                                  const nugpr_rows* z, const float* initial_state, const nugpr_rows* d_y, const float* d_final_state, const nugpr_rows* dx,
+                                  const nugpr_rows* ddt, const nugpr_heads* dB, const nugpr_heads* dC, const nugpr_rows* dz, float* dA, float* dD,
+                                  float* ddt_bias, float* d_initial_state, void* stream) {
+  NUGPR_TRY(check(p));
+  bool done;
+  NUGPR_TRY(check_call(p, true, &done));
+  const size_t v = value_size(p);
+  NUGPR_TRY(check_floats(dA, "dA", true));
+  NUGPR_TRY(check_floats(dD, "dD", p->D != nullptr));
+  NUGPR_TRY(check_floats(ddt_bias, "ddt_bias", p->dt_bias != nullptr));
+  NUGPR_TRY(check_floats(initial_state, "initial_state", false));
+  NUGPR_TRY(check_floats(d_final_state, "d_final_state", false));
+  NUGPR_TRY(check_floats(d_initial_state, "d_initial_state", false));
+  if (overlap(d_final_state, d_initial_state, (size_t)p->n_seqs * p->dim * p->dim_state * sizeof(float))) return invalid("d_initial_state overlaps d_final_state");
+  ScanArgs a = scan_args(p);
+  if (p->n_rows > 0) {
+    NUGPR_TRY(check_rows(x, "x", v));
+    NUGPR_TRY(check_rows(dt, "dt", v));
+    NUGPR_TRY(check_heads(B, "B", v));
+    NUGPR_TRY(check_heads(C, "C", v));
+    NUGPR_TRY(check_rows(d_y, "d_y", v));
+    NUGPR_TRY(check_rows(dx, "dx", v));
+    NUGPR_TRY(check_rows(ddt, "ddt", v));
+    NUGPR_TRY(check_heads(dB, "dB", v));
+    NUGPR_TRY(check_heads(dC, "dC", v));
+    if (z) {
+      NUGPR_TRY(check_rows(z, "z", v));
+      NUGPR_TRY(check_rows(dz, "dz", v));
+      a.z = z->data; a.z_row = z->row_stride; a.dz = dz->data; a.dz_row = dz->row_stride;
+    }
+    a.x = x->data; a.x_row = x->row_stride;
+    a.dt = dt->data; a.dt_row = dt->row_stride;
+    a.B = B->data; a.B_row = B->row_stride; a.B_head = B->head_stride;
+    a.C = C->data; a.C_row = C->row_stride; a.C_head = C->head_stride;
+    a.dy = d_y->data; a.dy_row = d_y->row_stride;
+    a.dx = dx->data; a.dx_row = dx->row_stride;
+    a.ddt = ddt->data; a.ddt_row = ddt->row_stride;
+  }
+  a.s_in = initial_state; a.ds_end = d_final_state; a.ds_in = d_initial_state;
+  lay_out(p, true, p->workspace, &a);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (done) {                                      // no rows, no sequences: the sums are zero
+    a.items = 0;
+    hipLaunchKernelGGL(k_scan_sum_items, dim3((unsigned)(((int64_t)p->dim * p->dim_state + 63) / 64), 3), dim3(256), 0, s, a, dA, p->D ? dD : nullptr,
+                       p->dt_bias ? ddt_bias : nullptr);
+  } else if (p->dtype == NUGPR_BFLOAT16) {
+    launch_backward<Bf16>(p, a, dB, dC, dA, dD, ddt_bias, s);
+  } else {
+    launch_backward<F32>(p, a, dB, dC, dA, dD, ddt_bias, s);
+  }
+  NUGPR_HIP(hipGetLastError());
+  return NUGPR_OK;
+}
+
+int nugpr_selective_scan_step(const nugpr_selective_scan* p, const nugpr_rows* x, const nugpr_rows* dt, const nugpr_heads* B, const nugpr_heads* C,
+                              const nugpr_rows* z, float* state, const int32_t* slots, const nugpr_rows* y, void* stream) {
+  NUGPR_TRY(check(p));
+  if (p->n_rows == 0) return NUGPR_OK;
+  const size_t v = value_size(p);
+  NUGPR_TRY(check_floats(p->A, "A", true));
+  NUGPR_TRY(check_floats(p->D, "D", false));
+  NUGPR_TRY(check_floats(p->dt_bias, "dt_bias", false));
+  NUGPR_TRY(check_floats(state, "state", p->n_seqs > 0));
+  NUGPR_TRY(check_rows(x, "x", v));
+  NUGPR_TRY(check_rows(dt, "dt", v));
+  NUGPR_TRY(check_heads(B, "B", v));
+  NUGPR_TRY(check_heads(C, "C", v));
+  if (z) NUGPR_TRY(check_rows(z, "z", v));
+  NUGPR_TRY(check_rows(y, "y", v));
+  if (!slots && p->n_rows > p->n_seqs) return invalid("more requests than states");
+  ScanStepArgs a{};
+  a.x = x->data; a.x_row = x->row_stride;
+  a.dt = dt->data; a.dt_row = dt->row_stride;
+  a.B = B->data; a.B_row = B->row_stride; a.B_head = B->head_stride;
+  a.C = C->data; a.C_row = C->row_stride; a.C_head = C->head_stride;
+  if (z) { a.z = z->data; a.z_row = z->row_stride; }
+  a.y = y->data; a.y_row = y->row_stride;
+  a.A = p->A; a.D = p->D; a.bias = p->dt_bias; a.state = state; a.slots = slots; a.n_states = p->n_seqs;
+  a.dim = p->dim; a.each = p->dim / p->groups; a.states = p->dim_state; a.softplus = p->softplus != 0;
+  const int lanes = p->dim_state > 32 ? 16 : waves_of(p);
+  a.col_blocks = (p->dim * lanes + 255) / 256;
+  const int64_t grid = p->n_rows * a.col_blocks;
+  if (grid > (int64_t)0xffffffff / 256) return invalid("too many requests and channels for one call");
+  const bool wide = p->dim_state % PER == 0;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const dim3 blocks((unsigned)grid), threads(256);
+  auto launch = [&](auto l) {
+    constexpr int L = decltype(l)::value;
+    if (p->dtype == NUGPR_BFLOAT16) {
+      if (wide) hipLaunchKernelGGL((k_scan_step<Bf16, L, true>), blocks, threads, 0, s, a);
+      else hipLaunchKernelGGL((k_scan_step<Bf16, L, false>), blocks, threads, 0, s, a);
+    } else {
+      if (wide) hipLaunchKernelGGL((k_scan_step<F32, L, true>), blocks, threads, 0, s, a);
+      else hipLaunchKernelGGL((k_scan_step<F32, L, false>), blocks, threads, 0, s, a);
+    }
+  };
+  switch (lanes) {
+    case 1: launch(std::integral_constant<int, 1>{}); break;
+    case 2: launch(std::integral_constant<int, 2>{}); break;
+    case 4: launch(std::integral_constant<int, 4>{}); break;
+    case 8: launch(std::integral_constant<int, 8>{}); break;
+    default: launch(std::integral_constant<int, 16>{}); break;
+  }
+  NUGPR_HIP(hipGetLastError());
+  return NUGPR_OK;
+}
+
+}  // extern "C"

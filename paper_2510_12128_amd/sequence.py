@@ -9,8 +9,8 @@ import ctypes as C
 
 import torch
 
-from .binding import (Adapter, DecayAttention, Heads, NUGPR_BFLOAT16, NUGPR_ERR_INVALID, NUGPR_FLOAT32, NugprError,
-                      _check, load_library)
+from .binding import (Adapter, DecayAttention, Gradient, Heads, NUGPR_BFLOAT16, NUGPR_ERR_INVALID, NUGPR_FLOAT32,
+                      NugprError, Rows, SelectiveScan, ShortConv, _check, load_library)
 
 _TYPES = {torch.float32: NUGPR_FLOAT32, torch.bfloat16: NUGPR_BFLOAT16}
 _byref = C.byref
@@ -220,3 +220,241 @@ def nugpr_adapter_backward(x, W, A, B, seq_offsets, d_y, adapter_of=None, scale=
     _call(lib.nugpr_adapter_backward, device, _byref(p), x.data_ptr(), _rows(x, "x"), d_y.data_ptr(), _rows(d_y, "d_y"),
           dx.data_ptr(), dA.data_ptr(), dB.data_ptr())
     return dx, dA, dB
+
+
+def _rows2(t, name, device, dtype, shape):
+    """A rows x width array of that device, type and shape, with its last dimension contiguous."""
+    _like(t, name, device, dtype, shape)
+    return _byref(Rows(t.data_ptr(), _rows(t, name)))
+
+
+def _none(t, name, device, dtype, shape):
+    """Address of an array that may be left out."""
+    return None if t is None else _dense(t, name, device, dtype, shape)
+
+
+def _refuse_if_recorded(**tensors):
+    if _recording():
+        _refuse_recorded(**tensors)
+
+
+def _conv(x, weight, bias, silu, n_seqs, offsets):
+    """The problem's structure, without workspace; device, type and the shape of the sequences' windows."""
+    device, dtype = _first(x, "x", 2)
+    if weight.dim() != 2:
+        _refuse("weight must be dim x width")
+    n, dim = x.shape
+    width = weight.shape[1]
+    w = _dense(weight, "weight", device, dtype, (dim, width))
+    b = _none(bias, "bias", device, dtype, (dim,))
+    return (ShortConv(_TYPES[dtype], dim, width, 1 if silu else 0, n, n_seqs, offsets, w, b, None, 0), device, dtype,
+            (n_seqs, max(width - 1, 0), dim))
+
+
+def nugpr_short_conv_forward(x, weight, seq_offsets, bias=None, silu=False, initial_state=None):
+    """Causal convolution along packed sequences, each channel by itself, with bias and x sigmoid(x) behind it where given.
+
+    x (rows, dim), weight (dim, width), bias (dim,) or None: float32 or bfloat16; the last column of weight is the row's own;
+    seq_offsets (n_seqs + 1,) int64; initial_state (n_seqs, width - 1, dim), the rows before each sequence, oldest first, or
+    None: zero.  Returns y (rows, dim) and the last rows of the sequences, for a call that goes on."""
+    lib = load_library()
+    _refuse_if_recorded(x=x, weight=weight, bias=bias, initial_state=initial_state)
+    p, device, dtype, shape = _conv(x, weight, bias, silu, *_offsets(seq_offsets, x.device))
+    s0 = _none(initial_state, "initial_state", device, dtype, shape)
+    y = torch.empty(x.shape, dtype=dtype, device=device)
+    s1 = torch.empty(shape, dtype=dtype, device=device)
+    _call(lib.nugpr_short_conv_forward, device, _byref(p), _rows2(x, "x", device, dtype, x.shape), s0,
+          _rows2(y, "y", device, dtype, x.shape), s1.data_ptr())
+    return y, s1
+
+
+def nugpr_short_conv_backward(x, weight, seq_offsets, d_y, bias=None, silu=False, initial_state=None, d_final_state=None):
+    """Gradients of nugpr_short_conv_forward's x, weight, bias (None without one) and initial state, in their type, from d_y
+    and, unless None, d_final_state."""
+    lib = load_library()
+    _refuse_if_recorded(x=x, weight=weight, bias=bias, d_y=d_y, initial_state=initial_state, d_final_state=d_final_state)
+    p, device, dtype, shape = _conv(x, weight, bias, silu, *_offsets(seq_offsets, x.device))
+    s0 = _none(initial_state, "initial_state", device, dtype, shape)
+    s1 = _none(d_final_state, "d_final_state", device, dtype, shape)
+    need = lib.nugpr_short_conv_workspace_bytes(_byref(p))
+    if need == 0:
+        raise NugprError(NUGPR_ERR_INVALID, lib.nugpr_last_error_string().decode())
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    p.workspace, p.workspace_bytes = ws.data_ptr(), need
+    dx, dw = torch.empty(x.shape, dtype=dtype, device=device), torch.empty_like(weight)
+    db = None if bias is None else torch.empty_like(bias)
+    ds = torch.empty(shape, dtype=dtype, device=device)
+    _call(lib.nugpr_short_conv_backward, device, _byref(p), _rows2(x, "x", device, dtype, x.shape), s0,
+          _rows2(d_y, "d_y", device, dtype, x.shape), s1, _rows2(dx, "dx", device, dtype, x.shape), dw.data_ptr(),
+          None if db is None else db.data_ptr(), ds.data_ptr())
+    return dx, dw, db, ds
+
+
+def nugpr_short_conv_step(x, weight, state, slots=None, bias=None, silu=False):
+    """One token for each request: x (requests, dim); state (n_states, width - 1, dim), of x's type, moves on by a row in
+    place, request b's at slots[b] (int32; None: b).  Returns y (requests, dim)."""
+    lib = load_library()
+    _refuse_if_recorded(x=x, weight=weight, bias=bias, state=state)
+    p, device, dtype, shape = _conv(x, weight, bias, silu, state.shape[0] if state.dim() else 0, None)
+    st = _dense(state, "state", device, dtype, shape)
+    at = _none(slots, "slots", device, torch.int32, (x.shape[0],))
+    y = torch.empty(x.shape, dtype=dtype, device=device)
+    _call(lib.nugpr_short_conv_step, device, _byref(p), _rows2(x, "x", device, dtype, x.shape), st, at,
+          _rows2(y, "y", device, dtype, x.shape))
+    _written(state)
+    return y
+
+
+def _scan(x, dt, A, B, C, D, z, dt_bias, softplus, n_seqs, offsets):
+    """The problem's structure, without workspace; device, type, the shape of the sequences' states, and the arrays x, dt, B,
+    C and z as the calls take them."""
+    device, dtype = _first(x, "x", 2)
+    if A.dim() != 2 or B.dim() != 3:
+        _refuse("A must be dim x dim_state, B and C rows x groups x dim_state")
+    n, dim = x.shape
+    groups, states = B.shape[1], A.shape[1]
+    _like(dt, "dt", device, dtype, x.shape)
+    _like(B, "B", device, dtype, (n, groups, states))
+    _like(C, "C", device, dtype, (n, groups, states))
+    a = _dense(A, "A", device, torch.float32, (dim, states))
+    d = _none(D, "D", device, torch.float32, (dim,))
+    bias = _none(dt_bias, "dt_bias", device, torch.float32, (dim,))
+    p = SelectiveScan(_TYPES[dtype], dim, groups, states, 1 if softplus else 0, n, n_seqs, offsets, a, d, bias, None, 0)
+    arrays = (_rows2(x, "x", device, dtype, x.shape), _rows2(dt, "dt", device, dtype, x.shape), _heads(B, "B"),
+              _heads(C, "C"), None if z is None else _rows2(z, "z", device, dtype, x.shape))
+    return p, device, dtype, (n_seqs, dim, states), arrays
+
+
+def nugpr_selective_scan_forward(x, dt, A, B, C, seq_offsets, D=None, z=None, dt_bias=None, softplus=True,
+                                 initial_state=None):
+    """State space layer whose decay depends on the token, over packed sequences: with d = softplus(dt + dt_bias) (without
+    `softplus`: dt + dt_bias), h_t = exp(d_t A) h_t-1 + d_t x_t B_t for each channel, y_t = (C_t . h_t + D x_t) silu(z_t).
+
+    x, dt, z (rows, dim), B, C (rows, groups, dim_state): float32 or bfloat16, channels in `groups` equal groups; A (dim,
+    dim_state), <= 0, D and dt_bias (dim,): float32; z, D and dt_bias may be None; seq_offsets (n_seqs + 1,) int64, n_seqs at
+    least 1 where there are rows; initial_state (n_seqs, dim, dim_state) float32 or None.  Returns y (rows, dim) and the
+    sequences' end states, float32."""
+    lib = load_library()
+    _refuse_if_recorded(x=x, dt=dt, A=A, B=B, C=C, D=D, z=z, dt_bias=dt_bias, initial_state=initial_state)
+    p, device, dtype, shape, arrays = _scan(x, dt, A, B, C, D, z, dt_bias, softplus, *_offsets(seq_offsets, x.device))
+    ws = _scratch(lib, lib.nugpr_selective_scan_workspace_bytes, p, 0, device)  # noqa: F841
+    s0 = _none(initial_state, "initial_state", device, torch.float32, shape)
+    y = torch.empty(x.shape, dtype=dtype, device=device)
+    s1 = torch.empty(shape, dtype=torch.float32, device=device)
+    _call(lib.nugpr_selective_scan_forward, device, _byref(p), *arrays, s0, _rows2(y, "y", device, dtype, x.shape),
+          s1.data_ptr())
+    return y, s1
+
+
+def nugpr_selective_scan_backward(x, dt, A, B, C, seq_offsets, d_y, D=None, z=None, dt_bias=None, softplus=True,
+                                  initial_state=None, d_final_state=None):
+    """Gradients of nugpr_selective_scan_forward's x, dt, A, B, C, D, z, dt_bias and initial state, in this order and in their
+    types (None for D, z and dt_bias that are None), from d_y and, unless None, d_final_state."""
+    lib = load_library()
+    _refuse_if_recorded(x=x, dt=dt, A=A, B=B, C=C, d_y=d_y, D=D, z=z, dt_bias=dt_bias, initial_state=initial_state,
+                        d_final_state=d_final_state)
+    p, device, dtype, shape, arrays = _scan(x, dt, A, B, C, D, z, dt_bias, softplus, *_offsets(seq_offsets, x.device))
+    ws = _scratch(lib, lib.nugpr_selective_scan_workspace_bytes, p, 1, device)  # noqa: F841
+    s0 = _none(initial_state, "initial_state", device, torch.float32, shape)
+    s1 = _none(d_final_state, "d_final_state", device, torch.float32, shape)
+    dx, ddt = (torch.empty(x.shape, dtype=dtype, device=device) for _ in range(2))
+    dB, dC = (torch.empty(B.shape, dtype=dtype, device=device) for _ in range(2))
+    dz = None if z is None else torch.empty(x.shape, dtype=dtype, device=device)
+    dA = torch.empty_like(A)
+    dD, dbias = (None if t is None else torch.empty_like(t) for t in (D, dt_bias))
+    ds = torch.empty(shape, dtype=torch.float32, device=device)
+
+    def rows(t, name):
+        return None if t is None else _rows2(t, name, device, dtype, x.shape)
+
+    _call(lib.nugpr_selective_scan_backward, device, _byref(p), *arrays, s0, rows(d_y, "d_y"), s1, rows(dx, "dx"),
+          rows(ddt, "ddt"), _heads(dB, "dB"), _heads(dC, "dC"), rows(dz, "dz"), dA.data_ptr(),
+          None if dD is None else dD.data_ptr(), None if dbias is None else dbias.data_ptr(), ds.data_ptr())
+    return dx, ddt, dA, dB, dC, dD, dz, dbias, ds
+
+
+def nugpr_selective_scan_step(x, dt, A, B, C, state, slots=None, D=None, z=None, dt_bias=None, softplus=True):
+    """One token for each request: x, dt, z (requests, dim), B, C (requests, groups, dim_state); state (n_states, dim,
+    dim_state) float32 is advanced in place, request b's at slots[b] (int32; None: b).  Returns y (requests, dim)."""
+    lib = load_library()
+    _refuse_if_recorded(x=x, dt=dt, A=A, B=B, C=C, D=D, z=z, dt_bias=dt_bias, state=state)
+    p, device, dtype, shape, arrays = _scan(x, dt, A, B, C, D, z, dt_bias, softplus,
+                                            state.shape[0] if state.dim() else 0, None)
+    st = _dense(state, "state", device, torch.float32, shape)
+    at = _none(slots, "slots", device, torch.int32, (x.shape[0],))
+    y = torch.empty(x.shape, dtype=dtype, device=device)
+    _call(lib.nugpr_selective_scan_step, device, _byref(p), *arrays, st, at, _rows2(y, "y", device, dtype, x.shape))
+    _written(state)
+    return y
+
+
+def _in_one_piece(t):
+    """Whether the values of a tensor fill one run of memory, in any order of its dimensions."""
+    if t.is_contiguous():
+        return True
+    expected = 1
+    for stride, size in sorted((st, si) for st, si in zip(t.stride(), t.shape) if si != 1):
+        if stride != expected:
+            return False
+        expected *= size
+    return True
+
+
+def _gradients(grads, out):
+    """The tensors as an array of the structure, and their device."""
+    grads = list(grads)
+    if not grads:
+        _refuse("there is no gradient")
+    device = grads[0].device
+    if device.type != "cuda":
+        _refuse("gradients must be on a GPU")
+    to = [None] * len(grads) if out is None else list(out)
+    if len(to) != len(grads):
+        _refuse("out must have as many tensors as there are gradients")
+    table = (Gradient * len(grads))()
+    for i, (g, o) in enumerate(zip(grads, to)):
+        if g.device != device or g.dtype not in _TYPES or not _in_one_piece(g):
+            _refuse(f"gradient {i} must be on {device}, float32 or bfloat16, and fill one run of memory")
+        if o is None:
+            table[i] = (g.data_ptr(), None, g.numel(), _TYPES[g.dtype], 0)
+            continue
+        if o.device != device or o.dtype not in _TYPES or o.shape != g.shape or (o.stride() != g.stride() and g.numel()):
+            _refuse(f"out {i} must be on {device}, float32 or bfloat16, with the gradient's shape and strides")
+        table[i] = (g.data_ptr(), o.data_ptr(), g.numel(), _TYPES[g.dtype], _TYPES[o.dtype])
+    return grads, to, table, device
+
+
+def _norm_call(lib, call, table, device, *args):
+    need = lib.nugpr_gradient_norm_workspace_bytes(table, len(table))
+    if need == 0:
+        raise NugprError(NUGPR_ERR_INVALID, lib.nugpr_last_error_string().decode())
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    _call(call, device, table, len(table), *args, norm.data_ptr(), ws.data_ptr(), need)
+    return norm
+
+
+def nugpr_gradient_norm(grads):
+    """The 2-norm of all values of the tensors in `grads` (float32 or bfloat16, on one GPU, any of them of either type), as a
+    float32 tensor without dimensions."""
+    lib = load_library()
+    grads, _, table, device = _gradients(grads, None)
+    if _recording():
+        for i, g in enumerate(grads):
+            if g.requires_grad:
+                _refuse(f"gradient {i} requires a gradient itself, which autograd does not get through this call")
+    return _norm_call(lib, lib.nugpr_gradient_norm, table, device)
+
+
+def nugpr_clip_gradients(grads, max_norm, out=None):
+    """The same, and multiplies every value by min(1, max_norm / norm): in place, or into the tensors in `out` (of the
+    gradients' shapes and strides, float32 or bfloat16).  No tensor that is written may share memory with another."""
+    lib = load_library()
+    grads, to, table, device = _gradients(grads, out)
+    if _recording():
+        for i, g in enumerate(grads):
+            if g.requires_grad or (to[i] is not None and to[i].requires_grad):
+                _refuse(f"gradient {i} requires a gradient itself, which autograd does not get through this call")
+    norm = _norm_call(lib, lib.nugpr_clip_gradients, table, device, float(max_norm))
+    _written(grads if out is None else to)
+    return norm
