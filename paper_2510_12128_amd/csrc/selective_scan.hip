@@ -30,7 +30,7 @@ namespace {
 
 constexpr int TILE_ROWS = 16;
 constexpr int CH = 64;               // channels of a workgroup
-constexpr int PER = 4;               // states of a wave
+constexpr int PER = 4;               // states of a wave, at most
 constexpr int ZERO_GROUPS = 128;     // workgroups that clear the rows without a sequence
 
 struct ScanArgs {
@@ -44,6 +44,7 @@ struct ScanArgs {
   const int64_t* off;
   int64_t n_rows;
   int n_seqs, dim, groups, each, blocks, states, softplus;     // each: channels of a group; blocks: of CH channels, all groups
+  int share;                         // states of a wave (of each chunk): as even as they can be shared out
   int span_log2, items;
   float* adds;                       // items x dim x states: what a span adds to the state, then its start state
   float* steps;                      // items x dim: sum of a span's d
@@ -56,7 +57,7 @@ struct ScanArgs {
 
 // Value I of those that 16 consecutive lanes hold.  (No instruction of its own: the one that uses it reads its operand so.)
 template <int I>
-__device__ inline float from_lane(float v) {
+__device__ __forceinline__ float from_lane(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x150 + I, 0xf, 0xf, true));
 }
 
@@ -69,7 +70,7 @@ struct Place {
   bool last;                         // the sequence ends with it
 };
 
-__device__ inline bool find(const ScanArgs& a, int item, int block, Place& p) {
+__device__ __forceinline__ bool find(const ScanArgs& a, int item, int block, Place& p) {
   const int of_group = a.blocks / a.groups, b = block % of_group;
   p.group = block / of_group;
   p.channel = p.group * a.each + b * CH;
@@ -102,9 +103,9 @@ struct Incoming {
     const int br = threadIdx.x / (PER * WAVES);
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) {
-      const int n = k * PER * WAVES + threadIdx.x % (PER * WAVES);
+      const int s = threadIdx.x % PER, n = (k * WAVES + threadIdx.x % (PER * WAVES) / PER) * a.share + s;
       b[k] = c[k] = 0.f;
-      if (live && br < n_rows && n < a.states) {
+      if (live && br < n_rows && s < a.share && n < a.states) {
         b[k] = TR::get(static_cast<const T*>(a.B)[(row0 + br) * a.B_row + p.group * a.B_head + n]);
         c[k] = TR::get(static_cast<const T*>(a.C)[(row0 + br) * a.C_row + p.group * a.C_head + n]);
       }
@@ -114,13 +115,13 @@ struct Incoming {
 
 // f(0), f(1), ..: with the number as a constant
 template <class F, int... I>
-__device__ inline void repeat_all(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+__device__ __forceinline__ void repeat_all(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
 template <int N, class F>
-__device__ inline void repeat(F f) { repeat_all(f, std::make_integer_sequence<int, N>{}); }
+__device__ __forceinline__ void repeat(F f) { repeat_all(f, std::make_integer_sequence<int, N>{}); }
 
 // Sum over the waves' parts.
 template <int V>
-__device__ inline void gather(const float (*part)[TILE_ROWS][CH], int waves, int r, int col, float (&out)[V]) {
+__device__ __forceinline__ void gather(const float (*part)[TILE_ROWS][CH], int waves, int r, int col, float (&out)[V]) {
 #pragma unroll
   for (int j = 0; j < V; ++j) out[j] = part[0][r][col + j];
   for (int w = 1; w < waves; ++w)
@@ -128,11 +129,11 @@ __device__ inline void gather(const float (*part)[TILE_ROWS][CH], int waves, int
     for (int j = 0; j < V; ++j) out[j] += part[w][r][col + j];
 }
 
-__device__ inline void load_states(float (&h)[PER], const float* from, int n) {
+__device__ __forceinline__ void load_states(float (&h)[PER], const float* from, int n) {
 #pragma unroll
   for (int s = 0; s < PER; ++s) h[s] = s < n ? from[s] : 0.f;
 }
-__device__ inline void store_states(const float (&h)[PER], float* to, int n) {
+__device__ __forceinline__ void store_states(const float (&h)[PER], float* to, int n) {
 #pragma unroll
   for (int s = 0; s < PER; ++s)
     if (s < n) to[s] = h[s];
@@ -143,16 +144,16 @@ template <int WAVES, int CHUNKS>
 struct States {
   float v[CHUNKS][PER];
   // the wave's number of chunk k's
-  static __device__ int count(const ScanArgs& a, int wave, int k) { return min(PER, a.states - (k * WAVES + wave) * PER); }
+  static __device__ int count(const ScanArgs& a, int wave, int k) { return min(a.share, a.states - (k * WAVES + wave) * a.share); }
   // from (or to) those of the lane's channel in an array channels x states, where live
   __device__ void load(const ScanArgs& a, const float* from, int wave, bool live) {
 #pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) load_states(v[k], from + (k * WAVES + wave) * PER, live ? count(a, wave, k) : 0);
+    for (int k = 0; k < CHUNKS; ++k) load_states(v[k], from + (k * WAVES + wave) * a.share, live ? count(a, wave, k) : 0);
   }
   __device__ void store(const ScanArgs& a, float* to, int wave, bool live) const {
     if (!live) return;
 #pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) store_states(v[k], to + (k * WAVES + wave) * PER, count(a, wave, k));
+    for (int k = 0; k < CHUNKS; ++k) store_states(v[k], to + (k * WAVES + wave) * a.share, count(a, wave, k));
   }
   __device__ void fill(float x) {
 #pragma unroll
@@ -170,7 +171,7 @@ struct States {
 
 // One number a channel for the V channels of a thread.
 template <int V>
-__device__ inline void load_channels(float (&v)[V], const float* p, int channel, int col, int valid) {
+__device__ __forceinline__ void load_channels(float (&v)[V], const float* p, int channel, int col, int valid) {
 #pragma unroll
   for (int j = 0; j < V; ++j) v[j] = p && col + j < valid ? p[channel + col + j] : 0.f;
 }
@@ -184,10 +185,10 @@ struct Tile {
 };
 
 // Makes a tile's rows from what came in.  Rows and channels that there are not: d = u = 0, which leaves a state as it is.  steps: sums
-// of d, a row of every tile a thread.
+// of d, a row of every tile a thread; bias: of the thread's channels.
 template <class TR, int WAVES, int CHUNKS, bool GRADIENT>
-__device__ inline void fill_tile(Tile<WAVES, CHUNKS, GRADIENT>& tile, const ScanArgs& a, const Incoming<TR, WAVES, CHUNKS, GRADIENT>& in, int n_rows,
-                                 int valid, const float (&bias)[TILE_ROWS / WAVES], float (&steps)[TILE_ROWS / WAVES]) {
+__device__ __forceinline__ void fill_tile(Tile<WAVES, CHUNKS, GRADIENT>& tile, const ScanArgs& a, const Incoming<TR, WAVES, CHUNKS, GRADIENT>& in, int n_rows,
+                                 int valid, const float* bias, float (&steps)[TILE_ROWS / WAVES]) {
   constexpr int V = TILE_ROWS / WAVES;
   const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
 #pragma unroll
@@ -212,7 +213,7 @@ __device__ inline void fill_tile(Tile<WAVES, CHUNKS, GRADIENT>& tile, const Scan
 
 // Sum over the rows of a tile's threads, of `steps` and the like; out[CH] in LDS.  (All threads.)
 template <int V>
-__device__ inline void sum_rows(float (&v)[V], float (*part)[CH], float* to, int valid) {
+__device__ __forceinline__ void sum_rows(float (&v)[V], float (*part)[CH], float* to, int valid) {
   const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
   __syncthreads();
 #pragma unroll
@@ -228,15 +229,15 @@ __device__ inline void sum_rows(float (&v)[V], float (*part)[CH], float* to, int
 
 // A wave's N states of chunk `k` over one tile; its part of y is stored where OUT, beside that of the chunks before.
 template <int N, bool OUT, class T>
-__device__ inline void walk_tile(float (&h)[PER], const float (&a2)[PER], const T& tile, int k, int wave, int lane, float (*part)[CH]) {
+__device__ __forceinline__ void walk_tile(float (&h)[PER], const float (&a2)[PER], const T& tile, int k, int wave, int lane, float (*part)[CH]) {
   const int row = (lane & 15) / PER, n = wave * PER + lane % PER;
-  repeat<TILE_ROWS / 4>([&](auto q) {
+  repeat<TILE_ROWS / 4>([&](auto q) __attribute__((always_inline)) {
     const float vb = tile.B[k][4 * q + row][n], vc = OUT ? tile.C[k][4 * q + row][n] : 0.f;
-    repeat<4>([&](auto i) {
+    repeat<4>([&](auto i) __attribute__((always_inline)) {
       constexpr int t = 4 * q + i;
       const float2 du = tile.du[t][lane];
       float y = 0.f;
-      repeat<N>([&](auto s) {
+      repeat<N>([&](auto s) __attribute__((always_inline)) {
         constexpr int at = PER * i + s;
         h[s] = fmaf(exp2_of(du.x * a2[s]), h[s], du.y * from_lane<at>(vb));
         if constexpr (OUT) y = s == 0 ? from_lane<at>(vc) * h[s] : fmaf(from_lane<at>(vc), h[s], y);
@@ -248,16 +249,16 @@ __device__ inline void walk_tile(float (&h)[PER], const float (&a2)[PER], const 
 
 // The same without output, and the product of the factors so far, and what e C adds to the gradient by the state before the tile's rows.
 template <int N, class T>
-__device__ inline void walk_tile_back(float (&h)[PER], float (&product)[PER], float (&g)[PER], const float (&a2)[PER], const T& tile, int k, int wave,
+__device__ __forceinline__ void walk_tile_back(float (&h)[PER], float (&product)[PER], float (&g)[PER], const float (&a2)[PER], const T& tile, int k, int wave,
                                       int lane) {
   const int row = (lane & 15) / PER, n = wave * PER + lane % PER;
-  repeat<TILE_ROWS / 4>([&](auto q) {
+  repeat<TILE_ROWS / 4>([&](auto q) __attribute__((always_inline)) {
     const float vb = tile.B[k][4 * q + row][n], vc = tile.C[k][4 * q + row][n];
-    repeat<4>([&](auto i) {
+    repeat<4>([&](auto i) __attribute__((always_inline)) {
       constexpr int t = 4 * q + i;
       const float2 du = tile.du[t][lane];
       const float e = tile.e[t][lane];
-      repeat<N>([&](auto s) {
+      repeat<N>([&](auto s) __attribute__((always_inline)) {
         constexpr int at = PER * i + s;
         const float f = exp2_of(du.x * a2[s]);
         h[s] = fmaf(f, h[s], du.y * from_lane<at>(vb));
@@ -270,8 +271,8 @@ __device__ inline void walk_tile_back(float (&h)[PER], float (&product)[PER], fl
 
 // For every chunk: f(the chunk, the number of the wave's states in it, as a constant); full: all have PER.
 template <int WAVES, int CHUNKS, bool FULL, class F>
-__device__ inline void with_states(const ScanArgs& a, int wave, F f) {
-  repeat<CHUNKS>([&](auto k) {
+__device__ __forceinline__ void with_states(const ScanArgs& a, int wave, F f) {
+  repeat<CHUNKS>([&](auto k) __attribute__((always_inline)) {
     if constexpr (FULL) {
       f(k, std::integral_constant<int, PER>{});
     } else {
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_scan(const ScanArgs a) {
   Place p;
   if (!find(a, item, block, p) || (ADDS && p.last)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int waves = min(WAVES, (a.states + PER - 1) / PER);      // (those that have states)
+  const int waves = min(WAVES, (a.states + a.share - 1) / a.share);      // (those that have states)
   const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
   const bool live = lane < p.valid;
   const int64_t of_lane = (int64_t)(p.channel + lane) * a.states, each = (int64_t)a.dim * a.states;
@@ -336,7 +337,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_scan(const ScanArgs a) {
     __syncthreads();
     const int64_t next = t0 + TILE_ROWS;
     in.load(a, p, next, (int)min((int64_t)TILE_ROWS, p.to - next), next < p.to);
-    with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) {
+    with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) __attribute__((always_inline)) {
       walk_tile<decltype(n)::value, !ADDS>(h.v[k], a2.v[k], tile, k, wave, lane, part[ADDS ? 0 : wave]);
     });
     if constexpr (!ADDS) {
@@ -418,7 +419,7 @@ __global__ __launch_bounds__(256) void k_scan_join(const ScanArgs a) {
 }
 
 // ---- gradients ------------------------------------------------------------------------------------------------------------
-__device__ inline int64_t first_tile(const Place& p) { return p.piece.lo / TILE_ROWS + p.piece.seq + (p.from - p.piece.lo) / TILE_ROWS; }
+__device__ __forceinline__ int64_t first_tile(const Place& p) { return p.piece.lo / TILE_ROWS + p.piece.seq + (p.from - p.piece.lo) / TILE_ROWS; }
 
 // The states at the begin of every tile, what a span adds, and what it adds to the gradient by the state before it.
 template <class TR, int WAVES, int CHUNKS, bool FULL>
@@ -461,11 +462,11 @@ __global__ __launch_bounds__(64 * WAVES) void k_scan_tiles(const ScanArgs a) {
         a.tile_steps[number * a.dim + p.channel + lane] = passed;
         for (int t = 0; t < TILE_ROWS; ++t) passed += tile.du[t][lane].x;
       }
-      with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) {
+      with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) __attribute__((always_inline)) {
         walk_tile_back<decltype(n)::value>(h.v[k], product.v[k], g.v[k], a2.v[k], tile, k, wave, lane);
       });
     } else {
-      with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) {
+      with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) __attribute__((always_inline)) {
         walk_tile<decltype(n)::value, false>(h.v[k], a2.v[k], tile, k, wave, lane, part);
       });
     }
@@ -476,24 +477,24 @@ __global__ __launch_bounds__(64 * WAVES) void k_scan_tiles(const ScanArgs a) {
   sum_rows(steps, part, a.steps + (int64_t)item * a.dim + p.channel, p.valid);
 }
 
-__device__ inline void swap_halves(float& x, float& y) {
+__device__ __forceinline__ void swap_halves(float& x, float& y) {
   const auto v = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
   x = __builtin_bit_cast(float, (uint32_t)v[0]);
   y = __builtin_bit_cast(float, (uint32_t)v[1]);
 }
-__device__ inline void swap_rows(float& x, float& y) {
+__device__ __forceinline__ void swap_rows(float& x, float& y) {
   const auto v = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
   x = __builtin_bit_cast(float, (uint32_t)v[0]);
   y = __builtin_bit_cast(float, (uint32_t)v[1]);
 }
 template <int CTRL>
-__device__ inline float moved(float v) {
+__device__ __forceinline__ float moved(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
 
 // Sums over the wave's lanes of four rows x four states: lane l gets the one of row l / 16, state l % 16 / 4.  Two numbers are joined in one
 // register at each step, so that 16 sums take 35 instructions instead of 96.
-__device__ inline float lane_sums(float (&v)[4][PER], int lane) {
+__device__ __forceinline__ float lane_sums(float (&v)[4][PER], int lane) {
   float w[2][PER], z[PER];
 #pragma unroll
   for (int s = 0; s < PER; ++s) {
@@ -517,71 +518,75 @@ __device__ inline float lane_sums(float (&v)[4][PER], int lane) {
 
 // A wave's N states of chunk k over one tile: forward from its first states, then back.  The parts stand beside those of the chunks before;
 // dB, dC: of the tile's first row and the wave's first state, rows `stride` apart.
-template <int N, class T>
-__device__ inline void back_tile(float (&g)[PER], float (&dA)[PER], const float (&h0)[PER], const float (&a2)[PER], const T& tile, int k, int wave,
+template <int N, bool GATE, class T>
+__device__ __forceinline__ void back_tile(float (&g)[PER], float (&dA)[PER], const float (&h0)[PER], const float (&a2)[PER], const T& tile, int k, int wave,
                                  int lane, float (*part_u)[CH], float (*part_d)[CH], float (*part_y)[CH], float* dB, float* dC, int64_t stride,
                                  int rows) {
   const int row = (lane & 15) / PER, n = wave * PER + lane % PER;
-  float h[TILE_ROWS + 1][PER], f[TILE_ROWS][PER];
+  const int sum_row = lane / 16, sum_state = lane % 16 / 4;       // (of lane_sums)
+  float h[PER], f[TILE_ROWS][PER], kept[TILE_ROWS][PER];          // a_t, and a_t h_{t-1}
 #pragma unroll
-  for (int s = 0; s < PER; ++s) h[0][s] = h0[s];
-  repeat<TILE_ROWS / 4>([&](auto q) {
+  for (int s = 0; s < PER; ++s) h[s] = h0[s];
+  repeat<TILE_ROWS / 4>([&](auto q) __attribute__((always_inline)) {
     const float vb = tile.B[k][4 * q + row][n], vc = tile.C[k][4 * q + row][n];
-    repeat<4>([&](auto i) {
+    float sums[4][PER];
+    repeat<4>([&](auto i) __attribute__((always_inline)) {
       constexpr int t = 4 * q + i;
       const float2 du = tile.du[t][lane];
+      const float e = tile.e[t][lane];
       float y = 0.f;
-      repeat<N>([&](auto s) {
+#pragma unroll
+      for (int s = N; s < PER; ++s) sums[i][s] = 0.f;
+      repeat<N>([&](auto s) __attribute__((always_inline)) {
         constexpr int at = PER * i + s;
         f[t][s] = exp2_of(du.x * a2[s]);
-        h[t + 1][s] = fmaf(f[t][s], h[t][s], du.y * from_lane<at>(vb));
-        y = s == 0 ? from_lane<at>(vc) * h[t + 1][s] : fmaf(from_lane<at>(vc), h[t + 1][s], y);
+        kept[t][s] = f[t][s] * h[s];
+        h[s] = fmaf(du.y, from_lane<at>(vb), kept[t][s]);
+        if constexpr (GATE) y = s == 0 ? from_lane<at>(vc) * h[s] : fmaf(from_lane<at>(vc), h[s], y);
+        sums[i][s] = e * h[s];
       });
-      part_y[t][lane] = k ? part_y[t][lane] + y : y;
+      if constexpr (GATE) part_y[t][lane] = k ? part_y[t][lane] + y : y;
     });
+    const float c = lane_sums(sums, lane);
+    if (lane % 4 == 0 && 4 * q + sum_row < rows && sum_state < N) dC[(4 * q + sum_row) * stride + sum_state] = c;
     __builtin_amdgcn_sched_barrier(0);             // (what comes later is not read earlier: its registers are needed)
   });
-  repeat<TILE_ROWS / 4>([&](auto back) {
+  repeat<TILE_ROWS / 4>([&](auto back) __attribute__((always_inline)) {
     constexpr int q = TILE_ROWS / 4 - 1 - back;
     const float vb = tile.B[k][4 * q + row][n], vc = tile.C[k][4 * q + row][n];
-    float sb[4][PER], sc[4][PER];
-    repeat<4>([&](auto j) {
+    float sums[4][PER];
+    repeat<4>([&](auto j) __attribute__((always_inline)) {
       constexpr int i = 3 - j, t = 4 * q + i;
       const float2 du = tile.du[t][lane];
       const float e = tile.e[t][lane];
       float by_u = 0.f, by_d = 0.f;
 #pragma unroll
-      for (int s = N; s < PER; ++s) sb[i][s] = sc[i][s] = 0.f;
-      repeat<N>([&](auto s) {
+      for (int s = N; s < PER; ++s) sums[i][s] = 0.f;
+      repeat<N>([&](auto s) __attribute__((always_inline)) {
         constexpr int at = PER * i + s;
         g[s] = fmaf(e, from_lane<at>(vc), g[s]);
-        sb[i][s] = g[s] * du.y;
-        sc[i][s] = e * h[t + 1][s];
+        sums[i][s] = g[s] * du.y;
         by_u = s == 0 ? from_lane<at>(vb) * g[s] : fmaf(from_lane<at>(vb), g[s], by_u);
+        const float x = g[s] * kept[t][s];
         g[s] *= f[t][s];
-        const float x = g[s] * h[t][s];
         dA[s] = fmaf(x, du.x, dA[s]);
         by_d = s == 0 ? x * a2[s] : fmaf(x, a2[s], by_d);
       });
       part_u[t][lane] = k ? part_u[t][lane] + by_u : by_u;
       part_d[t][lane] = k ? part_d[t][lane] + by_d : by_d;
     });
-    const float b = lane_sums(sb, lane), c = lane_sums(sc, lane);
-    const int at = 4 * q + lane / 16, s = lane % 16 / 4;
-    if (at < rows && s < N) {
-      if (lane % 4 == 0) dB[at * stride + s] = b;
-      if (lane % 4 == 1) dC[at * stride + s] = c;
-    }
+    const float b = lane_sums(sums, lane);
+    if (lane % 4 == 0 && 4 * q + sum_row < rows && sum_state < N) dB[(4 * q + sum_row) * stride + sum_state] = b;
     __builtin_amdgcn_sched_barrier(0);
   });
 }
 
-template <class TR, int WAVES, int CHUNKS, bool FULL>
+template <class TR, int WAVES, int CHUNKS, bool FULL, bool GATE>
 __global__ __launch_bounds__(64 * WAVES, 2) void k_scan_backward(const ScanArgs a) {
   typedef typename TR::T T;
   constexpr int V = TILE_ROWS / WAVES;
   __shared__ Tile<WAVES, CHUNKS, true> tile;
-  __shared__ float part[3][WAVES][TILE_ROWS][CH];
+  __shared__ float part[GATE ? 3 : 2][WAVES][TILE_ROWS][CH], of_channel[2][CH];      // (the channels' bias and D)
   const int item = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
   if (item >= a.items) {
     const int who = blockIdx.x - a.items * a.blocks;
@@ -593,7 +598,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_scan_backward(const ScanArgs 
   Place p;
   const bool found = find(a, item, block, p);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int waves = min(WAVES, (a.states + PER - 1) / PER);
+  const int waves = min(WAVES, (a.states + a.share - 1) / a.share);
   const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
   const bool live = lane < p.valid;
   const int64_t of_lane = (int64_t)(p.channel + lane) * a.states, each = (int64_t)a.dim * a.states;
@@ -604,13 +609,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_scan_backward(const ScanArgs 
   for (int j = 0; j < V; ++j) dD[j] = dbias[j] = 0.f;
   if (found) {
     States<WAVES, CHUNKS> g, a2;
-    float bias[V], D[V], steps[V];
+    float steps[V];
+    if (threadIdx.x < CH) {
+      const bool mine = (int)threadIdx.x < p.valid;
+      of_channel[0][threadIdx.x] = mine && a.bias ? a.bias[p.channel + threadIdx.x] : 0.f;
+      of_channel[1][threadIdx.x] = mine && a.D ? a.D[p.channel + threadIdx.x] : 0.f;
+    }
+    __syncthreads();
     a2.load(a, a.A + of_lane, wave, live);
     a2.scale(LOG2_E);
     const float* end = p.last && p.span == 0 ? (a.ds_end ? a.ds_end + p.piece.seq * each : nullptr) : a.back + item * each;
     g.load(a, end + of_lane, wave, live && end);
-    load_channels(bias, a.bias, p.channel, col, p.valid);
-    load_channels(D, a.D, p.channel, col, p.valid);
     const int tiles = (int)((p.to - p.from + TILE_ROWS - 1) / TILE_ROWS);
     const int64_t number = first_tile(p), stride = (int64_t)a.groups * a.states;
     // (of the group's blocks this one's parts of dB and dC)
@@ -632,25 +641,25 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_scan_backward(const ScanArgs 
           for (int s = 0; s < PER; ++s)
             h0.v[c][s] = start.v[c][s] == 0.f ? h0.v[c][s] : fmaf(exp2_of(a2.v[c][s] * d), start.v[c][s], h0.v[c][s]);
       }
-      fill_tile(tile, a, in, rows, p.valid, bias, steps);
+      fill_tile(tile, a, in, rows, p.valid, of_channel[0] + col, steps);
       const auto now = in;
       __syncthreads();
       if (k > 0) in.load(a, p, t0 - TILE_ROWS, TILE_ROWS, true);
-      with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto c, auto n) {
-        const int64_t at = part_at + t0 * stride + (c * WAVES + wave) * PER;
-        back_tile<decltype(n)::value>(g.v[c], dA.v[c], h0.v[c], a2.v[c], tile, c, wave, lane, part[0][wave], part[1][wave], part[2][wave], a.dB + at,
+      with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto c, auto n) __attribute__((always_inline)) {
+        const int64_t at = part_at + t0 * stride + (c * WAVES + wave) * a.share;
+        back_tile<decltype(n)::value, GATE>(g.v[c], dA.v[c], h0.v[c], a2.v[c], tile, c, wave, lane, part[0][wave], part[1][wave], part[GATE ? 2 : 0][wave], a.dB + at,
                                       a.dC + at, stride, rows);
       });
       __syncthreads();
       float du[V], dd[V], y[V], dx[V], ddt[V], dz[V];
       gather(part[0], waves, r, col, du);
       gather(part[1], waves, r, col, dd);
-      gather(part[2], waves, r, col, y);
+      if constexpr (GATE) gather(part[2], waves, r, col, y);
       const bool there = r < rows;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float d = tile.du[r][col + j].x, e = tile.e[r][col + j], x = now.x.get(j), raw = now.dt.get(j) + bias[j];
-        dx[j] = a.D ? fmaf(D[j], e, d * du[j]) : d * du[j];
+        const float d = tile.du[r][col + j].x, e = tile.e[r][col + j], x = now.x.get(j), raw = now.dt.get(j) + of_channel[0][col + j], D = of_channel[1][col + j];
+        dx[j] = a.D ? fmaf(D, e, d * du[j]) : d * du[j];
         ddt[j] = fmaf(x, du[j], LN_2 * dd[j]);
         if (a.softplus) ddt[j] *= sigmoid_of(raw);
         if (there && col + j < p.valid) {
@@ -658,9 +667,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_scan_backward(const ScanArgs 
           dbias[j] += ddt[j];
         }
         dz[j] = 0.f;
-        if (a.z) {
+        if constexpr (GATE) {
           const float z = now.z.get(j), s = sigmoid_of(z);
-          dz[j] = now.dy.get(j) * (a.D ? fmaf(D[j], x, y[j]) : y[j]) * s * fmaf(z, 1.f - s, 1.f);
+          dz[j] = now.dy.get(j) * (a.D ? fmaf(D, x, y[j]) : y[j]) * s * fmaf(z, 1.f - s, 1.f);
         }
       }
       if (there) {
@@ -669,7 +678,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_scan_backward(const ScanArgs 
         o.store(static_cast<T*>(a.dx) + (t0 + r) * a.dx_row + p.channel + col, p.valid - col);
         o.put(ddt);
         o.store(static_cast<T*>(a.ddt) + (t0 + r) * a.ddt_row + p.channel + col, p.valid - col);
-        if (a.z) {
+        if constexpr (GATE) {
           o.put(dz);
           o.store(static_cast<T*>(a.dz) + (t0 + r) * a.dz_row + p.channel + col, p.valid - col);
         }
@@ -827,11 +836,9 @@ bool overlap(const void* a, const void* b, size_t bytes) {
   return x && y && x < y + bytes && y < x + bytes;
 }
 
-int waves_of(const nugpr_selective_scan* p) {
-  int w = 1;
-  while (w < 8 && w * PER < p->dim_state) w *= 2;
-  return w;
-}
+// Four waves share out up to 16 states, eight up to 32, in two chunks up to 64.
+int waves_of(const nugpr_selective_scan* p) { return p->dim_state > 4 * PER ? 8 : 4; }
+int chunks_of(const nugpr_selective_scan* p) { return p->dim_state > 8 * PER ? 2 : 1; }
 
 int blocks_of(const nugpr_selective_scan* p) { return p->groups * ((p->dim / p->groups + CH - 1) / CH); }
 
@@ -908,25 +915,21 @@ ScanArgs scan_args(const nugpr_selective_scan* p) {
   ScanArgs a{};
   a.A = p->A; a.D = p->D; a.bias = p->dt_bias; a.off = p->seq_offsets; a.n_rows = p->n_rows; a.n_seqs = p->n_seqs;
   a.dim = p->dim; a.groups = p->groups; a.each = p->dim / p->groups; a.blocks = blocks_of(p); a.states = p->dim_state;
-  a.softplus = p->softplus != 0; a.span_log2 = span_log2(p); a.items = (int)items_of(p);
+  a.softplus = p->softplus != 0; a.share = (p->dim_state + waves_of(p) * chunks_of(p) - 1) / (waves_of(p) * chunks_of(p)); a.span_log2 = span_log2(p); a.items = (int)items_of(p);
   return a;
 }
 
-// f(waves, chunks, whether all of them have four states), as constants
+// f(waves, chunks, whether all of the waves have four states), as constants
 template <class F>
 void with_waves(const nugpr_selective_scan* p, F f) {
-  auto with = [&](auto waves, auto chunks) {
-    if (p->dim_state == decltype(waves)::value * decltype(chunks)::value * PER) f(waves, chunks, std::true_type{});
-    else f(waves, chunks, std::false_type{});
-  };
   constexpr std::integral_constant<int, 1> one{};
-  if (p->dim_state > 8 * PER) return with(std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
-  switch (waves_of(p)) {
-    case 1: return with(one, one);
-    case 2: return with(std::integral_constant<int, 2>{}, one);
-    case 4: return with(std::integral_constant<int, 4>{}, one);
-    default: return with(std::integral_constant<int, 8>{}, one);
-  }
+  constexpr std::integral_constant<int, 4> four{};
+  constexpr std::integral_constant<int, 8> eight{};
+  if (chunks_of(p) == 2) f(eight, std::integral_constant<int, 2>{}, std::false_type{});
+  else if (p->dim_state == 8 * PER) f(eight, one, std::true_type{});
+  else if (waves_of(p) == 8) f(eight, one, std::false_type{});
+  else if (p->dim_state == 4 * PER) f(four, one, std::true_type{});
+  else f(four, one, std::false_type{});
 }
 
 void launch_join(const ScanArgs& a, bool backward, hipStream_t s) {
@@ -958,7 +961,8 @@ void launch_backward(const nugpr_selective_scan* p, const ScanArgs& a, const nug
     const dim3 spans((unsigned)(a.items * a.blocks)), all((unsigned)(a.items * a.blocks + ZERO_GROUPS)), threads(64 * W);
     hipLaunchKernelGGL((k_scan_tiles<TR, W, K, FULL>), spans, threads, 0, s, a);
     if (!one_span(p)) launch_join(a, true, s);
-    hipLaunchKernelGGL((k_scan_backward<TR, W, K, FULL>), all, threads, 0, s, a);
+    if (a.z) hipLaunchKernelGGL((k_scan_backward<TR, W, K, FULL, true>), all, threads, 0, s, a);
+    else hipLaunchKernelGGL((k_scan_backward<TR, W, K, FULL, false>), all, threads, 0, s, a);
   });
   const int64_t values = a.n_rows * a.groups * a.states, each = (int64_t)a.dim * a.states;
   if (values)
@@ -1094,7 +1098,8 @@ int nugpr_selective_scan_step(const nugpr_selective_scan* p, const nugpr_rows* x
   a.y = y->data; a.y_row = y->row_stride;
   a.A = p->A; a.D = p->D; a.bias = p->dt_bias; a.state = state; a.slots = slots; a.n_states = p->n_seqs;
   a.dim = p->dim; a.each = p->dim / p->groups; a.states = p->dim_state; a.softplus = p->softplus != 0;
-  const int lanes = p->dim_state > 32 ? 16 : waves_of(p);
+  int lanes = 1;
+  while (lanes * PER < p->dim_state) lanes *= 2;
   a.col_blocks = (p->dim * lanes + 255) / 256;
   const int64_t grid = p->n_rows * a.col_blocks;
   if (grid > (int64_t)0xffffffff / 256) return invalid("too many requests and channels for one call");
