@@ -61,6 +61,40 @@ __device__ __forceinline__ float from_lane(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x150 + I, 0xf, 0xf, true));
 }
 
+// Products with N values side by side of those 16, from value I on, by instructions that read them where they are (s_nop: what a vector
+// instruction has just written can be read so two steps later).
+//   dot: sum of values times h;  add_times: h[s] += x value
+template <int I, int N>
+__device__ __forceinline__ float dot(float v, const float (&h)[PER]) {
+  float y;
+  if constexpr (N == 4)
+    asm("s_nop 1\n\tv_mul_f32_dpp %0, %1, %2 row_newbcast:%6 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %3 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %4 row_newbcast:%8 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %5 row_newbcast:%9 row_mask:0xf bank_mask:0xf"
+        : "=&v"(y) : "v"(v), "v"(h[0]), "v"(h[1]), "v"(h[2]), "v"(h[3]), "n"(I), "n"(I + 1), "n"(I + 2), "n"(I + 3));
+  else {
+    y = from_lane<I>(v) * h[0];
+    if constexpr (N > 1) y = fmaf(from_lane<I + 1>(v), h[1], y);
+    if constexpr (N > 2) y = fmaf(from_lane<I + 2>(v), h[2], y);
+  }
+  return y;
+}
+template <int I, int N>
+__device__ __forceinline__ void add_times(float (&h)[PER], float v, float x) {
+  if constexpr (N == 4)
+    asm("s_nop 1\n\tv_fmac_f32_dpp %0, %4, %5 row_newbcast:%6 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %1, %4, %5 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %2, %4, %5 row_newbcast:%8 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %3, %4, %5 row_newbcast:%9 row_mask:0xf bank_mask:0xf"
+        : "+v"(h[0]), "+v"(h[1]), "+v"(h[2]), "+v"(h[3]) : "v"(v), "v"(x), "n"(I), "n"(I + 1), "n"(I + 2), "n"(I + 3));
+  else {
+    h[0] = fmaf(from_lane<I>(v), x, h[0]);
+    if constexpr (N > 1) h[1] = fmaf(from_lane<I + 1>(v), x, h[1]);
+    if constexpr (N > 2) h[2] = fmaf(from_lane<I + 2>(v), x, h[2]);
+  }
+}
+
 // Where a workgroup stands.
 struct Place {
   int group, channel, valid;         // its first channel, and how many it has
@@ -85,30 +119,59 @@ __device__ __forceinline__ bool find(const ScanArgs& a, int item, int block, Pla
   return true;
 }
 
-// The tile's rows as memory has them: a thread holds V channels of one row, and one value of B and C.
-template <class TR, int WAVES, int CHUNKS, bool GRADIENT>
+// A tile's rows as memory has them: a thread holds V channels of one row, and one value of B and C for each chunk.  GRADIENT: dy too; OUT:
+// what the output needs beside the states.
+template <class TR, int WAVES, int CHUNKS, bool GRADIENT, bool OUT>
 struct Incoming {
+  typedef typename TR::T T;
   static constexpr int V = TILE_ROWS / WAVES;
   Values<TR, V> x, dt, z, dy;
-  float b[CHUNKS], c[CHUNKS];
-  __device__ void load(const ScanArgs& a, const Place& p, int64_t row0, int n_rows, bool live) {
-    typedef typename TR::T T;
-    const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
-    const int64_t row = row0 + r;
-    const int valid = r < n_rows && live ? p.valid - col : 0;
-    x.load(static_cast<const T*>(a.x) + row * a.x_row + p.channel + col, valid);
-    dt.load(static_cast<const T*>(a.dt) + row * a.dt_row + p.channel + col, valid);
-    if (a.z) z.load(static_cast<const T*>(a.z) + row * a.z_row + p.channel + col, valid);
-    if constexpr (GRADIENT) dy.load(static_cast<const T*>(a.dy) + row * a.dy_row + p.channel + col, valid);
-    const int br = threadIdx.x / (PER * WAVES);
+  T b[CHUNKS], c[CHUNKS];
+  const T *px, *pdt, *pz, *pdy, *pb, *pc;          // the thread's, of the tile that is loaded next
+  // row0: the tile's first row
+  __device__ __forceinline__ void begin(const ScanArgs& a, const Place& p, int64_t row0) {
+    const int64_t row = row0 + threadIdx.x / (CH / V), brow = row0 + threadIdx.x / (PER * WAVES);
+    const int at = p.channel + threadIdx.x % (CH / V) * V, n = threadIdx.x % (PER * WAVES) / PER * a.share + threadIdx.x % PER;
+    px = static_cast<const T*>(a.x) + row * a.x_row + at;
+    pdt = static_cast<const T*>(a.dt) + row * a.dt_row + at;
+    if (OUT) pz = static_cast<const T*>(a.z) + row * a.z_row + at;
+    if (GRADIENT) pdy = static_cast<const T*>(a.dy) + row * a.dy_row + at;
+    pb = static_cast<const T*>(a.B) + brow * a.B_row + p.group * a.B_head + n;
+    if (OUT) pc = static_cast<const T*>(a.C) + brow * a.C_row + p.group * a.C_head + n;
+  }
+  // n_rows of the tile, then the pointers move on by `way` tiles
+  template <bool FULL>
+  __device__ __forceinline__ void load(const ScanArgs& a, const Place& p, int n_rows, int way) {
+    const bool whole = n_rows == TILE_ROWS && p.valid == CH;
+    const int valid = whole ? V : (int)threadIdx.x / (CH / V) < n_rows ? p.valid - (int)threadIdx.x % (CH / V) * V : 0;
+    if (whole) {
+      x.load_all(px);
+      dt.load_all(pdt);
+      if (OUT && a.z) z.load_all(pz);
+      if (GRADIENT && OUT) dy.load_all(pdy);
+    } else {
+      x.load(px, valid);
+      dt.load(pdt, valid);
+      if (OUT && a.z) z.load(pz, valid);
+      if (GRADIENT && OUT) dy.load(pdy, valid);
+    }
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) {
       const int s = threadIdx.x % PER, n = (k * WAVES + threadIdx.x % (PER * WAVES) / PER) * a.share + s;
-      b[k] = c[k] = 0.f;
-      if (live && br < n_rows && s < a.share && n < a.states) {
-        b[k] = TR::get(static_cast<const T*>(a.B)[(row0 + br) * a.B_row + p.group * a.B_head + n]);
-        c[k] = TR::get(static_cast<const T*>(a.C)[(row0 + br) * a.C_row + p.group * a.C_head + n]);
+      b[k] = c[k] = T(0);
+      if ((FULL && whole) || ((int)threadIdx.x / (PER * WAVES) < n_rows && s < a.share && n < a.states)) {
+        b[k] = pb[k * WAVES * a.share];
+        if (OUT) c[k] = pc[k * WAVES * a.share];
       }
+    }
+    const int64_t rows = (int64_t)way * TILE_ROWS;
+    px += rows * a.x_row;
+    pdt += rows * a.dt_row;
+    pb += rows * a.B_row;
+    if (OUT) {
+      pz += rows * a.z_row;
+      pc += rows * a.C_row;
+      if (GRADIENT) pdy += rows * a.dy_row;
     }
   }
 };
@@ -186,28 +249,40 @@ struct Tile {
 
 // Makes a tile's rows from what came in.  Rows and channels that there are not: d = u = 0, which leaves a state as it is.  steps: sums
 // of d, a row of every tile a thread; bias: of the thread's channels.
-template <class TR, int WAVES, int CHUNKS, bool GRADIENT>
-__device__ __forceinline__ void fill_tile(Tile<WAVES, CHUNKS, GRADIENT>& tile, const ScanArgs& a, const Incoming<TR, WAVES, CHUNKS, GRADIENT>& in, int n_rows,
-                                 int valid, const float* bias, float (&steps)[TILE_ROWS / WAVES]) {
+template <class TR, int WAVES, int CHUNKS, bool GRADIENT, bool OUT>
+__device__ __forceinline__ void fill_tile(Tile<WAVES, CHUNKS, GRADIENT>& tile, const ScanArgs& a, const Incoming<TR, WAVES, CHUNKS, GRADIENT, OUT>& in,
+                                          int n_rows, int valid, const float* bias, float (&steps)[TILE_ROWS / WAVES]) {
   constexpr int V = TILE_ROWS / WAVES;
   const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
+  float d[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) d[j] = in.dt.get(j) + bias[j];
+  if (a.softplus)
+#pragma unroll
+    for (int j = 0; j < V; ++j) d[j] = softplus_of<TR>(d[j]);
+  if (n_rows < TILE_ROWS || valid < CH)
+#pragma unroll
+    for (int j = 0; j < V; ++j) d[j] = r < n_rows && col + j < valid ? d[j] : 0.f;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    float d = in.dt.get(j) + bias[j];
-    if (a.softplus) d = softplus_of(d);
-    if (r >= n_rows || col + j >= valid) d = 0.f;
-    steps[j] += d;
-    tile.du[r][col + j] = float2{d, d * in.x.get(j)};
-    if constexpr (GRADIENT) {
-      const float dy = in.dy.get(j), z = a.z ? in.z.get(j) : 0.f;
-      tile.e[r][col + j] = a.z ? dy * (z * sigmoid_of(z)) : dy;
-    }
+    steps[j] += d[j];
+    tile.du[r][col + j] = float2{d[j], d[j] * in.x.get(j)};
+  }
+  if constexpr (GRADIENT && OUT) {
+    float e[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) e[j] = in.dy.get(j);
+    if (a.z)
+#pragma unroll
+      for (int j = 0; j < V; ++j) e[j] *= in.z.get(j) * sigmoid_of<TR>(in.z.get(j));
+#pragma unroll
+    for (int j = 0; j < V; ++j) tile.e[r][col + j] = e[j];
   }
   const int br = threadIdx.x / (PER * WAVES), n = threadIdx.x % (PER * WAVES);
 #pragma unroll
   for (int k = 0; k < CHUNKS; ++k) {
-    tile.B[k][br][n] = in.b[k];
-    tile.C[k][br][n] = in.c[k];
+    tile.B[k][br][n] = TR::get(in.b[k]);
+    if (OUT) tile.C[k][br][n] = TR::get(in.c[k]);
   }
 }
 
@@ -236,13 +311,14 @@ __device__ __forceinline__ void walk_tile(float (&h)[PER], const float (&a2)[PER
     repeat<4>([&](auto i) __attribute__((always_inline)) {
       constexpr int t = 4 * q + i;
       const float2 du = tile.du[t][lane];
-      float y = 0.f;
       repeat<N>([&](auto s) __attribute__((always_inline)) {
         constexpr int at = PER * i + s;
         h[s] = fmaf(exp2_of(du.x * a2[s]), h[s], du.y * from_lane<at>(vb));
-        if constexpr (OUT) y = s == 0 ? from_lane<at>(vc) * h[s] : fmaf(from_lane<at>(vc), h[s], y);
       });
-      if constexpr (OUT) part[t][lane] = k ? part[t][lane] + y : y;
+      if constexpr (OUT) {
+        const float y = dot<PER * i, N>(vc, h);
+        part[t][lane] = k ? part[t][lane] + y : y;
+      }
     });
   });
 }
@@ -263,7 +339,7 @@ __device__ __forceinline__ void walk_tile_back(float (&h)[PER], float (&product)
         const float f = exp2_of(du.x * a2[s]);
         h[s] = fmaf(f, h[s], du.y * from_lane<at>(vb));
         product[s] *= f;
-        g[s] = fmaf(product[s] * e, from_lane<at>(vc), g[s]);
+        g[s] = fmaf(product[s], e * from_lane<at>(vc), g[s]);
       });
     });
   });
@@ -327,16 +403,16 @@ __global__ __launch_bounds__(64 * WAVES) void k_scan(const ScanArgs a) {
   load_channels(D, a.D, p.channel, col, p.valid);
 #pragma unroll
   for (int j = 0; j < V; ++j) steps[j] = 0.f;
-  Incoming<TR, WAVES, CHUNKS, false> in;
-  in.load(a, p, p.from, (int)min((int64_t)TILE_ROWS, p.to - p.from), true);
+  Incoming<TR, WAVES, CHUNKS, false, !ADDS> in;
+  in.begin(a, p, p.from);
+  in.template load<FULL>(a, p, (int)min((int64_t)TILE_ROWS, p.to - p.from), 1);
   for (int64_t t0 = p.from; t0 < p.to; t0 += TILE_ROWS) {
     const int rows = (int)min((int64_t)TILE_ROWS, p.to - t0);
     if (ADDS) __syncthreads();                     // (the walk's second one has this effect)
     fill_tile(tile, a, in, rows, p.valid, bias, steps);
     const auto now = in;
     __syncthreads();
-    const int64_t next = t0 + TILE_ROWS;
-    in.load(a, p, next, (int)min((int64_t)TILE_ROWS, p.to - next), next < p.to);
+    if (t0 + TILE_ROWS < p.to) in.template load<FULL>(a, p, (int)min((int64_t)TILE_ROWS, p.to - t0 - TILE_ROWS), 1);
     with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) __attribute__((always_inline)) {
       walk_tile<decltype(n)::value, !ADDS>(h.v[k], a2.v[k], tile, k, wave, lane, part[ADDS ? 0 : wave]);
     });
@@ -344,11 +420,12 @@ __global__ __launch_bounds__(64 * WAVES) void k_scan(const ScanArgs a) {
       __syncthreads();
       float y[V];
       gather(part, waves, r, col, y);
+      if (a.D)
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        y[j] = a.D ? fmaf(D[j], now.x.get(j), y[j]) : y[j];
-        if (a.z) y[j] *= now.z.get(j) * sigmoid_of(now.z.get(j));
-      }
+        for (int j = 0; j < V; ++j) y[j] = fmaf(D[j], now.x.get(j), y[j]);
+      if (a.z)
+#pragma unroll
+        for (int j = 0; j < V; ++j) y[j] *= now.z.get(j) * sigmoid_of<TR>(now.z.get(j));
       Values<TR, V> o;
       o.put(y);
       if (r < rows) o.store(static_cast<T*>(a.y) + (t0 + r) * a.y_row + p.channel + col, p.valid - col);
@@ -447,30 +524,32 @@ __global__ __launch_bounds__(64 * WAVES) void k_scan_tiles(const ScanArgs a) {
   for (int j = 0; j < V; ++j) steps[j] = 0.f;
   int64_t number = first_tile(p);
   float passed = 0.f;                              // sum of d before the tile (first wave)
-  Incoming<TR, WAVES, CHUNKS, true> in;
-  in.load(a, p, p.from, (int)min((int64_t)TILE_ROWS, p.to - p.from), true);
-  for (int64_t t0 = p.from; t0 < p.to; t0 += TILE_ROWS, ++number) {
-    const int rows = (int)min((int64_t)TILE_ROWS, p.to - t0);
-    h.store(a, a.tiles + number * each + of_lane, wave, live);
-    __syncthreads();
-    fill_tile(tile, a, in, rows, p.valid, bias, steps);
-    __syncthreads();
-    const int64_t next = t0 + TILE_ROWS;
-    in.load(a, p, next, (int)min((int64_t)TILE_ROWS, p.to - next), next < p.to);
-    if (p.span > 0) {
-      if (wave == 0 && live) {
+  // (a sequence's first span has no state before it whose gradient were wanted)
+  auto walk = [&](auto later) __attribute__((always_inline)) {
+    constexpr bool LATER = decltype(later)::value;
+    Incoming<TR, WAVES, CHUNKS, true, LATER> in;
+    in.begin(a, p, p.from);
+    if (p.from < p.to) in.template load<FULL>(a, p, (int)min((int64_t)TILE_ROWS, p.to - p.from), 1);
+    for (int64_t t0 = p.from; t0 < p.to; t0 += TILE_ROWS, ++number) {
+      const int rows = (int)min((int64_t)TILE_ROWS, p.to - t0);
+      h.store(a, a.tiles + number * each + of_lane, wave, live);
+      __syncthreads();
+      fill_tile(tile, a, in, rows, p.valid, bias, steps);
+      __syncthreads();
+      if (t0 + TILE_ROWS < p.to) in.template load<FULL>(a, p, (int)min((int64_t)TILE_ROWS, p.to - t0 - TILE_ROWS), 1);
+      if (LATER && wave == 0 && live) {
         a.tile_steps[number * a.dim + p.channel + lane] = passed;
+#pragma unroll
         for (int t = 0; t < TILE_ROWS; ++t) passed += tile.du[t][lane].x;
       }
       with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) __attribute__((always_inline)) {
-        walk_tile_back<decltype(n)::value>(h.v[k], product.v[k], g.v[k], a2.v[k], tile, k, wave, lane);
-      });
-    } else {
-      with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) __attribute__((always_inline)) {
-        walk_tile<decltype(n)::value, false>(h.v[k], a2.v[k], tile, k, wave, lane, part);
+        if constexpr (LATER) walk_tile_back<decltype(n)::value>(h.v[k], product.v[k], g.v[k], a2.v[k], tile, k, wave, lane);
+        else walk_tile<decltype(n)::value, false>(h.v[k], a2.v[k], tile, k, wave, lane, part);
       });
     }
-  }
+  };
+  if (p.span > 0) walk(std::true_type{});
+  else walk(std::false_type{});
   if (p.span == 0 && p.last) return;
   h.store(a, a.adds + item * each + of_lane, wave, live && !p.last);
   g.store(a, a.back + item * each + of_lane, wave, live && p.span > 0);
@@ -524,9 +603,9 @@ __device__ __forceinline__ void back_tile(float (&g)[PER], float (&dA)[PER], con
                                  int rows) {
   const int row = (lane & 15) / PER, n = wave * PER + lane % PER;
   const int sum_row = lane / 16, sum_state = lane % 16 / 4;       // (of lane_sums)
-  float h[PER], f[TILE_ROWS][PER], kept[TILE_ROWS][PER];          // a_t, and a_t h_{t-1}
+  float h[TILE_ROWS + 1][PER], f[TILE_ROWS][PER];                 // h_{t-1} and on, a_t
 #pragma unroll
-  for (int s = 0; s < PER; ++s) h[s] = h0[s];
+  for (int s = 0; s < PER; ++s) h[0][s] = h0[s];
   repeat<TILE_ROWS / 4>([&](auto q) __attribute__((always_inline)) {
     const float vb = tile.B[k][4 * q + row][n], vc = tile.C[k][4 * q + row][n];
     float sums[4][PER];
@@ -534,18 +613,18 @@ __device__ __forceinline__ void back_tile(float (&g)[PER], float (&dA)[PER], con
       constexpr int t = 4 * q + i;
       const float2 du = tile.du[t][lane];
       const float e = tile.e[t][lane];
-      float y = 0.f;
 #pragma unroll
       for (int s = N; s < PER; ++s) sums[i][s] = 0.f;
       repeat<N>([&](auto s) __attribute__((always_inline)) {
         constexpr int at = PER * i + s;
         f[t][s] = exp2_of(du.x * a2[s]);
-        kept[t][s] = f[t][s] * h[s];
-        h[s] = fmaf(du.y, from_lane<at>(vb), kept[t][s]);
-        if constexpr (GATE) y = s == 0 ? from_lane<at>(vc) * h[s] : fmaf(from_lane<at>(vc), h[s], y);
-        sums[i][s] = e * h[s];
+        h[t + 1][s] = fmaf(f[t][s], h[t][s], du.y * from_lane<at>(vb));
+        sums[i][s] = e * h[t + 1][s];
       });
-      if constexpr (GATE) part_y[t][lane] = k ? part_y[t][lane] + y : y;
+      if constexpr (GATE) {
+        const float y = dot<PER * i, N>(vc, h[t + 1]);
+        part_y[t][lane] = k ? part_y[t][lane] + y : y;
+      }
     });
     const float c = lane_sums(sums, lane);
     if (lane % 4 == 0 && 4 * q + sum_row < rows && sum_state < N) dC[(4 * q + sum_row) * stride + sum_state] = c;
@@ -559,16 +638,15 @@ __device__ __forceinline__ void back_tile(float (&g)[PER], float (&dA)[PER], con
       constexpr int i = 3 - j, t = 4 * q + i;
       const float2 du = tile.du[t][lane];
       const float e = tile.e[t][lane];
-      float by_u = 0.f, by_d = 0.f;
+      add_times<PER * i, N>(g, vc, e);
+      const float by_u = dot<PER * i, N>(vb, g);
+      float by_d = 0.f;
 #pragma unroll
       for (int s = N; s < PER; ++s) sums[i][s] = 0.f;
       repeat<N>([&](auto s) __attribute__((always_inline)) {
-        constexpr int at = PER * i + s;
-        g[s] = fmaf(e, from_lane<at>(vc), g[s]);
         sums[i][s] = g[s] * du.y;
-        by_u = s == 0 ? from_lane<at>(vb) * g[s] : fmaf(from_lane<at>(vb), g[s], by_u);
-        const float x = g[s] * kept[t][s];
         g[s] *= f[t][s];
+        const float x = g[s] * h[t][s];
         dA[s] = fmaf(x, du.x, dA[s]);
         by_d = s == 0 ? x * a2[s] : fmaf(x, a2[s], by_d);
       });
@@ -624,8 +702,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_scan_backward(const ScanArgs 
     const int64_t number = first_tile(p), stride = (int64_t)a.groups * a.states;
     // (of the group's blocks this one's parts of dB and dC)
     const int64_t part_at = (int64_t)(block % (a.blocks / a.groups)) * a.n_rows * stride + p.group * a.states;
-    Incoming<TR, WAVES, CHUNKS, true> in;
-    if (tiles > 0) in.load(a, p, p.from + (int64_t)(tiles - 1) * TILE_ROWS, (int)(p.to - p.from - (int64_t)(tiles - 1) * TILE_ROWS), true);
+    Incoming<TR, WAVES, CHUNKS, true, true> in;
+    in.begin(a, p, p.from + (int64_t)(tiles - 1) * TILE_ROWS);
+    if (tiles > 0) in.template load<FULL>(a, p, (int)(p.to - p.from - (int64_t)(tiles - 1) * TILE_ROWS), -1);
     for (int k = tiles - 1; k >= 0; --k) {
       const int64_t t0 = p.from + (int64_t)k * TILE_ROWS;
       const int rows = (int)min((int64_t)TILE_ROWS, p.to - t0);
@@ -644,7 +723,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_scan_backward(const ScanArgs 
       fill_tile(tile, a, in, rows, p.valid, of_channel[0] + col, steps);
       const auto now = in;
       __syncthreads();
-      if (k > 0) in.load(a, p, t0 - TILE_ROWS, TILE_ROWS, true);
+      if (k > 0) in.template load<FULL>(a, p, TILE_ROWS, -1);
       with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto c, auto n) __attribute__((always_inline)) {
         const int64_t at = part_at + t0 * stride + (c * WAVES + wave) * a.share;
         back_tile<decltype(n)::value, GATE>(g.v[c], dA.v[c], h0.v[c], a2.v[c], tile, c, wave, lane, part[0][wave], part[1][wave], part[GATE ? 2 : 0][wave], a.dB + at,
@@ -661,14 +740,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_scan_backward(const ScanArgs 
         const float d = tile.du[r][col + j].x, e = tile.e[r][col + j], x = now.x.get(j), raw = now.dt.get(j) + of_channel[0][col + j], D = of_channel[1][col + j];
         dx[j] = a.D ? fmaf(D, e, d * du[j]) : d * du[j];
         ddt[j] = fmaf(x, du[j], LN_2 * dd[j]);
-        if (a.softplus) ddt[j] *= sigmoid_of(raw);
+        if (a.softplus) ddt[j] *= sigmoid_of<TR>(raw);
         if (there && col + j < p.valid) {
           dD[j] = fmaf(e, x, dD[j]);
           dbias[j] += ddt[j];
         }
         dz[j] = 0.f;
         if constexpr (GATE) {
-          const float z = now.z.get(j), s = sigmoid_of(z);
+          const float z = now.z.get(j), s = sigmoid_of<TR>(z);
           dz[j] = now.dy.get(j) * (a.D ? fmaf(D, x, y[j]) : y[j]) * s * fmaf(z, 1.f - s, 1.f);
         }
       }
@@ -769,14 +848,14 @@ __global__ __launch_bounds__(256) void k_scan_step(const ScanStepArgs a) {
     }
     x = TR::get(static_cast<const T*>(a.x)[row * a.x_row + c]);
     float d = TR::get(static_cast<const T*>(a.dt)[row * a.dt_row + c]) + (a.bias ? a.bias[c] : 0.f);
-    if (a.softplus) d = softplus_of(d);
+    if (a.softplus) d = softplus_of<TR>(d);
     const float u = d * x;
 #pragma unroll
     for (int s = 0; s < PER; ++s) {
       if (s >= n) continue;
       const float b = TR::get(static_cast<const T*>(a.B)[row * a.B_row + group * a.B_head + n0 + s]);
       const float w = TR::get(static_cast<const T*>(a.C)[row * a.C_row + group * a.C_head + n0 + s]);
-      h[s] = fmaf(exp_of(d * f[s]), h[s], u * b);
+      h[s] = fmaf(exp_of<F32>(d * f[s]), h[s], u * b);
       out = fmaf(w, h[s], out);
     }
     if constexpr (WIDE) {
@@ -791,7 +870,7 @@ __global__ __launch_bounds__(256) void k_scan_step(const ScanStepArgs a) {
   if (a.D) out = fmaf(a.D[c], x, out);
   if (a.z) {
     const float z = TR::get(static_cast<const T*>(a.z)[row * a.z_row + c]);
-    out *= z * sigmoid_of(z);
+    out *= z * sigmoid_of<TR>(z);
   }
   *y = TR::put(out);
 }
@@ -842,15 +921,15 @@ int chunks_of(const nugpr_selective_scan* p) { return p->dim_state > 8 * PER ? 2
 
 int blocks_of(const nugpr_selective_scan* p) { return p->groups * ((p->dim / p->groups + CH - 1) / CH); }
 
-// Rows of a span: a power of two, a few tiles at least, so large that the spans of the rows give about that many waves.
-constexpr int64_t WAVES_WANTED = 2048;
-int span_log2(const nugpr_selective_scan* p) {
+// Rows of a span: a power of two, a few tiles at least, so large that the spans of the rows give about 8192 waves, 4096 in the gradients, of
+// which a compute unit holds a third as many.
+int span_log2(const nugpr_selective_scan* p, bool backward) {
   int k = 6;
-  while (k < 40 && ((p->n_rows * blocks_of(p) * waves_of(p)) >> k) > WAVES_WANTED) ++k;
+  while (k < 40 && ((p->n_rows * blocks_of(p) * waves_of(p)) >> k) > (backward ? 4096 : 8192)) ++k;
   return k;
 }
-bool one_span(const nugpr_selective_scan* p) { return p->n_rows <= (int64_t)1 << span_log2(p); }
-int64_t items_of(const nugpr_selective_scan* p) { return (p->n_rows >> span_log2(p)) + p->n_seqs; }
+bool one_span(const nugpr_selective_scan* p, bool backward) { return p->n_rows <= (int64_t)1 << span_log2(p, backward); }
+int64_t items_of(const nugpr_selective_scan* p, bool backward) { return (p->n_rows >> span_log2(p, backward)) + p->n_seqs; }
 int64_t tiles_of(const nugpr_selective_scan* p) { return p->n_rows / TILE_ROWS + p->n_seqs; }
 
 // Where the parts of the workspace begin.
@@ -869,8 +948,8 @@ size_t lay_out(const nugpr_selective_scan* p, bool backward, void* ws, ScanArgs*
   Workspace w(ws);
   ScanArgs none;
   if (!a) a = &none;
-  const size_t items = (size_t)items_of(p), tiles = (size_t)tiles_of(p), states = (size_t)p->dim * p->dim_state;
-  const bool spans = !one_span(p);
+  const size_t items = (size_t)items_of(p, backward), tiles = (size_t)tiles_of(p), states = (size_t)p->dim * p->dim_state;
+  const bool spans = !one_span(p, backward);
   a->adds = w.take(spans ? items * states : 0);
   a->steps = w.take(spans ? items * p->dim : 0);
   if (backward) {
@@ -902,7 +981,7 @@ int check_call(const nugpr_selective_scan* p, bool backward, bool* done) {
   if (*done) return NUGPR_OK;
   if (p->n_seqs < 1 || !p->seq_offsets) return invalid("seq_offsets is null, or there is no sequence");
   // (the threads of a launch are counted in 32 bits)
-  if (items_of(p) * blocks_of(p) + ZERO_GROUPS > (int64_t)0xffffffff / (64 * waves_of(p)) ||
+  if (items_of(p, backward) * blocks_of(p) + ZERO_GROUPS > (int64_t)0xffffffff / (64 * waves_of(p)) ||
       (backward && p->n_rows * p->groups * p->dim_state > (int64_t)0xffffffff - 256))
     return invalid("too many rows, sequences and channels for one call");
   const size_t need = lay_out(p, backward, nullptr, nullptr);
@@ -911,11 +990,11 @@ int check_call(const nugpr_selective_scan* p, bool backward, bool* done) {
   return NUGPR_OK;
 }
 
-ScanArgs scan_args(const nugpr_selective_scan* p) {
+ScanArgs scan_args(const nugpr_selective_scan* p, bool backward) {
   ScanArgs a{};
   a.A = p->A; a.D = p->D; a.bias = p->dt_bias; a.off = p->seq_offsets; a.n_rows = p->n_rows; a.n_seqs = p->n_seqs;
   a.dim = p->dim; a.groups = p->groups; a.each = p->dim / p->groups; a.blocks = blocks_of(p); a.states = p->dim_state;
-  a.softplus = p->softplus != 0; a.share = (p->dim_state + waves_of(p) * chunks_of(p) - 1) / (waves_of(p) * chunks_of(p)); a.span_log2 = span_log2(p); a.items = (int)items_of(p);
+  a.softplus = p->softplus != 0; a.share = (p->dim_state + waves_of(p) * chunks_of(p) - 1) / (waves_of(p) * chunks_of(p)); a.span_log2 = span_log2(p, backward); a.items = (int)items_of(p, backward);
   return a;
 }
 
@@ -944,7 +1023,7 @@ void launch_forward(const nugpr_selective_scan* p, const ScanArgs& a, hipStream_
     constexpr int W = decltype(w)::value, K = decltype(chunks)::value;
     constexpr bool FULL = decltype(full)::value;
     const dim3 spans((unsigned)(a.items * a.blocks)), all((unsigned)(a.items * a.blocks + ZERO_GROUPS)), threads(64 * W);
-    if (!one_span(p)) {
+    if (!one_span(p, false)) {
       hipLaunchKernelGGL((k_scan<TR, W, K, FULL, true>), spans, threads, 0, s, a);
       launch_join(a, false, s);
     }
@@ -960,7 +1039,7 @@ void launch_backward(const nugpr_selective_scan* p, const ScanArgs& a, const nug
     constexpr bool FULL = decltype(full)::value;
     const dim3 spans((unsigned)(a.items * a.blocks)), all((unsigned)(a.items * a.blocks + ZERO_GROUPS)), threads(64 * W);
     hipLaunchKernelGGL((k_scan_tiles<TR, W, K, FULL>), spans, threads, 0, s, a);
-    if (!one_span(p)) launch_join(a, true, s);
+    if (!one_span(p, true)) launch_join(a, true, s);
     if (a.z) hipLaunchKernelGGL((k_scan_backward<TR, W, K, FULL, true>), all, threads, 0, s, a);
     else hipLaunchKernelGGL((k_scan_backward<TR, W, K, FULL, false>), all, threads, 0, s, a);
   });
@@ -991,7 +1070,7 @@ int nugpr_selective_scan_forward(const nugpr_selective_scan* p, const nugpr_rows
   NUGPR_TRY(check_call(p, false, &done));
   if (done) return NUGPR_OK;
   const size_t v = value_size(p);
-  ScanArgs a = scan_args(p);
+  ScanArgs a = scan_args(p, false);
   if (p->n_rows > 0) {
     NUGPR_TRY(check_rows(x, "x", v));
     NUGPR_TRY(check_rows(dt, "dt", v));
@@ -1033,7 +1112,7 @@ int nugpr_selective_scan_backward(const nugpr_selective_scan* p, const nugpr_row
   NUGPR_TRY(check_floats(d_final_state, "d_final_state", false));
   NUGPR_TRY(check_floats(d_initial_state, "d_initial_state", false));
   if (overlap(d_final_state, d_initial_state, (size_t)p->n_seqs * p->dim * p->dim_state * sizeof(float))) return invalid("d_initial_state overlaps d_final_state");
-  ScanArgs a = scan_args(p);
+  ScanArgs a = scan_args(p, true);
   if (p->n_rows > 0) {
     NUGPR_TRY(check_rows(x, "x", v));
     NUGPR_TRY(check_rows(dt, "dt", v));

@@ -35,7 +35,7 @@ struct ConvArgs {
 
 template <class TR>
 __device__ inline float gate(float p) {
-  return p * (TR::E == 4 ? sigmoid_of(p) : __builtin_amdgcn_rcpf(1.f + exp2_of(-LOG2_E * p)));
+  return p * sigmoid_of<TR>(p);
 }
 
 // A run of rows of one sequence (or of none), ending where that does.
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(THREADS) void k_short_conv(const ConvArgs a) {
 // dp from p and dy
 template <class TR>
 __device__ inline float gate_gradient(float p, float dy) {
-  const float s = TR::E == 4 ? sigmoid_of(p) : __builtin_amdgcn_rcpf(1.f + exp2_of(-LOG2_E * p));
+  const float s = sigmoid_of<TR>(p);
   return dy * s * fmaf(p, 1.f - s, 1.f);
 }
 
