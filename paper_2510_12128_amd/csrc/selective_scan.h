@@ -1,0 +1,92 @@
+// What the files of the selective scan share: its arguments, where a workgroup stands, and clearing rows.  selective_scan.hip says what the kernels do.
+#pragma once
+
+#include <type_traits>
+#include <utility>
+
+#include "nugpr_internal.h"
+#include "packed_rows.h"
+#include "row_values.h"
+
+namespace nugpr {
+
+constexpr int TILE_ROWS = 16;
+constexpr int ZERO_GROUPS = 128;     // workgroups that clear the rows without a sequence
+
+struct ScanArgs {
+  const void *x, *dt, *z, *B, *C, *dy;
+  void *y, *dx, *ddt, *dz;
+  int64_t x_row, dt_row, z_row, y_row, dy_row, dx_row, ddt_row, dz_row;
+  int64_t B_row, B_head, C_row, C_head;
+  const float *A, *D, *bias;
+  const float *s_in, *ds_end;        // states at the sequences' begin; gradients of those at their end
+  float *s_out, *ds_in;
+  const int64_t* off;
+  int64_t n_rows;
+  int n_seqs, dim, groups, each, states, softplus;             // each: channels of a group
+  int width, blocks;                 // channels of a workgroup; workgroups that have all
+  int share;                         // states of a wave (of each chunk): as even as they can be shared out
+  int span_log2, items;
+  float* adds;                       // items x dim x states: what a span adds to the state, then its start state
+  float* steps;                      // items x dim: sum of a span's d
+  float* back;                       // the same as adds, of the gradients
+  float* tiles;                      // tiles x blocks x threads x 4: states at the tiles' begin (from zero, but in a sequence's first span)
+  float* tile_steps;                 // tiles x dim: sum of the span's d before the tile
+  float *dB, *dC;                    // blocks of a group x n_rows x groups x states
+  float *dA, *dD, *dbias;            // items x dim (x states)
+  void *dB_out, *dC_out;             // the gradients themselves, from these parts
+  int64_t dB_row, dB_head, dC_row, dC_head;
+  float *dA_out, *dD_out, *dbias_out;
+};
+
+// Where a workgroup stands.
+struct Place {
+  int group, channel, valid;         // its first channel, and how many it has
+  PieceOf piece;
+  int64_t from, to;                  // its rows
+  int span;                          // of the sequence
+  bool last;                         // the sequence ends with it
+};
+
+__device__ __forceinline__ bool find(const ScanArgs& a, int item, int block, Place& p) {
+  const int of_group = a.blocks / a.groups, b = block % of_group;
+  p.group = block / of_group;
+  p.channel = p.group * a.each + b * a.width;
+  p.valid = min(a.width, a.each - b * a.width);
+  p.piece = piece_of(a.off, a.n_seqs, a.n_rows, a.span_log2, item);
+  if (p.piece.seq < 0) return false;
+  p.span = item - (int)((p.piece.lo >> a.span_log2) + p.piece.seq);
+  p.from = p.piece.lo + ((int64_t)p.span << a.span_log2);
+  if (p.span > 0 && p.from >= p.piece.hi) return false;
+  p.to = min(p.piece.hi, p.from + ((int64_t)1 << a.span_log2));
+  p.last = p.to == p.piece.hi;
+  return true;
+}
+
+// f(0), f(1), ..: with the number as a constant
+template <class F, int... I>
+__device__ __forceinline__ void repeat_all(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void repeat(F f) { repeat_all(f, std::make_integer_sequence<int, N>{}); }
+
+// Rows before the first sequence and behind the last are cleared by workgroups of their own.
+template <class TR>
+__device__ void clear_rows(const ScanArgs& a, int who, void* to, int64_t stride) {
+  if (!to) return;
+  const int64_t first = clamped(a.off[0], 0, a.n_rows), last = clamped(a.off[a.n_seqs], first, a.n_rows);
+  Values<TR, 4> zero;
+  zero.clear();
+  for (int64_t row = who; row < a.n_rows - (last - first); row += ZERO_GROUPS) {
+    typename TR::T* p = static_cast<typename TR::T*>(to) + (row < first ? row : row + (last - first)) * stride;
+    for (int col = threadIdx.x * 4; col < a.dim; col += blockDim.x * 4) zero.store(p + col, a.dim - col);
+  }
+}
+
+// The gradients' kernels (selective_scan_backward.hip): their workgroups' shape, and the launches.  join: the kernel that goes from what
+// spans add to their start states.
+int scan_backward_width(int states);       // channels of a workgroup
+int scan_backward_threads(int states);     // its threads
+int scan_backward_states(int states);      // states of a thread
+int launch_scan_backward(int dtype, const ScanArgs& a, bool one_span, void (*join)(const ScanArgs&, bool, hipStream_t), hipStream_t s);
+
+}  // namespace nugpr

@@ -17,43 +17,15 @@
 // A sequence is cut into spans where there are too few workgroups otherwise: a first pass finds what each span adds to the state, a
 // small one the spans' start states, and the last walks through the spans.
 #include <algorithm>
-#include <type_traits>
-#include <utility>
 
-#include "nugpr_internal.h"
-#include "packed_rows.h"
-#include "row_values.h"
+#include "selective_scan.h"
 
 namespace nugpr {
 
 namespace {
 
-constexpr int TILE_ROWS = 16;
 constexpr int CH = 64;               // channels of a workgroup
 constexpr int PER = 4;               // states of a wave, at most
-constexpr int ZERO_GROUPS = 128;     // workgroups that clear the rows without a sequence
-
-struct ScanArgs {
-  const void *x, *dt, *z, *B, *C, *dy;
-  void *y, *dx, *ddt, *dz;
-  int64_t x_row, dt_row, z_row, y_row, dy_row, dx_row, ddt_row, dz_row;
-  int64_t B_row, B_head, C_row, C_head;
-  const float *A, *D, *bias;
-  const float *s_in, *ds_end;        // states at the sequences' begin; gradients of those at their end
-  float *s_out, *ds_in;
-  const int64_t* off;
-  int64_t n_rows;
-  int n_seqs, dim, groups, each, blocks, states, softplus;     // each: channels of a group; blocks: of CH channels, all groups
-  int share;                         // states of a wave (of each chunk): as even as they can be shared out
-  int span_log2, items;
-  float* adds;                       // items x dim x states: what a span adds to the state, then its start state
-  float* steps;                      // items x dim: sum of a span's d
-  float* back;                       // the same as adds, of the gradients
-  float* tiles;                      // tiles x dim x states: states at the tiles' begin (from zero, but in a sequence's first span)
-  float* tile_steps;                 // tiles x dim: sum of the span's d before the tile
-  float *dB, *dC;                    // blocks of a group x n_rows x groups x states
-  float *dA, *dD, *dbias;            // items x dim (x states)
-};
 
 // Value I of those that 16 consecutive lanes hold.  (No instruction of its own: the one that uses it reads its operand so.)
 template <int I>
@@ -61,9 +33,8 @@ __device__ __forceinline__ float from_lane(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x150 + I, 0xf, 0xf, true));
 }
 
-// Products with N values side by side of those 16, from value I on, by instructions that read them where they are (s_nop: what a vector
+// Sum of N values side by side of those 16, from value I on, times h, by instructions that read them where they are (s_nop: what a vector
 // instruction has just written can be read so two steps later).
-//   dot: sum of values times h;  add_times: h[s] += x value
 template <int I, int N>
 __device__ __forceinline__ float dot(float v, const float (&h)[PER]) {
   float y;
@@ -80,54 +51,15 @@ __device__ __forceinline__ float dot(float v, const float (&h)[PER]) {
   }
   return y;
 }
-template <int I, int N>
-__device__ __forceinline__ void add_times(float (&h)[PER], float v, float x) {
-  if constexpr (N == 4)
-    asm("s_nop 1\n\tv_fmac_f32_dpp %0, %4, %5 row_newbcast:%6 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %1, %4, %5 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %2, %4, %5 row_newbcast:%8 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %3, %4, %5 row_newbcast:%9 row_mask:0xf bank_mask:0xf"
-        : "+v"(h[0]), "+v"(h[1]), "+v"(h[2]), "+v"(h[3]) : "v"(v), "v"(x), "n"(I), "n"(I + 1), "n"(I + 2), "n"(I + 3));
-  else {
-    h[0] = fmaf(from_lane<I>(v), x, h[0]);
-    if constexpr (N > 1) h[1] = fmaf(from_lane<I + 1>(v), x, h[1]);
-    if constexpr (N > 2) h[2] = fmaf(from_lane<I + 2>(v), x, h[2]);
-  }
-}
-
-// Where a workgroup stands.
-struct Place {
-  int group, channel, valid;         // its first channel, and how many it has
-  PieceOf piece;
-  int64_t from, to;                  // its rows
-  int span;                          // of the sequence
-  bool last;                         // the sequence ends with it
-};
-
-__device__ __forceinline__ bool find(const ScanArgs& a, int item, int block, Place& p) {
-  const int of_group = a.blocks / a.groups, b = block % of_group;
-  p.group = block / of_group;
-  p.channel = p.group * a.each + b * CH;
-  p.valid = min(CH, a.each - b * CH);
-  p.piece = piece_of(a.off, a.n_seqs, a.n_rows, a.span_log2, item);
-  if (p.piece.seq < 0) return false;
-  p.span = item - (int)((p.piece.lo >> a.span_log2) + p.piece.seq);
-  p.from = p.piece.lo + ((int64_t)p.span << a.span_log2);
-  if (p.span > 0 && p.from >= p.piece.hi) return false;
-  p.to = min(p.piece.hi, p.from + ((int64_t)1 << a.span_log2));
-  p.last = p.to == p.piece.hi;
-  return true;
-}
-
-// A tile's rows as memory has them: a thread holds V channels of one row, and one value of B and C for each chunk.  GRADIENT: dy too; OUT:
-// what the output needs beside the states.
-template <class TR, int WAVES, int CHUNKS, bool GRADIENT, bool OUT>
+// A tile's rows as memory has them: a thread holds V channels of one row, and one value of B and C for each chunk.  OUT: what
+// the output needs beside the states.
+template <class TR, int WAVES, int CHUNKS, bool OUT>
 struct Incoming {
   typedef typename TR::T T;
   static constexpr int V = TILE_ROWS / WAVES;
-  Values<TR, V> x, dt, z, dy;
+  Values<TR, V> x, dt, z;
   T b[CHUNKS], c[CHUNKS];
-  const T *px, *pdt, *pz, *pdy, *pb, *pc;          // the thread's, of the tile that is loaded next
+  const T *px, *pdt, *pz, *pb, *pc;          // the thread's, of the tile that is loaded next
   // row0: the tile's first row
   __device__ __forceinline__ void begin(const ScanArgs& a, const Place& p, int64_t row0) {
     const int64_t row = row0 + threadIdx.x / (CH / V), brow = row0 + threadIdx.x / (PER * WAVES);
@@ -135,25 +67,22 @@ struct Incoming {
     px = static_cast<const T*>(a.x) + row * a.x_row + at;
     pdt = static_cast<const T*>(a.dt) + row * a.dt_row + at;
     if (OUT) pz = static_cast<const T*>(a.z) + row * a.z_row + at;
-    if (GRADIENT) pdy = static_cast<const T*>(a.dy) + row * a.dy_row + at;
     pb = static_cast<const T*>(a.B) + brow * a.B_row + p.group * a.B_head + n;
     if (OUT) pc = static_cast<const T*>(a.C) + brow * a.C_row + p.group * a.C_head + n;
   }
-  // n_rows of the tile, then the pointers move on by `way` tiles
+  // n_rows of the tile, then the pointers move on
   template <bool FULL>
-  __device__ __forceinline__ void load(const ScanArgs& a, const Place& p, int n_rows, int way) {
+  __device__ __forceinline__ void load(const ScanArgs& a, const Place& p, int n_rows) {
     const bool whole = n_rows == TILE_ROWS && p.valid == CH;
     const int valid = whole ? V : (int)threadIdx.x / (CH / V) < n_rows ? p.valid - (int)threadIdx.x % (CH / V) * V : 0;
     if (whole) {
       x.load_all(px);
       dt.load_all(pdt);
       if (OUT && a.z) z.load_all(pz);
-      if (GRADIENT && OUT) dy.load_all(pdy);
     } else {
       x.load(px, valid);
       dt.load(pdt, valid);
       if (OUT && a.z) z.load(pz, valid);
-      if (GRADIENT && OUT) dy.load(pdy, valid);
     }
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) {
@@ -164,23 +93,15 @@ struct Incoming {
         if (OUT) c[k] = pc[k * WAVES * a.share];
       }
     }
-    const int64_t rows = (int64_t)way * TILE_ROWS;
-    px += rows * a.x_row;
-    pdt += rows * a.dt_row;
-    pb += rows * a.B_row;
+    px += TILE_ROWS * a.x_row;
+    pdt += TILE_ROWS * a.dt_row;
+    pb += TILE_ROWS * a.B_row;
     if (OUT) {
-      pz += rows * a.z_row;
-      pc += rows * a.C_row;
-      if (GRADIENT) pdy += rows * a.dy_row;
+      pz += TILE_ROWS * a.z_row;
+      pc += TILE_ROWS * a.C_row;
     }
   }
 };
-
-// f(0), f(1), ..: with the number as a constant
-template <class F, int... I>
-__device__ __forceinline__ void repeat_all(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
-template <int N, class F>
-__device__ __forceinline__ void repeat(F f) { repeat_all(f, std::make_integer_sequence<int, N>{}); }
 
 // Sum over the waves' parts.
 template <int V>
@@ -240,18 +161,17 @@ __device__ __forceinline__ void load_channels(float (&v)[V], const float* p, int
 }
 
 // What a tile's rows are read from, while its states are walked through.
-template <int WAVES, int CHUNKS, bool GRADIENT>
+template <int WAVES, int CHUNKS>
 struct Tile {
   float2 du[TILE_ROWS][CH];                        // d and u
   float B[CHUNKS][TILE_ROWS][PER * WAVES], C[CHUNKS][TILE_ROWS][PER * WAVES];
-  float e[GRADIENT ? TILE_ROWS : 1][CH];
 };
 
 // Makes a tile's rows from what came in.  Rows and channels that there are not: d = u = 0, which leaves a state as it is.  steps: sums
 // of d, a row of every tile a thread; bias: of the thread's channels.
-template <class TR, int WAVES, int CHUNKS, bool GRADIENT, bool OUT>
-__device__ __forceinline__ void fill_tile(Tile<WAVES, CHUNKS, GRADIENT>& tile, const ScanArgs& a, const Incoming<TR, WAVES, CHUNKS, GRADIENT, OUT>& in,
-                                          int n_rows, int valid, const float* bias, float (&steps)[TILE_ROWS / WAVES]) {
+template <class TR, int WAVES, int CHUNKS, bool OUT>
+__device__ __forceinline__ void fill_tile(Tile<WAVES, CHUNKS>& tile, const ScanArgs& a, const Incoming<TR, WAVES, CHUNKS, OUT>& in, int n_rows, int valid,
+                                          const float* bias, float (&steps)[TILE_ROWS / WAVES]) {
   constexpr int V = TILE_ROWS / WAVES;
   const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
   float d[V];
@@ -267,16 +187,6 @@ __device__ __forceinline__ void fill_tile(Tile<WAVES, CHUNKS, GRADIENT>& tile, c
   for (int j = 0; j < V; ++j) {
     steps[j] += d[j];
     tile.du[r][col + j] = float2{d[j], d[j] * in.x.get(j)};
-  }
-  if constexpr (GRADIENT && OUT) {
-    float e[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) e[j] = in.dy.get(j);
-    if (a.z)
-#pragma unroll
-      for (int j = 0; j < V; ++j) e[j] *= in.z.get(j) * sigmoid_of<TR>(in.z.get(j));
-#pragma unroll
-    for (int j = 0; j < V; ++j) tile.e[r][col + j] = e[j];
   }
   const int br = threadIdx.x / (PER * WAVES), n = threadIdx.x % (PER * WAVES);
 #pragma unroll
@@ -323,28 +233,6 @@ __device__ __forceinline__ void walk_tile(float (&h)[PER], const float (&a2)[PER
   });
 }
 
-// The same without output, and the product of the factors so far, and what e C adds to the gradient by the state before the tile's rows.
-template <int N, class T>
-__device__ __forceinline__ void walk_tile_back(float (&h)[PER], float (&product)[PER], float (&g)[PER], const float (&a2)[PER], const T& tile, int k, int wave,
-                                      int lane) {
-  const int row = (lane & 15) / PER, n = wave * PER + lane % PER;
-  repeat<TILE_ROWS / 4>([&](auto q) __attribute__((always_inline)) {
-    const float vb = tile.B[k][4 * q + row][n], vc = tile.C[k][4 * q + row][n];
-    repeat<4>([&](auto i) __attribute__((always_inline)) {
-      constexpr int t = 4 * q + i;
-      const float2 du = tile.du[t][lane];
-      const float e = tile.e[t][lane];
-      repeat<N>([&](auto s) __attribute__((always_inline)) {
-        constexpr int at = PER * i + s;
-        const float f = exp2_of(du.x * a2[s]);
-        h[s] = fmaf(f, h[s], du.y * from_lane<at>(vb));
-        product[s] *= f;
-        g[s] = fmaf(product[s], e * from_lane<at>(vc), g[s]);
-      });
-    });
-  });
-}
-
 // For every chunk: f(the chunk, the number of the wave's states in it, as a constant); full: all have PER.
 template <int WAVES, int CHUNKS, bool FULL, class F>
 __device__ __forceinline__ void with_states(const ScanArgs& a, int wave, F f) {
@@ -361,25 +249,12 @@ __device__ __forceinline__ void with_states(const ScanArgs& a, int wave, F f) {
   });
 }
 
-// Rows before the first sequence and behind the last are cleared by workgroups of their own.
-template <class TR>
-__device__ void clear_rows(const ScanArgs& a, int who, void* to, int64_t stride) {
-  if (!to) return;
-  const int64_t first = clamped(a.off[0], 0, a.n_rows), last = clamped(a.off[a.n_seqs], first, a.n_rows);
-  Values<TR, 4> zero;
-  zero.clear();
-  for (int64_t row = who; row < a.n_rows - (last - first); row += ZERO_GROUPS) {
-    typename TR::T* p = static_cast<typename TR::T*>(to) + (row < first ? row : row + (last - first)) * stride;
-    for (int col = threadIdx.x * 4; col < a.dim; col += blockDim.x * 4) zero.store(p + col, a.dim - col);
-  }
-}
-
 // ADDS: what a span adds to the state, and the sum of its d; else the walk that writes y.
 template <class TR, int WAVES, int CHUNKS, bool FULL, bool ADDS>
 __global__ __launch_bounds__(64 * WAVES) void k_scan(const ScanArgs a) {
   typedef typename TR::T T;
   constexpr int V = TILE_ROWS / WAVES;
-  __shared__ Tile<WAVES, CHUNKS, false> tile;
+  __shared__ Tile<WAVES, CHUNKS> tile;
   __shared__ float part[ADDS ? 1 : WAVES][TILE_ROWS][CH];
   const int item = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
   if (!ADDS && item >= a.items) {
@@ -403,16 +278,16 @@ __global__ __launch_bounds__(64 * WAVES) void k_scan(const ScanArgs a) {
   load_channels(D, a.D, p.channel, col, p.valid);
 #pragma unroll
   for (int j = 0; j < V; ++j) steps[j] = 0.f;
-  Incoming<TR, WAVES, CHUNKS, false, !ADDS> in;
+  Incoming<TR, WAVES, CHUNKS, !ADDS> in;
   in.begin(a, p, p.from);
-  in.template load<FULL>(a, p, (int)min((int64_t)TILE_ROWS, p.to - p.from), 1);
+  in.template load<FULL>(a, p, (int)min((int64_t)TILE_ROWS, p.to - p.from));
   for (int64_t t0 = p.from; t0 < p.to; t0 += TILE_ROWS) {
     const int rows = (int)min((int64_t)TILE_ROWS, p.to - t0);
     if (ADDS) __syncthreads();                     // (the walk's second one has this effect)
     fill_tile(tile, a, in, rows, p.valid, bias, steps);
     const auto now = in;
     __syncthreads();
-    if (t0 + TILE_ROWS < p.to) in.template load<FULL>(a, p, (int)min((int64_t)TILE_ROWS, p.to - t0 - TILE_ROWS), 1);
+    if (t0 + TILE_ROWS < p.to) in.template load<FULL>(a, p, (int)min((int64_t)TILE_ROWS, p.to - t0 - TILE_ROWS));
     with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) __attribute__((always_inline)) {
       walk_tile<decltype(n)::value, !ADDS>(h.v[k], a2.v[k], tile, k, wave, lane, part[ADDS ? 0 : wave]);
     });
@@ -493,318 +368,6 @@ __global__ __launch_bounds__(256) void k_scan_join(const ScanArgs a) {
       }
     }
   }
-}
-
-// ---- gradients ------------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ int64_t first_tile(const Place& p) { return p.piece.lo / TILE_ROWS + p.piece.seq + (p.from - p.piece.lo) / TILE_ROWS; }
-
-// The states at the begin of every tile, what a span adds, and what it adds to the gradient by the state before it.
-template <class TR, int WAVES, int CHUNKS, bool FULL>
-__global__ __launch_bounds__(64 * WAVES) void k_scan_tiles(const ScanArgs a) {
-  constexpr int V = TILE_ROWS / WAVES;
-  __shared__ Tile<WAVES, CHUNKS, true> tile;
-  __shared__ float part[TILE_ROWS][CH];
-  const int item = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
-  Place p;
-  if (!find(a, item, block, p)) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int col = threadIdx.x % (CH / V) * V;
-  const bool live = lane < p.valid;
-  const int64_t of_lane = (int64_t)(p.channel + lane) * a.states, each = (int64_t)a.dim * a.states;
-  States<WAVES, CHUNKS> h, a2, product, g;
-  float bias[V], steps[V];
-  a2.load(a, a.A + of_lane, wave, live);
-  a2.scale(LOG2_E);
-  product.fill(1.f);
-  g.fill(0.f);
-  const float* start = p.span == 0 && a.s_in ? a.s_in + p.piece.seq * each : nullptr;
-  h.load(a, start + of_lane, wave, live && start);
-  load_channels(bias, a.bias, p.channel, col, p.valid);
-#pragma unroll
-  for (int j = 0; j < V; ++j) steps[j] = 0.f;
-  int64_t number = first_tile(p);
-  float passed = 0.f;                              // sum of d before the tile (first wave)
-  // (a sequence's first span has no state before it whose gradient were wanted)
-  auto walk = [&](auto later) __attribute__((always_inline)) {
-    constexpr bool LATER = decltype(later)::value;
-    Incoming<TR, WAVES, CHUNKS, true, LATER> in;
-    in.begin(a, p, p.from);
-    if (p.from < p.to) in.template load<FULL>(a, p, (int)min((int64_t)TILE_ROWS, p.to - p.from), 1);
-    for (int64_t t0 = p.from; t0 < p.to; t0 += TILE_ROWS, ++number) {
-      const int rows = (int)min((int64_t)TILE_ROWS, p.to - t0);
-      h.store(a, a.tiles + number * each + of_lane, wave, live);
-      __syncthreads();
-      fill_tile(tile, a, in, rows, p.valid, bias, steps);
-      __syncthreads();
-      if (t0 + TILE_ROWS < p.to) in.template load<FULL>(a, p, (int)min((int64_t)TILE_ROWS, p.to - t0 - TILE_ROWS), 1);
-      if (LATER && wave == 0 && live) {
-        a.tile_steps[number * a.dim + p.channel + lane] = passed;
-#pragma unroll
-        for (int t = 0; t < TILE_ROWS; ++t) passed += tile.du[t][lane].x;
-      }
-      with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto k, auto n) __attribute__((always_inline)) {
-        if constexpr (LATER) walk_tile_back<decltype(n)::value>(h.v[k], product.v[k], g.v[k], a2.v[k], tile, k, wave, lane);
-        else walk_tile<decltype(n)::value, false>(h.v[k], a2.v[k], tile, k, wave, lane, part);
-      });
-    }
-  };
-  if (p.span > 0) walk(std::true_type{});
-  else walk(std::false_type{});
-  if (p.span == 0 && p.last) return;
-  h.store(a, a.adds + item * each + of_lane, wave, live && !p.last);
-  g.store(a, a.back + item * each + of_lane, wave, live && p.span > 0);
-  sum_rows(steps, part, a.steps + (int64_t)item * a.dim + p.channel, p.valid);
-}
-
-__device__ __forceinline__ void swap_halves(float& x, float& y) {
-  const auto v = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
-  x = __builtin_bit_cast(float, (uint32_t)v[0]);
-  y = __builtin_bit_cast(float, (uint32_t)v[1]);
-}
-__device__ __forceinline__ void swap_rows(float& x, float& y) {
-  const auto v = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
-  x = __builtin_bit_cast(float, (uint32_t)v[0]);
-  y = __builtin_bit_cast(float, (uint32_t)v[1]);
-}
-template <int CTRL>
-__device__ __forceinline__ float moved(float v) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
-}
-
-// Sums over the wave's lanes of four rows x four states: lane l gets the one of row l / 16, state l % 16 / 4.  Two numbers are joined in one
-// register at each step, so that 16 sums take 35 instructions instead of 96.
-__device__ __forceinline__ float lane_sums(float (&v)[4][PER], int lane) {
-  float w[2][PER], z[PER];
-#pragma unroll
-  for (int s = 0; s < PER; ++s) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      swap_halves(v[i][s], v[i + 2][s]);
-      w[i][s] = v[i][s] + v[i + 2][s];
-    }
-    swap_rows(w[0][s], w[1][s]);
-    z[s] = w[0][s] + w[1][s];
-  }
-  const bool upper8 = lane & 8, upper4 = lane & 4;
-  float k[2];
-#pragma unroll
-  for (int s = 0; s < 2; ++s) k[s] = (upper8 ? z[s + 2] : z[s]) + moved<0x128>(upper8 ? z[s] : z[s + 2]);     // eight lanes on
-  float x = (upper4 ? k[1] : k[0]) + moved<0x141>(upper4 ? k[0] : k[1]);                                     // mirrored among eight
-  x += moved<0xb1>(x);
-  x += moved<0x4e>(x);
-  return x;
-}
-
-// A wave's N states of chunk k over one tile: forward from its first states, then back.  The parts stand beside those of the chunks before;
-// dB, dC: of the tile's first row and the wave's first state, rows `stride` apart.
-template <int N, bool GATE, class T>
-__device__ __forceinline__ void back_tile(float (&g)[PER], float (&dA)[PER], const float (&h0)[PER], const float (&a2)[PER], const T& tile, int k, int wave,
-                                 int lane, float (*part_u)[CH], float (*part_d)[CH], float (*part_y)[CH], float* dB, float* dC, int64_t stride,
-                                 int rows) {
-  const int row = (lane & 15) / PER, n = wave * PER + lane % PER;
-  const int sum_row = lane / 16, sum_state = lane % 16 / 4;       // (of lane_sums)
-  float h[TILE_ROWS + 1][PER], f[TILE_ROWS][PER];                 // h_{t-1} and on, a_t
-#pragma unroll
-  for (int s = 0; s < PER; ++s) h[0][s] = h0[s];
-  repeat<TILE_ROWS / 4>([&](auto q) __attribute__((always_inline)) {
-    const float vb = tile.B[k][4 * q + row][n], vc = tile.C[k][4 * q + row][n];
-    float sums[4][PER];
-    repeat<4>([&](auto i) __attribute__((always_inline)) {
-      constexpr int t = 4 * q + i;
-      const float2 du = tile.du[t][lane];
-      const float e = tile.e[t][lane];
-#pragma unroll
-      for (int s = N; s < PER; ++s) sums[i][s] = 0.f;
-      repeat<N>([&](auto s) __attribute__((always_inline)) {
-        constexpr int at = PER * i + s;
-        f[t][s] = exp2_of(du.x * a2[s]);
-        h[t + 1][s] = fmaf(f[t][s], h[t][s], du.y * from_lane<at>(vb));
-        sums[i][s] = e * h[t + 1][s];
-      });
-      if constexpr (GATE) {
-        const float y = dot<PER * i, N>(vc, h[t + 1]);
-        part_y[t][lane] = k ? part_y[t][lane] + y : y;
-      }
-    });
-    const float c = lane_sums(sums, lane);
-    if (lane % 4 == 0 && 4 * q + sum_row < rows && sum_state < N) dC[(4 * q + sum_row) * stride + sum_state] = c;
-    __builtin_amdgcn_sched_barrier(0);             // (what comes later is not read earlier: its registers are needed)
-  });
-  repeat<TILE_ROWS / 4>([&](auto back) __attribute__((always_inline)) {
-    constexpr int q = TILE_ROWS / 4 - 1 - back;
-    const float vb = tile.B[k][4 * q + row][n], vc = tile.C[k][4 * q + row][n];
-    float sums[4][PER];
-    repeat<4>([&](auto j) __attribute__((always_inline)) {
-      constexpr int i = 3 - j, t = 4 * q + i;
-      const float2 du = tile.du[t][lane];
-      const float e = tile.e[t][lane];
-      add_times<PER * i, N>(g, vc, e);
-      const float by_u = dot<PER * i, N>(vb, g);
-      float by_d = 0.f;
-#pragma unroll
-      for (int s = N; s < PER; ++s) sums[i][s] = 0.f;
-      repeat<N>([&](auto s) __attribute__((always_inline)) {
-        sums[i][s] = g[s] * du.y;
-        g[s] *= f[t][s];
-        const float x = g[s] * h[t][s];
-        dA[s] = fmaf(x, du.x, dA[s]);
-        by_d = s == 0 ? x * a2[s] : fmaf(x, a2[s], by_d);
-      });
-      part_u[t][lane] = k ? part_u[t][lane] + by_u : by_u;
-      part_d[t][lane] = k ? part_d[t][lane] + by_d : by_d;
-    });
-    const float b = lane_sums(sums, lane);
-    if (lane % 4 == 0 && 4 * q + sum_row < rows && sum_state < N) dB[(4 * q + sum_row) * stride + sum_state] = b;
-    __builtin_amdgcn_sched_barrier(0);
-  });
-}
-
-template <class TR, int WAVES, int CHUNKS, bool FULL, bool GATE>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_scan_backward(const ScanArgs a) {
-  typedef typename TR::T T;
-  constexpr int V = TILE_ROWS / WAVES;
-  __shared__ Tile<WAVES, CHUNKS, true> tile;
-  __shared__ float part[GATE ? 3 : 2][WAVES][TILE_ROWS][CH], of_channel[2][CH];      // (the channels' bias and D)
-  const int item = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
-  if (item >= a.items) {
-    const int who = blockIdx.x - a.items * a.blocks;
-    clear_rows<TR>(a, who, a.dx, a.dx_row);
-    clear_rows<TR>(a, who, a.ddt, a.ddt_row);
-    clear_rows<TR>(a, who, a.dz, a.dz_row);
-    return;
-  }
-  Place p;
-  const bool found = find(a, item, block, p);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int waves = min(WAVES, (a.states + a.share - 1) / a.share);
-  const int r = threadIdx.x / (CH / V), col = threadIdx.x % (CH / V) * V;
-  const bool live = lane < p.valid;
-  const int64_t of_lane = (int64_t)(p.channel + lane) * a.states, each = (int64_t)a.dim * a.states;
-  States<WAVES, CHUNKS> dA;
-  float dD[V], dbias[V];
-  dA.fill(0.f);
-#pragma unroll
-  for (int j = 0; j < V; ++j) dD[j] = dbias[j] = 0.f;
-  if (found) {
-    States<WAVES, CHUNKS> g, a2;
-    float steps[V];
-    if (threadIdx.x < CH) {
-      const bool mine = (int)threadIdx.x < p.valid;
-      of_channel[0][threadIdx.x] = mine && a.bias ? a.bias[p.channel + threadIdx.x] : 0.f;
-      of_channel[1][threadIdx.x] = mine && a.D ? a.D[p.channel + threadIdx.x] : 0.f;
-    }
-    __syncthreads();
-    a2.load(a, a.A + of_lane, wave, live);
-    a2.scale(LOG2_E);
-    const float* end = p.last && p.span == 0 ? (a.ds_end ? a.ds_end + p.piece.seq * each : nullptr) : a.back + item * each;
-    g.load(a, end + of_lane, wave, live && end);
-    const int tiles = (int)((p.to - p.from + TILE_ROWS - 1) / TILE_ROWS);
-    const int64_t number = first_tile(p), stride = (int64_t)a.groups * a.states;
-    // (of the group's blocks this one's parts of dB and dC)
-    const int64_t part_at = (int64_t)(block % (a.blocks / a.groups)) * a.n_rows * stride + p.group * a.states;
-    Incoming<TR, WAVES, CHUNKS, true, true> in;
-    in.begin(a, p, p.from + (int64_t)(tiles - 1) * TILE_ROWS);
-    if (tiles > 0) in.template load<FULL>(a, p, (int)(p.to - p.from - (int64_t)(tiles - 1) * TILE_ROWS), -1);
-    for (int k = tiles - 1; k >= 0; --k) {
-      const int64_t t0 = p.from + (int64_t)k * TILE_ROWS;
-      const int rows = (int)min((int64_t)TILE_ROWS, p.to - t0);
-      States<WAVES, CHUNKS> h0;
-      h0.load(a, a.tiles + (number + k) * each + of_lane, wave, live);
-      if (p.span > 0 && live) {
-        States<WAVES, CHUNKS> start;
-        start.load(a, a.adds + item * each + of_lane, wave, true);
-        const float d = a.tile_steps[(number + k) * a.dim + p.channel + lane];
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-          for (int s = 0; s < PER; ++s)
-            h0.v[c][s] = start.v[c][s] == 0.f ? h0.v[c][s] : fmaf(exp2_of(a2.v[c][s] * d), start.v[c][s], h0.v[c][s]);
-      }
-      fill_tile(tile, a, in, rows, p.valid, of_channel[0] + col, steps);
-      const auto now = in;
-      __syncthreads();
-      if (k > 0) in.template load<FULL>(a, p, TILE_ROWS, -1);
-      with_states<WAVES, CHUNKS, FULL>(a, wave, [&](auto c, auto n) __attribute__((always_inline)) {
-        const int64_t at = part_at + t0 * stride + (c * WAVES + wave) * a.share;
-        back_tile<decltype(n)::value, GATE>(g.v[c], dA.v[c], h0.v[c], a2.v[c], tile, c, wave, lane, part[0][wave], part[1][wave], part[GATE ? 2 : 0][wave], a.dB + at,
-                                      a.dC + at, stride, rows);
-      });
-      __syncthreads();
-      float du[V], dd[V], y[V], dx[V], ddt[V], dz[V];
-      gather(part[0], waves, r, col, du);
-      gather(part[1], waves, r, col, dd);
-      if constexpr (GATE) gather(part[2], waves, r, col, y);
-      const bool there = r < rows;
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float d = tile.du[r][col + j].x, e = tile.e[r][col + j], x = now.x.get(j), raw = now.dt.get(j) + of_channel[0][col + j], D = of_channel[1][col + j];
-        dx[j] = a.D ? fmaf(D, e, d * du[j]) : d * du[j];
-        ddt[j] = fmaf(x, du[j], LN_2 * dd[j]);
-        if (a.softplus) ddt[j] *= sigmoid_of<TR>(raw);
-        if (there && col + j < p.valid) {
-          dD[j] = fmaf(e, x, dD[j]);
-          dbias[j] += ddt[j];
-        }
-        dz[j] = 0.f;
-        if constexpr (GATE) {
-          const float z = now.z.get(j), s = sigmoid_of<TR>(z);
-          dz[j] = now.dy.get(j) * (a.D ? fmaf(D, x, y[j]) : y[j]) * s * fmaf(z, 1.f - s, 1.f);
-        }
-      }
-      if (there) {
-        Values<TR, V> o;
-        o.put(dx);
-        o.store(static_cast<T*>(a.dx) + (t0 + r) * a.dx_row + p.channel + col, p.valid - col);
-        o.put(ddt);
-        o.store(static_cast<T*>(a.ddt) + (t0 + r) * a.ddt_row + p.channel + col, p.valid - col);
-        if constexpr (GATE) {
-          o.put(dz);
-          o.store(static_cast<T*>(a.dz) + (t0 + r) * a.dz_row + p.channel + col, p.valid - col);
-        }
-      }
-      __syncthreads();                             // (the tile is read above)
-    }
-    if (p.span == 0 && a.ds_in) g.store(a, a.ds_in + p.piece.seq * each + of_lane, wave, live);
-  }
-  // (items that are no span have sums too: zero)
-  dA.store(a, a.dA + item * each + of_lane, wave, live);
-  if (a.D) sum_rows(dD, part[0][0], a.dD + (int64_t)item * a.dim + p.channel, p.valid);
-  if (a.bias) sum_rows(dbias, part[0][0], a.dbias + (int64_t)item * a.dim + p.channel, p.valid);
-}
-
-// dB and dC from the channel blocks' parts, in their order; zero where no sequence owns the row.
-template <class TR>
-__global__ __launch_bounds__(256) void k_scan_sum_blocks(const ScanArgs a, void* dB, int64_t dB_row, int64_t dB_head, void* dC, int64_t dC_row,
-                                                         int64_t dC_head) {
-  typedef typename TR::T T;
-  const int64_t stride = (int64_t)a.groups * a.states, total = a.n_rows * stride, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= total) return;
-  const int64_t row = at / stride;
-  const int group = (int)(at % stride) / a.states, n = (int)(at % stride) % a.states, parts = a.blocks / a.groups;
-  const int64_t first = clamped(a.off[0], 0, a.n_rows), last = clamped(a.off[a.n_seqs], first, a.n_rows);
-  const float* from = (blockIdx.y ? a.dC : a.dB) + at;
-  float s = 0.f;
-  if (row >= first && row < last)
-    for (int k = 0; k < parts; ++k) s += from[k * total];
-  if (blockIdx.y) static_cast<T*>(dC)[row * dC_row + group * dC_head + n] = TR::put(s);
-  else static_cast<T*>(dB)[row * dB_row + group * dB_head + n] = TR::put(s);
-}
-
-// dA, dD and dbias from the spans' parts, in their order: each wave of a workgroup a quarter of them.
-__global__ __launch_bounds__(256) void k_scan_sum_items(const ScanArgs a, float* dA, float* dD, float* dbias) {
-  __shared__ float part[4][64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const float* from = blockIdx.y == 0 ? a.dA : blockIdx.y == 1 ? a.dD : a.dbias;
-  float* to = blockIdx.y == 0 ? dA : blockIdx.y == 1 ? dD : dbias;
-  const int64_t size = (int64_t)a.dim * (blockIdx.y == 0 ? a.states : 1), at = (int64_t)blockIdx.x * 64 + lane;
-  if (!to || (int64_t)blockIdx.x * 64 >= size) return;
-  const int each = (a.items + 3) / 4, end = min(a.items, (wave + 1) * each);
-  float s = 0.f;
-  if (at < size)
-    for (int k = wave * each; k < end; ++k) s += from[k * size + at];
-  part[wave][lane] = s;
-  __syncthreads();
-  if (wave == 0 && at < size) to[at] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
 }
 
 // ---- single tokens --------------------------------------------------------------------------------------------------------
@@ -919,13 +482,19 @@ bool overlap(const void* a, const void* b, size_t bytes) {
 int waves_of(const nugpr_selective_scan* p) { return p->dim_state > 4 * PER ? 8 : 4; }
 int chunks_of(const nugpr_selective_scan* p) { return p->dim_state > 8 * PER ? 2 : 1; }
 
-int blocks_of(const nugpr_selective_scan* p) { return p->groups * ((p->dim / p->groups + CH - 1) / CH); }
+// The workgroups' channels and threads, and how many have all channels.
+int width_of(const nugpr_selective_scan* p, bool backward) { return backward ? scan_backward_width(p->dim_state) : CH; }
+int threads_of(const nugpr_selective_scan* p, bool backward) { return backward ? scan_backward_threads(p->dim_state) : 64 * waves_of(p); }
+int blocks_of(const nugpr_selective_scan* p, bool backward) {
+  const int each = p->dim / p->groups, width = width_of(p, backward);
+  return p->groups * ((each + width - 1) / width);
+}
 
 // Rows of a span: a power of two, a few tiles at least, so large that the spans of the rows give about 8192 waves, 4096 in the gradients, of
 // which a compute unit holds a third as many.
 int span_log2(const nugpr_selective_scan* p, bool backward) {
   int k = 6;
-  while (k < 40 && ((p->n_rows * blocks_of(p) * waves_of(p)) >> k) > (backward ? 4096 : 8192)) ++k;
+  while (k < 40 && ((p->n_rows * blocks_of(p, backward) * (threads_of(p, backward) / 64)) >> k) > (backward ? 4096 : 8192)) ++k;
   return k;
 }
 bool one_span(const nugpr_selective_scan* p, bool backward) { return p->n_rows <= (int64_t)1 << span_log2(p, backward); }
@@ -953,9 +522,9 @@ size_t lay_out(const nugpr_selective_scan* p, bool backward, void* ws, ScanArgs*
   a->adds = w.take(spans ? items * states : 0);
   a->steps = w.take(spans ? items * p->dim : 0);
   if (backward) {
-    const size_t parts = (size_t)(blocks_of(p) / p->groups) * p->n_rows * p->groups * p->dim_state;
+    const size_t parts = (size_t)(blocks_of(p, true) / p->groups) * p->n_rows * p->groups * p->dim_state;
     a->back = w.take(spans ? items * states : 0);
-    a->tiles = w.take(tiles * states);
+    a->tiles = w.take(tiles * blocks_of(p, true) * threads_of(p, true) * scan_backward_states(p->dim_state));
     a->tile_steps = w.take(spans ? tiles * p->dim : 0);
     a->dB = w.take(parts);
     a->dC = w.take(parts);
@@ -981,7 +550,7 @@ int check_call(const nugpr_selective_scan* p, bool backward, bool* done) {
   if (*done) return NUGPR_OK;
   if (p->n_seqs < 1 || !p->seq_offsets) return invalid("seq_offsets is null, or there is no sequence");
   // (the threads of a launch are counted in 32 bits)
-  if (items_of(p, backward) * blocks_of(p) + ZERO_GROUPS > (int64_t)0xffffffff / (64 * waves_of(p)) ||
+  if (items_of(p, backward) * blocks_of(p, backward) + ZERO_GROUPS > (int64_t)0xffffffff / threads_of(p, backward) ||
       (backward && p->n_rows * p->groups * p->dim_state > (int64_t)0xffffffff - 256))
     return invalid("too many rows, sequences and channels for one call");
   const size_t need = lay_out(p, backward, nullptr, nullptr);
@@ -993,7 +562,7 @@ int check_call(const nugpr_selective_scan* p, bool backward, bool* done) {
 ScanArgs scan_args(const nugpr_selective_scan* p, bool backward) {
   ScanArgs a{};
   a.A = p->A; a.D = p->D; a.bias = p->dt_bias; a.off = p->seq_offsets; a.n_rows = p->n_rows; a.n_seqs = p->n_seqs;
-  a.dim = p->dim; a.groups = p->groups; a.each = p->dim / p->groups; a.blocks = blocks_of(p); a.states = p->dim_state;
+  a.dim = p->dim; a.groups = p->groups; a.each = p->dim / p->groups; a.width = width_of(p, backward); a.blocks = blocks_of(p, backward); a.states = p->dim_state;
   a.softplus = p->softplus != 0; a.share = (p->dim_state + waves_of(p) * chunks_of(p) - 1) / (waves_of(p) * chunks_of(p)); a.span_log2 = span_log2(p, backward); a.items = (int)items_of(p, backward);
   return a;
 }
@@ -1029,25 +598,6 @@ void launch_forward(const nugpr_selective_scan* p, const ScanArgs& a, hipStream_
     }
     hipLaunchKernelGGL((k_scan<TR, W, K, FULL, false>), all, threads, 0, s, a);
   });
-}
-
-template <class TR>
-void launch_backward(const nugpr_selective_scan* p, const ScanArgs& a, const nugpr_heads* dB, const nugpr_heads* dC, float* dA, float* dD, float* dbias,
-                     hipStream_t s) {
-  with_waves(p, [&](auto w, auto chunks, auto full) {
-    constexpr int W = decltype(w)::value, K = decltype(chunks)::value;
-    constexpr bool FULL = decltype(full)::value;
-    const dim3 spans((unsigned)(a.items * a.blocks)), all((unsigned)(a.items * a.blocks + ZERO_GROUPS)), threads(64 * W);
-    hipLaunchKernelGGL((k_scan_tiles<TR, W, K, FULL>), spans, threads, 0, s, a);
-    if (!one_span(p, true)) launch_join(a, true, s);
-    if (a.z) hipLaunchKernelGGL((k_scan_backward<TR, W, K, FULL, true>), all, threads, 0, s, a);
-    else hipLaunchKernelGGL((k_scan_backward<TR, W, K, FULL, false>), all, threads, 0, s, a);
-  });
-  const int64_t values = a.n_rows * a.groups * a.states, each = (int64_t)a.dim * a.states;
-  if (values)
-    hipLaunchKernelGGL(k_scan_sum_blocks<TR>, dim3((unsigned)((values + 255) / 256), 2), dim3(256), 0, s, a, dB->data, dB->row_stride, dB->head_stride,
-                       dC->data, dC->row_stride, dC->head_stride);
-  hipLaunchKernelGGL(k_scan_sum_items, dim3((unsigned)((each + 63) / 64), 3), dim3(256), 0, s, a, dA, a.D ? dD : nullptr, a.bias ? dbias : nullptr);
 }
 
 }  // namespace
@@ -1138,18 +688,13 @@ int nugpr_selective_scan_backward(const nugpr_selective_scan* p, const nugpr_row
   }
   a.s_in = initial_state; a.ds_end = d_final_state; a.ds_in = d_initial_state;
   lay_out(p, true, p->workspace, &a);
-  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (done) {                                      // no rows, no sequences: the sums are zero
-    a.items = 0;
-    hipLaunchKernelGGL(k_scan_sum_items, dim3((unsigned)(((int64_t)p->dim * p->dim_state + 63) / 64), 3), dim3(256), 0, s, a, dA, p->D ? dD : nullptr,
-                       p->dt_bias ? ddt_bias : nullptr);
-  } else if (p->dtype == NUGPR_BFLOAT16) {
-    launch_backward<Bf16>(p, a, dB, dC, dA, dD, ddt_bias, s);
-  } else {
-    launch_backward<F32>(p, a, dB, dC, dA, dD, ddt_bias, s);
+  if (done) a.items = 0;                           // no rows, no sequences: the sums are zero
+  a.dA_out = dA; a.dD_out = p->D ? dD : nullptr; a.dbias_out = p->dt_bias ? ddt_bias : nullptr;
+  if (p->n_rows > 0) {
+    a.dB_out = dB->data; a.dB_row = dB->row_stride; a.dB_head = dB->head_stride;
+    a.dC_out = dC->data; a.dC_row = dC->row_stride; a.dC_head = dC->head_stride;
   }
-  NUGPR_HIP(hipGetLastError());
-  return NUGPR_OK;
+  return launch_scan_backward(p->dtype, a, one_span(p, true), launch_join, reinterpret_cast<hipStream_t>(stream));
 }
 
 int nugpr_selective_scan_step(const nugpr_selective_scan* p, const nugpr_rows* x, const nugpr_rows* dt, const nugpr_heads* B, const nugpr_heads* C,
