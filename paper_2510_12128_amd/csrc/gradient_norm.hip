@@ -17,19 +17,21 @@ namespace nugpr {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int TABLE = 120;            // 32 bytes each, below the 4096 bytes that kernel arguments may have
+constexpr int TABLE = 232, TABLE_OUT = 155;      // tensors of a launch, without and with a place to go to: kernel arguments below 4096 bytes
 constexpr int CHUNK = 16384;          // values
 constexpr int GROUPS = 2048;          // workgroups of a call, about: partial sums that every clipping workgroup adds up
 
 struct Tensor {
-  void *data, *out;
-  int64_t count;
+  void* data;
   uint32_t first;       // its first chunk
-  uint16_t dtype, out_dtype;
+  uint32_t tail;        // values of its last chunk; the upper bits: its type, and that of where it goes
 };
+constexpr uint32_t BF16_DATA = 1u << 31, BF16_OUT = 1u << 30;
 
+template <int N, bool OUT>
 struct Table {
-  Tensor t[TABLE];
+  Tensor t[N];
+  void* out[OUT ? N : 1];
   double* sums;
   float* norm;
   double bound;
@@ -38,17 +40,27 @@ struct Table {
   int n_sums;           // partial sums of the whole call
   int sums_from;        // of them, this launch's
 };
+typedef Table<TABLE, false> InPlace;
+typedef Table<TABLE_OUT, true> ToOut;
+static_assert(sizeof(InPlace) < 4000 && sizeof(ToOut) < 4000, "kernel arguments");
 
-// The tensor of a chunk: the last that begins at or before it.  (Empty tensors begin where the next one does.)
-__device__ inline int tensor_of(const Table& a, uint32_t chunk) {
+// A chunk: its tensor is the last that begins at or before it.  (Empty tensors begin where the next one does.)
+struct Chunk {
+  int tensor, count;
+  int64_t from;
+};
+template <int N, bool OUT>
+__device__ inline Chunk chunk_at(const Table<N, OUT>& a, uint32_t chunk) {
   const int lane = threadIdx.x & 63;
   int n = 0;
 #pragma unroll
-  for (int k = 0; k < (TABLE + 63) / 64; ++k) {
+  for (int k = 0; k < (N + 63) / 64; ++k) {
     const int at = k * 64 + lane;
-    n += __popcll(__ballot(at < a.n && a.t[min(at, TABLE - 1)].first <= chunk));
+    n += __popcll(__ballot(at < a.n && a.t[min(at, N - 1)].first <= chunk));
   }
-  return __builtin_amdgcn_readfirstlane(n - 1);
+  n = __builtin_amdgcn_readfirstlane(n - 1);
+  const uint32_t first = a.t[n].first, end = n + 1 < a.n ? a.t[n + 1].first : a.chunks;
+  return Chunk{n, chunk + 1 == end ? (int)(a.t[n].tail & 0xffffu) : CHUNK, (int64_t)(chunk - first) * CHUNK};
 }
 
 __device__ inline double sum_of_workgroup(double x) {
@@ -80,14 +92,13 @@ __device__ double squares(const typename TR::T* p, int count) {
   return s0 + s1;
 }
 
-__global__ __launch_bounds__(THREADS) void k_square_sums(const Table a) {
+__global__ __launch_bounds__(THREADS) void k_square_sums(const InPlace a) {
   double s = 0.0;
   for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
-    const Tensor& t = a.t[tensor_of(a, c)];
-    const int64_t from = (int64_t)(c - t.first) * CHUNK;
-    const int count = (int)(t.count - from < CHUNK ? t.count - from : CHUNK);
-    if (t.dtype == NUGPR_BFLOAT16) s += squares<Bf16>(static_cast<const uint16_t*>(t.data) + from, count);
-    else s += squares<F32>(static_cast<const float*>(t.data) + from, count);
+    const Chunk k = chunk_at(a, c);
+    const Tensor& t = a.t[k.tensor];
+    if (t.tail & BF16_DATA) s += squares<Bf16>(static_cast<const uint16_t*>(t.data) + k.from, k.count);
+    else s += squares<F32>(static_cast<const float*>(t.data) + k.from, k.count);
   }
   s = sum_of_workgroup(s);
   if (threadIdx.x == 0) a.sums[a.sums_from + blockIdx.x] = s;
@@ -120,23 +131,25 @@ __device__ void scaled(const typename FROM::T* p, typename TO::T* q, int count, 
   }
 }
 
-__global__ __launch_bounds__(THREADS) void k_clip(const Table a) {
+template <int N, bool OUT>
+__global__ __launch_bounds__(THREADS) void k_clip(const Table<N, OUT> a) {
   const double norm = norm_of(a.sums, a.n_sums);
   if (a.sums_from == 0 && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
   const double factor = norm <= a.bound ? 1.0 : a.bound / norm;
+  if (!OUT && factor == 1.0) return;
   for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
-    const Tensor& t = a.t[tensor_of(a, c)];
-    if (t.out == t.data && factor == 1.0) continue;
-    const int64_t from = (int64_t)(c - t.first) * CHUNK;
-    const int count = (int)(t.count - from < CHUNK ? t.count - from : CHUNK);
-    if (t.dtype == NUGPR_BFLOAT16) {
-      const uint16_t* p = static_cast<const uint16_t*>(t.data) + from;
-      if (t.out_dtype == NUGPR_BFLOAT16) scaled<Bf16, Bf16>(p, static_cast<uint16_t*>(t.out) + from, count, factor);
-      else scaled<Bf16, F32>(p, static_cast<float*>(t.out) + from, count, factor);
+    const Chunk k = chunk_at(a, c);
+    const Tensor& t = a.t[k.tensor];
+    void* out = OUT ? a.out[k.tensor] : t.data;
+    if (OUT && factor == 1.0 && out == t.data) continue;           // (of its own type, then: others may not overlap)
+    if (t.tail & BF16_DATA) {
+      const uint16_t* p = static_cast<const uint16_t*>(t.data) + k.from;
+      if (!OUT || t.tail & BF16_OUT) scaled<Bf16, Bf16>(p, static_cast<uint16_t*>(out) + k.from, k.count, factor);
+      else scaled<Bf16, F32>(p, static_cast<float*>(out) + k.from, k.count, factor);
     } else {
-      const float* p = static_cast<const float*>(t.data) + from;
-      if (t.out_dtype == NUGPR_BFLOAT16) scaled<F32, Bf16>(p, static_cast<uint16_t*>(t.out) + from, count, factor);
-      else scaled<F32, F32>(p, static_cast<float*>(t.out) + from, count, factor);
+      const float* p = static_cast<const float*>(t.data) + k.from;
+      if (OUT && t.tail & BF16_OUT) scaled<F32, Bf16>(p, static_cast<uint16_t*>(out) + k.from, k.count, factor);
+      else scaled<F32, F32>(p, static_cast<float*>(out) + k.from, k.count, factor);
     }
   }
 }
@@ -217,23 +230,29 @@ int check_written(const nugpr_gradient* g, int32_t n) try {
   return invalid("no host memory for the tensors' ranges");
 }
 
-// Every launch of a kernel over the tables.
-template <class F>
-void for_tables(const nugpr_gradient* g, int32_t n, double* sums, float* norm, double bound, F launch) {
-  Table a;
+// Every launch of a kernel over the tables; `groups` at most.  The sums' places are those of the first kernel's workgroups.
+template <class T, class F>
+void for_tables(const nugpr_gradient* g, int32_t n, double* sums, float* norm, double bound, int64_t most, F launch) {
+  constexpr int N = sizeof(T::t) / sizeof(Tensor);
+  constexpr bool OUT = sizeof(T::out) > sizeof(void*);
+  T a;
   a.sums = sums; a.norm = norm; a.bound = bound;
   a.n_sums = (int)sums_in(g, n);
   a.sums_from = 0;
-  for (int k = 0; k < launches(n); ++k) {
-    a.n = std::min(TABLE, n - k * TABLE);
+  for (int64_t from = 0; from < n; from += N) {
+    a.n = (int)std::min<int64_t>(N, n - from);
     uint32_t chunk = 0;
     for (int i = 0; i < a.n; ++i) {
-      const nugpr_gradient& x = g[(int64_t)k * TABLE + i];
-      a.t[i] = Tensor{x.data, x.out ? x.out : x.data, x.count, chunk, (uint16_t)x.dtype, (uint16_t)(x.out ? x.out_dtype : x.dtype)};
-      chunk += (uint32_t)chunks_of(x.count);
+      const nugpr_gradient& x = g[from + i];
+      const int64_t chunks = chunks_of(x.count);
+      a.t[i] = Tensor{x.data, chunk, (uint32_t)(x.count - std::max<int64_t>(chunks - 1, 0) * CHUNK)};
+      if (x.dtype == NUGPR_BFLOAT16) a.t[i].tail |= BF16_DATA;
+      if (OUT) a.out[i] = x.out ? x.out : x.data;
+      if (OUT && (x.out ? x.out_dtype : x.dtype) == NUGPR_BFLOAT16) a.t[i].tail |= BF16_OUT;
+      chunk += (uint32_t)chunks;
     }
     a.chunks = chunk;
-    const int64_t groups = std::min<int64_t>(chunk, most_groups(n));
+    const int64_t groups = std::min<int64_t>(chunk, most);
     if (groups > 0) launch(a, dim3((unsigned)groups));
     a.sums_from += (int)groups;
   }
@@ -256,7 +275,7 @@ int nugpr_gradient_norm(const nugpr_gradient* g, int32_t n, float* norm, void* w
   if (const int c = check_call(g, n, norm, workspace, workspace_bytes)) return c;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   double* sums = static_cast<double*>(workspace);
-  for_tables(g, n, sums, norm, 0.0, [&](const Table& a, dim3 grid) { hipLaunchKernelGGL(k_square_sums, grid, dim3(THREADS), 0, s, a); });
+  for_tables<InPlace>(g, n, sums, norm, 0.0, most_groups(n), [&](const InPlace& a, dim3 grid) { hipLaunchKernelGGL(k_square_sums, grid, dim3(THREADS), 0, s, a); });
   hipLaunchKernelGGL(k_norm, dim3(1), dim3(THREADS), 0, s, sums, (int)sums_in(g, n), norm);
   NUGPR_HIP(hipGetLastError());
   return NUGPR_OK;
@@ -272,8 +291,16 @@ int nugpr_clip_gradients(const nugpr_gradient* g, int32_t n, double max_norm, fl
   if (sums_in(g, n) == 0) {
     hipLaunchKernelGGL(k_norm, dim3(1), dim3(THREADS), 0, s, sums, 0, norm);
   } else {
-    for_tables(g, n, sums, norm, max_norm, [&](const Table& a, dim3 grid) { hipLaunchKernelGGL(k_square_sums, grid, dim3(THREADS), 0, s, a); });
-    for_tables(g, n, sums, norm, max_norm, [&](const Table& a, dim3 grid) { hipLaunchKernelGGL(k_clip, grid, dim3(THREADS), 0, s, a); });
+    for_tables<InPlace>(g, n, sums, norm, max_norm, most_groups(n),
+                        [&](const InPlace& a, dim3 grid) { hipLaunchKernelGGL(k_square_sums, grid, dim3(THREADS), 0, s, a); });
+    bool elsewhere = false;
+    for (int32_t i = 0; i < n; ++i) elsewhere |= g[i].out && (g[i].out != g[i].data || g[i].out_dtype != g[i].dtype);
+    if (elsewhere)
+      for_tables<ToOut>(g, n, sums, norm, max_norm, GROUPS,
+                        [&](const ToOut& a, dim3 grid) { hipLaunchKernelGGL((k_clip<TABLE_OUT, true>), grid, dim3(THREADS), 0, s, a); });
+    else
+      for_tables<InPlace>(g, n, sums, norm, max_norm, GROUPS,
+                          [&](const InPlace& a, dim3 grid) { hipLaunchKernelGGL((k_clip<TABLE, false>), grid, dim3(THREADS), 0, s, a); });
   }
   NUGPR_HIP(hipGetLastError());
   return NUGPR_OK;

@@ -315,58 +315,54 @@ __global__ __launch_bounds__(64 * WAVES) void k_scan(const ScanArgs a) {
 }
 
 // Start states of a sequence's spans, in the place of what the spans add; the second half of the grid: gradients at their end, against time.
-__global__ __launch_bounds__(256) void k_scan_join(const ScanArgs a) {
-  const int64_t each = (int64_t)a.dim * a.states, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+// A chain of one multiply-add a span: what it reads comes AHEAD spans at a time, the next ones while these are worked through.
+template <bool BACK>
+__device__ __forceinline__ void join(float* at, const float* steps, int64_t each, int64_t dim, int spans, float a2, float h) {
+  constexpr int AHEAD = 8;
+  // the span at place k of the chain; forward, span 0's own is where it begins
+  const auto span = [&](int k) { return BACK ? spans - 1 - k : k; };
+  const int from = BACK ? 0 : 1, reads = spans - 1;      // (the last place's own adds to none)
+  float add[AHEAD], d[AHEAD];
+  const auto load = [&](int k0) {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const bool there = k0 + j < reads;
+      add[j] = there ? at[span(k0 + j) * each] : 0.f;
+      d[j] = there ? steps[span(k0 + j) * dim] : 0.f;
+    }
+  };
+  load(from);
+  for (int k = from; k < spans; k += AHEAD) {
+    float add_now[AHEAD], d_now[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      add_now[j] = add[j];
+      d_now[j] = d[j];
+    }
+    load(k + AHEAD);
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (k + j >= spans) break;
+      at[span(k + j) * each] = h;
+      const float f = exp2_of(a2 * d_now[j]);
+      // (a factor of many steps may be zero where none of a single step is)
+      h = h == 0.f || (f == 0.f && __builtin_isinf(h)) ? h + add_now[j] : fmaf(f, h, add_now[j]);
+    }
+  }
+}
+
+__global__ __launch_bounds__(64) void k_scan_join(const ScanArgs a) {
+  const int64_t each = (int64_t)a.dim * a.states, at = (int64_t)blockIdx.x * 64 + threadIdx.x;
   if (at >= each) return;
   for (int seq = blockIdx.y; seq < a.n_seqs; seq += gridDim.y) {
     const int64_t lo = clamped(a.off[seq], 0, a.n_rows), hi = clamped(a.off[seq + 1], lo, a.n_rows);
     const int spans = (int)((hi - lo + ((int64_t)1 << a.span_log2) - 1) >> a.span_log2);
     if (spans < 2) continue;
     const int64_t first = (lo >> a.span_log2) + seq;
-    const int c = (int)(at / a.states);
+    const float* steps = a.steps + first * a.dim + at / a.states;
     const float a2 = a.A[at] * LOG2_E;
-    constexpr int STEP = 8;
-    if (blockIdx.z == 0) {
-      float* adds = a.adds + first * each + at;
-      const float* steps = a.steps + first * a.dim + c;
-      float h = adds[0];
-      for (int k = 1; k < spans; k += STEP) {
-        float add[STEP], d[STEP];
-  #pragma unroll
-        for (int j = 0; j < STEP; ++j) {
-          const bool there = k + j < spans - 1;      // (the last span adds to none)
-          add[j] = there ? adds[(k + j) * each] : 0.f;
-          d[j] = there ? steps[(int64_t)(k + j) * a.dim] : 0.f;
-        }
-  #pragma unroll
-        for (int j = 0; j < STEP; ++j) {
-          if (k + j >= spans) break;
-          adds[(k + j) * each] = h;
-          const float f = exp2_of(a2 * d[j]);
-          h = h == 0.f || (f == 0.f && __builtin_isinf(h)) ? h + add[j] : fmaf(f, h, add[j]);
-        }
-      }
-    } else {
-      float* back = a.back + first * each + at;
-      const float* steps = a.steps + first * a.dim + c;
-      float g = a.ds_end ? a.ds_end[seq * each + at] : 0.f;
-      for (int k = spans - 1; k >= 0; k -= STEP) {
-        float add[STEP], d[STEP];
-  #pragma unroll
-        for (int j = 0; j < STEP; ++j) {
-          const bool there = k - j > 0;
-          add[j] = there ? back[(k - j) * each] : 0.f;
-          d[j] = there ? steps[(int64_t)(k - j) * a.dim] : 0.f;
-        }
-  #pragma unroll
-        for (int j = 0; j < STEP; ++j) {
-          if (k - j < 0) break;
-          back[(k - j) * each] = g;
-          const float f = exp2_of(a2 * d[j]);
-          g = g == 0.f || (f == 0.f && __builtin_isinf(g)) ? g + add[j] : fmaf(f, g, add[j]);
-        }
-      }
-    }
+    if (blockIdx.z == 0) join<false>(a.adds + first * each + at, steps, each, a.dim, spans, a2, a.adds[first * each + at]);
+    else join<true>(a.back + first * each + at, steps, each, a.dim, spans, a2, a.ds_end ? a.ds_end[seq * each + at] : 0.f);
   }
 }
 
@@ -490,11 +486,11 @@ int blocks_of(const nugpr_selective_scan* p, bool backward) {
   return p->groups * ((each + width - 1) / width);
 }
 
-// Rows of a span: a power of two, a few tiles at least, so large that the spans of the rows give about 8192 waves, 4096 in the gradients, of
+// Rows of a span: a power of two, a few tiles at least, so large that the spans of the rows give about 16384 waves, 4096 in the gradients, of
 // which a compute unit holds a third as many.
 int span_log2(const nugpr_selective_scan* p, bool backward) {
   int k = 6;
-  while (k < 40 && ((p->n_rows * blocks_of(p, backward) * (threads_of(p, backward) / 64)) >> k) > (backward ? 4096 : 8192)) ++k;
+  while (k < 40 && ((p->n_rows * blocks_of(p, backward) * (threads_of(p, backward) / 64)) >> k) > (backward ? 4096 : 16384)) ++k;
   return k;
 }
 bool one_span(const nugpr_selective_scan* p, bool backward) { return p->n_rows <= (int64_t)1 << span_log2(p, backward); }
@@ -582,8 +578,8 @@ void with_waves(const nugpr_selective_scan* p, F f) {
 
 void launch_join(const ScanArgs& a, bool backward, hipStream_t s) {
   const int64_t each = (int64_t)a.dim * a.states;
-  const int64_t x = (each + 255) / 256, y = std::min<int64_t>(a.n_seqs, std::max<int64_t>(1, 8192 / x));
-  hipLaunchKernelGGL(k_scan_join, dim3((unsigned)x, (unsigned)y, backward ? 2 : 1), dim3(256), 0, s, a);
+  const int64_t x = (each + 63) / 64, y = std::min<int64_t>(a.n_seqs, std::max<int64_t>(1, 32768 / x));
+  hipLaunchKernelGGL(k_scan_join, dim3((unsigned)x, (unsigned)y, backward ? 2 : 1), dim3(64), 0, s, a);
 }
 
 template <class TR>

@@ -502,6 +502,7 @@ __global__ __launch_bounds__(256) void k_scan_sum_blocks(const ScanArgs a) {
   const float* from = (blockIdx.y ? a.dC : a.dB) + at;
   float s = 0.f;
   if (row >= first && row < last)
+#pragma unroll 8
     for (int k = 0; k < parts; ++k) s += from[k * total];
   if (blockIdx.y) static_cast<T*>(a.dC_out)[row * a.dC_row + group * a.dC_head + n] = TR::put(s);
   else static_cast<T*>(a.dB_out)[row * a.dB_row + group * a.dB_head + n] = TR::put(s);
@@ -518,6 +519,7 @@ __global__ __launch_bounds__(256) void k_scan_sum_items(const ScanArgs a) {
   const int each = (a.items + 3) / 4, end = min(a.items, (wave + 1) * each);
   float s = 0.f;
   if (at < size)
+#pragma unroll 8
     for (int k = wave * each; k < end; ++k) s += from[k * size + at];
   part[wave][lane] = s;
   __syncthreads();

@@ -332,20 +332,24 @@ __global__ __launch_bounds__(THREADS) void k_short_conv_backward(const ConvArgs 
   }
 }
 
-// dw and db from the workgroups' sums, in their order: 64 channels a workgroup, each wave a quarter of the sums of one tap.
+// dw and db from the workgroups' sums, in their order: 64 channels a workgroup, each wave a part of the sums of one tap.
+constexpr int SUM_WAVES = 8;
 template <class TR>
-__global__ __launch_bounds__(THREADS) void k_conv_sums(const float* sums, int64_t n, int width, int dim, typename TR::T* dw, typename TR::T* db) {
-  __shared__ float part[WAVES][64];
+__global__ __launch_bounds__(64 * SUM_WAVES) void k_conv_sums(const float* sums, int64_t n, int width, int dim, typename TR::T* dw, typename TR::T* db) {
+  __shared__ float part[SUM_WAVES][64];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int c = blockIdx.x * 64 + lane, i = blockIdx.y;
-  const int64_t each = (n + WAVES - 1) / WAVES, to = min(n, (wave + 1) * each);
+  const int64_t each = (n + SUM_WAVES - 1) / SUM_WAVES, to = min(n, (wave + 1) * each);
   float s = 0.f;
   if (c < dim)
+#pragma unroll 8
     for (int64_t k = wave * each; k < to; ++k) s += sums[(k * (width + 1) + i) * dim + c];
   part[wave][lane] = s;
   __syncthreads();
   if (wave || c >= dim) return;
-  s = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+  s = part[0][lane];
+#pragma unroll
+  for (int k = 1; k < SUM_WAVES; ++k) s += part[k][lane];
   if (i < width) dw[(int64_t)c * width + i] = TR::put(s);
   else if (db) db[c] = TR::put(s);
 }
@@ -554,13 +558,13 @@ int nugpr_short_conv_backward(const nugpr_short_conv* p, const nugpr_rows* x, co
   a.w_in = initial_window; a.dw_end = d_final_window; a.dw_in = d_initial_window;
   a.sums = static_cast<float*>(p->workspace);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  const dim3 blocks((unsigned)grid), threads(THREADS), sum_grid((unsigned)(p->dim + 63) / 64, p->width + 1);
+  const dim3 blocks((unsigned)grid), threads(THREADS), sum_grid((unsigned)(p->dim + 63) / 64, p->width + 1), sum_threads(64 * SUM_WAVES);
   if (p->dtype == NUGPR_BFLOAT16) {
     if (grid) with_width<Bf16, 4>(p->width, [&](auto w) { hipLaunchKernelGGL((k_short_conv_backward<Bf16, decltype(w)::value, 4>), blocks, threads, 0, s, a); });
-    hipLaunchKernelGGL(k_conv_sums<Bf16>, sum_grid, threads, 0, s, a.sums, a.runs, p->width, p->dim, static_cast<uint16_t*>(dweight), static_cast<uint16_t*>(dbias));
+    hipLaunchKernelGGL(k_conv_sums<Bf16>, sum_grid, sum_threads, 0, s, a.sums, a.runs, p->width, p->dim, static_cast<uint16_t*>(dweight), static_cast<uint16_t*>(dbias));
   } else {
     if (grid) with_width<F32, 4>(p->width, [&](auto w) { hipLaunchKernelGGL((k_short_conv_backward<F32, decltype(w)::value, 4>), blocks, threads, 0, s, a); });
-    hipLaunchKernelGGL(k_conv_sums<F32>, sum_grid, threads, 0, s, a.sums, a.runs, p->width, p->dim, static_cast<float*>(dweight), static_cast<float*>(dbias));
+    hipLaunchKernelGGL(k_conv_sums<F32>, sum_grid, sum_threads, 0, s, a.sums, a.runs, p->width, p->dim, static_cast<float*>(dweight), static_cast<float*>(dbias));
   }
   NUGPR_HIP(hipGetLastError());
   return NUGPR_OK;

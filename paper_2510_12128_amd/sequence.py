@@ -6,10 +6,12 @@ torch.autograd.Function or by hand): inputs that require gradients are refused w
 from __future__ import annotations
 
 import ctypes as C
+from array import array
+from operator import attrgetter
 
 import torch
 
-from .binding import (Adapter, DecayAttention, Gradient, Heads, NUGPR_BFLOAT16, NUGPR_ERR_INVALID, NUGPR_FLOAT32,
+from .binding import (Adapter, DecayAttention, Heads, NUGPR_BFLOAT16, NUGPR_ERR_INVALID, NUGPR_FLOAT32,
                       NugprError, Rows, SelectiveScan, ShortConv, _check, load_library)
 
 _TYPES = {torch.float32: NUGPR_FLOAT32, torch.bfloat16: NUGPR_BFLOAT16}
@@ -263,8 +265,8 @@ def nugpr_short_conv_forward(x, weight, seq_offsets, bias=None, silu=False, init
     s0 = _none(initial_state, "initial_state", device, dtype, shape)
     y = torch.empty(x.shape, dtype=dtype, device=device)
     s1 = torch.empty(shape, dtype=dtype, device=device)
-    _call(lib.nugpr_short_conv_forward, device, _byref(p), _rows2(x, "x", device, dtype, x.shape), s0,
-          _rows2(y, "y", device, dtype, x.shape), s1.data_ptr())
+    _call(lib.nugpr_short_conv_forward, device, _byref(p), _byref(Rows(x.data_ptr(), _rows(x, "x"))), s0,
+          _byref(Rows(y.data_ptr(), x.shape[1])), s1.data_ptr())
     return y, s1
 
 
@@ -284,8 +286,8 @@ def nugpr_short_conv_backward(x, weight, seq_offsets, d_y, bias=None, silu=False
     dx, dw = torch.empty(x.shape, dtype=dtype, device=device), torch.empty_like(weight)
     db = None if bias is None else torch.empty_like(bias)
     ds = torch.empty(shape, dtype=dtype, device=device)
-    _call(lib.nugpr_short_conv_backward, device, _byref(p), _rows2(x, "x", device, dtype, x.shape), s0,
-          _rows2(d_y, "d_y", device, dtype, x.shape), s1, _rows2(dx, "dx", device, dtype, x.shape), dw.data_ptr(),
+    _call(lib.nugpr_short_conv_backward, device, _byref(p), _byref(Rows(x.data_ptr(), _rows(x, "x"))), s0,
+          _rows2(d_y, "d_y", device, dtype, x.shape), s1, _byref(Rows(dx.data_ptr(), x.shape[1])), dw.data_ptr(),
           None if db is None else db.data_ptr(), ds.data_ptr())
     return dx, dw, db, ds
 
@@ -299,8 +301,8 @@ def nugpr_short_conv_step(x, weight, state, slots=None, bias=None, silu=False):
     st = _dense(state, "state", device, dtype, shape)
     at = _none(slots, "slots", device, torch.int32, (x.shape[0],))
     y = torch.empty(x.shape, dtype=dtype, device=device)
-    _call(lib.nugpr_short_conv_step, device, _byref(p), _rows2(x, "x", device, dtype, x.shape), st, at,
-          _rows2(y, "y", device, dtype, x.shape))
+    _call(lib.nugpr_short_conv_step, device, _byref(p), _byref(Rows(x.data_ptr(), _rows(x, "x"))), st, at,
+          _byref(Rows(y.data_ptr(), x.shape[1])))
     _written(state)
     return y
 
@@ -313,14 +315,13 @@ def _scan(x, dt, A, B, C, D, z, dt_bias, softplus, n_seqs, offsets):
         _refuse("A must be dim x dim_state, B and C rows x groups x dim_state")
     n, dim = x.shape
     groups, states = B.shape[1], A.shape[1]
-    _like(dt, "dt", device, dtype, x.shape)
     _like(B, "B", device, dtype, (n, groups, states))
     _like(C, "C", device, dtype, (n, groups, states))
     a = _dense(A, "A", device, torch.float32, (dim, states))
     d = _none(D, "D", device, torch.float32, (dim,))
     bias = _none(dt_bias, "dt_bias", device, torch.float32, (dim,))
     p = SelectiveScan(_TYPES[dtype], dim, groups, states, 1 if softplus else 0, n, n_seqs, offsets, a, d, bias, None, 0)
-    arrays = (_rows2(x, "x", device, dtype, x.shape), _rows2(dt, "dt", device, dtype, x.shape), _heads(B, "B"),
+    arrays = (_byref(Rows(x.data_ptr(), _rows(x, "x"))), _rows2(dt, "dt", device, dtype, x.shape), _heads(B, "B"),
               _heads(C, "C"), None if z is None else _rows2(z, "z", device, dtype, x.shape))
     return p, device, dtype, (n_seqs, dim, states), arrays
 
@@ -341,7 +342,7 @@ def nugpr_selective_scan_forward(x, dt, A, B, C, seq_offsets, D=None, z=None, dt
     s0 = _none(initial_state, "initial_state", device, torch.float32, shape)
     y = torch.empty(x.shape, dtype=dtype, device=device)
     s1 = torch.empty(shape, dtype=torch.float32, device=device)
-    _call(lib.nugpr_selective_scan_forward, device, _byref(p), *arrays, s0, _rows2(y, "y", device, dtype, x.shape),
+    _call(lib.nugpr_selective_scan_forward, device, _byref(p), *arrays, s0, _byref(Rows(y.data_ptr(), x.shape[1])),
           s1.data_ptr())
     return y, s1
 
@@ -364,11 +365,12 @@ def nugpr_selective_scan_backward(x, dt, A, B, C, seq_offsets, d_y, D=None, z=No
     dD, dbias = (None if t is None else torch.empty_like(t) for t in (D, dt_bias))
     ds = torch.empty(shape, dtype=torch.float32, device=device)
 
-    def rows(t, name):
-        return None if t is None else _rows2(t, name, device, dtype, x.shape)
+    def out(t):
+        return None if t is None else _byref(Rows(t.data_ptr(), x.shape[1]))
 
-    _call(lib.nugpr_selective_scan_backward, device, _byref(p), *arrays, s0, rows(d_y, "d_y"), s1, rows(dx, "dx"),
-          rows(ddt, "ddt"), _heads(dB, "dB"), _heads(dC, "dC"), rows(dz, "dz"), dA.data_ptr(),
+    _call(lib.nugpr_selective_scan_backward, device, _byref(p), *arrays, s0,
+          _rows2(d_y, "d_y", device, dtype, x.shape), s1, out(dx), out(ddt),
+          _heads(dB, "dB"), _heads(dC, "dC"), out(dz), dA.data_ptr(),
           None if dD is None else dD.data_ptr(), None if dbias is None else dbias.data_ptr(), ds.data_ptr())
     return dx, ddt, dA, dB, dC, dD, dz, dbias, ds
 
@@ -383,15 +385,18 @@ def nugpr_selective_scan_step(x, dt, A, B, C, state, slots=None, D=None, z=None,
     st = _dense(state, "state", device, torch.float32, shape)
     at = _none(slots, "slots", device, torch.int32, (x.shape[0],))
     y = torch.empty(x.shape, dtype=dtype, device=device)
-    _call(lib.nugpr_selective_scan_step, device, _byref(p), *arrays, st, at, _rows2(y, "y", device, dtype, x.shape))
+    _call(lib.nugpr_selective_scan_step, device, _byref(p), *arrays, st, at, _byref(Rows(y.data_ptr(), x.shape[1])))
     _written(state)
     return y
 
 
-def _in_one_piece(t):
+_type_of, _shape_of, _asks = attrgetter("dtype"), attrgetter("shape"), attrgetter("requires_grad")
+_address, _count, _where, _contiguous = (torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device,
+                                         torch.Tensor.is_contiguous)
+
+
+def _run_of_memory(t):
     """Whether the values of a tensor fill one run of memory, in any order of its dimensions."""
-    if t.is_contiguous():
-        return True
     expected = 1
     for stride, size in sorted((st, si) for st, si in zip(t.stride(), t.shape) if si != 1):
         if stride != expected:
@@ -400,37 +405,60 @@ def _in_one_piece(t):
     return True
 
 
+def _on_one_gpu(tensors, index, what):
+    for i, t in enumerate(tensors):
+        if t.get_device() != index or t.dtype not in _TYPES:
+            _refuse(f"{what} {i} must be on the GPU of the first gradient, float32 or bfloat16")
+
+
 def _gradients(grads, out):
-    """The tensors as an array of the structure, and their device."""
+    """The tensors as an array of the structure, their number and their device.  (Checks go over all tensors at once: a model has
+    hundreds.)"""
     grads = list(grads)
     if not grads:
         _refuse("there is no gradient")
-    device = grads[0].device
-    if device.type != "cuda":
+    if not grads[0].is_cuda:
         _refuse("gradients must be on a GPU")
-    to = [None] * len(grads) if out is None else list(out)
-    if len(to) != len(grads):
-        _refuse("out must have as many tensors as there are gradients")
-    table = (Gradient * len(grads))()
-    for i, (g, o) in enumerate(zip(grads, to)):
-        if g.device != device or g.dtype not in _TYPES or not _in_one_piece(g):
-            _refuse(f"gradient {i} must be on {device}, float32 or bfloat16, and fill one run of memory")
-        if o is None:
-            table[i] = (g.data_ptr(), None, g.numel(), _TYPES[g.dtype], 0)
-            continue
-        if o.device != device or o.dtype not in _TYPES or o.shape != g.shape or (o.stride() != g.stride() and g.numel()):
-            _refuse(f"out {i} must be on {device}, float32 or bfloat16, with the gradient's shape and strides")
-        table[i] = (g.data_ptr(), o.data_ptr(), g.numel(), _TYPES[g.dtype], _TYPES[o.dtype])
-    return grads, to, table, device
+    device, index = grads[0].device, grads[0].get_device()
+    types = list(map(_type_of, grads))
+    if set(map(_where, grads)) != {index} or not _TYPES.keys() >= set(types):
+        _on_one_gpu(grads, index, "gradient")
+    dense = all(map(_contiguous, grads))
+    if not dense:
+        for i, g in enumerate(grads):
+            if g.numel() and not _run_of_memory(g):
+                _refuse(f"gradient {i} must fill one run of memory")
+    words = array("q", bytes(32 * len(grads)))                     # data, out, count, the two types
+    words[0::4] = array("q", map(_address, grads))
+    words[2::4] = array("q", map(_count, grads))
+    codes = [_TYPES[t] for t in types]
+    to = grads
+    if out is not None:
+        to = list(out)
+        if len(to) != len(grads):
+            _refuse("out must have as many tensors as there are gradients")
+        out_types = list(map(_type_of, to))
+        if set(map(_where, to)) != {index} or not _TYPES.keys() >= set(out_types):
+            _on_one_gpu(to, index, "out")
+        if (list(map(_shape_of, to)) != list(map(_shape_of, grads)) or
+                not (dense and all(map(_contiguous, to))) and any(o.stride() != g.stride() and g.numel() for o, g in zip(to, grads))):
+            _refuse("tensors of out must have the gradients' shapes and strides")
+        words[1::4] = array("q", map(_address, to))
+        codes = [c | _TYPES[t] << 32 for c, t in zip(codes, out_types)]
+    words[3::4] = array("q", codes)
+    if _recording() and (any(map(_asks, grads)) or any(map(_asks, to))):
+        _refuse("a gradient requires a gradient itself, which autograd does not get through this call")
+    return words, to, device
 
 
-def _norm_call(lib, call, table, device, *args):
-    need = lib.nugpr_gradient_norm_workspace_bytes(table, len(table))
+def _norm_call(lib, call, words, device, *args):
+    table, n = words.buffer_info()[0], len(words) // 4
+    need = lib.nugpr_gradient_norm_workspace_bytes(table, n)
     if need == 0:
         raise NugprError(NUGPR_ERR_INVALID, lib.nugpr_last_error_string().decode())
     ws = torch.empty(need, dtype=torch.uint8, device=device)
     norm = torch.empty((), dtype=torch.float32, device=device)
-    _call(call, device, table, len(table), *args, norm.data_ptr(), ws.data_ptr(), need)
+    _call(call, device, table, n, *args, norm.data_ptr(), ws.data_ptr(), need)
     return norm
 
 
@@ -438,23 +466,15 @@ def nugpr_gradient_norm(grads):
     """The 2-norm of all values of the tensors in `grads` (float32 or bfloat16, on one GPU, any of them of either type), as a
     float32 tensor without dimensions."""
     lib = load_library()
-    grads, _, table, device = _gradients(grads, None)
-    if _recording():
-        for i, g in enumerate(grads):
-            if g.requires_grad:
-                _refuse(f"gradient {i} requires a gradient itself, which autograd does not get through this call")
-    return _norm_call(lib, lib.nugpr_gradient_norm, table, device)
+    words, _, device = _gradients(grads, None)
+    return _norm_call(lib, lib.nugpr_gradient_norm, words, device)
 
 
 def nugpr_clip_gradients(grads, max_norm, out=None):
     """The same, and multiplies every value by min(1, max_norm / norm): in place, or into the tensors in `out` (of the
     gradients' shapes and strides, float32 or bfloat16).  No tensor that is written may share memory with another."""
     lib = load_library()
-    grads, to, table, device = _gradients(grads, out)
-    if _recording():
-        for i, g in enumerate(grads):
-            if g.requires_grad or (to[i] is not None and to[i].requires_grad):
-                _refuse(f"gradient {i} requires a gradient itself, which autograd does not get through this call")
-    norm = _norm_call(lib, lib.nugpr_clip_gradients, table, device, float(max_norm))
-    _written(grads if out is None else to)
+    words, to, device = _gradients(grads, out)
+    norm = _norm_call(lib, lib.nugpr_clip_gradients, words, device, float(max_norm))
+    _written(to)
     return norm

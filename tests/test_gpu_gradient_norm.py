@@ -72,7 +72,7 @@ def test_orders_and_alignments(lib):
         lib.nugpr_gradient_norm([base[:, ::2]])
     with pytest.raises(lib.NugprError, match="one run of memory"):
         lib.nugpr_gradient_norm([base[:1].expand(3, 30)])
-    with pytest.raises(lib.NugprError, match="shape and strides"):
+    with pytest.raises(lib.NugprError, match="shapes and strides"):
         lib.nugpr_clip_gradients([base.t()], 1.0, out=[torch.empty(30, 40, device="cuda")])
 
 
