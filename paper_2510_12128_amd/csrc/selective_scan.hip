@@ -390,47 +390,39 @@ __global__ __launch_bounds__(256) void k_scan_step(const ScanStepArgs a) {
     if (live && n0 == 0) *y = TR::put(0.f);
     return;
   }
-  float out = 0.f, x = 0.f;
-  if (live) {
-    const int64_t at = (int64_t)c * a.states + n0;
-    float* state = a.state + slot * a.dim * a.states + at;
-    const int n = min(PER, a.states - n0), group = c / a.each;
-    float h[PER], f[PER];
-    if constexpr (WIDE) {
-      if (n > 0) {
-        __builtin_memcpy(h, state, sizeof h);
-        __builtin_memcpy(f, a.A + at, sizeof f);
-      }
-    } else {
-      load_states(h, state, n);
-      load_states(f, a.A + at, n);
-    }
-    x = TR::get(static_cast<const T*>(a.x)[row * a.x_row + c]);
-    float d = TR::get(static_cast<const T*>(a.dt)[row * a.dt_row + c]) + (a.bias ? a.bias[c] : 0.f);
-    if (a.softplus) d = softplus_of<TR>(d);
-    const float u = d * x;
-#pragma unroll
-    for (int s = 0; s < PER; ++s) {
-      if (s >= n) continue;
-      const float b = TR::get(static_cast<const T*>(a.B)[row * a.B_row + group * a.B_head + n0 + s]);
-      const float w = TR::get(static_cast<const T*>(a.C)[row * a.C_row + group * a.C_head + n0 + s]);
-      h[s] = fmaf(exp_of<F32>(d * f[s]), h[s], u * b);
-      out = fmaf(w, h[s], out);
-    }
-    if constexpr (WIDE) {
-      if (n > 0) __builtin_memcpy(state, h, sizeof h);
-    } else {
-      store_states(h, state, n);
-    }
+  if (!live) return;                               // (all lanes of a channel)
+  const int64_t at = (int64_t)c * a.states + n0;
+  float* state = a.state + slot * a.dim * a.states + at;
+  const int n = min(PER, a.states - n0), group = c / a.each;
+  float h[PER], f[PER];
+  Values<TR, PER> b, w;
+  if (WIDE && n > 0) {
+    __builtin_memcpy(h, state, sizeof h);
+    __builtin_memcpy(f, a.A + at, sizeof f);
+  } else {
+    load_states(h, state, n);
+    load_states(f, a.A + at, n);
   }
+  b.load(static_cast<const T*>(a.B) + row * a.B_row + group * a.B_head + n0, n);
+  w.load(static_cast<const T*>(a.C) + row * a.C_row + group * a.C_head + n0, n);
+  const float x = TR::get(static_cast<const T*>(a.x)[row * a.x_row + c]), dt = TR::get(static_cast<const T*>(a.dt)[row * a.dt_row + c]);
+  const float bias = a.bias ? a.bias[c] : 0.f, D = a.D ? a.D[c] : 0.f;
+  const float z = a.z ? TR::get(static_cast<const T*>(a.z)[row * a.z_row + c]) : 0.f;
+  const float d = a.softplus ? softplus_of<TR>(dt + bias) : dt + bias, u = d * x;
+  float out = 0.f;
 #pragma unroll
-  for (int d = 1; d < LANES; d *= 2) out += __shfl_xor(out, d);
-  if (!live || n0) return;
-  if (a.D) out = fmaf(a.D[c], x, out);
-  if (a.z) {
-    const float z = TR::get(static_cast<const T*>(a.z)[row * a.z_row + c]);
-    out *= z * sigmoid_of<TR>(z);
-  }
+  for (int s = 0; s < PER; ++s)
+    if ((WIDE && n > 0) || s < n) {
+      h[s] = fmaf(exp2_of(d * (f[s] * LOG2_E)), h[s], u * b.get(s));
+      out = fmaf(w.get(s), h[s], out);
+    }
+  if (WIDE && n > 0) __builtin_memcpy(state, h, sizeof h);
+  else store_states(h, state, n);
+#pragma unroll
+  for (int k = 1; k < LANES; k *= 2) out += __shfl_xor(out, k);
+  if (n0) return;
+  if (a.D) out = fmaf(D, x, out);
+  if (a.z) out *= z * sigmoid_of<TR>(z);
   *y = TR::put(out);
 }
 

@@ -224,20 +224,33 @@ def nugpr_adapter_backward(x, W, A, B, seq_offsets, d_y, adapter_of=None, scale=
     return dx, dA, dB
 
 
-def _rows2(t, name, device, dtype, shape):
+# (The checks of the operators below ask for a tensor's GPU by its number: a call with single tokens is as long as its checks.)
+def _array(t, name, device, dtype, shape):
     """A rows x width array of that device, type and shape, with its last dimension contiguous."""
-    _like(t, name, device, dtype, shape)
-    return _byref(Rows(t.data_ptr(), _rows(t, name)))
+    if not (t.dtype is dtype and t.get_device() == device.index and t.shape == shape):
+        _like(t, name, device, dtype, shape)
+    s = t.stride()
+    if s[1] != 1 and shape[1] > 1 and t.numel():
+        _refuse(f"the last dimension of {name} must be contiguous")
+    return _byref(Rows(t.data_ptr(), s[0]))
 
 
-def _none(t, name, device, dtype, shape):
-    """Address of an array that may be left out."""
-    return None if t is None else _dense(t, name, device, dtype, shape)
+def _given(t, name, device, dtype, shape):
+    """Address of a contiguous array that may be left out."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.get_device() == device.index and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    return _dense(t, name, device, dtype, shape)
 
 
-def _refuse_if_recorded(**tensors):
+def _asked(*tensors):
+    """Whether autograd expects to follow a gradient through one of the tensors."""
     if _recording():
-        _refuse_recorded(**tensors)
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
 
 
 def _conv(x, weight, bias, silu, n_seqs, offsets):
@@ -247,8 +260,8 @@ def _conv(x, weight, bias, silu, n_seqs, offsets):
         _refuse("weight must be dim x width")
     n, dim = x.shape
     width = weight.shape[1]
-    w = _dense(weight, "weight", device, dtype, (dim, width))
-    b = _none(bias, "bias", device, dtype, (dim,))
+    w = _given(weight, "weight", device, dtype, (dim, width))
+    b = _given(bias, "bias", device, dtype, (dim,))
     return (ShortConv(_TYPES[dtype], dim, width, 1 if silu else 0, n, n_seqs, offsets, w, b, None, 0), device, dtype,
             (n_seqs, max(width - 1, 0), dim))
 
@@ -260,9 +273,10 @@ def nugpr_short_conv_forward(x, weight, seq_offsets, bias=None, silu=False, init
     seq_offsets (n_seqs + 1,) int64; initial_state (n_seqs, width - 1, dim), the rows before each sequence, oldest first, or
     None: zero.  Returns y (rows, dim) and the last rows of the sequences, for a call that goes on."""
     lib = load_library()
-    _refuse_if_recorded(x=x, weight=weight, bias=bias, initial_state=initial_state)
+    if _asked(x, weight, bias, initial_state):
+        _refuse_recorded(x=x, weight=weight, bias=bias, initial_state=initial_state)
     p, device, dtype, shape = _conv(x, weight, bias, silu, *_offsets(seq_offsets, x.device))
-    s0 = _none(initial_state, "initial_state", device, dtype, shape)
+    s0 = _given(initial_state, "initial_state", device, dtype, shape)
     y = torch.empty(x.shape, dtype=dtype, device=device)
     s1 = torch.empty(shape, dtype=dtype, device=device)
     _call(lib.nugpr_short_conv_forward, device, _byref(p), _byref(Rows(x.data_ptr(), _rows(x, "x"))), s0,
@@ -274,10 +288,11 @@ def nugpr_short_conv_backward(x, weight, seq_offsets, d_y, bias=None, silu=False
     """Gradients of nugpr_short_conv_forward's x, weight, bias (None without one) and initial state, in their type, from d_y
     and, unless None, d_final_state."""
     lib = load_library()
-    _refuse_if_recorded(x=x, weight=weight, bias=bias, d_y=d_y, initial_state=initial_state, d_final_state=d_final_state)
+    if _asked(x, weight, bias, d_y, initial_state, d_final_state):
+        _refuse_recorded(x=x, weight=weight, bias=bias, d_y=d_y, initial_state=initial_state, d_final_state=d_final_state)
     p, device, dtype, shape = _conv(x, weight, bias, silu, *_offsets(seq_offsets, x.device))
-    s0 = _none(initial_state, "initial_state", device, dtype, shape)
-    s1 = _none(d_final_state, "d_final_state", device, dtype, shape)
+    s0 = _given(initial_state, "initial_state", device, dtype, shape)
+    s1 = _given(d_final_state, "d_final_state", device, dtype, shape)
     need = lib.nugpr_short_conv_workspace_bytes(_byref(p))
     if need == 0:
         raise NugprError(NUGPR_ERR_INVALID, lib.nugpr_last_error_string().decode())
@@ -287,7 +302,7 @@ def nugpr_short_conv_backward(x, weight, seq_offsets, d_y, bias=None, silu=False
     db = None if bias is None else torch.empty_like(bias)
     ds = torch.empty(shape, dtype=dtype, device=device)
     _call(lib.nugpr_short_conv_backward, device, _byref(p), _byref(Rows(x.data_ptr(), _rows(x, "x"))), s0,
-          _rows2(d_y, "d_y", device, dtype, x.shape), s1, _byref(Rows(dx.data_ptr(), x.shape[1])), dw.data_ptr(),
+          _array(d_y, "d_y", device, dtype, x.shape), s1, _byref(Rows(dx.data_ptr(), x.shape[1])), dw.data_ptr(),
           None if db is None else db.data_ptr(), ds.data_ptr())
     return dx, dw, db, ds
 
@@ -296,10 +311,11 @@ def nugpr_short_conv_step(x, weight, state, slots=None, bias=None, silu=False):
     """One token for each request: x (requests, dim); state (n_states, width - 1, dim), of x's type, moves on by a row in
     place, request b's at slots[b] (int32; None: b).  Returns y (requests, dim)."""
     lib = load_library()
-    _refuse_if_recorded(x=x, weight=weight, bias=bias, state=state)
+    if _asked(x, weight, bias, state):
+        _refuse_recorded(x=x, weight=weight, bias=bias, state=state)
     p, device, dtype, shape = _conv(x, weight, bias, silu, state.shape[0] if state.dim() else 0, None)
-    st = _dense(state, "state", device, dtype, shape)
-    at = _none(slots, "slots", device, torch.int32, (x.shape[0],))
+    st = _given(state, "state", device, dtype, shape)
+    at = _given(slots, "slots", device, torch.int32, (x.shape[0],))
     y = torch.empty(x.shape, dtype=dtype, device=device)
     _call(lib.nugpr_short_conv_step, device, _byref(p), _byref(Rows(x.data_ptr(), _rows(x, "x"))), st, at,
           _byref(Rows(y.data_ptr(), x.shape[1])))
@@ -313,16 +329,18 @@ def _scan(x, dt, A, B, C, D, z, dt_bias, softplus, n_seqs, offsets):
     device, dtype = _first(x, "x", 2)
     if A.dim() != 2 or B.dim() != 3:
         _refuse("A must be dim x dim_state, B and C rows x groups x dim_state")
-    n, dim = x.shape
+    n, dim = rows = x.shape
     groups, states = B.shape[1], A.shape[1]
-    _like(B, "B", device, dtype, (n, groups, states))
-    _like(C, "C", device, dtype, (n, groups, states))
-    a = _dense(A, "A", device, torch.float32, (dim, states))
-    d = _none(D, "D", device, torch.float32, (dim,))
-    bias = _none(dt_bias, "dt_bias", device, torch.float32, (dim,))
+    if not (B.dtype is C.dtype is dtype and B.get_device() == C.get_device() == device.index and B.shape == C.shape and
+            B.shape[0] == n and B.shape[2] == states):
+        _like(B, "B", device, dtype, (n, groups, states))
+        _like(C, "C", device, dtype, (n, groups, states))
+    a = _given(A, "A", device, torch.float32, (dim, states))
+    d = _given(D, "D", device, torch.float32, (dim,))
+    bias = _given(dt_bias, "dt_bias", device, torch.float32, (dim,))
     p = SelectiveScan(_TYPES[dtype], dim, groups, states, 1 if softplus else 0, n, n_seqs, offsets, a, d, bias, None, 0)
-    arrays = (_byref(Rows(x.data_ptr(), _rows(x, "x"))), _rows2(dt, "dt", device, dtype, x.shape), _heads(B, "B"),
-              _heads(C, "C"), None if z is None else _rows2(z, "z", device, dtype, x.shape))
+    arrays = (_byref(Rows(x.data_ptr(), _rows(x, "x"))), _array(dt, "dt", device, dtype, rows), _heads(B, "B"),
+              _heads(C, "C"), None if z is None else _array(z, "z", device, dtype, rows))
     return p, device, dtype, (n_seqs, dim, states), arrays
 
 
@@ -336,10 +354,11 @@ def nugpr_selective_scan_forward(x, dt, A, B, C, seq_offsets, D=None, z=None, dt
     least 1 where there are rows; initial_state (n_seqs, dim, dim_state) float32 or None.  Returns y (rows, dim) and the
     sequences' end states, float32."""
     lib = load_library()
-    _refuse_if_recorded(x=x, dt=dt, A=A, B=B, C=C, D=D, z=z, dt_bias=dt_bias, initial_state=initial_state)
+    if _asked(x, dt, A, B, C, D, z, dt_bias, initial_state):
+        _refuse_recorded(x=x, dt=dt, A=A, B=B, C=C, D=D, z=z, dt_bias=dt_bias, initial_state=initial_state)
     p, device, dtype, shape, arrays = _scan(x, dt, A, B, C, D, z, dt_bias, softplus, *_offsets(seq_offsets, x.device))
     ws = _scratch(lib, lib.nugpr_selective_scan_workspace_bytes, p, 0, device)  # noqa: F841
-    s0 = _none(initial_state, "initial_state", device, torch.float32, shape)
+    s0 = _given(initial_state, "initial_state", device, torch.float32, shape)
     y = torch.empty(x.shape, dtype=dtype, device=device)
     s1 = torch.empty(shape, dtype=torch.float32, device=device)
     _call(lib.nugpr_selective_scan_forward, device, _byref(p), *arrays, s0, _byref(Rows(y.data_ptr(), x.shape[1])),
@@ -352,12 +371,13 @@ def nugpr_selective_scan_backward(x, dt, A, B, C, seq_offsets, d_y, D=None, z=No
     """Gradients of nugpr_selective_scan_forward's x, dt, A, B, C, D, z, dt_bias and initial state, in this order and in their
     types (None for D, z and dt_bias that are None), from d_y and, unless None, d_final_state."""
     lib = load_library()
-    _refuse_if_recorded(x=x, dt=dt, A=A, B=B, C=C, d_y=d_y, D=D, z=z, dt_bias=dt_bias, initial_state=initial_state,
-                        d_final_state=d_final_state)
+    if _asked(x, dt, A, B, C, d_y, D, z, dt_bias, initial_state, d_final_state):
+        _refuse_recorded(x=x, dt=dt, A=A, B=B, C=C, d_y=d_y, D=D, z=z, dt_bias=dt_bias, initial_state=initial_state,
+                         d_final_state=d_final_state)
     p, device, dtype, shape, arrays = _scan(x, dt, A, B, C, D, z, dt_bias, softplus, *_offsets(seq_offsets, x.device))
     ws = _scratch(lib, lib.nugpr_selective_scan_workspace_bytes, p, 1, device)  # noqa: F841
-    s0 = _none(initial_state, "initial_state", device, torch.float32, shape)
-    s1 = _none(d_final_state, "d_final_state", device, torch.float32, shape)
+    s0 = _given(initial_state, "initial_state", device, torch.float32, shape)
+    s1 = _given(d_final_state, "d_final_state", device, torch.float32, shape)
     dx, ddt = (torch.empty(x.shape, dtype=dtype, device=device) for _ in range(2))
     dB, dC = (torch.empty(B.shape, dtype=dtype, device=device) for _ in range(2))
     dz = None if z is None else torch.empty(x.shape, dtype=dtype, device=device)
@@ -369,7 +389,7 @@ def nugpr_selective_scan_backward(x, dt, A, B, C, seq_offsets, d_y, D=None, z=No
         return None if t is None else _byref(Rows(t.data_ptr(), x.shape[1]))
 
     _call(lib.nugpr_selective_scan_backward, device, _byref(p), *arrays, s0,
-          _rows2(d_y, "d_y", device, dtype, x.shape), s1, out(dx), out(ddt),
+          _array(d_y, "d_y", device, dtype, x.shape), s1, out(dx), out(ddt),
           _heads(dB, "dB"), _heads(dC, "dC"), out(dz), dA.data_ptr(),
           None if dD is None else dD.data_ptr(), None if dbias is None else dbias.data_ptr(), ds.data_ptr())
     return dx, ddt, dA, dB, dC, dD, dz, dbias, ds
@@ -379,11 +399,12 @@ def nugpr_selective_scan_step(x, dt, A, B, C, state, slots=None, D=None, z=None,
     """One token for each request: x, dt, z (requests, dim), B, C (requests, groups, dim_state); state (n_states, dim,
     dim_state) float32 is advanced in place, request b's at slots[b] (int32; None: b).  Returns y (requests, dim)."""
     lib = load_library()
-    _refuse_if_recorded(x=x, dt=dt, A=A, B=B, C=C, D=D, z=z, dt_bias=dt_bias, state=state)
+    if _asked(x, dt, A, B, C, D, z, dt_bias, state):
+        _refuse_recorded(x=x, dt=dt, A=A, B=B, C=C, D=D, z=z, dt_bias=dt_bias, state=state)
     p, device, dtype, shape, arrays = _scan(x, dt, A, B, C, D, z, dt_bias, softplus,
                                             state.shape[0] if state.dim() else 0, None)
-    st = _dense(state, "state", device, torch.float32, shape)
-    at = _none(slots, "slots", device, torch.int32, (x.shape[0],))
+    st = _given(state, "state", device, torch.float32, shape)
+    at = _given(slots, "slots", device, torch.int32, (x.shape[0],))
     y = torch.empty(x.shape, dtype=dtype, device=device)
     _call(lib.nugpr_selective_scan_step, device, _byref(p), *arrays, st, at, _byref(Rows(y.data_ptr(), x.shape[1])))
     _written(state)
