@@ -554,7 +554,7 @@ typedef struct {
 size_t nugpr_selective_scan_workspace_bytes(const nugpr_selective_scan* problem, int32_t backward);
 
 /* x, dt, z, y: dim wide; B, C: `groups` heads of width dim_state; z may be NULL.  initial_state: DEVICE float n_seqs x dim x
- * dim_state, or NULL = zero.  final_state: the same, out, or NULL; refused where it overlaps initial_state. */
+ * dim_state, or NULL = zero.  final_state: the same, out, or NULL; it may be initial_state. */
 int nugpr_selective_scan_forward(const nugpr_selective_scan* problem, const nugpr_rows* x, const nugpr_rows* dt, const nugpr_heads* B,
                                  const nugpr_heads* C, const nugpr_rows* z, const float* initial_state, const nugpr_rows* y,
                                  float* final_state, void* stream);

@@ -272,7 +272,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_scan(const ScanArgs a) {
   float bias[V], D[V], steps[V];
   a2.load(a, a.A + of_lane, wave, live);
   a2.scale(LOG2_E);
-  const float* start = p.span == 0 ? (a.s_in ? a.s_in + p.piece.seq * each : nullptr) : ADDS ? nullptr : a.adds + item * each;
+  // (the walk of several spans has the sequence's start state from k_scan_join too: the last of them may write over it)
+  const float* start = ADDS ? (p.span == 0 && a.s_in ? a.s_in + p.piece.seq * each : nullptr)
+                       : p.span == 0 && p.last ? (a.s_in ? a.s_in + p.piece.seq * each : nullptr) : a.adds + item * each;
   h.load(a, start + of_lane, wave, live && start);
   load_channels(bias, a.bias, p.channel, col, p.valid);
   load_channels(D, a.D, p.channel, col, p.valid);
@@ -361,8 +363,13 @@ __global__ __launch_bounds__(64) void k_scan_join(const ScanArgs a) {
     const int64_t first = (lo >> a.span_log2) + seq;
     const float* steps = a.steps + first * a.dim + at / a.states;
     const float a2 = a.A[at] * LOG2_E;
-    if (blockIdx.z == 0) join<false>(a.adds + first * each + at, steps, each, a.dim, spans, a2, a.adds[first * each + at]);
-    else join<true>(a.back + first * each + at, steps, each, a.dim, spans, a2, a.ds_end ? a.ds_end[seq * each + at] : 0.f);
+    if (blockIdx.z == 0) {
+      float* adds = a.adds + first * each + at;
+      const float h = adds[0];
+      adds[0] = a.s_in ? a.s_in[seq * each + at] : 0.f;
+      join<false>(adds, steps, each, a.dim, spans, a2, h);
+    }
+    if (blockIdx.z == 1) join<true>(a.back + first * each + at, steps, each, a.dim, spans, a2, a.ds_end ? a.ds_end[seq * each + at] : 0.f);
   }
 }
 
@@ -625,7 +632,8 @@ int nugpr_selective_scan_forward(const nugpr_selective_scan* p, const nugpr_rows
   }
   NUGPR_TRY(check_floats(initial_state, "initial_state", false));
   NUGPR_TRY(check_floats(final_state, "final_state", false));
-  if (overlap(initial_state, final_state, (size_t)p->n_seqs * p->dim * p->dim_state * sizeof(float))) return invalid("final_state overlaps initial_state");
+  if (initial_state != final_state && overlap(initial_state, final_state, (size_t)p->n_seqs * p->dim * p->dim_state * sizeof(float)))
+    return invalid("final_state overlaps initial_state, and is not it");
   a.s_in = initial_state; a.s_out = final_state;
   lay_out(p, false, p->workspace, &a);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);

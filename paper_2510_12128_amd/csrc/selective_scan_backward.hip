@@ -401,6 +401,11 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
         });
         if constexpr (GATE) part[2][wave][4 * q + lane % 4][ch] = sums_of_states<H::G>(y, lane);
         sums_of_channels<H>(of_c, &sums[buffer][1][wave][4 * q][0], lane);
+        if (4 * q + 4 > rows)                    // (rows that there are not have d = 0, which does not silence a state that is not finite)
+          repeat<4>([&](auto i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) h[4 * q + i + 1][s] = 4 * q + i + 1 >= rows ? 0.f : h[4 * q + i + 1][s];
+          });
         __builtin_amdgcn_sched_barrier(0);         // (what comes later is not read earlier: its registers are needed)
       });
       repeat<TILE_ROWS / 4>([&](auto back) __attribute__((always_inline)) {

@@ -309,3 +309,19 @@ def test_without_rows(lib):
     v, _, _, _, _ = inputs([4], 70, 1, 16, F32)
     with pytest.raises(lib.NugprError, match="no sequence"):
         forward(lib, v, none, start=False)
+
+
+@pytest.mark.parametrize("states", [16, 5, 40])
+@pytest.mark.parametrize("row", [36, 20, 41])
+def test_gradients_where_a_value_is_not_finite(lib, states, row):
+    """A NaN in a channel's x, in the last row of a sequence, amid it, or in the first: its gradients are NaN where the formulas make
+    them so and the numbers they were elsewhere."""
+    v, off, dev_off, dy, ds1 = inputs([37, 90], 70, 1, states, F32, seed=16)
+    clean = backward(lib, v, dev_off, dy, ds1)
+    v["x"][row, 3] = float("nan")
+    got = backward(lib, v, dev_off, dy, ds1)
+    want = wanted(v, off, dy, ds1, True)
+    for k in NAMES:
+        assert torch.equal(torch.isnan(got[k]).cpu(), torch.isnan(want[k])), k
+        fine = ~torch.isnan(got[k])
+        assert torch.equal(got[k][fine], clean[k][fine]), k

@@ -102,9 +102,11 @@ def test_bad_calls_of_scans(lib):  # noqa: F811
     for kw in (dict(A=None), dict(A=4097), dict(D=4098), dict(dt_bias=4097), dict(seq_offsets=None), dict(n_seqs=0)):
         assert list(scan_calls(lib, scan(**kw))) == [INVALID, INVALID]
     size = 3 * 64 * 16 * 4
-    for apart in (0, size - 4):
+    for apart in (4, size - 4):
         assert list(scan_calls(lib, scan(), s0=1 << 20, s1=(1 << 20) + apart)) == [INVALID, INVALID]
         assert b"overlaps" in lib.nugpr_last_error_string()
+    back = lib.nugpr_selective_scan_backward
+    assert back(C.byref(scan()), OK, OK, H, H, None, None, OK, 1 << 20, OK, OK, H, H, None, 4096, 4096, 4096, 1 << 20, None) == INVALID
     for kw in (dict(workspace=None), dict(workspace=4097), dict(workspace_bytes=10)):
         assert list(scan_calls(lib, scan(n_rows=1 << 20, **kw))) == [WORKSPACE, WORKSPACE]
     b = lib.nugpr_selective_scan_backward
