@@ -433,21 +433,24 @@ bool overlap(const void* a, const void* b, size_t bytes) {
 }
 
 // Channels of a lane: 16 bytes forward, four in the gradients, whose windows, weights and sums have to stay in registers.
-int lanes_forward(const nugpr_short_conv* p) { return p->dtype == NUGPR_BFLOAT16 ? 8 : 4; }
-constexpr int LANES_BACKWARD = 4;
+int channels_of(const nugpr_short_conv* p, bool backward) { return backward || p->dtype == NUGPR_FLOAT32 ? 4 : 8; }
+int64_t blocks_of(const nugpr_short_conv* p, bool backward) { return (p->dim + 64 * channels_of(p, backward) - 1) / (64 * channels_of(p, backward)); }
 
-// Rows of a wave: a power of two, 8 to 64, so that there are some 4096 waves.
-int run_of(const nugpr_short_conv* p, int v) {
-  const int64_t blocks = (p->dim + 64 * v - 1) / (64 * v);
+// Rows of a wave: a power of two, 8 to 64, so that there are some 2048 waves forward (16384 rows, 4096 channels, bfloat16: 67, 58 and 55 us with 8192,
+// 4096, 2048), twice as many in the gradients (16384 rows, 2048 channels: 68, 56 and 70).
+int run_of(const nugpr_short_conv* p, bool backward) {
   int run = 8;
-  while (run < 64 && p->n_rows / run * blocks > 4096) run *= 2;
+  while (run < 64 && p->n_rows / run * blocks_of(p, backward) > (backward ? 4096 : 2048)) run *= 2;
   return run;
 }
 
-int64_t groups_of(const nugpr_short_conv* p, int v) { return (p->n_rows + (int64_t)WAVES * run_of(p, v) - 1) / ((int64_t)WAVES * run_of(p, v)); }
+int64_t groups_of(const nugpr_short_conv* p, bool backward) {
+  const int64_t rows = (int64_t)WAVES * run_of(p, backward);
+  return (p->n_rows + rows - 1) / rows;
+}
 
 size_t sums_bytes(const nugpr_short_conv* p) {
-  return ((size_t)groups_of(p, LANES_BACKWARD) * (p->width + 1) * p->dim * sizeof(float) + 255) / 256 * 256;
+  return ((size_t)groups_of(p, true) * (p->width + 1) * p->dim * sizeof(float) + 255) / 256 * 256;
 }
 
 #define NUGPR_TRY(call)                 \
@@ -471,11 +474,11 @@ void with_width(int width, F f) {
 }
 
 // What both calls over sequences share; the grid's workgroups, behind those of the rows one for every four windows that are written.
-int conv_args(const nugpr_short_conv* p, int v, bool windows, ConvArgs& a, int64_t& grid) {
+int conv_args(const nugpr_short_conv* p, bool backward, bool windows, ConvArgs& a, int64_t& grid) {
   a.weight = p->weight; a.bias = p->bias; a.off = p->seq_offsets; a.n_rows = p->n_rows; a.n_seqs = p->n_seqs;
-  a.dim = p->dim; a.silu = p->silu != 0; a.run = run_of(p, v);
-  a.col_blocks = (p->dim + 64 * v - 1) / (64 * v);
-  a.runs = groups_of(p, v);
+  a.dim = p->dim; a.silu = p->silu != 0; a.run = run_of(p, backward);
+  a.col_blocks = (int)blocks_of(p, backward);
+  a.runs = groups_of(p, backward);
   grid = (a.runs + (windows ? (p->n_seqs + WAVES - 1) / WAVES : 0)) * a.col_blocks;
   // (the threads of a launch are counted in 32 bits)
   if (grid > (int64_t)0xffffffff / THREADS) return invalid("too many rows, sequences and channels for one call");
@@ -513,7 +516,7 @@ int nugpr_short_conv_forward(const nugpr_short_conv* p, const nugpr_rows* x, con
   ConvArgs a{};
   int64_t grid;
   const bool windows = final_window && p->width > 1;
-  NUGPR_TRY(conv_args(p, lanes_forward(p), windows, a, grid));
+  NUGPR_TRY(conv_args(p, false, windows, a, grid));
   if (p->n_rows > 0) { a.x = x->data; a.x_row = x->row_stride; a.y = y->data; a.y_row = y->row_stride; }
   a.w_in = initial_window; a.w_out = final_window;
   if (grid == 0) return NUGPR_OK;
@@ -551,7 +554,7 @@ int nugpr_short_conv_backward(const nugpr_short_conv* p, const nugpr_rows* x, co
   if (p->workspace_bytes < need) { set_error("workspace smaller than nugpr_short_conv_workspace_bytes()"); return NUGPR_ERR_WORKSPACE; }
   ConvArgs a{};
   int64_t grid;
-  NUGPR_TRY(conv_args(p, LANES_BACKWARD, d_initial_window && p->width > 1, a, grid));
+  NUGPR_TRY(conv_args(p, true, d_initial_window && p->width > 1, a, grid));
   if (p->n_rows > 0) {
     a.x = x->data; a.x_row = x->row_stride; a.dy = d_y->data; a.dy_row = d_y->row_stride; a.dx = dx->data; a.dx_row = dx->row_stride;
   }
