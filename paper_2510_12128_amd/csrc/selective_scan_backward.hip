@@ -230,8 +230,8 @@ __device__ __forceinline__ void swap_rows(float& x, float& y) {
   x = __builtin_bit_cast(float, (uint32_t)v[0]);
   y = __builtin_bit_cast(float, (uint32_t)v[1]);
 }
-// v of another lane: of those quad by quad, mirrored among 8 or 16, eight on among 16
-enum { SWAP_ONE = 0xb1, SWAP_TWO = 0x4e, MIRROR_16 = 0x140, MIRROR_8 = 0x141, EIGHT_ON = 0x128, FROM_ABOVE_4 = 0x104, FROM_BELOW_4 = 0x114 };
+// v of another lane: of those quad by quad, mirrored among 8 or 16, four above or below
+enum { SWAP_ONE = 0xb1, SWAP_TWO = 0x4e, MIRROR_16 = 0x140, MIRROR_8 = 0x141, FROM_ABOVE_4 = 0x104, FROM_BELOW_4 = 0x114 };
 template <int WHICH>
 __device__ __forceinline__ float moved(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), WHICH, 0xf, 0xf, true));
@@ -257,39 +257,78 @@ __device__ __forceinline__ float sums_of_states(float (&v)[4], int lane) {
   return (upper ? y : x) + moved<SWAP_TWO>(upper ? x : y);
 }
 
+// Numbers of two states (or of two pairs of them) joined in one register, for two rows: the sum with the lane eight on among 16, of the first in the
+// lower eight lanes and of the second in the upper; then, of what these leave of four states, the same with the lane four on or back.  An addition that
+// writes a part of the lanes does what otherwise takes two selections and an addition; the compiler does not make it.  (s_nop: what a vector
+// instruction has just written can be read so, and swapped, two steps later.)
+__device__ __forceinline__ void join_eight_on(float& x, float& y, float a0, float a1, float b0, float b1) {
+  asm("s_nop 1\n\t"
+      "v_add_f32_dpp %0, %2, %2 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+      "v_add_f32_dpp %1, %4, %4 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+      "v_add_f32_dpp %0, %3, %3 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+      "v_add_f32_dpp %1, %5, %5 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+      "s_nop 1"
+      : "=&v"(x), "=&v"(y)
+      : "v"(a0), "v"(a1), "v"(b0), "v"(b1));
+}
+__device__ __forceinline__ void join_four_states(float& x, float& y, const float (&a)[4], const float (&b)[4]) {
+  float p, q, r, s;
+  asm("s_nop 1\n\t"
+      "v_add_f32_dpp %2, %6, %6 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+      "v_add_f32_dpp %3, %7, %7 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+      "v_add_f32_dpp %2, %8, %8 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+      "v_add_f32_dpp %3, %9, %9 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+      "v_add_f32_dpp %4, %10, %10 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+      "v_add_f32_dpp %5, %11, %11 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+      "v_add_f32_dpp %4, %12, %12 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+      "v_add_f32_dpp %5, %13, %13 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+      "v_add_f32_dpp %0, %2, %2 row_shl:4 row_mask:0xf bank_mask:0x5\n\t"
+      "v_add_f32_dpp %0, %3, %3 row_shr:4 row_mask:0xf bank_mask:0xa\n\t"
+      "v_add_f32_dpp %1, %4, %4 row_shl:4 row_mask:0xf bank_mask:0x5\n\t"
+      "v_add_f32_dpp %1, %5, %5 row_shr:4 row_mask:0xf bank_mask:0xa\n\t"
+      "s_nop 1"
+      : "=&v"(x), "=&v"(y), "=&v"(p), "=&v"(q), "=&v"(r), "=&v"(s)
+      : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]));
+}
+
+// Four rows' numbers, one register each, to one: lane l gets the sum, over the lanes that differ in the upper two bits, of row l / 16.
+__device__ __forceinline__ float join_rows(float a, float b, float c, float d) {
+  swap_halves(a, c);
+  swap_halves(b, d);
+  float x = a + c, y = b + d;
+  swap_rows(x, y);
+  return x + y;
+}
+
 // Sums over the wave's channels of four rows' numbers for the lane's S states, to out[4][NS] in LDS.
 template <class H>
 __device__ __forceinline__ void sums_of_channels(float (&v)[4][H::S], float* out, int lane) {
   constexpr int S = H::S;
-  float w[2][S], z[S];
-#pragma unroll
-  for (int s = 0; s < S; ++s) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      swap_halves(v[i][s], v[i + 2][s]);
-      w[i][s] = v[i][s] + v[i + 2][s];
-    }
-    swap_rows(w[0][s], w[1][s]);
-    z[s] = w[0][s] + w[1][s];                      // row lane / 16
-  }
   out += lane / 16 * H::NS + lane % H::G * S;
   if constexpr (H::G == 16) {
-    *reinterpret_cast<float4*>(out) = float4{z[0], z[1], z[2], z[3]};
-  } else {
-    const bool upper = lane & 8;
-    float k[S / 2];
+    float4 z;
+    z.x = join_rows(v[0][0], v[1][0], v[2][0], v[3][0]);
+    z.y = join_rows(v[0][1], v[1][1], v[2][1], v[3][1]);
+    z.z = join_rows(v[0][2], v[1][2], v[2][2], v[3][2]);
+    z.w = join_rows(v[0][3], v[1][3], v[2][3], v[3][3]);
+    *reinterpret_cast<float4*>(out) = z;
+  } else if constexpr (H::G == 8) {                // lower eight lanes: states 0 and 1
+    float a[4], b[4];
 #pragma unroll
-    for (int s = 0; s < S / 2; ++s) k[s] = (upper ? z[s + S / 2] : z[s]) + moved<EIGHT_ON>(upper ? z[s] : z[s + S / 2]);
-    out += upper ? S / 2 : 0;
-    if constexpr (H::G == 8) {
-      *reinterpret_cast<float2*>(out) = float2{k[0], k[1]};
-    } else if constexpr (S == 4) {
-      const bool more = lane & 4;
-      out[more ? 1 : 0] = (more ? k[1] : k[0]) + across_four(more ? k[0] : k[1]);
-    } else {
-      const float x = k[0] + across_four(k[0]);
-      if (!(lane & 4)) out[0] = x;
-    }
+    for (int i = 0; i < 4; ++i) join_eight_on(a[i], b[i], v[i][0], v[i][2], v[i][1], v[i][3]);
+    *reinterpret_cast<float2*>(out + (lane & 8 ? 2 : 0)) = float2{join_rows(a[0], a[1], a[2], a[3]), join_rows(b[0], b[1], b[2], b[3])};
+  } else if constexpr (S == 4) {                   // lanes by four: states 0, 1, 2, 3
+    float a[4];
+    join_four_states(a[0], a[1], v[0], v[1]);
+    join_four_states(a[2], a[3], v[2], v[3]);
+    out[lane % 16 / 4] = join_rows(a[0], a[1], a[2], a[3]);
+  } else {
+    float a[4];
+    join_eight_on(a[0], a[1], v[0][0], v[0][1], v[1][0], v[1][1]);
+    join_eight_on(a[2], a[3], v[2][0], v[2][1], v[3][0], v[3][1]);
+    float x = join_rows(a[0], a[1], a[2], a[3]);
+    x += across_four(x);
+    if (!(lane & 4)) out[lane & 8 ? 1 : 0] = x;
   }
 }
 
