@@ -340,6 +340,8 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
   __shared__ float part[GATE ? 3 : 2][H::WAVES][TILE_ROWS][H::CW];       // sums over the states: du, dd, y, every wave's own
   __shared__ alignas(16) float sums[2][2][H::WAVES][TILE_ROWS][H::NS];               // over a wave's channels: dB, dC
   __shared__ float of_channel[2][H::CB];                                 // bias and D
+  constexpr bool NEAR = H::G < 16;
+  __shared__ alignas(16) float starts[NEAR ? H::THREADS : 1][S];         // the lanes' states at the span's begin, where there is room
   const int item = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
   if (item >= a.items) {
     const int who = blockIdx.x - a.items * a.blocks;
@@ -401,23 +403,39 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
     Incoming<TR, H, true> in;
     in.begin(a, p, wave, lane, p.from + (int64_t)(tiles - 1) * TILE_ROWS);
     if (tiles > 0) in.load(a, p, lane, (int)(p.to - p.from - (int64_t)(tiles - 1) * TILE_ROWS), valid, -1);
+    // the states at the next tile's begin, and the span's steps before it, on their way while a tile is worked through
+    float begin[S], passed = 0.f;
+    const auto load_begin = [&](int k) __attribute__((always_inline)) {
+      __builtin_memcpy(begin, kept<H>(a, number + k, block), sizeof begin);
+      if (p.span > 0 && ch < valid) passed = a.tile_steps[(number + k) * a.dim + channel + ch];
+    };
+    if (tiles > 0) load_begin(tiles - 1);
+    if (NEAR && p.span > 0) {
+      float start[S];
+      load_states(start, a.adds + item * each + of_lane, n);
+      __builtin_memcpy(starts[threadIdx.x], start, sizeof start);
+    }
     int buffer = 0;
     for (int k = tiles - 1; k >= 0; --k, buffer ^= 1) {
       const int64_t t0 = p.from + (int64_t)k * TILE_ROWS;
       const int rows = (int)min((int64_t)TILE_ROWS, p.to - t0);
       float h[TILE_ROWS + 1][S], f[TILE_ROWS][S];                        // h_{t-1} and on, a_t
-      __builtin_memcpy(h[0], kept<H>(a, number + k, block), sizeof h[0]);
+#pragma unroll
+      for (int s = 0; s < S; ++s) h[0][s] = begin[s];
+      if (p.span > 0) {                                                  // (its walk began at zero)
+        float start[S];
+        if constexpr (NEAR) read_states(start, starts[threadIdx.x]);
+        else load_states(start, a.adds + item * each + of_lane, n);
+#pragma unroll
+        for (int s = 0; s < S; ++s) h[0][s] = start[s] == 0.f ? h[0][s] : fmaf(exp2_of(a2[s] * passed), start[s], h[0][s]);
+      }
       fill_tile(tile, a, in, wave, lane, buffer, rows, valid, bias);
       const Values<TR, V> x_now = in.x, dt_now = in.dt, z_now = in.z, dy_now = in.dy;
       __syncthreads();
       if (k + 1 < tiles) gather(buffer ^ 1, t0 + TILE_ROWS, (int)min((int64_t)TILE_ROWS, p.to - t0 - TILE_ROWS));
-      if (k > 0) in.load(a, p, lane, TILE_ROWS, valid, -1);
-      if (p.span > 0) {                                                  // (its walk began at zero)
-        float start[S];
-        load_states(start, a.adds + item * each + of_lane, n);
-        const float d = ch < valid ? a.tile_steps[(number + k) * a.dim + channel + ch] : 0.f;
-#pragma unroll
-        for (int s = 0; s < S; ++s) h[0][s] = start[s] == 0.f ? h[0][s] : fmaf(exp2_of(a2[s] * d), start[s], h[0][s]);
+      if (k > 0) {
+        in.load(a, p, lane, TILE_ROWS, valid, -1);
+        load_begin(k - 1);
       }
       repeat<TILE_ROWS / 4>([&](auto q) __attribute__((always_inline)) {
         float of_c[4][S], y[4];
