@@ -6,6 +6,8 @@
 //
 // Memory traffic bounds it.  A wave takes a run of rows of 64 V channels, V side by side a lane, and keeps the rows that it
 // still needs in registers, so that a row is read once, and W - 1 rows more a run.
+#include <algorithm>
+
 #include "nugpr_internal.h"
 #include "packed_rows.h"
 #include "row_values.h"
@@ -16,6 +18,7 @@ namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int MAX_WIDTH = 8;
+constexpr int COMPUTE_UNITS = 256;
 constexpr int AHEAD = 4;               // rows that are loaded at one time
 
 struct ConvArgs {
@@ -30,7 +33,7 @@ struct ConvArgs {
   int64_t n_rows;
   int64_t runs;                        // workgroups along the rows
   int n_seqs, dim, silu, col_blocks;
-  int run;                             // rows of a wave
+  int64_t run;                         // rows of a wave
 };
 
 template <class TR>
@@ -436,16 +439,16 @@ bool overlap(const void* a, const void* b, size_t bytes) {
 int channels_of(const nugpr_short_conv* p, bool backward) { return backward || p->dtype == NUGPR_FLOAT32 ? 4 : 8; }
 int64_t blocks_of(const nugpr_short_conv* p, bool backward) { return (p->dim + 64 * channels_of(p, backward) - 1) / (64 * channels_of(p, backward)); }
 
-// Rows of a wave: a power of two, 8 to 64, so that there are some 2048 waves forward (16384 rows, 4096 channels, bfloat16: 67, 58 and 55 us with 8192,
-// 4096, 2048), twice as many in the gradients (16384 rows, 2048 channels: 68, 56 and 70).
-int run_of(const nugpr_short_conv* p, bool backward) {
-  int run = 8;
-  while (run < 64 && p->n_rows / run * blocks_of(p, backward) > (backward ? 4096 : 2048)) run *= 2;
-  return run;
+// Rows of a wave, eight or more, so many that the workgroups are two for each compute unit, four in the gradients, or somewhat fewer: a few more of
+// them than there is room for take a turn of their own (22980 rows, 1408 channels, float32: 71 us in 540 workgroups, 61 in 510).  16384 rows, 4096 channels,
+// bfloat16: 55, 58, 67 us with two, four, eight; gradients, 2048 channels: 68, 55, 66.
+int64_t run_of(const nugpr_short_conv* p, bool backward) {
+  const int64_t along = std::max<int64_t>(1, COMPUTE_UNITS * (backward ? 4 : 2) / blocks_of(p, backward));
+  return std::max<int64_t>(8, (p->n_rows + along * WAVES - 1) / (along * WAVES));
 }
 
 int64_t groups_of(const nugpr_short_conv* p, bool backward) {
-  const int64_t rows = (int64_t)WAVES * run_of(p, backward);
+  const int64_t rows = WAVES * run_of(p, backward);
   return (p->n_rows + rows - 1) / rows;
 }
 

@@ -73,9 +73,9 @@ def test_bad_calls_of_convolutions(lib):  # noqa: F811
 
 
 def test_convolutions_beyond_a_launch(lib):  # noqa: F811
-    """2^32 threads of one launch, 32 rows and 256 channels a workgroup of 256."""
-    p = conv(n_rows=1 << 36, dim=65536, workspace_bytes=1 << 62)
-    assert list(conv_calls(lib, p)) == [INVALID, INVALID]
+    """2^32 threads of one launch: rows there may be as many as there are, windows that are written not."""
+    p = conv(n_seqs=1 << 30, dim=65536, workspace_bytes=1 << 62)
+    assert list(conv_calls(lib, p, s1=1 << 20)) == [INVALID, INVALID]
     assert b"too many" in lib.nugpr_last_error_string()
     p = conv(n_rows=1 << 30, n_seqs=1 << 30, dim=65536)
     assert lib.nugpr_short_conv_step(C.byref(p), OK, 4096, None, OK, None) == INVALID
