@@ -39,6 +39,12 @@ struct ScanArgs {
   float *dA_out, *dD_out, *dbias_out;
 };
 
+// A as the exponents of two take it: a factor is 2^(d rate).  (-infinity as a number, so that rows with d = 0 keep the state; NaN stays.)
+__device__ __forceinline__ float rate_of(float A) {
+  const float r = A * LOG2_E;
+  return r < -3e38f ? -3e38f : r;
+}
+
 // Where a workgroup stands.
 struct Place {
   int group, channel, valid;         // its first channel, and how many it has

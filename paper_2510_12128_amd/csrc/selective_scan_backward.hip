@@ -165,7 +165,7 @@ __global__ __launch_bounds__(H::THREADS) void k_scan_tiles(const ScanArgs a) {
   load_states(a2, a.A + of_lane, n);
 #pragma unroll
   for (int s = 0; s < S; ++s) {
-    a2[s] *= LOG2_E;
+    a2[s] = rate_of(a2[s]);
     product[s] = 1.f;
     g[s] = 0.f;
   }
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
     const float* D = &of_channel[1][wave * H::CW + col];
     load_states(a2, a.A + of_lane, n);
 #pragma unroll
-    for (int s = 0; s < S; ++s) a2[s] *= LOG2_E;
+    for (int s = 0; s < S; ++s) a2[s] = rate_of(a2[s]);
     const float* end = p.last && p.span == 0 ? (a.ds_end ? a.ds_end + p.piece.seq * each : nullptr) : a.back + item * each;
     load_states(g, end + of_lane, end ? n : 0);
     const int tiles = (int)((p.to - p.from + TILE_ROWS - 1) / TILE_ROWS);

@@ -325,3 +325,23 @@ def test_gradients_where_a_value_is_not_finite(lib, states, row):
         assert torch.equal(torch.isnan(got[k]).cpu(), torch.isnan(want[k])), k
         fine = ~torch.isnan(got[k])
         assert torch.equal(got[k][fine], clean[k][fine]), k
+
+
+def test_rates_at_the_ends_of_their_range(lib):
+    """A = 0 keeps everything, -infinity nothing; in sequences of no, one and several spans, that end amid a tile."""
+    v, off, dev_off, dy, ds1 = inputs([5, 300, 0, 37], 40, 1, 8, F32, seed=21)
+    v["A"][:, 0], v["A"][:, 1], v["A"][:, 2] = 0.0, float("-inf"), -1e38
+    y, end = forward(lib, v, dev_off)
+    want, w_end = reference(double(v), off, True)
+    # (the states that keep everything are sums of 300 terms that nothing scales down)
+    close(y, want, 4 * TOL[F32], "y", reference(magnitudes(double(v)), off, True)[0])
+    close(end, w_end, 4 * TOL[F32], "state")
+    got = backward(lib, v, dev_off, dy, ds1)
+    assert all(bool(torch.isfinite(t).all()) for t in got.values())
+    state = v["s0"].clone()
+    y = lib.nugpr_selective_scan_step(v["x"][:4], v["dt"][:4], v["A"], v["B"][:4], v["C"][:4], state, D=v["D"], z=v["z"][:4],
+                                      dt_bias=v["dt_bias"])
+    one = {k: t[:4] if k in ("x", "dt", "B", "C", "z") else t for k, t in double(v).items()}
+    want, w_end = reference(one, [0, 1, 2, 3, 4], True)
+    close(y, want, TOL[F32])
+    close(state, w_end, TOL[F32])
