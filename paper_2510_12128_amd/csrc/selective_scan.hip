@@ -543,7 +543,7 @@ int check_call(const nugpr_selective_scan* p, bool backward, bool* done) {
   if (p->n_seqs < 1 || !p->seq_offsets) return invalid("seq_offsets is null, or there is no sequence");
   // (the threads of a launch are counted in 32 bits)
   if (items_of(p, backward) * blocks_of(p, backward) + ZERO_GROUPS > (int64_t)0xffffffff / threads_of(p, backward) ||
-      (backward && p->n_rows * p->groups * p->dim_state > (int64_t)0xffffffff - 256))
+      (backward && p->n_rows * p->groups * p->dim_state > (int64_t)0xffffffff / 2 - 3 * 4 * 65536 * 64))
     return invalid("too many rows, sequences and channels for one call");
   const size_t need = lay_out(p, backward, nullptr, nullptr);
   if (need && (!p->workspace || (reinterpret_cast<uintptr_t>(p->workspace) & 255u))) { set_error("workspace is null or not 256-byte aligned"); return NUGPR_ERR_WORKSPACE; }

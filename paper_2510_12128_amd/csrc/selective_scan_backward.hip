@@ -552,32 +552,38 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
   if (a.bias) of_rows(dbias, a.dbias + (int64_t)item * a.dim);
 }
 
-// dB and dC from the channel blocks' parts, in their order; zero where no sequence owns the row.
+// The gradients that are sums, from their parts in their order.  The first workgroups have dB and dC, from the channel blocks' parts (zero where no
+// sequence owns the row), then those of dA, dD and dbias, from the spans' parts, each wave of a workgroup a quarter of them.
+struct Sums {
+  int64_t rows;       // workgroups of dB, and of dC
+  int64_t channels;   // of dA, and of dD, and of dbias: 64 sums each
+};
 template <class TR>
-__global__ __launch_bounds__(256) void k_scan_sum_blocks(const ScanArgs a) {
+__global__ __launch_bounds__(256) void k_scan_sums(const ScanArgs a, const Sums w) {
   typedef typename TR::T T;
-  const int64_t stride = (int64_t)a.groups * a.states, total = a.n_rows * stride, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= total) return;
-  const int64_t row = at / stride;
-  const int group = (int)(at % stride) / a.states, n = (int)(at % stride) % a.states, parts = a.blocks / a.groups;
-  const int64_t first = clamped(a.off[0], 0, a.n_rows), last = clamped(a.off[a.n_seqs], first, a.n_rows);
-  const float* from = (blockIdx.y ? a.dC : a.dB) + at;
-  float s = 0.f;
-  if (row >= first && row < last)
-#pragma unroll 8
-    for (int k = 0; k < parts; ++k) s += from[k * total];
-  if (blockIdx.y) static_cast<T*>(a.dC_out)[row * a.dC_row + group * a.dC_head + n] = TR::put(s);
-  else static_cast<T*>(a.dB_out)[row * a.dB_row + group * a.dB_head + n] = TR::put(s);
-}
-
-// dA, dD and dbias from the spans' parts, in their order: each wave of a workgroup a quarter of them.
-__global__ __launch_bounds__(256) void k_scan_sum_items(const ScanArgs a) {
   __shared__ float part[4][64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const float* from = blockIdx.y == 0 ? a.dA : blockIdx.y == 1 ? a.dD : a.dbias;
-  float* to = blockIdx.y == 0 ? a.dA_out : blockIdx.y == 1 ? a.dD_out : a.dbias_out;
-  const int64_t size = (int64_t)a.dim * (blockIdx.y == 0 ? a.states : 1), at = (int64_t)blockIdx.x * 64 + lane;
-  if (!to || (int64_t)blockIdx.x * 64 >= size) return;
+  if (blockIdx.x < 2 * w.rows) {
+    const bool is_C = blockIdx.x >= w.rows;
+    const int64_t stride = (int64_t)a.groups * a.states, total = a.n_rows * stride, at = (blockIdx.x - (is_C ? w.rows : 0)) * 256 + threadIdx.x;
+    if (at >= total) return;
+    const int64_t row = at / stride;
+    const int group = (int)(at % stride) / a.states, n = (int)(at % stride) % a.states, parts = a.blocks / a.groups;
+    const int64_t first = clamped(a.off[0], 0, a.n_rows), last = clamped(a.off[a.n_seqs], first, a.n_rows);
+    const float* from = (is_C ? a.dC : a.dB) + at;
+    float s = 0.f;
+    if (row >= first && row < last)
+#pragma unroll 8
+      for (int k = 0; k < parts; ++k) s += from[k * total];
+    if (is_C) static_cast<T*>(a.dC_out)[row * a.dC_row + group * a.dC_head + n] = TR::put(s);
+    else static_cast<T*>(a.dB_out)[row * a.dB_row + group * a.dB_head + n] = TR::put(s);
+    return;
+  }
+  const int64_t block = blockIdx.x - 2 * w.rows;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, which = (int)(block / w.channels);
+  const float* from = which == 0 ? a.dA : which == 1 ? a.dD : a.dbias;
+  float* to = which == 0 ? a.dA_out : which == 1 ? a.dD_out : a.dbias_out;
+  const int64_t size = (int64_t)a.dim * (which == 0 ? a.states : 1), at = block % w.channels * 64 + lane;
+  if (!to || at - lane >= size) return;
   const int each = (a.items + 3) / 4, end = min(a.items, (wave + 1) * each);
   float s = 0.f;
   if (at < size)
@@ -616,8 +622,8 @@ void launch(const ScanArgs& a, bool one_span, void (*join)(const ScanArgs&, bool
       else hipLaunchKernelGGL((k_scan_backward<TR, H, EXACT, false>), all, threads, 0, s, a);
     });
   const int64_t values = a.n_rows * a.groups * a.states, each = (int64_t)a.dim * a.states;
-  if (values) hipLaunchKernelGGL(k_scan_sum_blocks<TR>, dim3((unsigned)((values + 255) / 256), 2), dim3(256), 0, s, a);
-  hipLaunchKernelGGL(k_scan_sum_items, dim3((unsigned)((each + 63) / 64), 3), dim3(256), 0, s, a);
+  const Sums w{(values + 255) / 256, (each + 63) / 64};
+  hipLaunchKernelGGL(k_scan_sums<TR>, dim3((unsigned)(2 * w.rows + 3 * w.channels)), dim3(256), 0, s, a, w);
 }
 
 }  // namespace
