@@ -345,3 +345,54 @@ def test_rates_at_the_ends_of_their_range(lib):
     want, w_end = reference(one, [0, 1, 2, 3, 4], True)
     close(y, want, TOL[F32])
     close(state, w_end, TOL[F32])
+
+
+@pytest.mark.parametrize("many", [3, 60, 250, 1100])
+def test_wide_layers(lib, many):
+    """So many channels that a sequence need not be cut for want of work: alone and among sequences by the thousand, where it is.
+    The reference has some of the channels, which do not read each other."""
+    dim, rows, keep = 32768, 700, [0, 63, 64, 20000, 32767]
+    lens = [1] * (many // 2) + [rows] + [1] * (many - many // 2)
+    off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+    dev = torch.from_numpy(off).cuda()
+    gen = torch.Generator(device="cuda").manual_seed(many)
+
+    def r(*shape):
+        return torch.randn(*shape, generator=gen, device="cuda")
+
+    n = sum(lens)
+    v = dict(x=r(n, dim), dt=r(n, dim) * 0.3 - 2.0, A=-torch.rand(dim, 2, generator=gen, device="cuda") - 0.2, B=r(n, 1, 2), C=r(n, 1, 2), D=r(dim),
+             z=None, dt_bias=None, s0=r(len(lens), dim, 2))
+    dy, ds1 = r(n, dim), r(len(lens), dim, 2)
+
+    def some(t, k):
+        if t is None or k in ("B", "C"):
+            return t
+        return t[:, keep] if k in ("x", "dt", "s0") else t[keep]
+
+    few = {k: some(t, k) for k, t in v.items()}
+    y, end = forward(lib, v, dev)
+    want, w_end = reference(double(few), off, True)
+    close(y[:, keep], want, TOL[F32], "y", reference(magnitudes(double(few)), off, True)[0])
+    close(end[:, keep], w_end, TOL[F32], "state")
+    got, g_want = backward(lib, v, dev, dy, ds1), wanted(few, off, dy[:, keep], ds1[:, keep], True)
+    terms = wanted(magnitudes(few), off, dy[:, keep].abs(), ds1[:, keep].abs(), True)
+    for k in ("x", "dt", "A", "D", "s0"):
+        close(some(got[k], k), g_want[k], TOL[F32], k, terms[k])
+
+
+def test_sequences_by_the_hundred(lib):
+    """Equal ones, which are walked through whole, and two long ones among them, for which all are cut: the same values."""
+    lens = [20] * 150 + [3000, 1200] + [20] * 90
+    v, off, dev, dy, ds1 = inputs(lens, 24, 1, 4, F32, seed=33)
+    y, end = forward(lib, v, dev)
+    want, w_end = reference(double(v), off, True)
+    close(y, want, TOL[F32], "y", reference(magnitudes(double(v)), off, True)[0])
+    close(end, w_end, TOL[F32], "state")
+    got, g_want = backward(lib, v, dev, dy, ds1), wanted(v, off, dy, ds1, True)
+    for k in NAMES:
+        close(got[k], g_want[k], TOL[F32], k)
+    short = {k: t[:3000] if k in ("x", "dt", "B", "C", "z") else t[:150] if k == "s0" else t for k, t in v.items()}
+    y, end = forward(lib, short, dev[:151])
+    close(y, want[:3000], TOL[F32], "y")
+    close(end, w_end[:150], TOL[F32], "state")
