@@ -486,16 +486,21 @@ int blocks_of(const nugpr_selective_scan* p, bool backward) {
   return p->groups * ((each + width - 1) / width);
 }
 
-// Rows of a span: a power of two, a few tiles at least, so large that the spans of the rows give about 16384 waves, 4096 in the gradients, of
-// which a compute unit holds a third as many.
 int64_t waves_a_row(const nugpr_selective_scan* p, bool backward) { return (int64_t)blocks_of(p, backward) * (threads_of(p, backward) / 64); }
+
+// Rows of a span: a power of two, a few tiles at least, so large that
+// - the spans of the rows give at most 12288 waves, 4096 in the gradients (1 x 8192 rows, 2048 channels: 141 us with up to 4096, 8192, 12288 waves, 153 with
+//   16384; 1 x 32768: 493, 464, 463, 460; 40 ragged sequences, 20011 rows, 1000 channels, float32: 227, 197, 176, 176), and
+// - a sequence has at most twice as many spans as a span has rows, as the spans are joined one after the other (64 channels: 1 x 65536 rows 213 us with
+//   spans of 64, 104 with 256; 1 x 262144 460 and 236; gradients 304 and 200, 558 and 473).  Sequences' lengths are not known here: four times the mean.
 int span_log2(const nugpr_selective_scan* p, bool backward) {
+  const int64_t length = p->n_seqs > 4 ? p->n_rows / p->n_seqs * 4 : p->n_rows, waves = p->n_rows * waves_a_row(p, backward);
   int k = 6;
-  while (k < 40 && ((p->n_rows * waves_a_row(p, backward)) >> k) > (backward ? 4096 : 16384)) ++k;
+  while (k < 40 && ((waves >> k) > (backward ? 4096 : 12288) || (length >> k) > (int64_t)2 << k)) ++k;
   return k;
 }
 // Sequences are walked through whole where none has more rows than leave 2048 waves, two for each SIMD: cutting them costs a second pass over their rows.
-// (16 x 1024 rows, 2048 channels: 265 us cut, 190 whole; 8 x 2048: 275 and 342.  In the gradients 676 and 610; 654 and 1157.)
+// (16 x 1024 rows, 2048 channels: 265 us cut, 202 whole; 8 x 2048: 242 and 342.  In the gradients 676 and 609; 654 and 1157.)
 int64_t whole_of(const nugpr_selective_scan* p, bool backward) {
   const int64_t span = (int64_t)1 << span_log2(p, backward);
   return p->n_seqs > COUNTED ? span : std::max(span, p->n_rows * waves_a_row(p, backward) / 2048);
