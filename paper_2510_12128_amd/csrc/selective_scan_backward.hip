@@ -147,6 +147,9 @@ __device__ __forceinline__ float* kept(const ScanArgs& a, int64_t tile, int bloc
 }
 __device__ __forceinline__ int64_t first_tile(const Place& p) { return p.piece.lo / TILE_ROWS + p.piece.seq + (p.from - p.piece.lo) / TILE_ROWS; }
 
+// The first walk.  Factors multiply up over a span for what it adds to the gradient before it; of a sequence's first span that is not wanted, so that
+// the walk of sequences that are not cut is the states' alone.  The vector pipe bounds it: 8 x 2048 rows, 2048 channels, 16 states, bfloat16: 180 us.
+//
 // EXACT: the states fill the lanes' places.  Else those that there are not stay zero (nothing is multiplied by a zero there, where an
 // infinity would become NaN): `n` are the lane's.
 template <class TR, class H, bool EXACT>
@@ -332,6 +335,10 @@ __device__ __forceinline__ void sums_of_channels(float (&v)[4][H::S], float* out
   }
 }
 
+// The second walk.  A tile's 16 states and factors, 32 S registers, are what lets it go back without computing them again or dividing by a factor that may be
+// zero; with them two waves fit into a SIMD, and the vector pipe is busy 73 % of the time: 8 x 2048 rows, 2048 channels, 16 states, bfloat16, 520 us, where
+// its instructions alone take 380.  The rest are waits for LDS that two waves cannot fill.  (Half tiles, with three waves a SIMD, took longer; waves that share
+// out a channel's states, as forward, with more barriers a tile, 160 us more.)
 template <class TR, class H, bool EXACT, bool GATE>
 __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs a) {
   typedef typename TR::T T;
@@ -553,7 +560,8 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
 }
 
 // The gradients that are sums, from their parts in their order.  The first workgroups have dB and dC, from the channel blocks' parts (zero where no
-// sequence owns the row), then those of dA, dD and dbias, from the spans' parts, each wave of a workgroup a quarter of them.
+// sequence owns the row), then those of dA, dD and dbias, from the spans' parts, each wave of a workgroup a quarter of them.  (15 us for 16384 rows, 2048
+// channels: 32 parts of dB and dC, 67 MB.)
 struct Sums {
   int64_t rows;       // workgroups of dB, and of dC
   int64_t channels;   // of dA, and of dD, and of dbias: 64 sums each

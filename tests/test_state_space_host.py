@@ -126,6 +126,11 @@ def test_scans_beyond_a_launch(lib):  # noqa: F811
     p = scan(n_seqs=1 << 27, n_rows=1 << 20, workspace_bytes=1 << 62)
     assert list(scan_calls(lib, p)) == [INVALID, INVALID]
     assert b"too many" in lib.nugpr_last_error_string()
+    for rows in (1 << 27, 1 << 40):         # (gradients of B and C: a thread for each of their values)
+        p = scan(n_rows=rows, groups=1, workspace_bytes=1 << 62)
+        assert lib.nugpr_selective_scan_backward(C.byref(p), OK, OK, H, H, None, None, OK, None, OK, OK, H, H, None, 4096, None,
+                                                 None, None, None) == INVALID
+        assert b"too many" in lib.nugpr_last_error_string()
     p = scan(n_rows=1 << 30, n_seqs=1 << 30, dim=4096)
     assert lib.nugpr_selective_scan_step(C.byref(p), OK, OK, H, H, None, 4096, None, OK, None) == INVALID
 
