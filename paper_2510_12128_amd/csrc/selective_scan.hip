@@ -350,8 +350,8 @@ __device__ __forceinline__ void join(float* at, const float* steps, int64_t each
   }
 }
 
-// A lane has one state of a channel.  What a span takes is the wait for its two loads, shared by the AHEAD that are on their way: 128 spans of 2048 channels and
-// 16 states take 26 us, 32 take 9; 16 at one time took longer where sequences are short (20 instead of 15 us for 40 of them).
+// A lane has one state of a channel.  What a span takes is the wait for its two loads, shared by the AHEAD that are on their way: 64 spans of 2048 channels and
+// 16 states take 16 us, 32 take 9; 16 at one time took longer where sequences are short (20 instead of 15 us for 40 of them).
 __global__ __launch_bounds__(64) void k_scan_join(const ScanArgs a) {
   const int64_t each = (int64_t)a.dim * a.states, mine = (int64_t)blockIdx.x * 64 + threadIdx.x;
   const int64_t at = min(mine, each - 1);            // (all lanes count; the last ones of the last workgroup only count)
