@@ -449,9 +449,9 @@ def _gradients(grads, out):
         for i, g in enumerate(grads):
             if g.numel() and not _run_of_memory(g):
                 _refuse(f"gradient {i} must fill one run of memory")
-    words = array("q", bytes(32 * len(grads)))                     # data, out, count, the two types
-    words[0::4] = array("q", map(_address, grads))
-    words[2::4] = array("q", map(_count, grads))
+    words = array("q", bytes(32 * len(grads)))                     # data, out, count, the two types  (of lists: faster than of a map)
+    words[0::4] = array("q", list(map(_address, grads)))
+    words[2::4] = array("q", list(map(_count, grads)))
     codes = [_TYPES[t] for t in types]
     to = grads
     if out is not None:
@@ -464,7 +464,7 @@ def _gradients(grads, out):
         if (list(map(_shape_of, to)) != list(map(_shape_of, grads)) or
                 not (dense and all(map(_contiguous, to))) and any(o.stride() != g.stride() and g.numel() for o, g in zip(to, grads))):
             _refuse("tensors of out must have the gradients' shapes and strides")
-        words[1::4] = array("q", map(_address, to))
+        words[1::4] = array("q", list(map(_address, to)))
         codes = [c | _TYPES[t] << 32 for c, t in zip(codes, out_types)]
     words[3::4] = array("q", codes)
     if _recording() and (any(map(_asks, grads)) or any(map(_asks, to))):
