@@ -165,6 +165,20 @@ def test_long_sequences(lib):
         close(got[k], g_want[k], TOL[F32], k)
 
 
+@pytest.mark.parametrize("lens", [[8400, 40, 700], [10] * 20 + [8900]], ids=["few", "many"])
+def test_long_sequences_of_few_channels(lib, lens):
+    """Longer spans, as their number is bounded: where that is known from the number of rows, and where it is not."""
+    v, off, dev_off, dy, ds1 = inputs(lens, 6, 1, 2, F32, seed=9)
+    y, end = forward(lib, v, dev_off)
+    want, w_end = reference(double(v), off, True)
+    close(y, want, TOL[F32])
+    close(end, w_end, TOL[F32])
+    got, g_want = backward(lib, v, dev_off, dy, ds1), wanted(v, off, dy, ds1, True)
+    terms = wanted(magnitudes(v), off, dy.abs(), ds1.abs(), True)
+    for k in NAMES:
+        close(got[k], g_want[k], TOL[F32], k, terms[k])
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_strides(lib, dtype):
     v, off, dev_off, dy, ds1 = inputs([70, 3, 130], 101, 1, 16, dtype, seed=5)

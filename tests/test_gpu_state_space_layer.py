@@ -64,7 +64,7 @@ def test_gradients_through_the_layer(lib, example):
     exact = {k: getattr(layer, k).detach().double().cpu().requires_grad_() for k in names}
     want = plain(exact, m, tokens.double(), off)
     (want @ exact["r"] - y.double()).square().mean().backward()
-    assert float((coords.detach().double().cpu() - want.detach()).norm()) <= 2.0 ** -15 * float(want.norm())
+    assert float((coords.detach().double().cpu() - want.detach()).norm()) <= 2.0 ** -15 * float(want.detach().norm())
     for k, p in zip(names, layer.trained()):
         got, w = p.grad.double().cpu(), exact[k].grad
         assert float((got - w).norm()) <= 2.0 ** -15 * float(w.norm()), k
