@@ -176,7 +176,7 @@ int check_counts(const nugpr_gradient* g, int32_t n) {
   return NUGPR_OK;
 }
 
-int launches(int32_t n) { return (n + TABLE - 1) / TABLE; }
+int launches(int32_t n) { return (int)(((int64_t)n + TABLE - 1) / TABLE); }
 
 // Most workgroups of one launch, by how many launches share the partial sums.
 int64_t most_groups(int32_t n) { return std::max<int64_t>(64, GROUPS / std::max(1, launches(n))); }

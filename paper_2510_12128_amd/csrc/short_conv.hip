@@ -489,7 +489,7 @@ int conv_args(const nugpr_short_conv* p, bool backward, bool windows, ConvArgs& 
   a.dim = p->dim; a.silu = p->silu != 0; a.run = run_of(p, backward);
   a.col_blocks = (int)blocks_of(p, backward);
   a.runs = groups_of(p, backward);
-  grid = (a.runs + (windows ? (p->n_seqs + WAVES - 1) / WAVES : 0)) * a.col_blocks;
+  grid = (a.runs + (windows ? ((int64_t)p->n_seqs + WAVES - 1) / WAVES : 0)) * a.col_blocks;
   // (the threads of a launch are counted in 32 bits)
   if (grid > (int64_t)0xffffffff / THREADS) return invalid("too many rows, sequences and channels for one call");
   return NUGPR_OK;
