@@ -161,8 +161,9 @@ __device__ inline float gate_gradient(float p, float dy) {
 // p is computed anew from x: the forward pass keeps nothing.  dw and db stay in registers over the run, join over the workgroup's waves in LDS and go to
 // memory once a workgroup.  16384 rows, 2048 channels, four taps, bfloat16: 47 us, 4.2 TB/s of x, dy and dx (behind it k_conv_sums, 5 us); runs of 32 rows,
 // for enough workgroups, read a tenth more than their own.
+// (The bound: up to four taps four waves a SIMD, for which the compiler would take a register too many by itself.)
 template <class TR, int W, int V>
-__global__ __launch_bounds__(THREADS) void k_short_conv_backward(const ConvArgs a) {
+__global__ __launch_bounds__(THREADS, W <= 4 ? 4 : 2) void k_short_conv_backward(const ConvArgs a) {
   typedef typename TR::T T;
   constexpr int UP = 2;                         // rows at one time
   __shared__ float red[WAVES - 1][W + 1][64 * V];
@@ -296,11 +297,21 @@ __global__ __launch_bounds__(THREADS) void k_short_conv_backward(const ConvArgs 
             for (int k = 0; k < W; ++k) s = fmaf(w[W - 1 - k][j], dp[r + k][j], s);
             d[j] = s;
           }
-          if (a.dw_end && row >= p.hi - (W - 1)) {
-            Values<TR, V> e;
-            e.load(static_cast<const T*>(a.dw_end) + ((int64_t)p.seq * (W - 1) + row - (p.hi - (W - 1))) * a.dim + col, valid);
+          if (row + W > p.hi) {                 // (a tap without a row behind it adds nothing, whatever the tap is)
 #pragma unroll
-            for (int j = 0; j < V; ++j) d[j] += e.get(j);
+            for (int j = 0; j < V; ++j) d[j] = w[W - 1][j] * dp[r][j];
+#pragma unroll
+            for (int k = 1; k < W; ++k)
+              if (row + k < p.hi) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) d[j] = fmaf(w[W - 1 - k][j], dp[r + k][j], d[j]);
+              }
+            if (a.dw_end) {
+              Values<TR, V> e;
+              e.load(static_cast<const T*>(a.dw_end) + ((int64_t)p.seq * (W - 1) + row - (p.hi - (W - 1))) * a.dim + col, valid);
+#pragma unroll
+              for (int j = 0; j < V; ++j) d[j] += e.get(j);
+            }
           }
           Values<TR, V> o;
           o.put(d);

@@ -1,0 +1,44 @@
+"""Infinities and NaN in the arrays that many channels or rows read (GPU), against autograd of the formulas in 64 bits: what is
+infinite, what is NaN, and the numbers beside them, with the tolerances of test_gpu_selective_scan.py and test_gpu_short_conv.py.
+
+All values that the sums are linear in are positive, so that infinities of two signs meet only where the formulas have both."""
+import pytest
+import torch
+
+import test_gpu_selective_scan as scan
+import test_gpu_short_conv as conv
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+INF, NAN = float("inf"), float("nan")
+
+
+def same(got, want, tol, what, terms=None):
+    got, want = got.double().cpu(), want.double().cpu()
+    assert got.shape == want.shape, what
+    for kind in (torch.isnan, torch.isposinf, torch.isneginf):
+        assert torch.equal(kind(got), kind(want)), (what, kind.__name__, int(kind(got).sum()), int(kind(want).sum()))
+    fine = torch.isfinite(want)
+    bound = tol * float(want[fine].norm())
+    if terms is not None:
+        bound += scan.TOL[F32] * float(terms.double().cpu()[fine].norm())
+    assert float((got[fine] - want[fine]).norm()) <= bound, what
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("value", [INF, NAN])
+@pytest.mark.parametrize("tap,width,dim", [(0, 4, 70), (1, 4, 301), (2, 3, 64), (0, 8, 33), (0, 2, 513)])
+def test_weights_that_are_not_finite(lib, tap, width, dim, value, dtype):
+    """A tap reaches the gradients of those rows alone that have a row so far behind them in their sequence."""
+    lens = [1, 0, 2, 5, 300, 33]
+    i = conv.inputs(lens, dim, width, dtype, seed=width)
+    i.update({k: i[k].abs() + 0.25 for k in ("x", "w", "dy", "s0", "ds1")})
+    i["w"][dim // 2, tap] = value
+    got = lib.nugpr_short_conv_backward(i["x"], i["w"], i["dev_off"], i["dy"], bias=i["b"], initial_state=i["s0"], d_final_state=i["ds1"])
+    want = conv.wanted(i, i["b"], False, i["s0"], i["ds1"])
+    for x, w, name in zip(got, want, ("dx", "dw", "db", "ds")):
+        same(x, w, conv.TOL[dtype], name)
+    y, _ = lib.nugpr_short_conv_forward(i["x"], i["w"], i["dev_off"], bias=i["b"], initial_state=i["s0"])
+    w, _ = conv.reference(conv.double(i["x"]), conv.double(i["w"]), conv.double(i["b"]), i["off"], False, conv.double(i["s0"]))
+    same(y, w, conv.TOL[dtype], "y")
