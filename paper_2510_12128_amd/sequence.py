@@ -426,6 +426,12 @@ def _run_of_memory(t):
     return True
 
 
+def _same_order(g, o):
+    """Whether two tensors of one shape that fill a run of memory have their values in the same order."""
+    return (g.is_contiguous() and o.is_contiguous()) or g.numel() == 0 or all(
+        a == b for a, b, size in zip(g.stride(), o.stride(), g.shape) if size != 1)
+
+
 def _on_one_gpu(tensors, index, what):
     for i, t in enumerate(tensors):
         if t.get_device() != index or t.dtype not in _TYPES:
@@ -462,7 +468,7 @@ def _gradients(grads, out):
         if set(map(_where, to)) != {index} or not _TYPES.keys() >= set(out_types):
             _on_one_gpu(to, index, "out")
         if (list(map(_shape_of, to)) != list(map(_shape_of, grads)) or
-                not (dense and all(map(_contiguous, to))) and any(o.stride() != g.stride() and g.numel() for o, g in zip(to, grads))):
+                not (dense and all(map(_contiguous, to))) and not all(map(_same_order, grads, to))):
             _refuse("tensors of out must have the gradients' shapes and strides")
         words[1::4] = array("q", list(map(_address, to)))
         codes = [c | _TYPES[t] << 32 for c, t in zip(codes, out_types)]
