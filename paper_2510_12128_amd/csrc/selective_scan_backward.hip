@@ -23,6 +23,7 @@ struct Shape {
   static constexpr int NS = G * S;                // places for a channel's states
   static constexpr int THREADS = 64 * WAVES;
   static constexpr int PAIRS = (TILE_ROWS * NS + THREADS - 1) / THREADS;      // values of a tile's B (and C) that a thread takes up
+  static constexpr bool ROOM = G < 16;            // in LDS, for what only some lanes read
 };
 
 // A tile's rows as memory has them: V channels of one row, and PAIRS values of B and C.  OUT: what the gradients need beside the states.
@@ -78,7 +79,9 @@ template <class H>
 struct alignas(16) Tile {
   float2 du[H::WAVES][TILE_ROWS][H::CW];          // d and u, every wave's own
   float e[H::WAVES][TILE_ROWS][H::CW];
-  float B[2][TILE_ROWS][H::NS], C[2][TILE_ROWS][H::NS];
+  // B, then C, two buffers of each; then as many zeros as lanes without a channel read in their place: d = u = e = 0 does not silence an infinity
+  float rows[4 + (H::ROOM ? 3 : 0)][TILE_ROWS][H::NS];
+  static constexpr int C = 2, NONE = 4;
 };
 
 // Rows and channels that there are not: d = u = e = 0, which leaves a state, and a gradient, as it is.
@@ -112,8 +115,8 @@ __device__ __forceinline__ void fill_tile(Tile<H>& tile, const ScanArgs& a, cons
   for (int k = 0; k < H::PAIRS; ++k) {
     const int at = k * H::THREADS + threadIdx.x;
     if (H::PAIRS * H::THREADS == TILE_ROWS * H::NS || at < TILE_ROWS * H::NS) {
-      (&tile.B[buffer][0][0])[at] = TR::get(in.b[k]);
-      if (OUT) (&tile.C[buffer][0][0])[at] = TR::get(in.c[k]);
+      (&tile.rows[buffer][0][0])[at] = TR::get(in.b[k]);
+      if (OUT) (&tile.rows[Tile<H>::C + buffer][0][0])[at] = TR::get(in.c[k]);
     }
   }
 }
@@ -198,8 +201,8 @@ __global__ __launch_bounds__(H::THREADS) void k_scan_tiles(const ScanArgs a) {
       for (int t = 0; t < TILE_ROWS; ++t) {
         const float2 du = tile.du[wave][t][ch];
         float b[S], c[S];
-        read_states(b, &tile.B[buffer][t][group * S]);
-        if (LATER) read_states(c, &tile.C[buffer][t][group * S]);
+        read_states(b, &tile.rows[buffer][t][group * S]);
+        if (LATER) read_states(c, &tile.rows[Tile<H>::C + buffer][t][group * S]);
         const float e = LATER ? tile.e[wave][t][ch] : 0.f;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
@@ -294,6 +297,15 @@ __device__ __forceinline__ void join_four_states(float& x, float& y, const float
       : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]));
 }
 
+// Without that room: channels that there are not have no part in sums over channels.
+template <int S>
+__device__ __forceinline__ void silence(float (&v)[4][S], bool live) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int s = 0; s < S; ++s) v[i][s] = live ? v[i][s] : 0.f;
+}
+
 // Four rows' numbers, one register each, to one: lane l gets the sum, over the lanes that differ in the upper two bits, of row l / 16.
 __device__ __forceinline__ float join_rows(float a, float b, float c, float d) {
   swap_halves(a, c);
@@ -347,8 +359,7 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
   __shared__ float part[GATE ? 3 : 2][H::WAVES][TILE_ROWS][H::CW];       // sums over the states: du, dd, y, every wave's own
   __shared__ alignas(16) float sums[2][2][H::WAVES][TILE_ROWS][H::NS];               // over a wave's channels: dB, dC
   __shared__ float of_channel[2][H::CB];                                 // bias and D
-  constexpr bool NEAR = H::G < 16;
-  __shared__ alignas(16) float starts[NEAR ? H::THREADS : 1][S];         // the lanes' states at the span's begin, where there is room
+  __shared__ alignas(16) float starts[H::ROOM ? H::THREADS : 1][S];      // the lanes' states at the span's begin, where there is room
   const int item = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
   if (item >= a.items) {
     const int who = blockIdx.x - a.items * a.blocks;
@@ -377,6 +388,8 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
       of_channel[0][threadIdx.x] = mine && a.bias ? a.bias[p.channel + threadIdx.x] : 0.f;
       of_channel[1][threadIdx.x] = mine && a.D ? a.D[p.channel + threadIdx.x] : 0.f;
     }
+    if (H::ROOM && p.valid < H::CB)
+      for (int at = threadIdx.x; at < 3 * TILE_ROWS * H::NS; at += H::THREADS) (&tile.rows[Tile<H>::NONE][0][0])[at] = 0.f;
     __syncthreads();
     const float* bias = &of_channel[0][wave * H::CW + col];
     const float* D = &of_channel[1][wave * H::CW + col];
@@ -417,7 +430,7 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
       if (p.span > 0 && ch < valid) passed = a.tile_steps[(number + k) * a.dim + channel + ch];
     };
     if (tiles > 0) load_begin(tiles - 1);
-    if (NEAR && p.span > 0) {
+    if (H::ROOM && p.span > 0) {
       float start[S];
       load_states(start, a.adds + item * each + of_lane, n);
       __builtin_memcpy(starts[threadIdx.x], start, sizeof start);
@@ -428,10 +441,10 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
       const int rows = (int)min((int64_t)TILE_ROWS, p.to - t0);
       float h[TILE_ROWS + 1][S], f[TILE_ROWS][S];                        // h_{t-1} and on, a_t
 #pragma unroll
-      for (int s = 0; s < S; ++s) h[0][s] = begin[s];
+      for (int s = 0; s < S; ++s) h[0][s] = ch < valid ? begin[s] : 0.f;
       if (p.span > 0) {                                                  // (its walk began at zero)
         float start[S];
-        if constexpr (NEAR) read_states(start, starts[threadIdx.x]);
+        if constexpr (H::ROOM) read_states(start, starts[threadIdx.x]);
         else load_states(start, a.adds + item * each + of_lane, n);
 #pragma unroll
         for (int s = 0; s < S; ++s) h[0][s] = start[s] == 0.f ? h[0][s] : fmaf(exp2_of(a2[s] * passed), start[s], h[0][s]);
@@ -444,6 +457,8 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
         in.load(a, p, lane, TILE_ROWS, valid, -1);
         load_begin(k - 1);
       }
+      const float* B = &tile.rows[H::ROOM && ch >= valid ? Tile<H>::NONE : buffer][0][group * S];
+      const float* C = B + Tile<H>::C * TILE_ROWS * H::NS;
       repeat<TILE_ROWS / 4>([&](auto q) __attribute__((always_inline)) {
         float of_c[4][S], y[4];
         repeat<4>([&](auto i) __attribute__((always_inline)) {
@@ -451,8 +466,8 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
           const float2 du = tile.du[wave][t][ch];
           const float e = tile.e[wave][t][ch];
           float b[S], c[S];
-          read_states(b, &tile.B[buffer][t][group * S]);
-          if (GATE) read_states(c, &tile.C[buffer][t][group * S]);
+          read_states(b, B + t * H::NS);
+          if (GATE) read_states(c, C + t * H::NS);
           y[i] = 0.f;
 #pragma unroll
           for (int s = 0; s < S; ++s) {
@@ -464,6 +479,7 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
           }
         });
         if constexpr (GATE) part[2][wave][4 * q + lane % 4][ch] = sums_of_states<H::G>(y, lane);
+        if (!H::ROOM && valid < H::CW) silence(of_c, ch < valid);
         sums_of_channels<H>(of_c, &sums[buffer][1][wave][4 * q][0], lane);
         if (4 * q + 4 > rows)                    // (rows that there are not have d = 0, which does not silence a state that is not finite)
           repeat<4>([&](auto i) __attribute__((always_inline)) {
@@ -480,8 +496,8 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
           const float2 du = tile.du[wave][t][ch];
           const float e = tile.e[wave][t][ch];
           float b[S], c[S];
-          read_states(b, &tile.B[buffer][t][group * S]);
-          read_states(c, &tile.C[buffer][t][group * S]);
+          read_states(b, B + t * H::NS);
+          read_states(c, C + t * H::NS);
           by_u[i] = by_d[i] = 0.f;
 #pragma unroll
           for (int s = 0; s < S; ++s) {
@@ -497,6 +513,7 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
         });
         part[0][wave][4 * q + lane % 4][ch] = sums_of_states<H::G>(by_u, lane);
         part[1][wave][4 * q + lane % 4][ch] = sums_of_states<H::G>(by_d, lane);
+        if (!H::ROOM && valid < H::CW) silence(of_b, ch < valid);
         sums_of_channels<H>(of_b, &sums[buffer][0][wave][4 * q][0], lane);
         __builtin_amdgcn_sched_barrier(0);
       });

@@ -26,6 +26,37 @@ def same(got, want, tol, what, terms=None):
     assert float((got[fine] - want[fine]).norm()) <= bound, what
 
 
+def positive(lens, dim, groups, states, dtype, seed):
+    v, off, dev_off, dy, ds1 = scan.inputs(lens, dim, groups, states, dtype, seed)
+    for k in ("x", "B", "C", "D", "z", "s0"):
+        v[k] = v[k].abs() + 0.25
+    return v, off, dev_off, dy.abs() + 0.25, ds1.abs() + 0.25
+
+
+def both(lib, v, off, dev_off, dy, ds1, clean):
+    y, end = scan.forward(lib, v, dev_off)
+    want, w_end = scan.reference(scan.double(v), off, True)
+    same(y, want, scan.tolerance(y), "y")
+    same(end, w_end, scan.TOL[F32], "end")
+    got, g_want = scan.backward(lib, v, dev_off, dy, ds1), scan.wanted(v, off, dy, ds1, True)
+    terms = scan.wanted(scan.magnitudes(clean), off, dy, ds1, True)
+    for k in scan.NAMES:
+        same(got[k], g_want[k], scan.tolerance(v[k]), k, terms[k])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("states", [5, 8, 16, 24, 32, 40, 64])
+@pytest.mark.parametrize("dim,groups", [(1, 1), (64, 1), (70, 1), (130, 2)])
+def test_infinite_rows_of_B_and_C(lib, dim, groups, states, dtype):
+    """Channels by which a group falls short of a workgroup's or a wave's are none: an infinity that they read goes nowhere."""
+    v, off, dev_off, dy, ds1 = positive([37, 41], dim, groups, states, dtype, seed=dim + states)
+    clean = dict(v)
+    v["B"], v["C"] = v["B"].clone(), v["C"].clone()
+    v["B"][11, groups - 1, states // 2] = INF          # (states are infinite from here on)
+    v["C"][37 + 20, 0, states - 1] = INF               # (gradients are, back to the begin)
+    both(lib, v, off, dev_off, dy, ds1, clean)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("value", [INF, NAN])
 @pytest.mark.parametrize("tap,width,dim", [(0, 4, 70), (1, 4, 301), (2, 3, 64), (0, 8, 33), (0, 2, 513)])
