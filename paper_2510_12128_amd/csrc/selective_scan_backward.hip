@@ -306,6 +306,33 @@ __device__ __forceinline__ void silence(float (&v)[4][S], bool live) {
     for (int s = 0; s < S; ++s) v[i][s] = live ? v[i][s] : 0.f;
 }
 
+// dA += x d, where the tile has row T.  Whether it has is the same for all lanes, and no lane's business: d = 0 would not silence an x that is not
+// finite, a selection a number takes an instruction of the vector pipe each, and a branch keeps the rows on its sides apart.  (exec: all lanes, as everywhere
+// in the walk.)
+template <int T, int S>
+__device__ __forceinline__ void add_where_row(float (&dA)[S], const float (&x)[S], const float (&d)[S], int rows) {
+  if constexpr (S == 4)
+    asm("s_cmp_gt_i32 %12, %13\n\t"
+        "s_cselect_b64 exec, -1, 0\n\t"
+        "v_fmac_f32_e32 %0, %4, %8\n\t"
+        "v_fmac_f32_e32 %1, %5, %9\n\t"
+        "v_fmac_f32_e32 %2, %6, %10\n\t"
+        "v_fmac_f32_e32 %3, %7, %11\n\t"
+        "s_mov_b64 exec, -1"
+        : "+v"(dA[0]), "+v"(dA[1]), "+v"(dA[2]), "+v"(dA[3])
+        : "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "v"(d[0]), "v"(d[1]), "v"(d[2]), "v"(d[3]), "s"(rows), "n"(T)
+        : "scc");
+  else
+    asm("s_cmp_gt_i32 %6, %7\n\t"
+        "s_cselect_b64 exec, -1, 0\n\t"
+        "v_fmac_f32_e32 %0, %2, %4\n\t"
+        "v_fmac_f32_e32 %1, %3, %5\n\t"
+        "s_mov_b64 exec, -1"
+        : "+v"(dA[0]), "+v"(dA[1])
+        : "v"(x[0]), "v"(x[1]), "v"(d[0]), "v"(d[1]), "s"(rows), "n"(T)
+        : "scc");
+}
+
 // Four rows' numbers, one register each, to one: lane l gets the sum, over the lanes that differ in the upper two bits, of row l / 16.
 __device__ __forceinline__ float join_rows(float a, float b, float c, float d) {
   swap_halves(a, c);
@@ -355,6 +382,11 @@ template <class TR, class H, bool EXACT, bool GATE>
 __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs a) {
   typedef typename TR::T T;
   constexpr int S = H::S, V = H::V;
+  // A branch between the quarters of a tile, for its registers: the states of rows that there are not, which it clears, are used nowhere.  Without it the float32
+  // kernel of 9 to 16 states with a gate has 25 registers in memory instead of 17 (8 x 2048 rows, 2048 channels, 16 states: 906 us instead of 845), and 64
+  // states take 1414 us instead of 1367 (8 x 1024 rows, bfloat16); with it other kernels take longer (bfloat16, 16 states: 667 us instead of 651, 4096 sequences
+  // of 4 rows 1960 instead of 1863).
+  constexpr bool APART = H::NS == 64 || (H::NS == 16 && GATE && sizeof(T) == 4);
   __shared__ Tile<H> tile;
   __shared__ float part[GATE ? 3 : 2][H::WAVES][TILE_ROWS][H::CW];       // sums over the states: du, dd, y, every wave's own
   __shared__ alignas(16) float sums[2][2][H::WAVES][TILE_ROWS][H::NS];               // over a wave's channels: dB, dC
@@ -481,7 +513,7 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
         if constexpr (GATE) part[2][wave][4 * q + lane % 4][ch] = sums_of_states<H::G>(y, lane);
         if (!H::ROOM && valid < H::CW) silence(of_c, ch < valid);
         sums_of_channels<H>(of_c, &sums[buffer][1][wave][4 * q][0], lane);
-        if (4 * q + 4 > rows)                    // (rows that there are not have d = 0, which does not silence a state that is not finite)
+        if (APART && 4 * q + 4 > rows)
           repeat<4>([&](auto i) __attribute__((always_inline)) {
 #pragma unroll
             for (int s = 0; s < S; ++s) h[4 * q + i + 1][s] = 4 * q + i + 1 >= rows ? 0.f : h[4 * q + i + 1][s];
@@ -499,6 +531,7 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
           read_states(b, B + t * H::NS);
           read_states(c, C + t * H::NS);
           by_u[i] = by_d[i] = 0.f;
+          float x[S], d[S];
 #pragma unroll
           for (int s = 0; s < S; ++s) {
             const bool there = EXACT || s < n;
@@ -506,10 +539,11 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
             of_b[i][s] = g[s] * (there ? du.y : 0.f);
             by_u[i] = fmaf(b[s], g[s], by_u[i]);
             g[s] *= f[t][s];
-            const float x = g[s] * h[t][s];
-            dA[s] = fmaf(x, there ? du.x : 0.f, dA[s]);
-            by_d[i] = fmaf(x, a2[s], by_d[i]);
+            x[s] = g[s] * h[t][s];
+            d[s] = there ? du.x : 0.f;
+            by_d[i] = fmaf(x[s], a2[s], by_d[i]);
           }
+          add_where_row<t>(dA, x, d, rows);
         });
         part[0][wave][4 * q + lane % 4][ch] = sums_of_states<H::G>(by_u, lane);
         part[1][wave][4 * q + lane % 4][ch] = sums_of_states<H::G>(by_d, lane);

@@ -58,6 +58,16 @@ def test_infinite_rows_of_B_and_C(lib, dim, groups, states, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("states", [1, 5, 16, 32, 40])
+@pytest.mark.parametrize("lens", [[1], [3, 5], [14], [16], [18, 31], [300]], ids=str)
+def test_an_infinite_gradient_at_the_end(lib, lens, states, dtype):
+    """Sequences that end amid a tile of rows: rows behind their end have no part in anything."""
+    v, off, dev_off, dy, ds1 = positive(lens, 70, 1, states, dtype, seed=len(lens) + states)
+    ds1[0, 3, states - 1] = ds1[-1, 65, 0] = INF
+    both(lib, v, off, dev_off, dy, ds1, v)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("value", [INF, NAN])
 @pytest.mark.parametrize("tap,width,dim", [(0, 4, 70), (1, 4, 301), (2, 3, 64), (0, 8, 33), (0, 2, 513)])
 def test_weights_that_are_not_finite(lib, tap, width, dim, value, dtype):
