@@ -531,8 +531,8 @@ int nugpr_short_conv_step(const nugpr_short_conv* problem, const nugpr_rows* x, 
  *   d_t = softplus(dt_t[c] + dt_bias[c]), or dt_t[c] + dt_bias[c] without softplus,
  *   h_t[c][n] = e^(d_t A[c][n]) h_{t-1}[c][n] + d_t x_t[c] B_t[n],
  *   y_t[c] = (sum_n C_t[n] h_t[c][n] + D[c] x_t[c]) silu(z_t[c])       (without D: no such term; without z: no such factor).
- * d_t A is meant to be <= 0 (A = -infinity: nothing is kept); exponents below -87 are a factor of zero.  (An infinite state that such a
- * factor meets becomes NaN.) */
+ * d_t A is meant to be <= 0 (A = -infinity: nothing is kept); exponents below -87 are a factor of zero.  (An infinite state, or
+ * gradient of one, that such a factor meets may become NaN; factors that are small only together do not make it one.) */
 typedef struct {
   int32_t dtype;              /* of x, dt, B, C, z, y and their gradients                           */
   int32_t dim;                /* channels, 1..65536                                                 */

@@ -29,9 +29,10 @@ struct ScanArgs {
   float *s_out, *ds_in;
   const int64_t* off;
   int64_t n_rows;
-  int n_seqs, dim, groups, each, states, softplus;             // each: channels of a group
+  int n_seqs, dim, groups, each, states, softplus, bf16;       // each: channels of a group
   int width, blocks;                 // channels of a workgroup; workgroups that have all
   int share;                         // states of a wave (of each chunk): as even as they can be shared out
+  int threads, per_thread;           // the gradients': of a workgroup; states of a thread
   int span_log2, items;
   int64_t whole;                     // sequences are not cut into spans where none has more rows
   float* adds;                       // items x dim x states: what a span adds to the state, then its start state
@@ -50,6 +51,11 @@ struct ScanArgs {
 __device__ __forceinline__ float rate_of(float A) {
   const float r = A * LOG2_E;
   return r < -3e38f ? -3e38f : r;
+}
+
+// f h + add with the factor of many steps, which may be zero where none of a single step is: an infinite h stays so.
+__device__ __forceinline__ float over_steps(float f, float h, float add) {
+  return h == 0.f || (f == 0.f && __builtin_isinf(h)) ? h + add : fmaf(f, h, add);
 }
 
 // Sum over the lanes up to this one.
@@ -173,7 +179,7 @@ __device__ void clear_rows(const ScanArgs& a, int who, void* to, int64_t stride)
 // spans add to their start states.
 int scan_backward_width(int states);       // channels of a workgroup
 int scan_backward_threads(int states);     // its threads
-int scan_backward_states(int states);      // states of a thread
+int scan_backward_states(int states);      // states of a thread: side by side, neighbouring threads have a channel's next
 int launch_scan_backward(int dtype, const ScanArgs& a, bool one_span, void (*join)(const ScanArgs&, bool, hipStream_t), hipStream_t s);
 
 }  // namespace nugpr

@@ -314,9 +314,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_scan(const ScanArgs a) {
 }
 
 // Start states of a sequence's spans, in the place of what the spans add; the second half of the grid: gradients at their end, against time.
-// A chain of one multiply-add a span: what it reads comes AHEAD spans at a time, the next ones while these are worked through.
+// A chain of one multiply-add a span: what it reads comes AHEAD spans at a time, the next ones while these are worked through.  Returns the last link.
 template <bool BACK>
-__device__ __forceinline__ void join(float* at, const float* steps, int64_t each, int64_t dim, int spans, float a2, float h) {
+__device__ __forceinline__ float join(float* at, const float* steps, int64_t each, int64_t dim, int spans, float a2, float h) {
   constexpr int AHEAD = 8;
   // the span at place k of the chain; forward, span 0's own is where it begins
   const auto span = [&](int k) { return BACK ? spans - 1 - k : k; };
@@ -343,15 +343,75 @@ __device__ __forceinline__ void join(float* at, const float* steps, int64_t each
     for (int j = 0; j < AHEAD; ++j) {
       if (k + j >= spans) break;
       at[span(k + j) * each] = h;
-      const float f = exp2_of(a2 * d_now[j]);
-      // (a factor of many steps may be zero where none of a single step is)
-      h = h == 0.f || (f == 0.f && __builtin_isinf(h)) ? h + add_now[j] : fmaf(f, h, add_now[j]);
+      h = over_steps(exp2_of(a2 * d_now[j]), h, add_now[j]);
     }
+  }
+  return h;
+}
+
+// What rows from .. to - 1 add to the gradient by a channel's state before them, one after the other from the last.
+template <class TR>
+__device__ float add_row_by_row(const ScanArgs& a, int channel, int state, float a2, int64_t from, int64_t to) {
+  typedef typename TR::T T;
+  const float bias = a.bias ? a.bias[channel] : 0.f;
+  float g = 0.f;
+#pragma unroll 1
+  for (int64_t row = to - 1; row >= from; --row) {
+    float d = TR::get(static_cast<const T*>(a.dt)[row * a.dt_row + channel]) + bias, e = TR::get(static_cast<const T*>(a.dy)[row * a.dy_row + channel]);
+    if (a.softplus) d = softplus_of<TR>(d);
+    if (a.z) {
+      const float z = TR::get(static_cast<const T*>(a.z)[row * a.z_row + channel]);
+      e *= z * sigmoid_of<TR>(z);
+    }
+    g = exp2_of(d * a2) * fmaf(e, TR::get(static_cast<const T*>(a.C)[row * a.C_row + channel / a.each * a.C_head + state]), g);
+  }
+  return g;
+}
+
+// The chain of gradients once more where it has come to NaN, from the span on that made it so: that is gone through row by row.  The product of its factors may
+// be zero though none of them is, and an infinity times that is NaN.  (The rest of the chain has been written over what its spans add, so these are gone
+// through too, which only an infinity asks for: a NaN that is one ends it.)
+__device__ __forceinline__ void join_again(const ScanArgs& a, int64_t mine, float* at, const float* steps, int64_t each, int spans, float a2, int64_t lo, int64_t hi) {
+  const int channel = (int)(mine / a.states), state = (int)(mine % a.states);
+  int k = spans - 1;                                 // the last span whose gradient at its end is no NaN
+  while (k >= 0 && !__builtin_isnan(at[k * each])) --k;
+  if (++k == spans) return;
+  float h = at[k * each];
+#pragma unroll 1
+  for (; k > 0; --k) {
+    const int64_t from = lo + ((int64_t)k << a.span_log2), to = min(hi, from + ((int64_t)1 << a.span_log2));
+    h = over_steps(exp2_of(a2 * steps[(int64_t)k * a.dim]), h,
+                   a.bf16 ? add_row_by_row<Bf16>(a, channel, state, a2, from, to) : add_row_by_row<F32>(a, channel, state, a2, from, to));
+    if (__builtin_isnan(h)) return;
+    at[(k - 1) * each] = h;
+  }
+}
+
+// Infinite start states of spans go into the states that the gradients' first walk has kept of their tiles, in the place of what the second walk does with
+// the others: it multiplies them by the factor of the steps before a tile, which may be zero though none of these is.
+__device__ __forceinline__ void spread_infinities(const ScanArgs& a, int64_t mine, float* starts, int64_t each, int seq, int spans, float a2, int64_t lo, int64_t hi) {
+  const int channel = (int)(mine / a.states), state = (int)(mine % a.states), in_group = channel % a.each;
+  const int lanes = a.threads / a.width;             // of a channel
+  const int64_t block = (int64_t)channel / a.each * (a.blocks / a.groups) + in_group / a.width;
+  const int at = (in_group % a.width * lanes + state / a.per_thread) * a.per_thread + state % a.per_thread;
+#pragma unroll 1
+  for (int k = 1; k < spans; ++k) {
+    if (!__builtin_isinf(starts[k * each])) continue;
+    const int64_t from = lo + ((int64_t)k << a.span_log2), to = min(hi, from + ((int64_t)1 << a.span_log2));
+    int64_t tile = lo / TILE_ROWS + seq + (from - lo) / TILE_ROWS;
+#pragma unroll 1
+    for (int64_t row = from; row < to; row += TILE_ROWS, ++tile) {
+      float* kept = a.tiles + (tile * a.blocks + block) * a.threads * a.per_thread + at;
+      *kept = over_steps(exp2_of(a2 * a.tile_steps[tile * a.dim + channel]), starts[k * each], *kept);
+    }
+    starts[k * each] = 0.f;
   }
 }
 
 // A lane has one state of a channel.  What a span takes is the wait for its two loads, shared by the AHEAD that are on their way: 64 spans of 2048 channels and
-// 16 states take 16 us, 32 take 9; 16 at one time took longer where sequences are short (20 instead of 15 us for 40 of them).
+// 16 states take 16 us, 32 take 9; 16 at one time took longer where sequences are short (20 instead of 15 us for 40 of them).  (What values that are not finite
+// ask for in the gradients is kept out of the way of the others: between their instructions it cost 2 us of 9, 9 sequences of 5003 rows, behind them 0.4.)
+template <bool BACKWARD>
 __global__ __launch_bounds__(64) void k_scan_join(const ScanArgs a) {
   const int64_t each = (int64_t)a.dim * a.states, mine = (int64_t)blockIdx.x * 64 + threadIdx.x;
   const int64_t at = min(mine, each - 1);            // (all lanes count; the last ones of the last workgroup only count)
@@ -370,9 +430,14 @@ __global__ __launch_bounds__(64) void k_scan_join(const ScanArgs a) {
       float* adds = a.adds + first * each + at;
       const float h = adds[0];
       adds[0] = a.s_in ? a.s_in[seq * each + at] : 0.f;
-      join<false>(adds, steps, each, a.dim, spans, a2, h);
+      const float end = join<false>(adds, steps, each, a.dim, spans, a2, h);
+      if (BACKWARD && __builtin_expect(!__builtin_isfinite(end), 0)) spread_infinities(a, at, adds, each, seq, spans, a2, lo, hi);
     }
-    if (blockIdx.z == 1) join<true>(a.back + first * each + at, steps, each, a.dim, spans, a2, a.ds_end ? a.ds_end[seq * each + at] : 0.f);
+    if (BACKWARD && blockIdx.z == 1) {
+      float* adds = a.back + first * each + at;
+      const float g = join<true>(adds, steps, each, a.dim, spans, a2, a.ds_end ? a.ds_end[seq * each + at] : 0.f);
+      if (__builtin_expect(__builtin_isnan(g), 0)) join_again(a, at, adds, steps, each, spans, a2, lo, hi);
+    }
   }
 }
 
@@ -574,8 +639,9 @@ ScanArgs scan_args(const nugpr_selective_scan* p, bool backward) {
   ScanArgs a{};
   a.A = p->A; a.D = p->D; a.bias = p->dt_bias; a.off = p->seq_offsets; a.n_rows = p->n_rows; a.n_seqs = p->n_seqs;
   a.dim = p->dim; a.groups = p->groups; a.each = p->dim / p->groups; a.width = width_of(p, backward); a.blocks = blocks_of(p, backward); a.states = p->dim_state;
-  a.softplus = p->softplus != 0; a.share = (p->dim_state + waves_of(p) * chunks_of(p) - 1) / (waves_of(p) * chunks_of(p)); a.span_log2 = span_log2(p, backward); a.items = (int)items_of(p, backward);
+  a.softplus = p->softplus != 0; a.bf16 = p->dtype == NUGPR_BFLOAT16; a.share = (p->dim_state + waves_of(p) * chunks_of(p) - 1) / (waves_of(p) * chunks_of(p)); a.span_log2 = span_log2(p, backward); a.items = (int)items_of(p, backward);
   a.whole = whole_of(p, backward);
+  a.threads = threads_of(p, backward); a.per_thread = scan_backward_states(p->dim_state);
   return a;
 }
 
@@ -595,7 +661,8 @@ void with_waves(const nugpr_selective_scan* p, F f) {
 void launch_join(const ScanArgs& a, bool backward, hipStream_t s) {
   const int64_t each = (int64_t)a.dim * a.states;
   const int64_t x = (each + 63) / 64, y = std::min<int64_t>(a.n_seqs, std::max<int64_t>(1, 32768 / x));
-  hipLaunchKernelGGL(k_scan_join, dim3((unsigned)x, (unsigned)y, backward ? 2 : 1), dim3(64), 0, s, a);
+  if (backward) hipLaunchKernelGGL(k_scan_join<true>, dim3((unsigned)x, (unsigned)y, 2), dim3(64), 0, s, a);
+  else hipLaunchKernelGGL(k_scan_join<false>, dim3((unsigned)x, (unsigned)y, 1), dim3(64), 0, s, a);
 }
 
 template <class TR>

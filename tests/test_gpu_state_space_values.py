@@ -67,6 +67,26 @@ def test_an_infinite_gradient_at_the_end(lib, lens, states, dtype):
     both(lib, v, off, dev_off, dy, ds1, v)
 
 
+@pytest.mark.parametrize("where", ["start", "x", "C", "end"])
+@pytest.mark.parametrize("many", [0, 300])
+@pytest.mark.parametrize("states", [1, 16, 40])
+def test_infinities_of_far_rows(lib, states, many, where):
+    """Over many rows a state's factors come to less than float32 holds, though none of them is zero: what is infinite stays so, over
+    spans of 64 rows and between them.  In sequences numbered one after the other, and by their place."""
+    v, off, dev_off, dy, ds1 = positive([300] + [1] * many, 6, 1, states, F32, seed=states)
+    clean = dict(v)
+    v["A"] = -torch.linspace(0.5, 16.0, 6 * states, device="cuda").reshape(6, states)
+    if where == "start":
+        v["s0"][0, 5, states - 1] = INF
+    elif where == "x":
+        v["x"][70, 4] = INF
+    elif where == "C":
+        v["C"][290, 0, 0] = INF
+    else:
+        ds1[0, 3, 0] = INF
+    both(lib, v, off, dev_off, dy, ds1, dict(clean, A=v["A"]))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("value", [INF, NAN])
 @pytest.mark.parametrize("tap,width,dim", [(0, 4, 70), (1, 4, 301), (2, 3, 64), (0, 8, 33), (0, 2, 513)])
