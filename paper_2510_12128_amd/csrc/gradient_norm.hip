@@ -9,7 +9,7 @@
 #include <new>
 #include <vector>
 
-#include "nugpr_internal.h"
+#include "call_checks.h"
 #include "row_values.h"
 
 namespace nugpr {
@@ -160,11 +160,6 @@ __global__ __launch_bounds__(THREADS) void k_clip(const Table<N, OUT> a) {
 
 // ---- host --------------------------------------------------------------------------------------------------------------
 size_t size_of(int dtype) { return dtype == NUGPR_BFLOAT16 ? 2 : 4; }
-
-int invalid(const std::string& what) {
-  set_error(what);
-  return NUGPR_ERR_INVALID;
-}
 
 int check_counts(const nugpr_gradient* g, int32_t n) {
   if (n < 0 || (n > 0 && !g)) return invalid("gradients is null or their number negative");

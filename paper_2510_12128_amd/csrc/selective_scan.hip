@@ -20,6 +20,7 @@
 // workgroup for 64 channels of it 32 compute units of 256 would work.
 #include <algorithm>
 
+#include "call_checks.h"
 #include "selective_scan.h"
 
 namespace nugpr {
@@ -503,11 +504,6 @@ __global__ __launch_bounds__(256) void k_scan_step(const ScanStepArgs a) {
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------
-int invalid(const std::string& what) {
-  set_error(what);
-  return NUGPR_ERR_INVALID;
-}
-
 int check(const nugpr_selective_scan* p) {
   if (!p) return invalid("problem is null");
   if (p->dtype != NUGPR_FLOAT32 && p->dtype != NUGPR_BFLOAT16) return invalid("dtype must be NUGPR_FLOAT32 or NUGPR_BFLOAT16");
@@ -521,25 +517,15 @@ int check(const nugpr_selective_scan* p) {
 
 size_t value_size(const nugpr_selective_scan* p) { return p->dtype == NUGPR_BFLOAT16 ? 2 : 4; }
 
-int check_array(const void* data, int64_t stride, int64_t more, const char* name, size_t value) {
-  if (!data) return invalid(std::string(name) + " is null");
-  if (stride < 0 || more < 0) return invalid(std::string(name) + ": negative stride");
-  if (reinterpret_cast<uintptr_t>(data) % value) return invalid(std::string(name) + " misaligned");
-  return NUGPR_OK;
-}
-int check_rows(const nugpr_rows* x, const char* name, size_t value) { return check_array(x ? x->data : nullptr, x ? x->row_stride : 0, 0, name, value); }
 int check_heads(const nugpr_heads* x, const char* name, size_t value) {
-  return check_array(x ? x->data : nullptr, x ? x->row_stride : 0, x ? x->head_stride : 0, name, value);
+  const nugpr_rows rows{x ? x->data : nullptr, x ? x->row_stride : 0};
+  NUGPR_TRY(check_rows(&rows, name, value));
+  return x->head_stride < 0 ? invalid(std::string(name) + ": negative stride") : NUGPR_OK;
 }
 int check_floats(const float* x, const char* name, bool needed) {
   if (!x && needed) return invalid(std::string(name) + " is null");
   if (reinterpret_cast<uintptr_t>(x) % 4) return invalid(std::string(name) + " misaligned");
   return NUGPR_OK;
-}
-
-bool overlap(const void* a, const void* b, size_t bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x && y && x < y + bytes && y < x + bytes;
 }
 
 // Four waves share out up to 16 states, eight up to 32, in two chunks up to 64.
@@ -610,12 +596,6 @@ size_t lay_out(const nugpr_selective_scan* p, bool backward, void* ws, ScanArgs*
   }
   return w.bytes;
 }
-
-#define NUGPR_TRY(call)                 \
-  do {                                  \
-    const int c__ = (call);             \
-    if (c__ != NUGPR_OK) return c__;    \
-  } while (0)
 
 // What both calls over sequences check; *done: nothing is left to do.
 int check_call(const nugpr_selective_scan* p, bool backward, bool* done) {

@@ -8,7 +8,7 @@
 // still needs in registers, so that a row is read once, and W - 1 rows more a run.
 #include <algorithm>
 
-#include "nugpr_internal.h"
+#include "call_checks.h"
 #include "packed_rows.h"
 #include "row_values.h"
 
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(64 * SUM_WAVES) void k_conv_sums(const float* sums,
 struct ConvStepArgs {
   const void* x;
   void *y, *window;
-  int64_t x_row, y_row, n_rows;
+  int64_t x_row, y_row;
   const void *weight, *bias;
   const int32_t* slots;
   int n_windows, dim, silu, col_blocks;
@@ -418,11 +418,6 @@ __global__ __launch_bounds__(THREADS) void k_short_conv_step(const ConvStepArgs 
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------
-int invalid(const std::string& what) {
-  set_error(what);
-  return NUGPR_ERR_INVALID;
-}
-
 int check(const nugpr_short_conv* p) {
   if (!p) return invalid("problem is null");
   if (p->dtype != NUGPR_FLOAT32 && p->dtype != NUGPR_BFLOAT16) return invalid("dtype must be NUGPR_FLOAT32 or NUGPR_BFLOAT16");
@@ -435,22 +430,10 @@ int check(const nugpr_short_conv* p) {
 
 size_t value_size(const nugpr_short_conv* p) { return p->dtype == NUGPR_BFLOAT16 ? 2 : 4; }
 
-int check_rows(const nugpr_rows* x, const char* name, size_t value) {
-  if (!x || !x->data) return invalid(std::string(name) + " is null");
-  if (x->row_stride < 0) return invalid(std::string(name) + ": negative stride");
-  if (reinterpret_cast<uintptr_t>(x->data) % value) return invalid(std::string(name) + " misaligned");
-  return NUGPR_OK;
-}
-
 int check_pointer(const void* x, const char* name, size_t value, bool needed) {
   if (!x && needed) return invalid(std::string(name) + " is null");
   if (reinterpret_cast<uintptr_t>(x) % value) return invalid(std::string(name) + " misaligned");
   return NUGPR_OK;
-}
-
-bool overlap(const void* a, const void* b, size_t bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x && y && x < y + bytes && y < x + bytes;
 }
 
 // Channels of a lane: 16 bytes forward, four in the gradients, whose windows, weights and sums have to stay in registers.
@@ -473,12 +456,6 @@ int64_t groups_of(const nugpr_short_conv* p, bool backward) {
 size_t sums_bytes(const nugpr_short_conv* p) {
   return ((size_t)groups_of(p, true) * (p->width + 1) * p->dim * sizeof(float) + 255) / 256 * 256;
 }
-
-#define NUGPR_TRY(call)                 \
-  do {                                  \
-    const int c__ = (call);             \
-    if (c__ != NUGPR_OK) return c__;    \
-  } while (0)
 
 template <class TR, int V, class F>
 void with_width(int width, F f) {
@@ -606,7 +583,7 @@ int nugpr_short_conv_step(const nugpr_short_conv* p, const nugpr_rows* x, void* 
   NUGPR_TRY(check_pointer(window, "window", z, p->n_seqs > 0 && p->width > 1));
   if (!slots && p->n_rows > p->n_seqs) return invalid("more requests than windows");
   ConvStepArgs a{};
-  a.x = x->data; a.x_row = x->row_stride; a.y = y->data; a.y_row = y->row_stride; a.window = window; a.n_rows = p->n_rows;
+  a.x = x->data; a.x_row = x->row_stride; a.y = y->data; a.y_row = y->row_stride; a.window = window;
   a.weight = p->weight; a.bias = p->bias; a.slots = slots; a.n_windows = p->n_seqs; a.dim = p->dim; a.silu = p->silu != 0;
   constexpr int V = 2;                          // (few values a lane: a single request is spread over more of the card)
   a.col_blocks = (p->dim + V * THREADS - 1) / (V * THREADS);
