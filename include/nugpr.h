@@ -593,8 +593,8 @@ size_t nugpr_gradient_norm_workspace_bytes(const nugpr_gradient* gradients, int3
 int nugpr_gradient_norm(const nugpr_gradient* gradients, int32_t n_gradients, float* norm, void* workspace, size_t workspace_bytes,
                         void* stream);
 
-/* The same, and every value is multiplied by min(1, max_norm / norm): out = data x factor, multiplied in 64 bits.  In place,
- * nothing is written where norm <= max_norm.  A norm that is infinite makes the factor zero, a NaN NaN.  max_norm >= 0, infinity
+/* The same, and every value is multiplied by min(1, max_norm / norm): out = data x factor, multiplied in 64 bits, rounded to
+ * float32 and, where `out` is bfloat16, from there.  In place, nothing is written where norm <= max_norm.  A norm that is infinite makes the factor zero, a NaN NaN.  max_norm >= 0, infinity
  * allowed.  Tensors that are written must not overlap any other. */
 int nugpr_clip_gradients(const nugpr_gradient* gradients, int32_t n_gradients, double max_norm, float* norm, void* workspace,
                          size_t workspace_bytes, void* stream);

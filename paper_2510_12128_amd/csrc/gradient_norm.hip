@@ -117,7 +117,8 @@ __global__ __launch_bounds__(THREADS) void k_norm(const double* sums, int n, flo
   if (threadIdx.x == 0) *norm = (float)x;
 }
 
-// (the product in 64 bits: a factor below float32's range times a large value is not lost)
+// (The product in 64 bits: a factor below float32's range times a large value is not lost.  To bfloat16 by way of float32, as its instruction rounds: off by
+// 2^-24 more than half a step.)
 template <class FROM, class TO>
 __device__ void scaled(const typename FROM::T* p, typename TO::T* q, int count, double factor) {
   constexpr int V = 4;
@@ -134,7 +135,8 @@ __device__ void scaled(const typename FROM::T* p, typename TO::T* q, int count, 
 }
 
 // Every workgroup adds up the partial sums for itself, 16 KB from L2, which saves a launch between two others; in place within the bound that is all it
-// does (5 us).
+// does (5 us).  Beyond it memory bounds this too: 252 million bfloat16 values in place in 162 us, 6.2 TB/s, and 303 with the norm, whose reads wait for what the
+// call before has written (two reads and a write are 296 at the rate of a copy); float32, half as many values, 330.
 template <int N, bool OUT>
 __global__ __launch_bounds__(THREADS) void k_clip(const Table<N, OUT> a) {
   const double norm = norm_of(a.sums, a.n_sums);

@@ -151,7 +151,8 @@ __device__ __forceinline__ float* kept(const ScanArgs& a, int64_t tile, int bloc
 __device__ __forceinline__ int64_t first_tile(const Place& p) { return p.piece.lo / TILE_ROWS + p.piece.seq + (p.from - p.piece.lo) / TILE_ROWS; }
 
 // The first walk.  Factors multiply up over a span for what it adds to the gradient before it; of a sequence's first span that is not wanted, so that
-// the walk of sequences that are not cut is the states' alone.  The vector pipe bounds it: 8 x 2048 rows, 2048 channels, 16 states, bfloat16: 180 us.
+// the walk of sequences that are not cut is the states' alone.  The vector pipe bounds it, busy 80 % of the time: 8 x 2048 rows, 2048 channels, 16 states,
+// bfloat16: 172 us.
 //
 // EXACT: the states fill the lanes' places.  Else those that there are not stay zero (nothing is multiplied by a zero there, where an
 // infinity would become NaN): `n` are the lane's.
@@ -375,8 +376,9 @@ __device__ __forceinline__ void sums_of_channels(float (&v)[4][H::S], float* out
 }
 
 // The second walk.  A tile's 16 states and factors, 32 S registers, are what lets it go back without computing them again or dividing by a factor that may be
-// zero; with them two waves fit into a SIMD, and the vector pipe is busy 73 % of the time: 8 x 2048 rows, 2048 channels, 16 states, bfloat16, 520 us, where
-// its instructions alone take 380.  The rest are waits for LDS that two waves cannot fill.  (Half tiles, with three waves a SIMD, took longer; waves that share
+// zero; with them two waves fit into a SIMD, and the vector pipe is busy 73 % of the time: 8 x 2048 rows, 2048 channels, 16 states, bfloat16, 494 us, where
+// its instructions alone take 375.  (In float32, 9 to 16 states with a gate, 17 to 19 registers a lane are in memory: x, dt, z and dy of a tile wait for its end.  16
+// states: 644 us, the pipe busy 58 %.)  The rest are waits for LDS that two waves cannot fill.  (Half tiles, with three waves a SIMD, took longer; waves that share
 // out a channel's states, as forward, with more barriers a tile, 160 us more.)
 template <class TR, class H, bool EXACT, bool GATE>
 __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs a) {
@@ -385,7 +387,7 @@ __global__ __launch_bounds__(H::THREADS, 2) void k_scan_backward(const ScanArgs 
   // A branch between the quarters of a tile, for its registers: the states of rows that there are not, which it clears, are used nowhere.  Without it the float32
   // kernel of 9 to 16 states with a gate has 25 registers in memory instead of 17 (8 x 2048 rows, 2048 channels, 16 states: 906 us instead of 845), and 64
   // states take 1414 us instead of 1367 (8 x 1024 rows, bfloat16); with it other kernels take longer (bfloat16, 16 states: 667 us instead of 651, 4096 sequences
-  // of 4 rows 1960 instead of 1863).
+  // of 4 rows 1960 instead of 1863; 10 states 755 instead of 750, though two registers are in memory there without it).
   constexpr bool APART = H::NS == 64 || (H::NS == 16 && GATE && sizeof(T) == 4);
   __shared__ Tile<H> tile;
   __shared__ float part[GATE ? 3 : 2][H::WAVES][TILE_ROWS][H::CW];       // sums over the states: du, dd, y, every wave's own
@@ -653,7 +655,8 @@ __global__ __launch_bounds__(256) void k_scan_sums(const ScanArgs a, const Sums 
   if (wave == 0 && at < size) to[at] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
 }
 
-// f(shape, whether the states fill it)
+// f(shape, whether the states fill it).  That they do is known at 16 and 32 states, the usual numbers, which saves a selection an operand: 8 x 2048 rows, 2048
+// channels, bfloat16, 655 us instead of 762 without it; 8 x 1024, 32 states, 600 instead of 702.  (8 and 64 states fill theirs too, and go without.)
 typedef Shape<4, 4, 2> To8;
 typedef Shape<4, 4, 4> To16;
 typedef Shape<8, 8, 4> To32;
