@@ -26,22 +26,25 @@ def same(got, want, tol, what, terms=None):
     assert float((got[fine] - want[fine]).norm()) <= bound, what
 
 
-def positive(lens, dim, groups, states, dtype, seed):
-    v, off, dev_off, dy, ds1 = scan.inputs(lens, dim, groups, states, dtype, seed)
+def positive(lens, dim, groups, states, dtype, seed, more=True):
+    """more: with a gate, D, bias and softplus."""
+    v, off, dev_off, dy, ds1 = scan.inputs(lens, dim, groups, states, dtype, seed, gate=more, more=more, softplus=more)
     for k in ("x", "B", "C", "D", "z", "s0"):
-        v[k] = v[k].abs() + 0.25
+        if v[k] is not None:
+            v[k] = v[k].abs() + 0.25
     return v, off, dev_off, dy.abs() + 0.25, ds1.abs() + 0.25
 
 
-def both(lib, v, off, dev_off, dy, ds1, clean):
-    y, end = scan.forward(lib, v, dev_off)
-    want, w_end = scan.reference(scan.double(v), off, True)
+def both(lib, v, off, dev_off, dy, ds1, clean, more=True):
+    y, end = scan.forward(lib, v, dev_off, more)
+    want, w_end = scan.reference(scan.double(v), off, more)
     same(y, want, scan.tolerance(y), "y")
     same(end, w_end, scan.TOL[F32], "end")
-    got, g_want = scan.backward(lib, v, dev_off, dy, ds1), scan.wanted(v, off, dy, ds1, True)
-    terms = scan.wanted(scan.magnitudes(clean), off, dy, ds1, True)
+    got, g_want = scan.backward(lib, v, dev_off, dy, ds1, more), scan.wanted(v, off, dy, ds1, more)
+    terms = scan.wanted(scan.magnitudes(clean), off, dy, ds1, more)
     for k in scan.NAMES:
-        same(got[k], g_want[k], scan.tolerance(v[k]), k, terms[k])
+        if v[k] is not None:
+            same(got[k], g_want[k], scan.tolerance(v[k]), k, terms[k])
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -69,11 +72,12 @@ def test_an_infinite_gradient_at_the_end(lib, lens, states, dtype):
 
 @pytest.mark.parametrize("where", ["start", "x", "C", "end"])
 @pytest.mark.parametrize("many", [0, 300])
-@pytest.mark.parametrize("states", [1, 16, 40])
-def test_infinities_of_far_rows(lib, states, many, where):
+@pytest.mark.parametrize("states,groups,dtype,more", [(1, 1, F32, True), (16, 1, F32, True), (40, 1, F32, True), (16, 2, BF16, True), (5, 3, F32, False),
+                                                      (32, 2, BF16, False)])
+def test_infinities_of_far_rows(lib, states, groups, dtype, more, many, where):
     """Over many rows a state's factors come to less than float32 holds, though none of them is zero: what is infinite stays so, over
     spans of 64 rows and between them.  In sequences numbered one after the other, and by their place."""
-    v, off, dev_off, dy, ds1 = positive([300] + [1] * many, 6, 1, states, F32, seed=states)
+    v, off, dev_off, dy, ds1 = positive([300] + [1] * many, 6, groups, states, dtype, states, more)
     clean = dict(v)
     v["A"] = -torch.linspace(0.5, 16.0, 6 * states, device="cuda").reshape(6, states)
     if where == "start":
@@ -84,7 +88,7 @@ def test_infinities_of_far_rows(lib, states, many, where):
         v["C"][290, 0, 0] = INF
     else:
         ds1[0, 3, 0] = INF
-    both(lib, v, off, dev_off, dy, ds1, dict(clean, A=v["A"]))
+    both(lib, v, off, dev_off, dy, ds1, dict(clean, A=v["A"]), more)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
