@@ -554,7 +554,7 @@ int span_log2(const nugpr_selective_scan* p, bool backward) {
   return k;
 }
 // Sequences are walked through whole where none has more rows than leave 2048 waves, two for each SIMD: cutting them costs a second pass over their rows.
-// (16 x 1024 rows, 2048 channels: 265 us cut, 202 whole; 8 x 2048: 242 and 342.  In the gradients 676 and 609; 654 and 1157.)
+// (16 x 1024 rows, 2048 channels: 244 us cut, 176 whole; 8 x 2048: 242 either way.  In the gradients 661 and 605; 653 and 920.)
 int64_t whole_of(const nugpr_selective_scan* p, bool backward) {
   const int64_t span = (int64_t)1 << span_log2(p, backward);
   return p->n_seqs > COUNTED ? span : std::max(span, p->n_rows * waves_a_row(p, backward) / 2048);
